@@ -163,7 +163,7 @@ def _inputs(case, seed):
         x = {"branch": g.activations(r, c).to(dt), "residual": g.activations(r, c, 2.0).to(dt),
              "w_post": 1.0 + g.normal(c, scale=0.1), "w_pre": 1.0 + g.normal(c, scale=0.1)}
         x["gate"] = {"none": lambda: None, "channel": lambda: g.normal(c, scale=0.5),
-                     "row": lambda: g.normal(r, scale=0.5), "full": lambda: g.normal(r, c).to(dt)}[case["gate"]]()
+                     "row": lambda: g.normal(r, 1, scale=0.5), "full": lambda: g.normal(r, c).to(dt)}[case["gate"]]()
         x["b_post"] = g.normal(c, scale=0.1) if case["bias"] else None
         x["b_pre"] = g.normal(c, scale=0.1) if case["bias"] else None
         if case["backward"]:
@@ -350,8 +350,6 @@ def _run_plain(s):
         gate = 1.0
         if case["gate"] != "none":
             gate = act(s["gate"].float())
-            if case["gate"] == "row":
-                gate = gate[:, None]
         drop = 1.0
         if case["p"] > 0:
             keep = _keep(case["rows"], case["cols"], case["p"], s["key"])
@@ -372,7 +370,7 @@ def _run_plain(s):
             if case["gate"] != "none":
                 slope = {"none": lambda a: 1.0, "sigmoid": lambda a: a * (1.0 - a), "tanh": lambda a: 1.0 - a * a}
                 dg = du * z * slope[case["act"]](gate)
-                out["dgate"] = {"channel": lambda: dg.sum(dim=0), "row": lambda: dg.sum(dim=1),
+                out["dgate"] = {"channel": lambda: dg.sum(dim=0), "row": lambda: dg.sum(dim=1, keepdim=True),
                                 "full": lambda: dg.to(dt)}[case["gate"]]()
             out["dw_pre"] = (dh * xh_pre).sum(dim=0)
             if case["bias"]:
@@ -502,7 +500,7 @@ def _exact_norm(case, x, key):
     z = xh1 * x["w_post"] + (x["b_post"] if case["bias"] else 0.0)
     a, slope = 1.0, 0.0
     if case["gate"] != "none":
-        g = x["gate"].unsqueeze(1) if case["gate"] == "row" else x["gate"]
+        g = x["gate"]
         if case["act"] == "none":
             a, slope = g, torch.ones_like(g)
         elif case["act"] == "sigmoid":
@@ -529,7 +527,7 @@ def _exact_norm(case, x, key):
         out["db_post"] = dz.sum(0)
     if case["gate"] != "none":
         dg = ds * m * z * slope
-        out["dgate"] = dg if case["gate"] == "full" else dg.sum(0 if case["gate"] == "channel" else 1)
+        out["dgate"] = dg if case["gate"] == "full" else (dg.sum(0) if case["gate"] == "channel" else dg.sum(1, keepdim=True))
     out["dw_pre"] = (x["dnormed"] * xh2).sum(0)
     if case["bias"]:
         out["db_pre"] = x["dnormed"].sum(0)
