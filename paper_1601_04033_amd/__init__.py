@@ -9,6 +9,8 @@ keep the C ABI's names (include/fasgd.h):
     bfasgd_workspace_bytes, bfasgd_select_compact, bfasgd_apply_sparse,
     sgd_sync_apply, bfasgd_apply_cached, bfasgd_apply_fetch
 
+and those of the client's operators (include/fasgd_client.h, module client).
+
 There is no fallback: if libfasgd.so is missing or cannot be loaded, every
 call raises.
 
@@ -672,3 +674,8 @@ def allocate_state(P: int, device="cuda", with_stats: bool = True):
 def allocate_workspace(P: int, device="cuda"):
     import torch
     return torch.empty(bfasgd_workspace_bytes(P), device=device, dtype=torch.uint8)
+
+
+from .client import (CLIENT_ABI_FUNCTIONS, GATE_IDENTITY, GATE_SIGMOID, GATE_TANH, NORM_LAYER,  # noqa: E402,F401
+                     NORM_RMS, client_dropout, client_residual_norm_backward, client_residual_norm_forward,
+                     client_residual_norm_workspace_bytes)

@@ -1,0 +1,59 @@
+// Launchers of the client's kernels, called by the C ABI after it has
+// validated every argument.  Each returns the HIP launch status.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "client_math.hpp"
+
+namespace fasgd {
+
+enum : int { DTYPE_F32 = 0, DTYPE_BF16 = 1, DTYPE_F16 = 2 };
+constexpr size_t dtype_size(int dtype) { return dtype == DTYPE_F32 ? 4 : 2; }
+
+struct DropoutArgs {
+    const void* x;
+    const void* residual;   // NULL: none
+    void* y;
+    int64_t ldx, ldr, ldy;
+    int64_t rows, cols;
+    DropKey key;
+};
+hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s);
+
+enum : int { GATE_NONE = 0, GATE_CHANNEL = 1, GATE_ROW = 2, GATE_FULL = 3 };
+enum : int { ACT_IDENTITY = 0, ACT_SIGMOID = 1, ACT_TANH = 2 };
+
+// The residual norm (include/fasgd_client.h), forward and backward.
+struct NormArgs {
+    int64_t rows;
+    int32_t cols;
+    float n_cols, inv_cols; // cols, 1 / cols
+    int32_t layer;          // layer norm (mean subtracted), else rms
+    int32_t gate_form, gate_act;
+    int32_t drop;           // 0: no dropout
+    float rho, eps;
+    const float *w_post, *b_post, *w_pre, *b_pre;
+    const void* gate;       // channel, row: fp32; full: activations
+    const void *branch, *residual;
+    void* sum;              // read in the backward pass
+    void* normed;
+    float* stats;           // [rows][4]: mean, rstd of the branch; mean, rstd of the sum
+    int64_t ld_branch, ld_residual, ld_gate, ld_sum, ld_normed;
+    DropKey key;
+    // backward
+    const void *dsum, *dnormed;
+    void *dbranch, *dresidual;
+    void* dgate;
+    int64_t ld_dsum, ld_dnormed, ld_dbranch, ld_dresidual, ld_dgate;
+    float *dw_post, *db_post, *dw_pre, *db_pre;
+    float* partial;         // [4][blocks][cols]
+};
+hipError_t launch_norm_forward(const NormArgs& a, int dtype, hipStream_t s);
+hipError_t launch_norm_backward(const NormArgs& a, int dtype, hipStream_t s);
+// Workspace of the backward pass's column sums.
+size_t norm_workspace_bytes(int64_t rows, int64_t cols);
+
+}  // namespace fasgd

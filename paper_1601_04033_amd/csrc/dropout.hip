@@ -1,0 +1,60 @@
+// client_dropout: y = [residual +] drop(x), the mask drawn where it is used.
+#include "client_kernels.hpp"
+
+namespace fasgd {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kChunk = 8;
+
+// One chunk of 8 consecutive matrix elements per thread: one Philox call and
+// one wide access each way.  A chunk that crosses a row's end (rows of a
+// length that is no multiple of 8) goes element by element.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
+{
+    const T* x = static_cast<const T*>(a.x);
+    const T* res = static_cast<const T*>(a.residual);
+    T* y = static_cast<T*>(a.y);
+    const int64_t n = a.rows * a.cols;
+    const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * kChunk;
+    if (i >= n) return;
+    int64_t r = i / a.cols, c = i % a.cols;
+    const uint32_t keep = keep_bits(a.key, a.key.chunk_base + i / kChunk);
+    if (c + kChunk <= a.cols) {
+        Pack<T, kChunk> v = load_pack<T, kChunk>(x + r * a.ldx + c);
+        Pack<T, kChunk> q;
+        if (res) q = load_pack<T, kChunk>(res + r * a.ldr + c);
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            float f = (keep >> e) & 1 ? to_float(v.v[e]) * a.key.scale : 0.0f;
+            if (res) f += to_float(q.v[e]);
+            v.v[e] = from_float<T>(f);
+        }
+        store_pack(y + r * a.ldy + c, v);
+        return;
+    }
+    for (int e = 0; e < kChunk && i + e < n; ++e) {
+        float f = (keep >> e) & 1 ? to_float(x[r * a.ldx + c]) * a.key.scale : 0.0f;
+        if (res) f += to_float(res[r * a.ldr + c]);
+        y[r * a.ldy + c] = from_float<T>(f);
+        if (++c == a.cols) {
+            c = 0;
+            ++r;
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s)
+{
+    const int64_t chunks = (a.rows * a.cols + kChunk - 1) / kChunk;
+    const unsigned blocks = static_cast<unsigned>((chunks + kBlock - 1) / kBlock);
+    if (dtype == DTYPE_F32) dropout<float><<<blocks, kBlock, 0, s>>>(a);
+    else if (dtype == DTYPE_BF16) dropout<bf16><<<blocks, kBlock, 0, s>>>(a);
+    else dropout<f16><<<blocks, kBlock, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace fasgd

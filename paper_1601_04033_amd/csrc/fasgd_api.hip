@@ -1,8 +1,6 @@
 // C ABI of libfasgd.so (declared in include/fasgd.h): host-side argument
 // checks, step-staleness bookkeeping (Sec. 2.1) and kernel dispatch.
 #include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
 #include <string.h>
 
 #include <mutex>
@@ -10,13 +8,17 @@
 #include "../../include/fasgd.h"
 #include "anchor.hpp"
 #include "kernels.hpp"
+#include "status.hpp"
 
 static_assert(FASGD_MAX_K == fasgd::kMaxK, "K limit mismatch");
 static_assert(FASGD_MAX_BATCH == fasgd::kMaxBatch, "batch limit mismatch");
 
 namespace {
 
-thread_local char g_err[512];
+using fasgd::aligned;
+using fasgd::fail;
+using fasgd::hip_fail;
+using fasgd::ok;
 
 // fasgd_record_next_pass: events recorded around the next FASGD pass kernel
 // this thread launches (one-shot)
@@ -35,28 +37,6 @@ hipError_t pass_end(hipStream_t stream)
     g_pass_start = g_pass_stop = nullptr;
     return e;
 }
-
-fasgd_status fail(fasgd_status s, const char* fmt, ...)
-{
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof g_err, fmt, ap);
-    va_end(ap);
-    return s;
-}
-
-fasgd_status ok()
-{
-    g_err[0] = '\0';
-    return FASGD_OK;
-}
-
-fasgd_status hip_fail(hipError_t e, const char* what)
-{
-    return fail(FASGD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 fasgd_status check_state(const fasgd_state* st, bool need_stats)
 {
@@ -888,7 +868,7 @@ const char* fasgd_status_string(fasgd_status s)
     return "unknown status";
 }
 
-const char* fasgd_last_error(void) { return g_err; }
+const char* fasgd_last_error(void) { return fasgd::g_err; }
 
 fasgd_status fasgd_copy_anchor(const float* src, float* dst, int64_t n, hipStream_t stream)
 {

@@ -1,0 +1,313 @@
+"""GPU: the residual norm, forward and backward, against the 64-bit forms.
+
+Tolerances.  The kernels compute in fp32 and round once: an output of type t
+is within half an ulp of t, plus fp32 rounding of what it is made of.  A sum
+over n terms in fp32 (each thread's few dozen, then a tree) is within 64
+roundings of the sum of magnitudes, and the elementwise chains below have
+fewer than 64 operations, so the fp32 part is bounded by 128 * 2^-24 times the
+size of the terms: the row's largest magnitude for elementwise outputs (the
+means over a row are at most that), the sum of magnitudes for the column
+sums."""
+import numpy as np
+import pytest
+
+import client_reference as ref
+import paper_1601_04033_amd as fa
+from helpers import gpu
+
+pytestmark = pytest.mark.gpu
+
+U32 = 128 * 2.0 ** -24
+ROUND = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+ACT = {"identity": fa.GATE_IDENTITY, "sigmoid": fa.GATE_SIGMOID, "tanh": fa.GATE_TANH}
+
+
+def _np(t):
+    return None if t is None else t.double().cpu().numpy()
+
+
+def _close(got, want, dtype, size, what):
+    got = _np(got)
+    bound = ROUND[dtype] * np.abs(want) + U32 * size + 2.0 ** -24 * (dtype == "float16")
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size}, worst {np.abs(got - want)[bad].max()}"
+
+
+def _row(x):
+    return np.abs(x).max(1, keepdims=True)
+
+
+class Problem:
+    def __init__(self, rows, cols, dtype, layer, gate, act, p, bias, post=True, pre=True, residual=True, pad=0, seed=0,
+                 offset=0):
+        import torch
+        self.rows, self.cols, self.dtype, self.layer, self.act, self.rho, self.eps = rows, cols, dtype, layer, act, 0.7, 1e-5
+        g = torch.Generator().manual_seed(seed + rows * 7 + cols)
+        dt = getattr(torch, dtype)
+
+        def matrix(scale=1.0, shift=0.0):
+            ld = cols + pad
+            buf = torch.zeros(rows * ld + offset, dtype=dt)
+            v = buf[offset:].view(rows, ld)[:, :cols]
+            v.copy_(torch.randn(rows, cols, generator=g) * scale + shift)
+            d = buf.cuda()
+            return d[offset:].view(rows, ld)[:, :cols]
+
+        def vector(there, shift):
+            # an odd element of a longer vector: 4-byte aligned only
+            return (torch.randn(cols + 1, generator=g) * 0.3 + shift).cuda()[1:] if there else None
+
+        self.matrix = matrix
+        self.branch, self.residual = matrix(1.0, 0.5), matrix(2.0) if residual else None
+        self.w_post, self.b_post = vector(post, 1.0), vector(post and bias, 0.0)
+        self.w_pre, self.b_pre = vector(pre, 1.0), vector(pre and bias, 0.0)
+        self.gate = {None: lambda: None, "channel": lambda: vector(True, 0.0),
+                     "row": lambda: torch.randn(rows, 1, generator=g).cuda(), "full": lambda: matrix()}[gate]()
+        self.dropout = (p, 0xABCDEF0123456789, 31, 4, 2) if p else None
+        self.m = ref.drop_factor(rows, cols, self.dropout, 16) if p else np.ones((rows, cols))
+        self.opts = dict(kind=fa.NORM_LAYER if layer else fa.NORM_RMS, w_post=self.w_post, b_post=self.b_post,
+                         gate=self.gate, gate_act=ACT[act], w_pre=self.w_pre, b_pre=self.b_pre,
+                         residual_scale=self.rho, eps=self.eps, dropout=self.dropout, index_base=16)
+
+    def forward(self):
+        import torch
+        total = self.matrix()
+        h = self.matrix() if self.w_pre is not None else None
+        stats = torch.empty(self.rows, 4, device="cuda")
+        fa.client_residual_norm_forward(self.branch, self.residual, total, h, stats, **self.opts)
+        return total, h, stats
+
+    def check_forward(self, total, h):
+        x, r = _np(self.branch), _np(self.residual)
+        gate = _np(self.gate)
+        want = ref.residual_norm_sum(x, r, self.layer, _np(self.w_post), _np(self.b_post), gate, self.act,
+                                     np.float64(np.float32(self.rho)), np.float64(np.float32(self.eps)), self.m)
+        u = ref.residual_norm_sum(x, None, self.layer, _np(self.w_post), _np(self.b_post), gate, self.act, 0.0,
+                                  np.float64(np.float32(self.eps)), self.m)
+        size = _row(u) + (0 if r is None else _row(r)) + np.abs(_np(self.b_post) if self.b_post is not None else np.zeros(1)).max() * 4
+        _close(total, want, self.dtype, size, "sum")
+        if h is not None:
+            want = ref.residual_norm_normed(_np(total), self.layer, _np(self.w_pre), _np(self.b_pre),
+                                            np.float64(np.float32(self.eps)))
+            _close(h, want, self.dtype, _row(want) + _row(_np(total)) / np.sqrt(_np(total).var(1, keepdims=True) + 1e-5),
+                   "normed")
+
+    def backward(self, total, stats, with_dsum=True, with_dresidual=True):
+        import torch
+        self.dsum = self.matrix(0.1) if with_dsum else None
+        self.dnormed = self.matrix(0.1) if self.w_pre is not None else None
+        out = {"dbranch": self.matrix(), "dresidual": self.matrix() if with_dresidual else None}
+        args = {}
+        for name in ("w_post", "b_post", "w_pre", "b_pre", "gate"):
+            p = getattr(self, name)
+            if p is not None:
+                args["d" + name] = torch.full_like(p, 3.0) if name != "gate" or p.dim() == 1 or p.shape[1] == 1 else self.matrix()
+        ws = torch.empty(fa.client_residual_norm_workspace_bytes(self.rows, self.cols), device="cuda", dtype=torch.uint8)
+        ws.fill_(255)
+        fa.client_residual_norm_backward(self.branch, total, stats, self.dsum, self.dnormed, out["dbranch"],
+                                         out["dresidual"], workspace=ws, **args, **self.opts)
+        out.update(args)
+        return out
+
+    def check_backward(self, total, got):
+        x = _np(self.branch)
+        eps, rho = np.float64(np.float32(self.eps)), np.float64(np.float32(self.rho))
+        want = ref.residual_norm_backward(x, _np(total), _np(self.dsum), _np(self.dnormed), self.layer,
+                                          _np(self.w_post), _np(self.b_post), _np(self.w_pre), _np(self.b_pre),
+                                          _np(self.gate), self.act, rho, eps, self.m)
+        # sizes of the terms of ds and of dbranch, by row
+        ds = np.abs(_np(self.dsum)).max(1, keepdims=True) if self.dsum is not None else np.zeros((self.rows, 1))
+        if self.dnormed is not None:
+            xh2, r2 = ref.normed(_np(total), self.layer, eps)
+            q = _row(_np(self.dnormed) * _np(self.w_pre))
+            ds = ds + r2 * q * (2 + _row(xh2) ** 2)
+        a = np.ones((1, 1)) if self.gate is None else np.abs(ref.act(_np(self.gate), self.act)).max()
+        dz = ds * self.m.max() * a
+        xh1, r1 = ref.normed(x, self.layer, eps) if self.w_post is not None else (x, np.ones((self.rows, 1)))
+        w = 1.0 if self.w_post is None else np.abs(_np(self.w_post)).max()
+        b = 0.0 if self.b_post is None else np.abs(_np(self.b_post)).max()
+        z = _row(xh1) * w + b
+        # the centred values carry an fp32 rounding of the mean's size
+        shift = 1.0 + np.abs(x).max() + np.abs(_np(total)).max()
+        size = {"dresidual": ds * shift, "dbranch": r1 * dz * w * (2 + _row(xh1) ** 2) * shift}
+        if self.gate is not None and self.gate.dim() == 2 and (self.gate.shape[1] != 1 or self.cols == 1):
+            size["dgate"] = dz / a * z * shift
+        for name, t in got.items():
+            if t is None:
+                continue
+            if name in size:
+                _close(t, want[name], self.dtype, size[name], name)
+                continue
+            s = want["abs_" + name] * shift
+            if name == "dgate" and self.gate.dim() == 2:
+                s = s + (ds * self.m.max() * z).sum(1, keepdims=True) * shift
+            else:
+                # each term's own fp32 error is relative to its row's sizes
+                per_row = {"dw_post": dz * _row(xh1), "db_post": dz, "dgate": dz / a * z,
+                           "dw_pre": _row(_np(self.dnormed)) * (_row(ref.normed(_np(total), self.layer, eps)[0]))
+                           if self.dnormed is not None else 0,
+                           "db_pre": _row(_np(self.dnormed)) if self.dnormed is not None else 0}[name]
+                s = s + np.sum(per_row) * shift
+            err = np.abs(_np(t) - want[name])
+            assert np.all(err <= U32 * s), f"{name}: {err.max()} against {np.min(U32 * s)}"
+
+
+SHAPES = [(1, 1), (1, 4), (3, 7), (5, 8), (9, 33), (70, 64), (33, 100), (7, 200), (40, 257), (300, 512), (13, 513),
+          (5, 1000), (3, 1031), (2, 2050), (3, 4096), (600, 1024), (2, 5003), (3, 8192), (2, 12_000), (2, 16_384),
+          (2, 20_001), (520, 17_001)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("rows, cols", SHAPES)
+def test_shapes(dtype, rows, cols):
+    gpu()
+    i = rows + cols
+    pr = Problem(rows, cols, dtype, i % 2 == 0, [None, "channel", "row", "full"][i % 4 if cols > 1 else 1],
+                 ["identity", "sigmoid", "tanh"][i % 3], 0.25 if i % 5 < 3 else 0.0, i % 2 == 0)
+    total, h, stats = pr.forward()
+    pr.check_forward(total, h)
+    pr.check_backward(total, pr.backward(total, stats))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("layer", [False, True])
+@pytest.mark.parametrize("gate", [None, "channel", "row", "full"])
+@pytest.mark.parametrize("cols", [61, 1500])
+def test_forms(dtype, layer, gate, cols):
+    """Every gate and activation, each norm present and absent, biases, dropout, strides."""
+    gpu()
+    for k, act in enumerate(["identity", "sigmoid", "tanh"]):
+        for post, pre in ((True, True), (True, False), (False, True), (False, False)):
+            pr = Problem(19, cols, dtype, layer, gate, act, 0.5 if k != 1 else 0.0, k != 2, post, pre,
+                         residual=not (k == 2 and post), pad=3 * k, offset=k)
+            total, h, stats = pr.forward()
+            pr.check_forward(total, h)
+            got = pr.backward(total, stats, with_dsum=k != 0 or not pre, with_dresidual=k != 1)
+            pr.check_backward(total, got)
+
+
+def test_every_row_dropped_or_zero():
+    """p = 1 leaves the scaled residual; a row of zeros, or of one value under a layer norm, stays finite."""
+    import torch
+    gpu()
+    pr = Problem(6, 300, "float32", True, "channel", "tanh", 1.0, True)
+    total, h, stats = pr.forward()
+    assert torch.equal(total, (pr.residual * np.float32(0.7)))
+    got = pr.backward(total, stats)
+    assert not got["dbranch"].any() and not got["dgate"].any() and not got["dw_post"].any()
+    pr = Problem(6, 300, "float32", True, None, "identity", 0.0, False)
+    pr.branch.fill_(0.0)
+    pr.branch[3:] = 5.0
+    pr.residual.fill_(0.0)
+    total, h, stats = pr.forward()
+    assert torch.equal(total, torch.zeros_like(total)) and torch.equal(h, torch.zeros_like(h))
+    got = pr.backward(total, stats)
+    assert all(torch.isfinite(t).all() for t in got.values() if t is not None)
+
+
+def test_non_finite_values_stay_in_their_row():
+    import torch
+    gpu()
+    for bad in (float("nan"), float("inf")):
+        pr = Problem(8, 520, "bfloat16", False, "channel", "identity", 0.0, False)
+        want, hw, _ = pr.forward()
+        pr.branch[5, 77] = bad
+        total, h, stats = pr.forward()
+        rows = torch.arange(8) != 5
+        assert torch.equal(total[rows], want[rows]) and torch.equal(h[rows], hw[rows])
+        assert not torch.isfinite(h[5]).all()
+    # without a norm after the block, a dropped infinity is gone
+    pr = Problem(4, 520, "float32", False, "channel", "identity", 0.5, False, post=False)
+    pr.branch[torch.from_numpy(pr.m == 0).cuda()] = float("inf")
+    total, h, stats = pr.forward()
+    got = pr.backward(total, stats)
+    assert torch.isfinite(total).all() and all(torch.isfinite(t).all() for t in got.values() if t is not None)
+
+
+def test_in_place_and_repeatable():
+    """sum over residual, normed over branch, dresidual over dsum give the same bits; so does a second run."""
+    import torch
+    gpu()
+    for rows, cols in ((300, 640), (1000, 96), (3, 17_001)):
+        pr = Problem(rows, cols, "bfloat16", True, "row", "sigmoid", 0.1, True)
+        total, h, stats = pr.forward()
+        got = pr.backward(total, stats)
+        branch, residual = pr.branch.clone(), pr.residual.clone()
+        st2 = torch.empty_like(stats)
+        fa.client_residual_norm_forward(branch, residual, residual, branch, st2, **pr.opts)
+        assert torch.equal(residual, total) and torch.equal(branch, h) and torch.equal(st2, stats)
+        dsum = pr.dsum.clone()
+        args = {k: torch.empty_like(v) for k, v in got.items() if k not in ("dbranch", "dresidual")}
+        db = torch.empty_like(pr.branch)
+        ws = torch.empty(fa.client_residual_norm_workspace_bytes(rows, cols), device="cuda", dtype=torch.uint8)
+        fa.client_residual_norm_backward(pr.branch, total, stats, dsum, pr.dnormed, db, dsum, workspace=ws, **args,
+                                         **pr.opts)
+        assert torch.equal(dsum, got["dresidual"]) and torch.equal(db, got["dbranch"])
+        for k, v in args.items():
+            assert torch.equal(v, got[k]), k
+
+
+def test_no_rows():
+    import torch
+    gpu()
+    z = torch.empty(0, 40, device="cuda")
+    w, dw, g, dg = (torch.ones(40, device="cuda") for _ in range(4))
+    stats = torch.empty(0, 4, device="cuda")
+    fa.client_residual_norm_forward(z, z, z, z, stats, w_post=w, w_pre=w, gate=g)
+    dwp = torch.ones(40, device="cuda")
+    fa.client_residual_norm_backward(z, z, stats, z, z, z, z, w_post=w, w_pre=w, gate=g, dw_post=dw, dw_pre=dwp, dgate=dg)
+    assert not dw.any() and not dwp.any() and not dg.any()
+
+
+def test_gradients_match_differences():
+    """A directional derivative of a loss taken through the forward kernel in fp32: the loss is summed in fp64 from
+    outputs of relative error 2^-24 or a few of them, so a step of 1e-2 leaves 1e-4 of its size; the third derivative
+    adds 1e-4 of the same order."""
+    import torch
+    gpu()
+    pr = Problem(40, 300, "float32", True, "channel", "tanh", 0.2, True)
+    total, h, stats = pr.forward()
+    got = pr.backward(total, stats)
+    names = ["branch", "residual", "w_post", "b_post", "w_pre", "b_pre", "gate"]
+
+    def loss():
+        total, h, _ = pr.forward()
+        return ((total.double() * pr.dsum.double()).sum() + (h.double() * pr.dnormed.double()).sum()).item()
+
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for name in names:
+        t = getattr(pr, name)
+        d = torch.randn(t.shape, device="cuda", generator=g)
+        keep = t.clone()
+        step = 1e-2
+        t.copy_(keep + step * d)
+        up = loss()
+        t.copy_(keep - step * d)
+        down = loss()
+        t.copy_(keep)
+        grad = got["d" + name].double()
+        want = (grad * d.double()).sum().item()
+        size = (grad.abs() * d.double().abs()).sum().item()
+        assert abs((up - down) / (2 * step) - want) <= 1e-3 * size + 1e-3, name
+
+
+def test_other_stream_and_graph():
+    import torch
+    gpu()
+    pr = Problem(200, 1024, "bfloat16", False, "channel", "tanh", 0.1, False)
+    total, h, stats = pr.forward()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    t2, h2, st2 = torch.zeros_like(total), torch.zeros_like(h), torch.zeros_like(stats)
+    fa.client_residual_norm_forward(pr.branch, pr.residual, t2, h2, st2, stream=s, **pr.opts)
+    s.synchronize()
+    assert torch.equal(t2, total) and torch.equal(h2, h)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fa.client_residual_norm_forward(pr.branch, pr.residual, t2, h2, st2, **pr.opts)
+    for k in range(3):
+        pr.branch.mul_(1.25)
+        graph.replay()
+        want, hw, _ = pr.forward()
+        torch.cuda.synchronize()
+        assert torch.equal(t2, want) and torch.equal(h2, hw)
