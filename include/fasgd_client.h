@@ -146,6 +146,78 @@ fasgd_status client_residual_norm_backward(const client_residual_norm* op, const
                                            float* db_pre, void* workspace, size_t workspace_bytes,
                                            hipStream_t stream);
 
+/*
+ * Matrix products in 8-bit floating point with a scale for each block of 128.
+ *
+ * An operand is a matrix [rows][k] held for products over k.  Each row's k
+ * values lie in blocks of 128, and block kb of row r is held as
+ *   value = q 2^(scales[kb lds + r] - 127),
+ * q an 8-bit float (OCP e4m3, largest 448; or e5m2, largest 57344) at
+ * data[r ld + k].  Scales are powers of two: multiplying by one is exact, so
+ * an operand is rounded once, and the matrix instruction applies them.
+ * A product needs data to be 16-byte aligned, ld a multiple of 128 and at
+ * least k rounded up to one (the values past k must be 0), scales 4-byte
+ * aligned and lds a multiple of 4 of at least rows.  k and ld are at most
+ * 2^23.
+ */
+typedef enum client_fp8_format {
+    CLIENT_FP8_E4M3 = 0,
+    CLIENT_FP8_E5M2 = 1
+} client_fp8_format;
+
+typedef struct client_fp8_operand {
+    uint8_t* data;              /* [rows][ld] */
+    uint8_t* scales;            /* [ceil(k / 128)][lds], an exponent + 127 each */
+    int64_t rows, k, ld, lds;
+    int32_t format;             /* client_fp8_format */
+} client_fp8_operand;
+
+/*
+ * Quantizes x ([rows][cols] of dtype) into by_rows (rows x cols, blocks of
+ * 128 along each row of x) and / or by_cols (the transpose, cols x rows,
+ * blocks of 128 along each column), from one read of x.  Either may be NULL;
+ * both have one format.  block_rows = 1: a scale for each row of an operand
+ * and block of 128 (activations and their gradients).  block_rows = 128: one
+ * for each 128 x 128 block of x (weights), written for each row all the same,
+ * so that both operands hold the same values.
+ * The scale of a block with largest finite magnitude amax is 2^e with e the
+ * smallest integer that has amax <= 448 2^e (57344 2^e) and e >= -126; e = 0
+ * for a block of zeros.  q = x 2^-e rounded to nearest even; what is not
+ * finite becomes NaN.  The values past k in an operand's last block are
+ * written as zeros.
+ */
+fasgd_status client_fp8_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype,
+                                 int32_t block_rows, const client_fp8_operand* by_rows,
+                                 const client_fp8_operand* by_cols, hipStream_t stream);
+
+/*
+ * c[m][n] = sum over k of a[m][k] b[n][k] (with accumulate != 0: added to
+ * what c holds), [a->rows][b->rows] of c_dtype, for two operands of one k.
+ * A linear layer y = x W^T is the product of x and W; its input gradient
+ * that of dy and W transposed, its weight gradient that of dy transposed and
+ * x transposed.  Sums are fp32 and rounded once.  Where few outputs leave
+ * most of the chip idle, the contraction is split and its parts joined in
+ * order through the workspace, so the result is the same run to run.
+ * workspace: client_fp8_workspace_bytes(a->rows, b->rows, k) bytes of device
+ * scratch, 16-byte aligned, contents irrelevant (the same size serves
+ * client_fp8_linear, which also holds its quantized x there).
+ */
+size_t client_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k);
+fasgd_status client_fp8_matmul(const client_fp8_operand* a, const client_fp8_operand* b, void* c, int64_t ldc,
+                               int32_t c_dtype, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+
+/*
+ * y = x W^T for activations x ([m][w->k] of dtype, not quantized before) and
+ * weights held as an operand, as serving and evaluation need it: x is
+ * quantized in e4m3 as client_fp8_quantize does with block_rows = 1, then
+ * multiplied.  y is [m][w->rows] of dtype.  workspace:
+ * client_fp8_workspace_bytes(m, w->rows, w->k) bytes, as above.
+ */
+fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const client_fp8_operand* w, void* y,
+                               int64_t ldy, int32_t dtype, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -676,6 +676,8 @@ def allocate_workspace(P: int, device="cuda"):
     return torch.empty(bfasgd_workspace_bytes(P), device=device, dtype=torch.uint8)
 
 
-from .client import (CLIENT_ABI_FUNCTIONS, GATE_IDENTITY, GATE_SIGMOID, GATE_TANH, NORM_LAYER,  # noqa: E402,F401
-                     NORM_RMS, client_dropout, client_residual_norm_backward, client_residual_norm_forward,
+from .client import (CLIENT_ABI_FUNCTIONS, FP8_E4M3, FP8_E5M2, GATE_IDENTITY, GATE_SIGMOID,  # noqa: E402,F401
+                     GATE_TANH, NORM_LAYER, NORM_RMS, Fp8Operand, client_dropout, client_fp8_linear,
+                     client_fp8_matmul, client_fp8_operand, client_fp8_quantize, client_fp8_workspace_bytes,
+                     client_residual_norm_backward, client_residual_norm_forward,
                      client_residual_norm_workspace_bytes)

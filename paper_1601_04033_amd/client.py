@@ -15,7 +15,11 @@ import ctypes
 
 # every function include/fasgd_client.h declares
 CLIENT_ABI_FUNCTIONS = ("client_dropout", "client_residual_norm_workspace_bytes", "client_residual_norm_forward",
-                        "client_residual_norm_backward")
+                        "client_residual_norm_backward", "client_fp8_workspace_bytes", "client_fp8_quantize",
+                        "client_fp8_matmul", "client_fp8_linear")
+
+FP8_E4M3 = 0
+FP8_E5M2 = 1
 
 NORM_RMS = 0
 NORM_LAYER = 1
@@ -35,6 +39,12 @@ class client_residual_norm(ctypes.Structure):
                 ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float), ("p", ctypes.c_double),
                 ("seed", ctypes.c_uint64), ("T", ctypes.c_int64), ("client", ctypes.c_int32),
                 ("site", ctypes.c_int32), ("index_base", ctypes.c_int64)]
+
+
+class client_fp8_operand_struct(ctypes.Structure):
+    """Mirror of the C struct client_fp8_operand."""
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("k", ctypes.c_int64), ("ld", ctypes.c_int64), ("lds", ctypes.c_int64), ("format", ctypes.c_int32)]
 
 
 _DTYPES = None
@@ -60,6 +70,11 @@ def bind(lib):
     lib.client_residual_norm_backward.argtypes = [N, P, i64, P, i64, P, P, i64, P, i64, P, i64, P, i64,
                                                   P, P, P, i64, P, P, P, sz, P]
     lib.client_residual_norm_workspace_bytes.argtypes = [i64, i64]
+    O = ctypes.POINTER(client_fp8_operand_struct)
+    lib.client_fp8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.client_fp8_quantize.argtypes = [P, i64, i64, i64, i32, i32, O, O, P]
+    lib.client_fp8_matmul.argtypes = [O, O, P, i64, i32, i32, P, sz, P]
+    lib.client_fp8_linear.argtypes = [P, i64, i64, O, P, i64, i32, P, sz, P]
     for name in CLIENT_ABI_FUNCTIONS:
         getattr(lib, name).restype = sz if name.endswith("_bytes") else ctypes.c_int
     return lib
@@ -240,3 +255,85 @@ def client_residual_norm_backward(branch, sum_in, stats, dsum, dnormed, dbranch,
         _vector(dw_post, "dw_post", cols), _vector(db_post, "db_post", cols), pg, lg,
         _vector(dw_pre, "dw_pre", cols), _vector(db_pre, "db_pre", cols), pw,
         0 if workspace is None else workspace.numel(), _stream(stream)))
+
+
+class Fp8Operand:
+    """A matrix [rows, k] held in 8 bits in blocks of 128 along k (the C struct client_fp8_operand) and its tensors:
+    data uint8 [rows, k rounded up to 128], scales uint8 [ceil(k / 128), rows rounded up to 4]."""
+
+    def __init__(self, data, scales, rows: int, k: int, fmt: int):
+        import torch
+        ld, lds = -(-k // 128) * 128, -(-rows // 4) * 4
+        for t, name, shape in ((data, "data", (rows, ld)), (scales, "scales", (ld // 128, lds))):
+            if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+                raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+            if t.dtype != torch.uint8 or not t.is_contiguous():
+                raise TypeError(f"{name} must be a contiguous uint8 tensor")
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} is {tuple(t.shape)}, expected {shape}")
+        self.data, self.scales, self.rows, self.k, self.format = data, scales, rows, k, fmt
+        self.c = client_fp8_operand_struct(data.data_ptr(), scales.data_ptr(), rows, k, ld, lds, fmt)
+
+    def values(self):
+        """The fp32 values held, [rows, k] (for inspection; torch operations)."""
+        import torch
+        q = self.data.view(torch.float8_e4m3fn if self.format == FP8_E4M3 else torch.float8_e5m2).float()
+        s = (self.scales[:, :self.rows].int() << 23).view(torch.float32)     # 2^(byte - 127), bytes 1 .. 253
+        return (q.view(self.rows, -1, 128) * s.t().unsqueeze(2)).view(self.rows, -1)[:, :self.k]
+
+
+def client_fp8_operand(rows: int, k: int, fmt: int = FP8_E4M3, device="cuda") -> Fp8Operand:
+    """An operand of new, unset tensors."""
+    import torch
+    f = dict(device=device, dtype=torch.uint8)
+    return Fp8Operand(torch.empty(rows, -(-k // 128) * 128, **f), torch.empty(-(-k // 128), -(-rows // 4) * 4, **f),
+                      int(rows), int(k), int(fmt))
+
+
+def client_fp8_workspace_bytes(m: int, n: int, k: int) -> int:
+    """Bytes of workspace of client_fp8_matmul and client_fp8_linear for an [m, n] product over k."""
+    return int(_library().client_fp8_workspace_bytes(int(m), int(n), int(k)))
+
+
+def client_fp8_quantize(x, by_rows=None, by_cols=None, block_rows: int = 1, stream=None) -> None:
+    """Quantizes x [rows, cols] into the operand by_rows ([rows, k = cols]) and / or by_cols (the transpose,
+    [cols, k = rows]); block_rows = 128 takes one scale per 128 x 128 block (weights)."""
+    px, ldx = _matrix(x, "x")
+    rows, cols = _shape(x)
+    _check(_library().client_fp8_quantize(px, ldx, rows, cols, _dtype(x, "x"), int(block_rows),
+                                          None if by_rows is None else ctypes.byref(by_rows.c),
+                                          None if by_cols is None else ctypes.byref(by_cols.c), _stream(stream)))
+
+
+def _workspace(workspace):
+    import torch
+    from . import _dev_ptr
+    if workspace is None:
+        return None, 0
+    return _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel()
+
+
+def client_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out, accumulate: bool = False, workspace=None, stream=None) -> None:
+    """out [a.rows, b.rows] = a b^T over their common k (accumulate: added to out).  workspace: uint8,
+    client_fp8_workspace_bytes(a.rows, b.rows, k) bytes."""
+    pc, ldc = _matrix(out, "out")
+    if _shape(out) != (a.rows, b.rows):
+        raise ValueError(f"out is {tuple(out.shape)}, expected {(a.rows, b.rows)}")
+    pw, nw = _workspace(workspace)
+    _check(_library().client_fp8_matmul(ctypes.byref(a.c), ctypes.byref(b.c), pc, ldc, _dtype(out, "out"),
+                                        1 if accumulate else 0, pw, nw, _stream(stream)))
+
+
+def client_fp8_linear(x, w: Fp8Operand, out, workspace=None, stream=None) -> None:
+    """out [m, w.rows] = x w^T for x [m, w.k] of out's dtype, quantized in e4m3 on the way.  workspace: uint8,
+    client_fp8_workspace_bytes(m, w.rows, w.k) bytes."""
+    px, ldx = _matrix(x, "x")
+    py, ldy = _matrix(out, "out")
+    if out.dtype != x.dtype:
+        raise TypeError(f"out is {out.dtype}, expected {x.dtype}")
+    m, k = _shape(x)
+    if k != w.k or _shape(out) != (m, w.rows):
+        raise ValueError(f"x {tuple(x.shape)} and out {tuple(out.shape)} do not fit weights [{w.rows}, {w.k}]")
+    pw, nw = _workspace(workspace)
+    _check(_library().client_fp8_linear(px, ldx, m, ctypes.byref(w.c), py, ldy, _dtype(x, "x"), pw, nw,
+                                        _stream(stream)))

@@ -124,6 +124,48 @@ fasgd_status norm_setup(const client_residual_norm* op, fasgd::NormArgs& a)
     return FASGD_OK;
 }
 
+constexpr int64_t kMaxK = int64_t(1) << 23;    // of an operand: 256 rows of it stay within 32-bit offsets
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// An 8-bit operand; its arrays are needed where it holds anything.
+fasgd_status check_operand(const char* name, const client_fp8_operand* op, fasgd::Fp8View& v)
+{
+    if (!op) return fail(FASGD_ERR_NULL, "%s is NULL", name);
+    if (op->format != CLIENT_FP8_E4M3 && op->format != CLIENT_FP8_E5M2)
+        return fail(FASGD_ERR_ARG, "%s: format = %d is not a client_fp8_format value", name, op->format);
+    if (op->rows < 0 || op->rows > kMaxElements) return fail(FASGD_ERR_ARG, "%s: rows = %lld is not in [0, 2^40]", name, (long long)op->rows);
+    if (op->k < 0 || op->k > kMaxK) return fail(FASGD_ERR_ARG, "%s: k = %lld is not in [0, 2^23]", name, (long long)op->k);
+    v = fasgd::Fp8View{op->data, op->scales, op->rows, op->k, op->ld, op->lds, op->format};
+    if (op->rows == 0 || op->k == 0) return FASGD_OK;
+    if (!op->data || !op->scales) return fail(FASGD_ERR_NULL, "%s: data or scales is NULL", name);
+    if (!aligned(op->data, 16) || !aligned(op->scales, 4))
+        return fail(FASGD_ERR_ALIGN, "%s: data must be 16-byte and scales 4-byte aligned", name);
+    if (op->ld < round_up(op->k, 128) || op->ld % 128 != 0 || op->ld > kMaxK)
+        return fail(FASGD_ERR_ARG, "%s: ld = %lld must be a multiple of 128 in [k = %lld rounded up, 2^23]", name,
+                    (long long)op->ld, (long long)op->k);
+    if (op->lds < op->rows || op->lds % 4 != 0 || op->lds > kMaxElements)
+        return fail(FASGD_ERR_ARG, "%s: lds = %lld must be a multiple of 4 of at least rows = %lld", name,
+                    (long long)op->lds, (long long)op->rows);
+    return FASGD_OK;
+}
+
+fasgd_status check_workspace(const void* workspace, size_t bytes, size_t need)
+{
+    if (need == 0) return FASGD_OK;
+    if (!workspace) return fail(FASGD_ERR_NULL, "workspace is NULL");
+    if (!aligned(workspace, 16)) return fail(FASGD_ERR_ALIGN, "workspace must be 16-byte aligned");
+    if (bytes < need)
+        return fail(FASGD_ERR_CAPACITY, "workspace of %zu bytes is smaller than the %zu needed", bytes, need);
+    return FASGD_OK;
+}
+
+// client_fp8_linear's quantized x at the front of its workspace.
+size_t linear_operand_bytes(int64_t m, int64_t k)
+{
+    return static_cast<size_t>(round_up(m * round_up(k, 128) + round_up(k, 128) / 128 * round_up(m, 4), 256));
+}
+
 }  // namespace
 
 extern "C" {
@@ -244,6 +286,106 @@ fasgd_status client_residual_norm_backward(const client_residual_norm* op, const
     a.partial = static_cast<float*>(workspace);
     const hipError_t e = fasgd::launch_norm_backward(a, op->dtype, stream);
     if (e != hipSuccess) return hip_fail(e, "client_residual_norm_backward");
+    return ok();
+}
+
+size_t client_fp8_workspace_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (m < 1 || n < 1 || k < 1 || k > kMaxK || m > kMaxElements / n || m > kMaxElements / k) return 0;
+    return linear_operand_bytes(m, k) + fasgd::fp8_workspace_bytes(m, n, k);
+}
+
+fasgd_status client_fp8_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int32_t dtype,
+                                 int32_t block_rows, const client_fp8_operand* by_rows,
+                                 const client_fp8_operand* by_cols, hipStream_t stream)
+{
+    FASGD_TRY(check_shape(rows, cols, dtype));
+    if (block_rows != 1 && block_rows != 128) return fail(FASGD_ERR_ARG, "block_rows = %d is neither 1 nor 128", block_rows);
+    if (!by_rows && !by_cols) return fail(FASGD_ERR_NULL, "by_rows and by_cols are both NULL");
+    fasgd::QuantizeArgs a;
+    memset(&a, 0, sizeof a);
+    if (by_rows) FASGD_TRY(check_operand("by_rows", by_rows, a.row));
+    if (by_cols) FASGD_TRY(check_operand("by_cols", by_cols, a.col));
+    if (by_rows && (by_rows->rows != rows || by_rows->k != cols))
+        return fail(FASGD_ERR_ARG, "by_rows is %lld x %lld, x is %lld x %lld", (long long)by_rows->rows,
+                    (long long)by_rows->k, (long long)rows, (long long)cols);
+    if (by_cols && (by_cols->rows != cols || by_cols->k != rows))
+        return fail(FASGD_ERR_ARG, "by_cols is %lld x %lld, x transposed is %lld x %lld", (long long)by_cols->rows,
+                    (long long)by_cols->k, (long long)cols, (long long)rows);
+    if (by_rows && by_cols && by_rows->format != by_cols->format)
+        return fail(FASGD_ERR_ARG, "by_rows and by_cols differ in format");
+    if (rows == 0 || cols == 0) return ok();
+    FASGD_TRY(check_matrix("x", x, ldx, rows, cols, dtype));
+    a.x = x;
+    a.ldx = ldx;
+    a.rows = rows;
+    a.cols = cols;
+    a.whole = block_rows == 128;
+    const hipError_t e = fasgd::launch_quantize(a, dtype, stream);
+    if (e != hipSuccess) return hip_fail(e, "client_fp8_quantize");
+    return ok();
+}
+
+fasgd_status client_fp8_matmul(const client_fp8_operand* a, const client_fp8_operand* b, void* c, int64_t ldc,
+                               int32_t c_dtype, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream)
+{
+    fasgd::Fp8Product p;
+    memset(&p, 0, sizeof p);
+    FASGD_TRY(check_operand("a", a, p.a));
+    FASGD_TRY(check_operand("b", b, p.b));
+    if (a->k != b->k)
+        return fail(FASGD_ERR_ARG, "a and b differ in k: %lld and %lld", (long long)a->k, (long long)b->k);
+    FASGD_TRY(check_shape(a->rows, b->rows, c_dtype));
+    if (a->rows == 0 || b->rows == 0) return ok();
+    FASGD_TRY(check_matrix("c", c, ldc, a->rows, b->rows, c_dtype));
+    FASGD_TRY(check_workspace(workspace, workspace_bytes, fasgd::fp8_workspace_bytes(a->rows, b->rows, a->k)));
+    if (a->k == 0 && accumulate) return ok();
+    p.c = c;
+    p.ldc = ldc;
+    p.c_dtype = c_dtype;
+    p.accumulate = accumulate != 0;
+    p.partial = static_cast<float*>(workspace);
+    const hipError_t e = fasgd::launch_fp8_product(p, stream);
+    if (e != hipSuccess) return hip_fail(e, "client_fp8_matmul");
+    return ok();
+}
+
+fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const client_fp8_operand* w, void* y,
+                               int64_t ldy, int32_t dtype, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream)
+{
+    fasgd::Fp8Product p;
+    memset(&p, 0, sizeof p);
+    FASGD_TRY(check_operand("w", w, p.b));
+    FASGD_TRY(check_shape(m, w->rows, dtype));
+    FASGD_TRY(check_shape(m, w->k, dtype));
+    if (m == 0 || w->rows == 0) return ok();
+    FASGD_TRY(check_matrix("y", y, ldy, m, w->rows, dtype));
+    if (w->k > 0) {
+        FASGD_TRY(check_matrix("x", x, ldx, m, w->k, dtype));
+        FASGD_TRY(check_workspace(workspace, workspace_bytes, client_fp8_workspace_bytes(m, w->rows, w->k)));
+    }
+    const int64_t ld = round_up(w->k, 128);
+    uint8_t* base = static_cast<uint8_t*>(workspace);
+    p.a = fasgd::Fp8View{base, base + m * ld, m, w->k, ld, round_up(m, 4), fasgd::FP8_E4M3};
+    p.c = y;
+    p.ldc = ldy;
+    p.c_dtype = dtype;
+    p.partial = reinterpret_cast<float*>(base + (w->k > 0 ? linear_operand_bytes(m, w->k) : 0));
+    hipError_t e = hipSuccess;
+    if (w->k > 0) {
+        fasgd::QuantizeArgs q;
+        memset(&q, 0, sizeof q);
+        q.x = x;
+        q.ldx = ldx;
+        q.rows = m;
+        q.cols = w->k;
+        q.row = p.a;
+        e = fasgd::launch_quantize(q, dtype, stream);
+    }
+    if (e == hipSuccess) e = fasgd::launch_fp8_product(p, stream);
+    if (e != hipSuccess) return hip_fail(e, "client_fp8_linear");
     return ok();
 }
 

@@ -56,4 +56,40 @@ hipError_t launch_norm_backward(const NormArgs& a, int dtype, hipStream_t s);
 // Workspace of the backward pass's column sums.
 size_t norm_workspace_bytes(int64_t rows, int64_t cols);
 
+
+// ---- 8-bit operands (include/fasgd_client.h)
+
+constexpr int kFp8Block = 128;      // contraction length under one scale
+enum : int { FP8_E4M3 = 0, FP8_E5M2 = 1 };
+
+struct Fp8View {
+    uint8_t* data;          // [rows][ld], ld a multiple of 128
+    uint8_t* scales;        // [ceil(k / 128)][lds]
+    int64_t rows, k, ld, lds;
+    int32_t format;
+};
+
+// x quantized into `row` (x's rows, blocks along its columns) and / or `col`
+// (x's columns, blocks along its rows); data NULL: not wanted.  whole: one
+// scale per 128 x 128 tile.
+struct QuantizeArgs {
+    const void* x;
+    int64_t ldx, rows, cols;
+    Fp8View row, col;
+    int32_t whole;
+};
+hipError_t launch_quantize(const QuantizeArgs& a, int dtype, hipStream_t s);
+
+// c[m][n] (+)= sum_k a[m][k] b[n][k]
+struct Fp8Product {
+    Fp8View a, b;
+    void* c;
+    int64_t ldc;
+    int32_t c_dtype;
+    int32_t accumulate;
+    float* partial;         // [splits][m][n], unused with one split
+};
+size_t fp8_workspace_bytes(int64_t m, int64_t n, int64_t k);
+hipError_t launch_fp8_product(const Fp8Product& p, hipStream_t s);
+
 }  // namespace fasgd

@@ -138,3 +138,63 @@ def test_binding_rejects_host_tensors_and_shapes():
         fa.client_dropout(x, x, 0.5, 1, 0, 0)
     with pytest.raises(TypeError):
         fa.client_residual_norm_forward(x, x, x, x, x)
+
+
+def _operand(rows=4, k=100, **kw):
+    o = fa.client.client_fp8_operand_struct(P, P, rows, k, -(-k // 128) * 128, -(-rows // 4) * 4, 0)
+    for name, v in kw.items():
+        setattr(o, name, v)
+    return o
+
+
+OPERAND_FAULTS = [(dict(data=None), NULL, b"data"), (dict(scales=None), NULL, b"scales"), (dict(data=P + 8), ALIGN, b"16-byte"),
+                  (dict(scales=P + 2), ALIGN, b"scales"), (dict(ld=100), ARG, b"ld ="), (dict(ld=129), ARG, b"ld ="),
+                  (dict(ld=2 ** 24), ARG, b"ld ="), (dict(lds=3), ARG, b"lds ="), (dict(lds=6), ARG, b"lds ="),
+                  (dict(format=2), ARG, b"format"), (dict(rows=-1), ARG, b"rows"), (dict(k=-1), ARG, b"k ="),
+                  (dict(k=2 ** 23 + 1), ARG, b"k =")]
+
+
+@pytest.mark.parametrize("fault, status, text", OPERAND_FAULTS)
+def test_operands_are_checked(lib, fault, status, text):
+    good, bad, ref = _operand(), _operand(**fault), ctypes.byref
+    calls = [lambda: lib.client_fp8_matmul(ref(bad), ref(good), P, 8, 0, 0, P, 1 << 20, None),
+             lambda: lib.client_fp8_matmul(ref(good), ref(bad), P, 8, 0, 0, P, 1 << 20, None),
+             lambda: lib.client_fp8_quantize(P, 100, 4, 100, 0, 1, ref(bad), None, None),
+             lambda: lib.client_fp8_linear(P, 100, 4, ref(bad), P, 8, 0, P, 1 << 20, None)]
+    for call in calls:
+        assert call() == status
+        assert text in lib.fasgd_last_error()
+
+
+def test_fp8_calls_reject(lib):
+    a, b, ref = _operand(), _operand(6), ctypes.byref
+
+    def matmul(a=a, b=b, c=P, ldc=8, dtype=0, ws=P, n=1 << 20):
+        return lib.client_fp8_matmul(ref(a) if a else None, ref(b) if b else None, c, ldc, dtype, 0, ws, n, None)
+    assert matmul(a=None) == NULL and matmul(b=None) == NULL and matmul(c=None) == NULL
+    assert matmul(c=P + 2) == ALIGN and matmul(ldc=5) == ARG and matmul(dtype=5) == ARG
+    assert matmul(b=_operand(6, 101)) == ARG and b"differ in k" in lib.fasgd_last_error()
+
+    def quantize(x=P, ldx=100, rows=4, cols=100, dtype=0, block=1, r=a, t=None):
+        return lib.client_fp8_quantize(x, ldx, rows, cols, dtype, block, ref(r) if r else None, ref(t) if t else None, None)
+    assert quantize(r=None) == NULL and quantize(x=None) == NULL and quantize(x=P + 1) == ALIGN
+    assert quantize(block=64) == ARG and quantize(dtype=-1) == ARG and quantize(ldx=99) == ARG
+    assert quantize(rows=5) == ARG and b"by_rows is" in lib.fasgd_last_error()
+    assert quantize(t=_operand(100, 5)) == ARG and b"by_cols is" in lib.fasgd_last_error()
+    assert quantize(t=_operand(100, 4, format=1)) == ARG and b"format" in lib.fasgd_last_error()
+
+    def linear(x=P, m=4, w=b, y=P, ldy=6, dtype=1, ws=P, n=1 << 20, ldx=100):
+        return lib.client_fp8_linear(x, ldx, m, ref(w) if w else None, y, ldy, dtype, ws, n, None)
+    assert linear(x=None) == NULL and linear(w=None) == NULL and linear(y=None) == NULL
+    assert linear(m=-1) == ARG and linear(ldy=5) == ARG and linear(ldx=99) == ARG
+    assert linear(ws=None) == NULL and linear(ws=P + 4) == ALIGN and linear(n=8) == CAPACITY
+    # nothing to do
+    assert linear(m=0, x=None, y=None, ws=None, n=0) == 0
+    assert quantize(rows=0, x=None, r=_operand(0, 100, data=None, scales=None)) == 0
+    assert matmul(a=_operand(0), c=None, ws=None, n=0) == 0
+
+
+def test_fp8_workspace_bytes(lib):
+    f = fa.client_fp8_workspace_bytes
+    assert f(0, 5, 5) == f(5, 0, 5) == f(5, 5, 0) == f(-1, 5, 5) == f(2 ** 40, 2 ** 40, 2 ** 20) == 0
+    assert f(1, 1000, 784) >= 784 and f(8192, 4096, 4096) >= 8192 * 4096
