@@ -40,101 +40,129 @@ template <int W> struct Geometry {
     static constexpr int kLoads = kStage / (kThreads * 16);     // 16-byte loads per thread and operand
 };
 
+#if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources
+
 // The 16-byte chunk of a row that lies in slot s of its 128 LDS bytes.  Rows
 // that one read touches together (kTiles apart) get their chunks in
 // different banks.
 template <int W> __device__ __forceinline__ int swizzle(int row) { return (row / Geometry<W>::kTiles) & 7; }
 
-typedef const __attribute__((address_space(1))) void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
-// One operand's stage, global memory straight to LDS.
-template <int W>
-__device__ __forceinline__ void load_stage(const uint8_t* base, const uint32_t (&offset)[Geometry<W>::kLoads],
-                                           uint8_t* stage, int wave)
+// A buffer of the bytes from p on (all of `bytes` that 32 bits can say; the
+// offsets used stay below 2^31 + 2^23).
+__device__ __forceinline__ auto buffer(const uint8_t* p, int64_t bytes)
 {
-#pragma unroll
-    for (int p = 0; p < Geometry<W>::kLoads; ++p)
-        __builtin_amdgcn_global_load_lds((global_ptr)(base + offset[p]),
-                                         (lds_ptr)(stage + (p * 4 + wave) * 1024), 16, 0, 0);
+    constexpr int kRaw = 0x00020000;    // raw buffer, 32-bit data
+    const uint32_t n = bytes < 0xffffffffll ? static_cast<uint32_t>(bytes) : 0xffffffffu;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, static_cast<int>(n), kRaw);
 }
 
-// The fragments of one half stage (64 of the contraction): lane l holds row
-// l % 32 of each tile, two chunks of it.
-template <int W>
-__device__ __forceinline__ void read_fragments(const uint8_t* stage, int row, int lane, int half,
-                                               v8i (&f)[Geometry<W>::kTiles])
+// A stage is worked through in sub-steps of 1,024 matrix cycles per wave (at
+// W = 128): 64 of the contraction in the 8-bit instruction, 32 in bf16.  A
+// sub-step's fragments (lane l: row l % 32 of a tile, the 16-byte chunks of
+// its half of the sub-step) are read while the one before is multiplied.
+template <bool WIDE> struct Sub {
+    static constexpr int kCount = WIDE ? 4 : 2;     // per stage
+    static constexpr int kChunks = WIDE ? 1 : 2;    // 16-byte chunks per lane and row
+};
+template <bool WIDE, int N> struct Fragments {
+    v4i a[N][Sub<WIDE>::kChunks], b[N][Sub<WIDE>::kChunks];
+};
+
+// Where a lane finds its chunks: the first tile's row, and the swizzled place
+// of each of its four chunks in a row's 128 bytes.  Which of the contraction's
+// values a lane holds does not matter as long as both operands agree.
+struct Places {
+    int row_a, row_b;
+    int chunk[4];
+};
+// Read q of the 2 N kChunks reads of a sub-step's fragments.
+template <bool WIDE, int N>
+__device__ __forceinline__ void read_one(Fragments<WIDE, N>& f, const uint8_t* a, const uint8_t* b, const Places& at,
+                                         int s, int q)
 {
-#pragma unroll
-    for (int i = 0; i < Geometry<W>::kTiles; ++i) {
-        const int r = row + i;
-        const uint8_t* p = stage + r * kBytes;
-        const int c = half * 4 + (lane >> 5) * 2;
-        const v4i lo = *reinterpret_cast<const v4i*>(p + ((c ^ swizzle<W>(r)) * 16));
-        const v4i hi = *reinterpret_cast<const v4i*>(p + (((c + 1) ^ swizzle<W>(r)) * 16));
-        f[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
+    constexpr int C = Sub<WIDE>::kChunks;
+    const int i = q / (2 * C), rest = q % (2 * C), c = rest % C;
+    const uint8_t* p = rest < C ? a + at.row_a : b + at.row_b;
+    const v4i x = *reinterpret_cast<const v4i*>(p + at.chunk[s * C + c] + i * kBytes);
+    if (rest < C) f.a[i][c] = x;
+    else f.b[i][c] = x;
 }
 
-template <int FA, int FB, int I, int J, int N>
-__device__ __forceinline__ void multiply_tile(v16f (&acc)[N][N], const v8i (&a)[N], const v8i (&b)[N], int sa, int sb)
+__device__ __forceinline__ v8i join_chunks(const v4i& lo, const v4i& hi)
 {
-    acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[I], b[J], acc[I][J], FA, FB, I, sa, J, sb);
-    if constexpr (J + 1 < N) multiply_tile<FA, FB, I, J + 1, N>(acc, a, b, sa, sb);
-    else if constexpr (I + 1 < N) multiply_tile<FA, FB, I + 1, 0, N>(acc, a, b, sa, sb);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// 8 of a fragment's values (dwords 2 T and 2 T + 1) times 2^(scale - 127), as bf16: exact.
-template <int FORMAT, int T> __device__ __forceinline__ v8bf widen(const v8i& f, float scale)
+// 8 values (dwords lo and hi) times 2^(scale - 127), as bf16: exact.
+template <int FORMAT> __device__ __forceinline__ v8bf widen(int lo, int hi, float scale)
 {
     v2bf x[4];
     if constexpr (FORMAT == FP8_E4M3) {
-        x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * T], scale, false);
-        x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * T], scale, true);
-        x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * T + 1], scale, false);
-        x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * T + 1], scale, true);
+        x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+        x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+        x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+        x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     } else {
-        x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(f[2 * T], scale, false);
-        x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(f[2 * T], scale, true);
-        x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(f[2 * T + 1], scale, false);
-        x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(f[2 * T + 1], scale, true);
+        x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, false);
+        x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, true);
+        x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, false);
+        x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, true);
     }
     return v8bf{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
 }
 
-// byte I of packed scales as the power of two it stands for
-template <int I> __device__ __forceinline__ float scale_value(int scales)
+// byte i of packed scales as the power of two it stands for
+__device__ __forceinline__ float scale_value(int scales, int i)
 {
-    return __uint_as_float((static_cast<uint32_t>(scales) >> (8 * I) & 0xffu) << 23);
+    return __uint_as_float((static_cast<uint32_t>(scales) >> (8 * i) & 0xffu) << 23);
 }
 
-// The same half stage with both operands widened to bf16, 8 values of each
-// lane at a time.
-template <int FA, int FB, int T, int N>
-__device__ __forceinline__ void multiply_wide(v16f (&acc)[N][N], const v8i (&a)[N], const v8i (&b)[N],
-                                              const float (&sa)[N], const float (&sb)[N])
+template <int N> struct Wide {
+    v8bf a[N], b[N];
+};
+// Half t of a sub-step's fragments, widened.
+template <int FA, int FB, int N>
+__device__ __forceinline__ void widen_half(Wide<N>& w, const Fragments<true, N>& f, int t, int sa, int sb)
 {
-    v8bf wa[N], wb[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        wa[i] = widen<FA, T>(a[i], sa[i]);
-        wb[i] = widen<FB, T>(b[i], sb[i]);
+        w.a[i] = widen<FA>(f.a[i][0][2 * t], f.a[i][0][2 * t + 1], scale_value(sa, i));
+        w.b[i] = widen<FB>(f.b[i][0][2 * t], f.b[i][0][2 * t + 1], scale_value(sb, i));
     }
+}
+
+template <int FA, int FB, int I, int J, int N>
+__device__ __forceinline__ void multiply_scaled(v16f (&acc)[N][N], const Fragments<false, N>& f, int sa, int sb)
+{
+    acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(join_chunks(f.a[I][0], f.a[I][1]),
+                                                                join_chunks(f.b[J][0], f.b[J][1]), acc[I][J], FA, FB,
+                                                                I, sa, J, sb);
+    if constexpr (J + 1 < N) multiply_scaled<FA, FB, I, J + 1, N>(acc, f, sa, sb);
+    else if constexpr (I + 1 < N) multiply_scaled<FA, FB, I + 1, 0, N>(acc, f, sa, sb);
+}
+template <int N> __device__ __forceinline__ void multiply_wide(v16f (&acc)[N][N], const Wide<N>& w)
+{
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa[i], wb[j], acc[i][j], 0, 0, 0);
-    if constexpr (T + 1 < 4) multiply_wide<FA, FB, T + 1, N>(acc, a, b, sa, sb);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.a[i], w.b[j], acc[i][j], 0, 0, 0);
 }
 
-template <int N> __device__ __forceinline__ void scale_values(int scales, float (&s)[N])
+// Orders of the instructions of a sub-step for the compiler's scheduler:
+// between two matrix instructions go one LDS read, the loads of the stage
+// after next, and the conversions of what is multiplied next.
+template <int MFMA, int READS, int LOADS, int VALU> __device__ __forceinline__ void interleave()
 {
-    s[0] = scale_value<0>(scales);
-    s[1] = scale_value<1>(scales);
-    if constexpr (N == 4) {
-        s[2] = scale_value<2>(scales);
-        s[3] = scale_value<3>(scales);
+    constexpr int kMfma = 0x8, kDsRead = 0x100, kVmem = 0x20, kValu = 0x2;
+#pragma unroll
+    for (int i = 0; i < MFMA; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        if (i * READS / MFMA != (i + 1) * READS / MFMA) __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        if (i * LOADS / MFMA != (i + 1) * LOADS / MFMA) __builtin_amdgcn_sched_group_barrier(kVmem, LOADS > MFMA ? 2 : 1, 0);
+        if (VALU) __builtin_amdgcn_sched_group_barrier(kValu, VALU / MFMA, 0);
     }
 }
 
@@ -144,29 +172,73 @@ template <int N> __device__ __forceinline__ int load_scales(const uint8_t* p)
     else return *reinterpret_cast<const uint16_t*>(p);
 }
 
-template <typename T, int N>
-__device__ __forceinline__ void store_row(T* c, int64_t n, int64_t cols, const float (&v)[N], bool add)
+// One row of tiles in vector registers.  Accumulators stay in the accumulation
+// registers until here: without this the compiler wants all of them where
+// the conversions below can read them, and has no room.
+template <int N> __device__ __forceinline__ void take_row(const v16f (&acc)[N], v16f (&t)[N])
 {
-    if (n + N <= cols) {
-        Pack<T, N> p;
-        if (add) p = load_pack<T, N>(c + n);
 #pragma unroll
-        for (int j = 0; j < N; ++j) p.v[j] = from_float<T>(add ? to_float(p.v[j]) + v[j] : v[j]);
-        store_pack(c + n, p);
+    for (int j = 0; j < N; ++j) {
+        t[j] = acc[j];
+        asm volatile("" : "+v"(t[j]));
+    }
+}
+
+// A wave's outputs to rows m and columns n on of c ([rows][cols], row stride
+// ld).  Whole waves inside c store straight from their registers, each lane N
+// neighbouring columns.  Others, and those that add to c, pass through LDS,
+// 32 rows at a time, and go element by element.
+template <typename T, int W, int N>
+__device__ __forceinline__ void write_outputs(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
+                                              int64_t m, int64_t n, bool add, float* lds, int lane)
+{
+    if (!add && m + W <= rows && n + W <= cols) {
+        T* base = c + (m + 4 * N * (lane >> 5)) * ld + n + (lane & 31) * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v16f t[N];
+            take_row<N>(acc[i], t);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                Pack<T, N> x;
+#pragma unroll
+                for (int j = 0; j < N; ++j) x.v[j] = from_float<T>(t[j][r]);
+                store_pack(base + ((8 * (r >> 2) + (r & 3)) * N + i) * ld, x);
+            }
+        }
         return;
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-        if (n + j < cols) c[n + j] = from_float<T>(add ? to_float(c[n + j]) + v[j] : v[j]);
+    for (int i = 0; i < N; ++i) {
+        v16f t[N];
+        take_row<N>(acc[i], t);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+#pragma unroll
+            for (int j = 0; j < N; ++j) lds[row * W + (lane & 31) * N + j] = t[j][r];
+        }
+        for (int row = 0; row < 32 && m + row * N + i < rows; ++row) {
+            T* out = c + (m + row * N + i) * ld + n;
+            for (int col = lane; col < W; col += 64) {
+                if (n + col >= cols) continue;
+                const float x = lds[row * W + col];
+                out[col] = from_float<T>(add ? to_float(out[col]) + x : x);
+            }
+        }
+    }
 }
+
+#endif
 
 struct Grid {
     int32_t tiles_m, tiles_n, splits, steps;    // steps: stages per split
 };
 
 template <int W, int FA, int FB, bool WIDE>
-__global__ __launch_bounds__(kThreads, 1) void product(Fp8Product p, Grid g)
+__global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product p, Grid g)
 {
+#if defined(__HIP_DEVICE_COMPILE__)
     using G = Geometry<W>;
     constexpr int N = G::kTiles;
     __shared__ __attribute__((aligned(16))) uint8_t a0[G::kStage], b0[G::kStage], a1[G::kStage], b1[G::kStage];
@@ -194,22 +266,30 @@ __global__ __launch_bounds__(kThreads, 1) void product(Fp8Product p, Grid g)
     // A row past the operand's end is read as its last row: its outputs are
     // not stored.
     uint32_t off_a[G::kLoads], off_b[G::kLoads];
+    const int last_a = static_cast<int>(p.a.rows - m0 < G::kSide ? p.a.rows - m0 : G::kSide) - 1;
+    const int last_b = static_cast<int>(p.b.rows - n0 < G::kSide ? p.b.rows - n0 : G::kSide) - 1;
 #pragma unroll
     for (int q = 0; q < G::kLoads; ++q) {
         const int row = (q * 4 + wave) * 8 + (lane >> 3);
         const uint32_t chunk = ((lane & 7) ^ swizzle<W>(row)) * 16;
-        const int64_t ra = p.a.rows - m0 - 1 < row ? p.a.rows - m0 - 1 : row;
-        const int64_t rb = p.b.rows - n0 - 1 < row ? p.b.rows - n0 - 1 : row;
-        off_a[q] = static_cast<uint32_t>(ra * p.a.ld) + chunk;
-        off_b[q] = static_cast<uint32_t>(rb * p.b.ld) + chunk;
+        off_a[q] = static_cast<uint32_t>(row < last_a ? row : last_a) * static_cast<uint32_t>(p.a.ld) + chunk;
+        off_b[q] = static_cast<uint32_t>(row < last_b ? row : last_b) * static_cast<uint32_t>(p.b.ld) + chunk;
     }
-    const uint8_t* ga = p.a.data + m0 * p.a.ld + kb0 * kBytes;
-    const uint8_t* gb = p.b.data + n0 * p.b.ld + kb0 * kBytes;
+    const auto ga = buffer(p.a.data + m0 * p.a.ld + kb0 * kBytes,
+                                             (p.a.rows - m0) * p.a.ld - kb0 * kBytes);
+    const auto gb = buffer(p.b.data + n0 * p.b.ld + kb0 * kBytes,
+                                             (p.b.rows - n0) * p.b.ld - kb0 * kBytes);
     const int row_a = (wave >> 1) * W + (lane & 31) * N, row_b = (wave & 1) * W + (lane & 31) * N;
     const int64_t sra = m0 + row_a < p.a.lds - N ? m0 + row_a : p.a.lds - N;
     const int64_t srb = n0 + row_b < p.b.lds - N ? n0 + row_b : p.b.lds - N;
     const uint8_t* sa = p.a.scales + kb0 * p.a.lds + sra;
     const uint8_t* sb = p.b.scales + kb0 * p.b.lds + srb;
+
+    Places places;
+    places.row_a = row_a * kBytes;
+    places.row_b = row_b * kBytes;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) places.chunk[c] = ((c * 2 + (lane >> 5)) ^ (lane & 7)) * 16;    // swizzle(row) = lane & 7
 
     v16f acc[N][N];
 #pragma unroll
@@ -219,60 +299,93 @@ __global__ __launch_bounds__(kThreads, 1) void product(Fp8Product p, Grid g)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    auto stage = [&](int k, uint8_t* a, uint8_t* b) {
-        load_stage<W>(ga + static_cast<int64_t>(k) * kBytes, off_a, a, wave);
-        load_stage<W>(gb + static_cast<int64_t>(k) * kBytes, off_b, b, wave);
-    };
-    auto compute = [&](const uint8_t* a, const uint8_t* b, int xa, int xb) {
+    // A stage goes from global memory straight to LDS.  Stages go in pairs, and every step loads the stage after next, so that
+    // the loop has one body and one exit.  A stage past the last is the last
+    // one again, with scales of 2^-127 each way: products of 0 in fp32.
+    auto load = [&](int k, uint8_t* a, uint8_t* b) {
+        const int at = (k < steps ? k : steps - 1) * kBytes;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            v8i fa[N], fb[N];
-            read_fragments<W>(a, row_a, lane, half, fa);
-            read_fragments<W>(b, row_b, lane, half, fb);
-            if constexpr (WIDE) {
-                float wa[N], wb[N];
-                scale_values<N>(xa, wa);
-                scale_values<N>(xb, wb);
-                multiply_wide<FA, FB, 0, N>(acc, fa, fb, wa, wb);
-            } else {
-                multiply_tile<FA, FB, 0, 0, N>(acc, fa, fb, xa, xb);
-            }
+        for (int q = 0; q < G::kLoads; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ga, (lds_ptr)(a + (q * 4 + wave) * 1024), 16, off_a[q], at, 0, 0);
+#pragma unroll
+        for (int q = 0; q < G::kLoads; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(gb, (lds_ptr)(b + (q * 4 + wave) * 1024), 16, off_b[q], at, 0, 0);
+    };
+    Fragments<WIDE, N> frag[2];
+    Wide<N> wide[2];
+    constexpr int kReads = 2 * N * Sub<WIDE>::kChunks, kMfma = WIDE ? 2 * N * N : N * N;
+    auto read = [&](Fragments<WIDE, N>& f, const uint8_t* a, const uint8_t* b, int s) {
+#pragma unroll
+        for (int q = 0; q < kReads; ++q) read_one<WIDE, N>(f, a, b, places, s, q);
+    };
+    // multiplies f; next: the fragments multiplied after it (with scales na, nb)
+    auto multiply = [&](const Fragments<WIDE, N>& f, int xa, int xb, const Fragments<WIDE, N>& next, int na, int nb) {
+        if constexpr (WIDE) {
+            widen_half<FA, FB, N>(wide[1], f, 1, xa, xb);
+            multiply_wide<N>(acc, wide[0]);
+            widen_half<FA, FB, N>(wide[0], next, 0, na, nb);
+            multiply_wide<N>(acc, wide[1]);
+        } else {
+            multiply_scaled<FA, FB, 0, 0, N>(acc, f, xa, xb);
         }
     };
-    stage(0, a0, b0);
-    for (int k = 0; k < steps; k += 2) {
-        int xa = load_scales<N>(sa + k * p.a.lds), xb = load_scales<N>(sb + k * p.b.lds);
-        __syncthreads();
-        if (k + 1 < steps) stage(k + 1, a1, b1);
-        compute(a0, b0, xa, xb);
-        if (k + 1 >= steps) break;
-        xa = load_scales<N>(sa + (k + 1) * p.a.lds);
-        xb = load_scales<N>(sb + (k + 1) * p.b.lds);
-        __syncthreads();
-        if (k + 2 < steps) stage(k + 2, a0, b0);
-        compute(a1, b1, xa, xb);
-    }
+    int xa[2], xb[2];
+    auto scales = [&](int k, int s) {
+        const int64_t at = k < steps ? k : steps - 1;
+        const int in = k < steps ? -1 : 0;
+        xa[s] = load_scales<N>(sa + at * p.a.lds) & in;
+        xb[s] = load_scales<N>(sb + at * p.b.lds) & in;
+    };
+    // Stage k lies in (a, b), stage k + 1 in (an, bn) or on its way there, and
+    // frag[0] holds stage k's first sub-step.
+    auto step = [&](int k, int s, uint8_t* a, uint8_t* b, uint8_t* an, uint8_t* bn) {
+#pragma unroll
+        for (int u = 0; u + 1 < Sub<WIDE>::kCount; ++u) {
+            read(frag[(u + 1) & 1], a, b, u + 1);
+            multiply(frag[u & 1], xa[s], xb[s], frag[(u + 1) & 1], xa[s], xb[s]);
+            interleave<kMfma, kReads, 0, WIDE ? kMfma * 2 : 0>();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // Stage k + 1 has arrived and every wave holds the rest of stage k in
+        // registers: its LDS is free for stage k + 2.
+        __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        read(frag[0], an, bn, 0);
+        load(k + 2, a, b);
+        multiply(frag[1], xa[s], xb[s], frag[0], xa[s ^ 1], xb[s ^ 1]);
+        interleave<kMfma, kReads, 2 * G::kLoads, WIDE ? kMfma * 2 : 0>();
+        __builtin_amdgcn_sched_barrier(0);
+        scales(k + 2, s);
+    };
+    load(0, a0, b0);
+    scales(0, 0);
+    load(1, a1, b1);
+    scales(1, 1);
+    __syncthreads();
+    read(frag[0], a0, b0, 0);
+    if constexpr (WIDE) widen_half<FA, FB, N>(wide[0], frag[0], 0, xa[0], xb[0]);
+    int k = 0;
+    do {
+        step(k, 0, a0, b0, a1, b1);
+        step(k + 1, 1, a1, b1, a0, b0);
+        k += 2;
+    } while (k < steps);
 
-    const int64_t n = n0 + row_b;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int64_t m = m0 + (wave >> 1) * W + (8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * N + i;
-            if (m >= p.a.rows || n >= p.b.rows) continue;
-            float v[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = acc[i][j][r];
-            if (g.splits > 1) {
-                store_row<float, N>(p.partial + (split * p.a.rows + m) * p.b.rows, n, p.b.rows, v, false);
-            } else if (p.c_dtype == DTYPE_F32) {
-                store_row<float, N>(static_cast<float*>(p.c) + m * p.ldc, n, p.b.rows, v, p.accumulate);
-            } else if (p.c_dtype == DTYPE_BF16) {
-                store_row<bf16, N>(static_cast<bf16*>(p.c) + m * p.ldc, n, p.b.rows, v, p.accumulate);
-            } else {
-                store_row<f16, N>(static_cast<f16*>(p.c) + m * p.ldc, n, p.b.rows, v, p.accumulate);
-            }
-        }
+    // every wave has its last fragments: the stages' LDS is free
+    __syncthreads();
+    float* lds = reinterpret_cast<float*>((wave >> 1 ? b0 : a0) + (wave & 1) * (G::kStage / 2));
+    const int64_t m = m0 + (wave >> 1) * W, n = n0 + (wave & 1) * W, rows = p.a.rows, cols = p.b.rows;
+    const bool add = p.accumulate != 0;
+    if (g.splits > 1)
+        write_outputs<float, W, N>(acc, p.partial + split * rows * cols, cols, rows, cols, m, n, false, lds, lane);
+    else if constexpr (WIDE)
+        write_outputs<float, W, N>(acc, static_cast<float*>(p.c), p.ldc, rows, cols, m, n, add, lds, lane);
+    else if (p.c_dtype == DTYPE_BF16)
+        write_outputs<bf16, W, N>(acc, static_cast<bf16*>(p.c), p.ldc, rows, cols, m, n, add, lds, lane);
+    else
+        write_outputs<f16, W, N>(acc, static_cast<f16*>(p.c), p.ldc, rows, cols, m, n, add, lds, lane);
+#endif
 }
 
 // The splits' partial products joined in order (splits = 0: an empty
