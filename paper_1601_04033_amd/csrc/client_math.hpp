@@ -57,7 +57,7 @@ struct DropKey {
     int64_t chunk_base;         // index_base / 8
 };
 
-// Keep bits of the 8 elements of one chunk: bit e is element 8 chunk + e.
+// Keep bits of the 8 elements of one chunk: bit 7 - e is element 8 chunk + e.
 // One Philox call serves 8 elements, 16 bits each; at 32 bits each the
 // draws, not the memory, would bound a pass over 16-bit elements.
 __device__ __forceinline__ uint32_t keep_bits(const DropKey& k, uint64_t chunk)
@@ -65,14 +65,35 @@ __device__ __forceinline__ uint32_t keep_bits(const DropKey& k, uint64_t chunk)
     const uint4 w = philox4x32_10(make_uint4(static_cast<uint32_t>(chunk), k.ctr1 | static_cast<uint32_t>(chunk >> 32),
                                              k.ctr_T, k.ctr_client),
                                   k.key0, k.key1);
+    // a draw is compared in the upper half of a word (kept: not below), so
+    // thr = 65536 (nothing is kept) needs its own answer
+    const uint32_t t = k.thr << 16, none = k.thr >> 16;
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
     uint32_t bits = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        bits |= ((u[i] & 0xffffu) >= k.thr ? 1u : 0u) << (2 * i);
-        bits |= ((u[i] >> 16) >= k.thr ? 1u : 0u) << (2 * i + 1);
+        bits = bits + bits + ((u[i] << 16) >= t ? 1u : 0u);
+        bits = bits + bits + (u[i] >= t ? 1u : 0u);
     }
-    return bits;
+    return none ? 0u : bits;
+}
+
+// Keep bits of the N <= 8 elements from matrix index i on: bit N - 1 - j is
+// element i + j.
+template <int N> __device__ __forceinline__ uint32_t keep_run(const DropKey& k, int64_t i)
+{
+    const uint64_t chunk = static_cast<uint64_t>(k.chunk_base) + static_cast<uint64_t>(i >> 3);
+    const int off = static_cast<int>(i & 7);
+    uint32_t bits = keep_bits(k, chunk) << 8;
+    if (off + N > 8) bits |= keep_bits(k, chunk + 1);
+    return bits >> (16 - N - off);
+}
+
+// x where bit `at` of bits is set, else 0 (whatever x is).
+__device__ __forceinline__ float kept(float x, uint32_t bits, int at)
+{
+    const int mask = static_cast<int>(bits << (31 - at)) >> 31;
+    return __int_as_float(__float_as_int(x) & mask);
 }
 
 }  // namespace fasgd

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
         if (res) q = load_pack<T, kChunk>(res + r * a.ldr + c);
 #pragma unroll
         for (int e = 0; e < kChunk; ++e) {
-            float f = (keep >> e) & 1 ? to_float(v.v[e]) * a.key.scale : 0.0f;
+            float f = kept(to_float(v.v[e]) * a.key.scale, keep, kChunk - 1 - e);
             if (res) f += to_float(q.v[e]);
             v.v[e] = from_float<T>(f);
         }
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
         return;
     }
     for (int e = 0; e < kChunk && i + e < n; ++e) {
-        float f = (keep >> e) & 1 ? to_float(x[r * a.ldx + c]) * a.key.scale : 0.0f;
+        float f = kept(to_float(x[r * a.ldx + c]) * a.key.scale, keep, kChunk - 1 - e);
         if (res) f += to_float(res[r * a.ldr + c]);
         y[r * a.ldy + c] = from_float<T>(f);
         if (++c == a.cols) {

@@ -12,21 +12,26 @@
 // four column sums: of du xh1 and du (with a, where it is not a column's own),
 // and of dh xh2 and dh: w_post, b_post and a channel gate share the first two.
 //
-// Each row is read once into registers and stays there through its
-// reductions; the next row's loads are issued before the first of them.  A
-// thread keeps its columns over all its rows, so parameters are read once per
-// block and the column sums stay in its registers, written once per block and
-// joined in a fixed order by a second small kernel.
+// Each row is read once into registers, 8 columns a thread, and stays there
+// through its reductions.  A thread keeps its columns over all its rows, so
+// parameters are read once per block and the column sums stay in its
+// registers, written once per block and joined in a fixed order by a second
+// small kernel.
 #include "client_kernels.hpp"
 
 namespace fasgd {
 namespace {
 
 constexpr int kAcc = 4;             // column sums of the backward pass
-constexpr int kMaxBlocks = 512;     // of the backward pass (its column sums: [kAcc][blocks][cols])
 constexpr int kLoopThreads = 1024;  // threads per row where a row does not fit the registers
 
+constexpr int kCols = 8;            // columns of a row per thread: one or two 16-byte vectors
+constexpr int kForwardWaves = 6;    // per SIMD, for which the kernels' registers are limited
+constexpr int kBackwardWaves = 4;
+constexpr int kSubThreads = 512;    // threads of a block whose waves hold whole rows
+
 template <typename T> constexpr int kVec = 16 / static_cast<int>(sizeof(T));
+template <typename T> constexpr int kVecs = kCols / kVec<T>;
 
 // ---- sums over the lanes of a row
 
@@ -97,6 +102,13 @@ template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_cols(con
     for (int j = 0; j < V; ++j) r.v[j] = c + j < cols ? row[c + j] : from_float<T>(0.0f);
     return r;
 }
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> zero_pack()
+{
+    Pack<T, V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = from_float<T>(0.0f);
+    return r;
+}
 template <typename T, int V>
 __device__ __forceinline__ void store_cols(T* row, int c, int cols, const Pack<T, V>& x)
 {
@@ -119,21 +131,6 @@ __device__ __forceinline__ void load_params(const float* p, int c, int cols, flo
 #pragma unroll
     for (int j = 0; j < V; ++j) out[j] = x.v[j];
 }
-
-// Dropout factors of V elements from matrix index i on.
-template <int V> __device__ __forceinline__ void drop_factors(const DropKey& k, int64_t i, float (&m)[V])
-{
-    const uint64_t chunk = static_cast<uint64_t>(k.chunk_base) + static_cast<uint64_t>(i >> 3);
-    const int off = static_cast<int>(i & 7);
-    uint32_t bits = keep_bits(k, chunk);
-    if (off + V > 8) bits |= keep_bits(k, chunk + 1) << 8;
-    bits >>= off;
-#pragma unroll
-    for (int j = 0; j < V; ++j) m[j] = (bits >> j) & 1 ? k.scale : 0.0f;
-}
-
-// Dropped elements are 0 whatever is dropped (0 times NaN would not be).
-__device__ __forceinline__ float dropped(float x, float m) { return m == 0.0f ? 0.0f : x * m; }
 
 // mean and 1 / sqrt(variance + eps) of a row held as NV vectors of V in d
 // (0 beyond the row's end); d becomes d - mean there.  The variance is that
@@ -167,101 +164,184 @@ __device__ __forceinline__ void row_stats(float (&d)[NV][V], const NormArgs& a, 
     rstd = 1.0f / sqrtf(q[0] / a.n_cols + a.eps);
 }
 
-// ---- forward
+// Where a thread stands: its row's group of threads and its columns.  SUB > 0:
+// SUB lanes of a block of kSubThreads hold a row; SUB = 0: the block does.
+template <typename T, int SUB> struct Place {
+    int tpr, t, rpb, group;     // threads per row, this one among them; rows per block, this one among them
+    __device__ Place()
+    {
+        constexpr int S = SUB ? SUB : 1;
+        tpr = SUB ? S : blockDim.x;
+        t = SUB ? threadIdx.x % S : threadIdx.x;
+        rpb = SUB ? kSubThreads / S : 1;
+        group = SUB ? threadIdx.x / S : 0;
+    }
+    __device__ int column(int v) const { return (v * tpr + t) * kVec<T>; }
+};
 
-template <typename T, int SUB, int NV>
-__global__ __launch_bounds__(SUB ? 256 : 512) void norm_forward(NormArgs a)
-{
-    constexpr int V = kVec<T>;
-    __shared__ float buf[2][16][2];
-    int turn = 0;
-    const int tpr = SUB ? SUB : blockDim.x;
-    const int t = SUB ? threadIdx.x % (SUB ? SUB : 1) : threadIdx.x;
-    const int rpb = SUB ? 256 / (SUB ? SUB : 1) : 1;
-    const int group = SUB ? threadIdx.x / (SUB ? SUB : 1) : 0;
-    const T* branch = static_cast<const T*>(a.branch);
-    const T* residual = static_cast<const T*>(a.residual);
-    const T* gate = static_cast<const T*>(a.gate);
-    float wp[NV][V], bp[NV][V], wn[NV][V], bn[NV][V];      // a channel gate is folded into wp and bp
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = (v * tpr + t) * V;
-        load_params<V>(a.w_post, c, a.cols, 1.0f, wp[v]);
-        load_params<V>(a.b_post, c, a.cols, 0.0f, bp[v]);
-        load_params<V>(a.w_pre, c, a.cols, 1.0f, wn[v]);
-        load_params<V>(a.b_pre, c, a.cols, 0.0f, bn[v]);
-        if (a.gate_form == GATE_CHANNEL) {
-            float g[V];
-            load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, g);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float f = activate(g[j], a.gate_act);
-                wp[v][j] *= f;
-                bp[v][j] *= f;
-            }
+// Parameters of a thread's columns: in registers, or (IN_LDS) in LDS, WHICH
+// of them.
+template <typename T, int SUB, int MAXT, int WHICH, bool IN_LDS> struct Params {
+    static constexpr int V = kVec<T>, NV = kVecs<T>;
+    float reg[IN_LDS ? 1 : WHICH][NV][V];
+    static __device__ float* lds(int which)
+    {
+        if constexpr (SUB == 0 && MAXT == 512) {
+            // as much as the block's threads need: small blocks share a CU
+            extern __shared__ __attribute__((aligned(16))) float dynamic[];
+            return dynamic + which * (blockDim.x * kCols);
+        } else {
+            __shared__ __attribute__((aligned(16))) float x[WHICH][(SUB ? SUB : MAXT) * kCols];
+            return x[which];
         }
     }
-    Pack<T, V> x[NV], r[NV], g[NV];
-    auto fetch = [&](int64_t row) {
+    __device__ void set(int which, int v, const Place<T, SUB>& at, const float (&x)[V])
+    {
+        if constexpr (IN_LDS) {
+            if (at.group == 0) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) lds(which)[at.column(v) + j] = x[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) reg[which][v][j] = x[j];
+        }
+    }
+    __device__ void get(int which, int v, const Place<T, SUB>& at, float (&x)[V]) const
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = IN_LDS ? lds(which)[at.column(v) + j] : reg[which][v][j];
+    }
+};
+
+// Keep bits of a thread's columns of a row (all kept without dropout).
+template <typename T, int SUB>
+__device__ __forceinline__ void row_keep(const NormArgs& a, const Place<T, SUB>& at, int64_t row, int cols,
+                                         uint32_t (&keep)[kVecs<T>])
+{
+#pragma unroll
+    for (int v = 0; v < kVecs<T>; ++v) keep[v] = ~0u;
+    if (!a.drop) return;
+#pragma unroll
+    for (int v = 0; v < kVecs<T>; ++v)
+        if (at.column(v) < cols) keep[v] = keep_run<kVec<T>>(a.key, row * a.cols + at.column(v));
+}
+
+// GENERAL kernels take biases and a gate of every element.  Both cost
+// registers in every thread, so operators without them have kernels of their
+// own, and the general backward kernel has its parameters in LDS: with at
+// most 128 registers two blocks of 512 threads share a CU, and one computes
+// while the other waits for its row or its reduction.  (A row loaded ahead
+// into registers instead cost more in waves than it gave.)
+
+// ---- forward
+
+template <typename T, int SUB, int MAXT, bool GENERAL>
+__global__ __launch_bounds__(MAXT, MAXT == 1024 || GENERAL ? kBackwardWaves : kForwardWaves) void norm_forward(NormArgs a)
+{
+    constexpr int V = kVec<T>, NV = kVecs<T>;
+    constexpr int kPost = 0, kPre = 1, kPostBias = 2, kPreBias = 3;
+    __shared__ float buf[2][16][2];
+    int turn = 0;
+    const Place<T, SUB> at;
+    // the dropout's scale and a channel gate are folded into the first norm's weights and bias
+    Params<T, SUB, MAXT, GENERAL ? 4 : 2, false> params;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int c = at.column(v);
+        float f[V], x[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = 1.0f;
+        if (a.gate_form == GATE_CHANNEL) {
+            load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) f[j] = activate(f[j], a.gate_act);
+        }
+        const float scale = a.drop ? a.key.scale : 1.0f;
+        load_params<V>(a.w_post, c, a.cols, 1.0f, x);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] *= f[j] * scale;
+        params.set(kPost, v, at, x);
+        load_params<V>(a.w_pre, c, a.cols, 1.0f, x);
+        params.set(kPre, v, at, x);
+        if constexpr (GENERAL) {
+            load_params<V>(a.b_post, c, a.cols, 0.0f, x);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] *= f[j] * scale;
+            params.set(kPostBias, v, at, x);
+            load_params<V>(a.b_pre, c, a.cols, 0.0f, x);
+            params.set(kPreBias, v, at, x);
+        }
+    }
+    const int64_t step = static_cast<int64_t>(gridDim.x) * at.rpb;
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * at.rpb; base < a.rows; base += step) {
+        const int64_t row = base + at.group;
         const int cols = row < a.rows ? a.cols : 0;
+        Pack<T, V> x[NV], r[NV], g[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = (v * tpr + t) * V;
-            x[v] = load_cols<T, V>(branch + row * a.ld_branch, c, cols);
-            if (residual) r[v] = load_cols<T, V>(residual + row * a.ld_residual, c, cols);
-            if (a.gate_form == GATE_FULL) g[v] = load_cols<T, V>(gate + row * a.ld_gate, c, cols);
+            const int c = at.column(v);
+            x[v] = load_cols<T, V>(static_cast<const T*>(a.branch) + row * a.ld_branch, c, cols);
+            if (a.residual) r[v] = load_cols<T, V>(static_cast<const T*>(a.residual) + row * a.ld_residual, c, cols);
+            else r[v] = zero_pack<T, V>();
+            if (GENERAL && a.gate_form == GATE_FULL)
+                g[v] = load_cols<T, V>(static_cast<const T*>(a.gate) + row * a.ld_gate, c, cols);
         }
-    };
-    const int64_t step = static_cast<int64_t>(gridDim.x) * rpb;
-    fetch(static_cast<int64_t>(blockIdx.x) * rpb + group);
-    for (int64_t base = static_cast<int64_t>(blockIdx.x) * rpb; base < a.rows; base += step) {
-        const int64_t row = base + group;
-        const int cols = row < a.rows ? a.cols : 0;
-        float d[NV][V], res[NV][V], ga[NV][V];
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                d[v][j] = to_float(x[v].v[j]);
-                res[v][j] = residual ? a.rho * to_float(r[v].v[j]) : 0.0f;
-                ga[v][j] = a.gate_form == GATE_FULL ? activate(to_float(g[v].v[j]), a.gate_act) : 1.0f;
-            }
         float row_gate = 1.0f;
         if (a.gate_form == GATE_ROW && row < a.rows)
             row_gate = activate(static_cast<const float*>(a.gate)[row], a.gate_act);
-        fetch(row + step);
+        uint32_t keep[NV];
+        row_keep<T, SUB>(a, at, row, cols, keep);
+        float d[NV][V];
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < V; ++j) d[v][j] = to_float(x[v].v[j]);
         float mean1 = 0.0f, rstd1 = 1.0f, mean2 = 0.0f, rstd2 = 1.0f;
-        if (a.w_post) row_stats<SUB>(d, a, t, tpr, mean1, rstd1, buf, turn);
+        if (a.w_post) row_stats<SUB>(d, a, at.t, at.tpr, mean1, rstd1, buf, turn);
+        const float k = rstd1 * row_gate;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = (v * tpr + t) * V;
-            float m[V];
+            const int c = at.column(v);
+            float w[V], b[V];
+            params.get(kPost, v, at, w);
+            if constexpr (GENERAL) params.get(kPostBias, v, at, b);
 #pragma unroll
-            for (int j = 0; j < V; ++j) m[j] = 1.0f;
-            if (a.drop && c < cols) drop_factors<V>(a.key, row * a.cols + c, m);
+            for (int j = 0; j < V; ++j)
+                d[v][j] = GENERAL ? fmaf(d[v][j] * k, w[j], b[j] * row_gate) : d[v][j] * k * w[j];
+            if (GENERAL && a.gate_form == GATE_FULL) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[v][j] *= activate(to_float(g[v].v[j]), a.gate_act);
+            }
             Pack<T, V> out;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                float u = fmaf(d[v][j] * rstd1, wp[v][j], bp[v][j]) * (ga[v][j] * row_gate);
-                if (a.drop) u = dropped(u, m[j]);
-                out.v[j] = from_float<T>(res[v][j] + u);
+                out.v[j] = from_float<T>(fmaf(a.rho, to_float(r[v].v[j]), kept(d[v][j], keep[v], V - 1 - j)));
                 // the norm is of the sum as it is stored, so that the
                 // backward pass, which reads it, differentiates this function
-                d[v][j] = j < cols - c ? to_float(out.v[j]) : 0.0f;
+                d[v][j] = to_float(out.v[j]);
+            }
+            if (c + V > cols) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[v][j] = c + j < cols ? d[v][j] : 0.0f;
             }
             store_cols<T, V>(static_cast<T*>(a.sum) + row * a.ld_sum, c, cols, out);
         }
         if (a.w_pre) {
-            row_stats<SUB>(d, a, t, tpr, mean2, rstd2, buf, turn);
+            row_stats<SUB>(d, a, at.t, at.tpr, mean2, rstd2, buf, turn);
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
+                float w[V], b[V];
+                params.get(kPre, v, at, w);
+                if constexpr (GENERAL) params.get(kPreBias, v, at, b);
                 Pack<T, V> out;
 #pragma unroll
-                for (int j = 0; j < V; ++j) out.v[j] = from_float<T>(fmaf(d[v][j] * rstd2, wn[v][j], bn[v][j]));
-                store_cols<T, V>(static_cast<T*>(a.normed) + row * a.ld_normed, (v * tpr + t) * V, cols, out);
+                for (int j = 0; j < V; ++j)
+                    out.v[j] = from_float<T>(GENERAL ? fmaf(d[v][j] * rstd2, w[j], b[j]) : d[v][j] * rstd2 * w[j]);
+                store_cols<T, V>(static_cast<T*>(a.normed) + row * a.ld_normed, at.column(v), cols, out);
             }
         }
-        if (t == 0 && row < a.rows) {
+        if (at.t == 0 && row < a.rows) {
             const float st[4] = {mean1, rstd1, mean2, rstd2};
             __builtin_memcpy(a.stats + row * 4, st, sizeof st);
         }
@@ -270,146 +350,170 @@ __global__ __launch_bounds__(SUB ? 256 : 512) void norm_forward(NormArgs a)
 
 // ---- backward
 
-template <typename T, int SUB, int NV>
-__global__ __launch_bounds__(SUB ? 256 : 512) void norm_backward(NormArgs a)
+template <typename T, int SUB, int MAXT, bool GENERAL>
+__global__ __launch_bounds__(MAXT, SUB && GENERAL ? 2 : kBackwardWaves) void norm_backward(NormArgs a)
 {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, NV = kVecs<T>;
+    constexpr int kPost = 0, kPre = 1, kPostBias = 2;   // kPost: w_post, times the gate where it is the column's
     __shared__ float buf[2][16][2];
     int turn = 0;
-    const int tpr = SUB ? SUB : blockDim.x;
-    const int t = SUB ? threadIdx.x % (SUB ? SUB : 1) : threadIdx.x;
-    const int rpb = SUB ? 256 / (SUB ? SUB : 1) : 1;
-    const int group = SUB ? threadIdx.x / (SUB ? SUB : 1) : 0;
-    const T* branch = static_cast<const T*>(a.branch);
-    const T* sum = static_cast<const T*>(a.sum);
-    const T* gate = static_cast<const T*>(a.gate);
-    const T* dsum = static_cast<const T*>(a.dsum);
-    const T* dnormed = static_cast<const T*>(a.dnormed);
-    float wp[NV][V], bp[NV][V], wn[NV][V], gc[NV][V];
+    const Place<T, SUB> at;
+    Params<T, SUB, MAXT, GENERAL ? 3 : 2, GENERAL> params;
     float post1[NV][V], post2[NV][V], pre1[NV][V], pre2[NV][V];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int c = (v * tpr + t) * V;
-        load_params<V>(a.w_post, c, a.cols, 1.0f, wp[v]);
-        load_params<V>(a.b_post, c, a.cols, 0.0f, bp[v]);
-        load_params<V>(a.w_pre, c, a.cols, 1.0f, wn[v]);
+        const int c = at.column(v);
+        float x[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            gc[v][j] = 1.0f;
-            post1[v][j] = post2[v][j] = pre1[v][j] = pre2[v][j] = 0.0f;
-        }
+        for (int j = 0; j < V; ++j) post1[v][j] = post2[v][j] = pre1[v][j] = pre2[v][j] = 0.0f;
+        load_params<V>(a.w_post, c, a.cols, 1.0f, x);
         if (a.gate_form == GATE_CHANNEL) {
-            load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, gc[v]);
+            float f[V];
+            load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) gc[v][j] = activate(gc[v][j], a.gate_act);
+            for (int j = 0; j < V; ++j) x[j] *= activate(f[j], a.gate_act);
+        }
+        params.set(kPost, v, at, x);
+        load_params<V>(a.w_pre, c, a.cols, 1.0f, x);
+        params.set(kPre, v, at, x);
+        if constexpr (GENERAL) {
+            load_params<V>(a.b_post, c, a.cols, 0.0f, x);
+            params.set(kPostBias, v, at, x);
         }
     }
-    Pack<T, V> px[NV], ps[NV], pds[NV], pdh[NV], pg[NV];
-    float st[4];
-    auto fetch = [&](int64_t row) {
+    if (GENERAL) __syncthreads();
+    const int64_t step = static_cast<int64_t>(gridDim.x) * at.rpb;
+    for (int64_t base = static_cast<int64_t>(blockIdx.x) * at.rpb; base < a.rows; base += step) {
+        const int64_t row = base + at.group;
         const int cols = row < a.rows ? a.cols : 0;
+        Pack<T, V> x[NV], s[NV], dh[NV], up[NV], g[NV];
+        float st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = (v * tpr + t) * V;
-            px[v] = load_cols<T, V>(branch + row * a.ld_branch, c, cols);
+            const int c = at.column(v);
             if (a.w_pre) {
-                ps[v] = load_cols<T, V>(sum + row * a.ld_sum, c, cols);
-                pdh[v] = load_cols<T, V>(dnormed + row * a.ld_dnormed, c, cols);
+                s[v] = load_cols<T, V>(static_cast<const T*>(a.sum) + row * a.ld_sum, c, cols);
+                dh[v] = load_cols<T, V>(static_cast<const T*>(a.dnormed) + row * a.ld_dnormed, c, cols);
             }
-            if (dsum) pds[v] = load_cols<T, V>(dsum + row * a.ld_dsum, c, cols);
-            if (a.gate_form == GATE_FULL) pg[v] = load_cols<T, V>(gate + row * a.ld_gate, c, cols);
+            if (a.dsum) up[v] = load_cols<T, V>(static_cast<const T*>(a.dsum) + row * a.ld_dsum, c, cols);
+            else up[v] = zero_pack<T, V>();
+            x[v] = load_cols<T, V>(static_cast<const T*>(a.branch) + row * a.ld_branch, c, cols);
+            if (GENERAL && a.gate_form == GATE_FULL)
+                g[v] = load_cols<T, V>(static_cast<const T*>(a.gate) + row * a.ld_gate, c, cols);
         }
         if (cols) __builtin_memcpy(st, a.stats + row * 4, sizeof st);
-        else st[0] = st[1] = st[2] = st[3] = 0.0f;
-    };
-    const int64_t step = static_cast<int64_t>(gridDim.x) * rpb;
-    fetch(static_cast<int64_t>(blockIdx.x) * rpb + group);
-    for (int64_t base = static_cast<int64_t>(blockIdx.x) * rpb; base < a.rows; base += step) {
-        const int64_t row = base + group;
-        const int cols = row < a.rows ? a.cols : 0;
         const float mean1 = st[0], rstd1 = st[1], mean2 = st[2], rstd2 = st[3];
-        float ds[NV][V], xh1[NV][V], q[NV][V], xh2[NV][V];
-        float ga[NV][V];
+        float row_gate = 1.0f;
+        if (a.gate_form == GATE_ROW && row < a.rows)
+            row_gate = activate(static_cast<const float*>(a.gate)[row], a.gate_act);
+        uint32_t keep[NV];
+        row_keep<T, SUB>(a, at, row, cols, keep);
+        float ds[NV][V], q[NV][V], xh[NV][V];
         float two[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                ds[v][j] = dsum ? to_float(pds[v].v[j]) : 0.0f;
-                xh1[v][j] = (to_float(px[v].v[j]) - mean1) * rstd1;
-                ga[v][j] = a.gate_form == GATE_FULL ? activate(to_float(pg[v].v[j]), a.gate_act) : gc[v][j];
-                if (a.w_pre) {
-                    const float dh = to_float(pdh[v].v[j]);
-                    xh2[v][j] = (to_float(ps[v].v[j]) - mean2) * rstd2;
-                    q[v][j] = dh * wn[v][j];
-                    pre1[v][j] = fmaf(dh, xh2[v][j], pre1[v][j]);
-                    pre2[v][j] += dh;
-                    two[0] = fmaf(q[v][j], xh2[v][j], two[0]);
-                    two[1] += q[v][j];
+            for (int j = 0; j < V; ++j) ds[v][j] = to_float(up[v].v[j]);
+        if (a.w_pre) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                float w[V];
+                params.get(kPre, v, at, w);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float h = to_float(dh[v].v[j]);
+                    xh[v][j] = (to_float(s[v].v[j]) - mean2) * rstd2;
+                    q[v][j] = h * w[j];
+                    pre1[v][j] = fmaf(h, xh[v][j], pre1[v][j]);
+                    if (GENERAL) pre2[v][j] += h;
+                    two[0] = fmaf(q[v][j], xh[v][j], two[0]);
+                }
+                if (a.layer) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) two[1] += q[v][j];
                 }
             }
-        float row_gate = 1.0f;
-        if (a.gate_form == GATE_ROW && row < a.rows)
-            row_gate = activate(static_cast<const float*>(a.gate)[row], a.gate_act);
-        fetch(row + step);
-        if (a.w_pre) {
             row_sum<SUB>(two, buf, turn);
-            const float m0 = two[0] * a.inv_cols, m1 = a.layer ? two[1] * a.inv_cols : 0.0f;
+            const float m0 = two[0] * a.inv_cols * rstd2, m1 = a.layer ? two[1] * a.inv_cols * rstd2 : 0.0f;
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int j = 0; j < V; ++j) ds[v][j] = fmaf(rstd2, q[v][j] - m1 - xh2[v][j] * m0, ds[v][j]);
+                for (int j = 0; j < V; ++j) ds[v][j] += fmaf(rstd2, q[v][j], fmaf(-m0, xh[v][j], -m1));
         }
-        float dg_row[1] = {0.0f};
+        const float scale = a.drop ? a.key.scale : 1.0f;
         two[0] = two[1] = 0.0f;
+        float dg_row[1] = {0.0f};
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = (v * tpr + t) * V;
-            float m[V];
+            const int c = at.column(v);
+            Pack<T, V> out;
 #pragma unroll
-            for (int j = 0; j < V; ++j) m[j] = 1.0f;
-            if (a.drop && c < cols) drop_factors<V>(a.key, row * a.cols + c, m);
-            Pack<T, V> dr, dgp;
+            for (int j = 0; j < V; ++j) out.v[j] = from_float<T>(a.rho * ds[v][j]);
+            if (a.dresidual) store_cols<T, V>(static_cast<T*>(a.dresidual) + row * a.ld_dresidual, c, cols, out);
+            if (c + V > cols) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) ds[v][j] = c + j < cols ? ds[v][j] : 0.0f;
+            }
+            // ds becomes du, and then the gradient of z
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const bool in = j < cols - c;
-                dr.v[j] = from_float<T>(a.rho * ds[v][j]);
-                float du = in ? ds[v][j] : 0.0f;
-                if (a.drop) du = dropped(du, m[j]);
-                // what is dropped takes no part, were it infinite or NaN
-                const float xa = a.drop && m[j] == 0.0f ? 0.0f : xh1[v][j];
-                const float z = fmaf(xa, wp[v][j], bp[v][j]);
-                if (a.gate_form == GATE_FULL) dgp.v[j] = from_float<T>(du * z * slope(ga[v][j], a.gate_act));
-                if (a.gate_form == GATE_ROW) {
-                    dg_row[0] = fmaf(du, z, dg_row[0]);
-                    du *= row_gate;
-                }
-                // a channel gate's a is the column's own: its sums go without it
-                const float dz = du * ga[v][j];
-                const float acc = a.gate_form == GATE_CHANNEL ? du : dz;
-                post1[v][j] = fmaf(acc, xa, post1[v][j]);
-                post2[v][j] += acc;
-                q[v][j] = dz * wp[v][j];
-                two[0] = fmaf(q[v][j], xa, two[0]);
-                two[1] += q[v][j];
+                ds[v][j] = kept(ds[v][j], keep[v], V - 1 - j) * scale;
+                xh[v][j] = (to_float(x[v].v[j]) - mean1) * rstd1;
             }
-            if (a.dresidual) store_cols<T, V>(static_cast<T*>(a.dresidual) + row * a.ld_dresidual, c, cols, dr);
-            if (a.gate_form == GATE_FULL) store_cols<T, V>(static_cast<T*>(a.dgate) + row * a.ld_dgate, c, cols, dgp);
+            if (a.drop && !a.w_post) {
+                // what is dropped takes no part, were it infinite or NaN
+#pragma unroll
+                for (int j = 0; j < V; ++j) xh[v][j] = kept(xh[v][j], keep[v], V - 1 - j);
+            }
+            float w[V], b[V];
+            params.get(kPost, v, at, w);
+            if constexpr (GENERAL) params.get(kPostBias, v, at, b);
+            if (GENERAL && a.gate_form == GATE_FULL) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float f = activate(to_float(g[v].v[j]), a.gate_act);
+                    out.v[j] = from_float<T>(ds[v][j] * fmaf(xh[v][j], w[j], b[j]) * slope(f, a.gate_act));
+                    ds[v][j] *= f;
+                }
+                store_cols<T, V>(static_cast<T*>(a.dgate) + row * a.ld_dgate, c, cols, out);
+            } else if (a.gate_form == GATE_ROW) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    dg_row[0] = fmaf(ds[v][j], GENERAL ? fmaf(xh[v][j], w[j], b[j]) : xh[v][j] * w[j], dg_row[0]);
+                    ds[v][j] *= row_gate;
+                }
+            }
+            // a channel gate is the column's own: the column sums go without it
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                post1[v][j] = fmaf(ds[v][j], xh[v][j], post1[v][j]);
+                if (GENERAL) post2[v][j] += ds[v][j];
+                q[v][j] = ds[v][j] * w[j];
+                two[0] = fmaf(q[v][j], xh[v][j], two[0]);
+            }
+            if (a.layer) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) two[1] += q[v][j];
+            }
         }
-        if (a.w_post) row_sum<SUB>(two, buf, turn);
         if (a.gate_form == GATE_ROW) {
             row_sum<SUB>(dg_row, buf, turn);
-            if (t == 0 && row < a.rows) static_cast<float*>(a.dgate)[row] = dg_row[0] * slope(row_gate, a.gate_act);
+            if (at.t == 0 && row < a.rows) static_cast<float*>(a.dgate)[row] = dg_row[0] * slope(row_gate, a.gate_act);
         }
-        const float m0 = a.w_post ? two[0] * a.inv_cols : 0.0f;
-        const float m1 = a.w_post && a.layer ? two[1] * a.inv_cols : 0.0f;
+        if (a.w_post) {
+            row_sum<SUB>(two, buf, turn);
+            const float m0 = two[0] * a.inv_cols * rstd1, m1 = a.layer ? two[1] * a.inv_cols * rstd1 : 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int j = 0; j < V; ++j) q[v][j] = fmaf(rstd1, q[v][j], fmaf(-m0, xh[v][j], -m1));
+        }
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             Pack<T, V> out;
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                out.v[j] = from_float<T>(a.w_post ? rstd1 * (q[v][j] - m1 - xh1[v][j] * m0) : q[v][j]);
-            store_cols<T, V>(static_cast<T*>(a.dbranch) + row * a.ld_dbranch, (v * tpr + t) * V, cols, out);
+            for (int j = 0; j < V; ++j) out.v[j] = from_float<T>(q[v][j]);
+            store_cols<T, V>(static_cast<T*>(a.dbranch) + row * a.ld_dbranch, at.column(v), cols, out);
         }
     }
     // column sums: groups of a wave, then the block's waves, then one row of the partial sums per block
@@ -421,10 +525,11 @@ __global__ __launch_bounds__(SUB ? 256 : 512) void norm_backward(NormArgs a)
                 Pack<float, V> p;
 #pragma unroll
                 for (int j = 0; j < V; ++j) p.v[j] = acc[v][j];
-                store_cols<float, V>(out, (v * tpr + t) * V, a.cols, p);
+                store_cols<float, V>(out, at.column(v), a.cols, p);
             }
         } else {
-            __shared__ float join[4][SUB * NV * V];
+            constexpr int kWaves = kSubThreads / 64;
+            __shared__ float join[kWaves][SUB * kCols];
             __syncthreads();
 #pragma unroll
             for (int v = 0; v < NV; ++v)
@@ -433,39 +538,56 @@ __global__ __launch_bounds__(SUB ? 256 : 512) void norm_backward(NormArgs a)
                     float x = acc[v][j];
 #pragma unroll
                     for (int lanes = SUB; lanes < 64; lanes *= 2) x += __shfl_xor(x, lanes);
-                    if ((threadIdx.x & 63) < SUB) join[threadIdx.x >> 6][(v * SUB + t) * V + j] = x;
+                    if ((threadIdx.x & 63) < SUB) join[threadIdx.x >> 6][at.column(v) + j] = x;
                 }
             __syncthreads();
-            for (int c = threadIdx.x; c < a.cols; c += 256)
-                out[c] = (join[0][c] + join[1][c]) + (join[2][c] + join[3][c]);
+            for (int c = threadIdx.x; c < a.cols; c += kSubThreads) {
+                float x = join[0][c];
+                for (int w = 1; w < kWaves; ++w) x += join[w][c];
+                out[c] = x;
+            }
         }
     };
     put(0, post1);
-    put(1, post2);
-    put(2, pre1);
-    put(3, pre2);
+    put(1, pre1);
+    if (GENERAL) {
+        put(2, post2);
+        put(3, pre2);
+    }
 }
 
-// The column sums of `blocks` blocks joined in block order within each of
-// the wave's slices and then slice by slice: a fixed order.
-__global__ __launch_bounds__(1024) void norm_columns(NormArgs a, int blocks)
+// The column sums of `blocks` blocks joined: each of the block's 16 waves
+// takes every 16th, and the waves' sums are added in order, so the order is
+// fixed.  blockIdx.y: the norm after the block, or the one before the next.
+__global__ __launch_bounds__(1024) void norm_columns(NormArgs a, int blocks, int bias)
 {
-    __shared__ float part[kAcc][16][64];
-    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6;
+    __shared__ float part[2][16][64];
+    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, pre = blockIdx.y;
     const int c = blockIdx.x * 64 + lane;
-    float s[kAcc] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float s[2] = {0.0f, 0.0f};
     if (c < a.cols) {
-        for (int b = slice; b < blocks; b += 16)
-#pragma unroll
-            for (int i = 0; i < kAcc; ++i) s[i] += a.partial[(static_cast<int64_t>(i) * blocks + b) * a.cols + c];
+        const float* p = a.partial + static_cast<int64_t>(pre) * blocks * a.cols + c;
+#pragma unroll 8
+        for (int b = slice; b < blocks; b += 16) s[0] += p[static_cast<int64_t>(b) * a.cols];
+        if (bias) {
+            p += static_cast<int64_t>(2) * blocks * a.cols;
+#pragma unroll 8
+            for (int b = slice; b < blocks; b += 16) s[1] += p[static_cast<int64_t>(b) * a.cols];
+        }
     }
-#pragma unroll
-    for (int i = 0; i < kAcc; ++i) part[i][slice][lane] = s[i];
+    part[0][slice][lane] = s[0];
+    part[1][slice][lane] = s[1];
     __syncthreads();
     if (slice != 0 || c >= a.cols) return;
-#pragma unroll
-    for (int i = 0; i < kAcc; ++i)
-        for (int k = 1; k < 16; ++k) s[i] += part[i][k][lane];
+    for (int k = 1; k < 16; ++k) {
+        s[0] += part[0][k][lane];
+        s[1] += part[1][k][lane];
+    }
+    if (pre) {
+        if (a.dw_pre) a.dw_pre[c] = s[0];
+        if (a.db_pre) a.db_pre[c] = s[1];
+        return;
+    }
     float f = 1.0f;
     if (a.gate_form == GATE_CHANNEL) {
         f = activate(static_cast<const float*>(a.gate)[c], a.gate_act);
@@ -474,8 +596,11 @@ __global__ __launch_bounds__(1024) void norm_columns(NormArgs a, int blocks)
     }
     if (a.dw_post) a.dw_post[c] = f * s[0];
     if (a.db_post) a.db_post[c] = f * s[1];
-    if (a.dw_pre) a.dw_pre[c] = s[2];
-    if (a.db_pre) a.db_pre[c] = s[3];
+}
+
+void launch_columns(const NormArgs& a, int blocks, int bias, hipStream_t s)
+{
+    norm_columns<<<dim3((a.cols + 63) / 64, a.w_pre ? 2 : 1), 1024, 0, s>>>(a, blocks, bias);
 }
 
 // ---- rows too long for the registers: the same sums with the row read again
@@ -513,11 +638,7 @@ template <typename T> __global__ __launch_bounds__(kLoopThreads) void norm_forwa
             if (a.gate_form == GATE_CHANNEL) u *= activate(static_cast<const float*>(a.gate)[c], a.gate_act);
             if (a.gate_form == GATE_FULL)
                 u *= activate(to_float(static_cast<const T*>(a.gate)[row * a.ld_gate + c]), a.gate_act);
-            if (a.drop) {
-                float m[1];
-                drop_factors<1>(a.key, row * a.cols + c, m);
-                u = dropped(u, m[0]);
-            }
+            if (a.drop) u = kept(u * a.key.scale, keep_run<1>(a.key, row * a.cols + c), 0);
             if (r) u += a.rho * to_float(r[c]);
             sum[c] = from_float<T>(u);
         }
@@ -567,10 +688,9 @@ template <typename T> __global__ __launch_bounds__(kLoopThreads) void norm_backw
             du = ds;
             xa = xh1 = (to_float(x[c]) - st[0]) * st[1];
             if (a.drop) {
-                float m[1];
-                drop_factors<1>(a.key, row * a.cols + c, m);
-                du = dropped(du, m[0]);
-                if (m[0] == 0.0f) xa = 0.0f;
+                const uint32_t keep = keep_run<1>(a.key, row * a.cols + c);
+                du = kept(du * a.key.scale, keep, 0);
+                xa = kept(xa, keep, 0);
             }
         };
         auto gate_of = [&](int c) {
@@ -588,13 +708,13 @@ template <typename T> __global__ __launch_bounds__(kLoopThreads) void norm_backw
             if (a.gate_form == GATE_ROW) dg_row[0] = fmaf(du, z, dg_row[0]);
             const float own = a.gate_form == GATE_CHANNEL ? du : du * g;
             acc[0][c] = fmaf(own, xa, first ? 0.0f : acc[0][c]);
-            acc[1][c] = own + (first ? 0.0f : acc[1][c]);
+            acc[2][c] = own + (first ? 0.0f : acc[2][c]);
             float d = 0.0f, xh2 = 0.0f;
             if (a.w_pre) {
                 d = to_float(dh[c]);
                 xh2 = (to_float(s[c]) - st[2]) * st[3];
             }
-            acc[2][c] = fmaf(d, xh2, first ? 0.0f : acc[2][c]);
+            acc[1][c] = fmaf(d, xh2, first ? 0.0f : acc[1][c]);
             acc[3][c] = d + (first ? 0.0f : acc[3][c]);
             const float q = du * g * w;
             three[0] = fmaf(q, xa, three[0]);
@@ -623,40 +743,66 @@ template <typename T> __global__ __launch_bounds__(kLoopThreads) void norm_backw
 
 // ---- launches
 
-template <typename T, int SUB, int NV>
-hipError_t launch_form(const NormArgs& a, int threads, bool backward, hipStream_t s)
+// Blocks loop over their rows, so there are as many as fit the 256 CUs at
+// once: more would wait for the first ones to end.
+int64_t resident_blocks(int waves_per_simd, int64_t cols)
 {
-    const int64_t rpb = SUB ? 256 / (SUB ? SUB : 1) : 1;
-    const int64_t need = (a.rows + rpb - 1) / rpb;
+    const int64_t waves = cols <= 64 * kCols ? kSubThreads / 64 : (cols + 64 * kCols - 1) / (64 * kCols);
+    const int64_t per_cu = 4 * waves_per_simd / waves;
+    return 256 * (per_cu > 0 ? per_cu : 1);
+}
+
+// Blocks of the backward pass: fewer where a block would have less than 8
+// rows to write its column sums for (but 256 if there are the rows).
+int64_t backward_blocks(int64_t groups, int64_t cols)
+{
+    int64_t blocks = resident_blocks(kBackwardWaves, cols);
+    const int64_t eighth = groups / 8 > 256 ? groups / 8 : 256;
+    if (blocks > eighth) blocks = eighth;
+    return blocks < groups ? blocks : groups;
+}
+
+template <typename T, int SUB, int MAXT, bool GENERAL>
+void launch_kernel(const NormArgs& a, int threads, bool backward, hipStream_t s)
+{
+    const int64_t rpb = SUB ? kSubThreads / (SUB ? SUB : 1) : 1;
+    const int64_t groups = (a.rows + rpb - 1) / rpb;
     if (!backward) {
-        const int64_t most = 256 * (2048 / threads);
-        norm_forward<T, SUB, NV><<<static_cast<unsigned>(need < most ? need : most), threads, 0, s>>>(a);
-        return hipGetLastError();
+        const int64_t most = resident_blocks(GENERAL ? kBackwardWaves : kForwardWaves, a.cols);
+        norm_forward<T, SUB, MAXT, GENERAL><<<static_cast<unsigned>(groups < most ? groups : most), threads, 0, s>>>(a);
+    } else {
+        const int blocks = static_cast<int>(backward_blocks(groups, a.cols));
+        const size_t lds = GENERAL && SUB == 0 && MAXT == 512 ? 3 * sizeof(float) * kCols * threads : 0;
+        norm_backward<T, SUB, MAXT, GENERAL><<<blocks, threads, lds, s>>>(a);
+        launch_columns(a, blocks, GENERAL, s);
     }
-    const int blocks = static_cast<int>(need < kMaxBlocks ? need : kMaxBlocks);
-    norm_backward<T, SUB, NV><<<blocks, threads, 0, s>>>(a);
-    norm_columns<<<(a.cols + 63) / 64, 1024, 0, s>>>(a, blocks);
+}
+
+template <typename T, int SUB, int MAXT>
+hipError_t launch_layout(const NormArgs& a, int threads, bool backward, hipStream_t s)
+{
+    if (a.b_post || a.b_pre || a.gate_form == GATE_FULL) launch_kernel<T, SUB, MAXT, true>(a, threads, backward, s);
+    else launch_kernel<T, SUB, MAXT, false>(a, threads, backward, s);
     return hipGetLastError();
 }
 
 template <typename T> hipError_t launch_type(const NormArgs& a, bool backward, hipStream_t s)
 {
-    const int nvec = (a.cols + kVec<T> - 1) / kVec<T>;
-    if (nvec <= 8) return launch_form<T, 8, 1>(a, 256, backward, s);
-    if (nvec <= 16) return launch_form<T, 16, 1>(a, 256, backward, s);
-    if (nvec <= 32) return launch_form<T, 32, 1>(a, 256, backward, s);
-    if (nvec <= 64) return launch_form<T, 64, 1>(a, 256, backward, s);
-    // whole waves share a row: at most 8 of them
-    const auto threads = [&](int nv) { return (nvec + 64 * nv - 1) / (64 * nv) * 64; };
-    if (nvec <= 512) return launch_form<T, 0, 1>(a, threads(1), backward, s);
-    if (nvec <= 1024) return launch_form<T, 0, 2>(a, threads(2), backward, s);
-    if (nvec <= 2048) return launch_form<T, 0, 4>(a, threads(4), backward, s);
-    const int blocks = static_cast<int>(a.rows < kMaxBlocks ? a.rows : kMaxBlocks);
+    // threads that a row needs
+    const int need = (a.cols + kCols - 1) / kCols;
+    if (need <= 8) return launch_layout<T, 8, kSubThreads>(a, kSubThreads, backward, s);
+    if (need <= 16) return launch_layout<T, 16, kSubThreads>(a, kSubThreads, backward, s);
+    if (need <= 32) return launch_layout<T, 32, kSubThreads>(a, kSubThreads, backward, s);
+    if (need <= 64) return launch_layout<T, 64, kSubThreads>(a, kSubThreads, backward, s);
+    const int threads = (need + 63) / 64 * 64;
+    if (need <= 512) return launch_layout<T, 0, 512>(a, threads, backward, s);
+    if (need <= 1024) return launch_layout<T, 0, 1024>(a, threads, backward, s);
+    const int blocks = static_cast<int>(a.rows < 256 ? a.rows : 256);
     if (!backward) {
         norm_forward_loop<T><<<blocks, kLoopThreads, 0, s>>>(a);
     } else {
         norm_backward_loop<T><<<blocks, kLoopThreads, 0, s>>>(a);
-        norm_columns<<<(a.cols + 63) / 64, 1024, 0, s>>>(a, blocks);
+        launch_columns(a, blocks, 1, s);
     }
     return hipGetLastError();
 }
@@ -683,8 +829,7 @@ hipError_t launch(const NormArgs& a, int dtype, bool backward, hipStream_t s)
 
 size_t norm_workspace_bytes(int64_t rows, int64_t cols)
 {
-    const int64_t blocks = rows < kMaxBlocks ? rows : kMaxBlocks;
-    return sizeof(float) * kAcc * static_cast<size_t>(blocks) * static_cast<size_t>(cols);
+    return sizeof(float) * kAcc * static_cast<size_t>(backward_blocks(rows, cols)) * static_cast<size_t>(cols);
 }
 
 hipError_t launch_norm_forward(const NormArgs& a, int dtype, hipStream_t s) { return launch(a, dtype, false, s); }
