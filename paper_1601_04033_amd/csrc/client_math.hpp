@@ -89,6 +89,16 @@ template <int N> __device__ __forceinline__ uint32_t keep_run(const DropKey& k, 
     return bits >> (16 - N - off);
 }
 
+// a x + y with the product rounded to fp32 before the sum: a x alone (y = 0)
+// is then the fp32 product, not a wider one that a 16-bit store would round
+// differently at ties.
+__device__ __forceinline__ float scaled_sum(float a, float x, float y)
+{
+#pragma clang fp contract(off)
+    const float t = a * x;
+    return t + y;
+}
+
 // x where bit `at` of bits is set, else 0 (whatever x is).
 __device__ __forceinline__ float kept(float x, uint32_t bits, int at)
 {

@@ -316,7 +316,7 @@ __global__ __launch_bounds__(MAXT, MAXT == 1024 || GENERAL ? kBackwardWaves : kF
             Pack<T, V> out;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                out.v[j] = from_float<T>(fmaf(a.rho, to_float(r[v].v[j]), kept(d[v][j], keep[v], V - 1 - j)));
+                out.v[j] = from_float<T>(scaled_sum(a.rho, to_float(r[v].v[j]), kept(d[v][j], keep[v], V - 1 - j)));
                 // the norm is of the sum as it is stored, so that the
                 // backward pass, which reads it, differentiates this function
                 d[v][j] = to_float(out.v[j]);
@@ -639,7 +639,7 @@ template <typename T> __global__ __launch_bounds__(kLoopThreads) void norm_forwa
             if (a.gate_form == GATE_FULL)
                 u *= activate(to_float(static_cast<const T*>(a.gate)[row * a.ld_gate + c]), a.gate_act);
             if (a.drop) u = kept(u * a.key.scale, keep_run<1>(a.key, row * a.cols + c), 0);
-            if (r) u += a.rho * to_float(r[c]);
+            if (r) u = scaled_sum(a.rho, to_float(r[c]), u);
             sum[c] = from_float<T>(u);
         }
         if (a.w_pre) {
