@@ -14,16 +14,10 @@
 //   fp32 c: 8-bit values times their scales are exact in bf16, whose
 //     instruction (v_mfma_f32_32x32x16_bf16) sums in fp32 throughout: half the
 //     rate, and as accurate as c can hold.
-#include "client_kernels.hpp"
+#include "fp8_math.hpp"
 
 namespace fasgd {
 namespace {
-
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;       // 4 waves, 2 x 2 of them
 constexpr int kBytes = kFp8Block;   // contraction per stage: one scale each way
@@ -93,24 +87,6 @@ __device__ __forceinline__ void read_one(Fragments<WIDE, N>& f, const uint8_t* a
 __device__ __forceinline__ v8i join_chunks(const v4i& lo, const v4i& hi)
 {
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-// 8 values (dwords lo and hi) times 2^(scale - 127), as bf16: exact.
-template <int FORMAT> __device__ __forceinline__ v8bf widen(int lo, int hi, float scale)
-{
-    v2bf x[4];
-    if constexpr (FORMAT == FP8_E4M3) {
-        x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
-        x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-        x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
-        x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-    } else {
-        x[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, false);
-        x[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, true);
-        x[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, false);
-        x[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, true);
-    }
-    return v8bf{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
 }
 
 // byte i of packed scales as the power of two it stands for
