@@ -13,7 +13,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfasgd.so")
 SOURCES = ["fasgd_api.hip", "dense.hip", "bfasgd.hip", "segments.hip", "pushes.hip", "selfcheck.hip", "anchor.hip",
            "client_api.hip", "dropout.hip", "residual_norm.hip",
-           "fp8_quantize.hip", "fp8_product.hip"]
+           "fp8_quantize.hip", "fp8_product.hip", "fp8_few.hip"]
 
 MARSHAL = os.path.join(PKG, "_marshal.so")
 

@@ -374,7 +374,10 @@ fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const clie
     p.c_dtype = dtype;
     p.partial = reinterpret_cast<float*>(base + (w->k > 0 ? linear_operand_bytes(m, w->k) : 0));
     hipError_t e = hipSuccess;
-    if (w->k > 0) {
+    const bool few = w->k > 0 && fasgd::fp8_linear_few(m, w->k);
+    if (few) {
+        e = fasgd::launch_fp8_linear_few(x, ldx, p, stream);
+    } else if (w->k > 0) {
         fasgd::QuantizeArgs q;
         memset(&q, 0, sizeof q);
         q.x = x;
@@ -384,7 +387,7 @@ fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const clie
         q.row = p.a;
         e = fasgd::launch_quantize(q, dtype, stream);
     }
-    if (e == hipSuccess) e = fasgd::launch_fp8_product(p, stream);
+    if (e == hipSuccess && !few) e = fasgd::launch_fp8_product(p, stream);
     if (e != hipSuccess) return hip_fail(e, "client_fp8_linear");
     return ok();
 }

@@ -89,6 +89,14 @@ struct Fp8Product {
     int32_t accumulate;
     float* partial;         // [splits][m][n], unused with one split
 };
+// Products that read their operands straight into registers: launch_fp8_few,
+// where fp8_few says so.  launch_fp8_linear_few takes q.a's rows from x and
+// quantizes them on the way, where fp8_linear_few says that they fit.
+constexpr int64_t kFewRows = 64;
+bool fp8_few(int64_t m, int64_t n, int64_t k);
+bool fp8_linear_few(int64_t m, int64_t k);
+hipError_t launch_fp8_few(const Fp8Product& p, hipStream_t s);
+hipError_t launch_fp8_linear_few(const void* x, int64_t ldx, const Fp8Product& q, hipStream_t s);
 size_t fp8_workspace_bytes(int64_t m, int64_t n, int64_t k);
 hipError_t launch_fp8_product(const Fp8Product& p, hipStream_t s);
 

@@ -1,0 +1,307 @@
+// 8-bit products that read their operands straight into registers: few rows
+// on one side (up to 16: single tokens and small batches through a linear
+// layer, or a layer of few outputs), and products so small that latency is
+// all they cost.
+//
+// Bound by reading the larger operand once.  A block takes 16 or 32 of its
+// rows, its 8 waves take the contraction's blocks of 128 in turn and read
+// fragments straight from memory (16 rows of 128 bytes: whole lines), each
+// value once; the few rows come from the caches.  The waves' sums are joined
+// through LDS, so one launch writes the result.
+// Up to 16 rows of unquantized activations (48 KB once quantized) are
+// quantized on the way: every block does it again, into LDS, while its first
+// loads of the larger operand are under way, which costs less than a launch
+// before this one.
+#include "fp8_math.hpp"
+
+namespace fasgd {
+namespace {
+
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * 64;
+
+struct Few {
+    Fp8View big, few;
+    const void* x;          // activations in place of few.data (FUSED)
+    int64_t ldx;
+    void* c;                // element (row of big, row of few) at c[r * stride_big + m * stride_few]
+    int64_t stride_big, stride_few;
+    int32_t c_dtype;
+    int32_t accumulate;
+};
+
+__device__ __forceinline__ v8i join_chunks(const v4i& lo, const v4i& hi)
+{
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// 16 rows x 128 of an operand: lane l holds row l % 16, the 16-byte chunks
+// l / 16 of the block's two halves (both sides agree, so which of the
+// contraction's values these are does not matter).
+__device__ __forceinline__ v8i read_rows(const Fp8View& v, int64_t row, int64_t kb, int lane)
+{
+    const int64_t r = row + (lane & 15) < v.rows ? row + (lane & 15) : v.rows - 1;
+    const uint8_t* p = v.data + r * v.ld + kb * kFp8Block + (lane >> 4) * 16;
+    return join_chunks(*reinterpret_cast<const v4i*>(p), *reinterpret_cast<const v4i*>(p + 64));
+}
+__device__ __forceinline__ int read_scale(const Fp8View& v, int64_t row, int64_t kb, int lane)
+{
+    const int64_t r = row + (lane & 15) < v.rows ? row + (lane & 15) : v.rows - 1;
+    return v.scales[kb * v.lds + r];
+}
+
+// Activations in LDS: rows of k rounded up to 128 and 16 bytes (so that 16
+// rows lie in different banks), then the scales, 16 to a block of 128.
+struct Held {
+    uint8_t* data;
+    uint8_t* scales;
+    int stride;
+};
+inline int held_stride(int64_t k) { return static_cast<int>((k + kFp8Block - 1) / kFp8Block * kFp8Block) + 16; }
+inline size_t held_bytes(int64_t rows, int64_t k)
+{
+    return static_cast<size_t>(rows) * held_stride(k) + static_cast<size_t>((k + kFp8Block - 1) / kFp8Block) * 16;
+}
+
+// x quantized in e4m3 into LDS, 16 threads to a block of a row.
+template <typename T> __device__ __forceinline__ void hold(const Few& p, const Held& h, int blocks)
+{
+    const int lane = threadIdx.x & 15, rows = static_cast<int>(p.few.rows), k = static_cast<int>(p.few.k);
+    for (int i = threadIdx.x >> 4; i < rows * blocks; i += kThreads / 16) {
+        const int r = i / blocks, kb = i % blocks, c = kb * kFp8Block + lane * 8;
+        const T* x = static_cast<const T*>(p.x) + r * p.ldx;
+        Pack<T, 8> q;
+        if (c + 8 <= k) {
+            q = load_pack<T, 8>(x + c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q.v[j] = c + j < k ? x[c + j] : from_float<T>(0.0f);
+        }
+        float v[8], m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = to_float(q.v[j]);
+            m = fmaxf(m, finite_abs(v[j]));
+        }
+        const int e = block_exponent(max_of_16(m), kFmaxExponent<FP8_E4M3>);
+        const float s = exp2_int(-e);
+        uint2 out;
+        out.x = pack4<FP8_E4M3>(v[0], v[1], v[2], v[3], s);
+        out.y = pack4<FP8_E4M3>(v[4], v[5], v[6], v[7], s);
+        *reinterpret_cast<uint2*>(h.data + r * h.stride + c) = out;
+        if (lane == 0) h.scales[kb * 16 + r] = static_cast<uint8_t>(e + 127);
+    }
+}
+
+template <int FORMAT> __device__ __forceinline__ void widen_rows(const v8i& f, int scale, v8bf (&w)[4])
+{
+    const float s = __uint_as_float(static_cast<uint32_t>(scale) << 23);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) w[t] = widen<FORMAT>(f[2 * t], f[2 * t + 1], s);
+}
+
+// MT tiles of 16 few rows, NT tiles of 16 of the larger operand's rows.
+// X: the activations' type (FUSED), else unused.
+template <typename X, bool FUSED, bool WIDE, int FBIG, int FFEW, int MT, int NT>
+__global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_stride)
+{
+    // blocks of 128 loaded while as many are multiplied, within 128 registers
+    constexpr int kAhead = NT * MT >= 4 ? 1 : 4 / (NT * MT);
+    extern __shared__ __attribute__((aligned(16))) uint8_t dynamic[];
+    __shared__ __attribute__((aligned(16))) float sums[kWaves][NT][MT][64][4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * (16 * NT), m0 = static_cast<int64_t>(blockIdx.y) * (16 * MT);
+    const int blocks = static_cast<int>((p.big.k + kFp8Block - 1) / kFp8Block);
+    v4f acc[NT][MT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[n][m] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+    constexpr int kFew = FUSED ? 1 : MT;
+    struct Group {
+        v8i big[kAhead][NT], few[kAhead][kFew];
+        int scale_big[kAhead][NT], scale_few[kAhead][kFew];
+    };
+    // A block past the last is the last again, with scales of 2^-127: products of 0.
+    auto load = [&](Group& g, int k) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int kb = k + u * kWaves < blocks ? k + u * kWaves : blocks - 1;
+            const int in = k + u * kWaves < blocks ? -1 : 0;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                g.big[u][n] = read_rows(p.big, r0 + n * 16, kb, lane);
+                g.scale_big[u][n] = read_scale(p.big, r0 + n * 16, kb, lane) & in;
+            }
+            if constexpr (!FUSED) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    g.few[u][m] = read_rows(p.few, m0 + m * 16, kb, lane);
+                    g.scale_few[u][m] = read_scale(p.few, m0 + m * 16, kb, lane) & in;
+                }
+            }
+        }
+    };
+    Held h;
+    h.data = dynamic;
+    h.stride = held_stride;
+    h.scales = dynamic + p.few.rows * held_stride;
+    const int held_row = (lane & 15) < p.few.rows ? lane & 15 : static_cast<int>(p.few.rows) - 1;
+    auto multiply = [&](const Group& g, int k) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            v8i few[MT];
+            int scale_few[MT];
+            if constexpr (FUSED) {
+                const int kb = k + u * kWaves < blocks ? k + u * kWaves : blocks - 1;
+                const uint8_t* q = h.data + held_row * h.stride + kb * kFp8Block + (lane >> 4) * 16;
+                few[0] = join_chunks(*reinterpret_cast<const v4i*>(q), *reinterpret_cast<const v4i*>(q + 64));
+                scale_few[0] = h.scales[kb * 16 + held_row];
+            } else {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    few[m] = g.few[u][m];
+                    scale_few[m] = g.scale_few[u][m];
+                }
+            }
+            if constexpr (WIDE) {
+                v8bf wb[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) widen_rows<FBIG>(g.big[u][n], g.scale_big[u][n], wb[n]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    v8bf wf[4];
+                    widen_rows<FFEW>(few[m], scale_few[m], wf);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+                            acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[n][t], wf[t], acc[n][m], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+                        acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                            g.big[u][n], few[m], acc[n][m], FBIG, FFEW, 0, g.scale_big[u][n], 0, scale_few[m]);
+            }
+        }
+    };
+    Group g[2];
+    constexpr int kStep = kWaves * kAhead;
+    load(g[0], wave);
+    if constexpr (FUSED) {
+        hold<X>(p, h, blocks);
+        // only LDS has to be there: the loads above stay under way
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    }
+    for (int k = wave; k < blocks; k += 2 * kStep) {
+        load(g[1], k + kStep);
+        multiply(g[0], k);
+        if (k + kStep >= blocks) break;
+        load(g[0], k + 2 * kStep);
+        multiply(g[1], k + kStep);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) *reinterpret_cast<v4f*>(sums[wave][n][m][lane]) = acc[n][m];
+    __syncthreads();
+    // element e of lane l: row 4 (l / 16) + e of the larger operand's tile, row l % 16 of the few's
+    for (int i = threadIdx.x; i < NT * MT * 256; i += kThreads) {
+        const int e = i & 3, l = i >> 2 & 63, m = (i >> 8) % MT, n = (i >> 8) / MT;
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) s += sums[w][n][m][l][e];
+        const int64_t row = r0 + n * 16 + (l >> 4) * 4 + e, col = m0 + m * 16 + (l & 15);
+        if (row >= p.big.rows || col >= p.few.rows) continue;
+        const int64_t at = row * p.stride_big + col * p.stride_few;
+        if (p.c_dtype == DTYPE_F32) {
+            float* c = static_cast<float*>(p.c) + at;
+            *c = p.accumulate ? *c + s : s;
+        } else if (p.c_dtype == DTYPE_BF16) {
+            bf16* c = static_cast<bf16*>(p.c) + at;
+            *c = from_float<bf16>(p.accumulate ? to_float(*c) + s : s);
+        } else {
+            f16* c = static_cast<f16*>(p.c) + at;
+            *c = from_float<f16>(p.accumulate ? to_float(*c) + s : s);
+        }
+    }
+}
+
+// 32 rows a block where that still gives every CU one, else 16.
+template <typename X, bool FUSED, bool WIDE, int FBIG, int FFEW, int MT>
+hipError_t launch_rows(const Few& p, hipStream_t s)
+{
+    const size_t lds = FUSED ? held_bytes(p.few.rows, p.few.k) : 0;
+    const int stride = FUSED ? held_stride(p.few.k) : 0;
+    const unsigned along = static_cast<unsigned>((p.few.rows + 16 * MT - 1) / (16 * MT));
+    if (MT == 1 && p.big.rows >= 256 * 32)
+        product_few<X, FUSED, WIDE, FBIG, FFEW, MT, MT == 1 ? 2 : 1>
+            <<<dim3(static_cast<unsigned>((p.big.rows + 31) / 32), along), kThreads, lds, s>>>(p, stride);
+    else
+        product_few<X, FUSED, WIDE, FBIG, FFEW, MT, 1>
+            <<<dim3(static_cast<unsigned>((p.big.rows + 15) / 16), along), kThreads, lds, s>>>(p, stride);
+    return hipGetLastError();
+}
+
+template <bool WIDE, int FBIG, int FFEW> hipError_t launch_few_rows(const Few& p, hipStream_t s)
+{
+    if (p.few.rows <= 16) return launch_rows<float, false, WIDE, FBIG, FFEW, 1>(p, s);
+    return launch_rows<float, false, WIDE, FBIG, FFEW, 2>(p, s);
+}
+
+template <bool WIDE> hipError_t launch_formats(const Few& p, hipStream_t s)
+{
+    if (p.big.format == FP8_E4M3)
+        return p.few.format == FP8_E4M3 ? launch_few_rows<WIDE, 0, 0>(p, s) : launch_few_rows<WIDE, 0, 1>(p, s);
+    return p.few.format == FP8_E4M3 ? launch_few_rows<WIDE, 1, 0>(p, s) : launch_few_rows<WIDE, 1, 1>(p, s);
+}
+
+template <typename X> hipError_t launch_fused(const Few& p, hipStream_t s)
+{
+    constexpr bool WIDE = sizeof(X) == 4;
+    return p.big.format == FP8_E4M3 ? launch_rows<X, true, WIDE, 0, 0, 1>(p, s) : launch_rows<X, true, WIDE, 1, 0, 1>(p, s);
+}
+
+}  // namespace
+
+// Beyond 16 rows, blocks of 16 x 32 outputs read (16 + 32) k bytes each from
+// the caches: taken up to 48 MB, about 6 us.
+bool fp8_few(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t few = m < n ? m : n, big = m < n ? n : m;
+    return few <= 16 || ((big + 15) / 16) * ((few + 31) / 32) * 48 * k <= int64_t(48) << 20;
+}
+
+bool fp8_linear_few(int64_t m, int64_t k) { return m <= 16 && held_bytes(m, k) <= 48 * 1024; }
+
+hipError_t launch_fp8_few(const Fp8Product& q, hipStream_t s)
+{
+    Few p;
+    const bool b_few = q.b.rows <= q.a.rows;
+    p.big = b_few ? q.a : q.b;
+    p.few = b_few ? q.b : q.a;
+    p.x = nullptr;
+    p.ldx = 0;
+    p.c = q.c;
+    p.stride_big = b_few ? q.ldc : 1;
+    p.stride_few = b_few ? 1 : q.ldc;
+    p.c_dtype = q.c_dtype;
+    p.accumulate = q.accumulate;
+    return q.c_dtype == DTYPE_F32 ? launch_formats<true>(p, s) : launch_formats<false>(p, s);
+}
+
+hipError_t launch_fp8_linear_few(const void* x, int64_t ldx, const Fp8Product& q, hipStream_t s)
+{
+    const Few p{q.b, q.a, x, ldx, q.c, 1, q.ldc, q.c_dtype, 0};
+    if (q.c_dtype == DTYPE_F32) return launch_fused<float>(p, s);
+    if (q.c_dtype == DTYPE_BF16) return launch_fused<bf16>(p, s);
+    return launch_fused<f16>(p, s);
+}
+
+}  // namespace fasgd

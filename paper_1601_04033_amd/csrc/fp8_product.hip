@@ -19,19 +19,22 @@
 namespace fasgd {
 namespace {
 
-constexpr int kThreads = 256;       // 4 waves, 2 x 2 of them
+constexpr int kThreads = 256;       // 4 waves
 constexpr int kBytes = kFp8Block;   // contraction per stage: one scale each way
 constexpr int kMaxSplits = 16;
 
-// A wave owns W x W outputs as (W/32)^2 matrix tiles.  Row r of tile i is the
-// wave's row (W/32) r + i, so a lane's scales for its tiles are neighbouring
-// bytes (one load; the instruction picks the byte) and its outputs are
-// neighbouring columns.
-template <int W> struct Geometry {
+// A wave owns W x W outputs as (W/32)^2 matrix tiles, and WM of the block's 4
+// waves stand along a's rows.  Row r of tile i is the wave's row
+// (W/32) r + i, so a lane's scales for its tiles are neighbouring bytes (one
+// load; the instruction picks the byte) and its outputs are neighbouring
+// columns.
+template <int W, int WM> struct Geometry {
     static constexpr int kTiles = W / 32;
-    static constexpr int kSide = 2 * W;                         // block tile
-    static constexpr int kStage = kSide * kBytes;               // LDS bytes of one operand's stage
-    static constexpr int kLoads = kStage / (kThreads * 16);     // 16-byte loads per thread and operand
+    static constexpr int kWavesN = 4 / WM;
+    static constexpr int kRowsA = W * WM, kRowsB = W * kWavesN;             // block tile
+    static constexpr int kStageA = kRowsA * kBytes, kStageB = kRowsB * kBytes;  // LDS bytes of a stage
+    static constexpr int kLoadsA = kStageA / (kThreads * 16);               // 16-byte loads per thread
+    static constexpr int kLoadsB = kStageB / (kThreads * 16);
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources
@@ -39,7 +42,7 @@ template <int W> struct Geometry {
 // The 16-byte chunk of a row that lies in slot s of its 128 LDS bytes.  Rows
 // that one read touches together (kTiles apart) get their chunks in
 // different banks.
-template <int W> __device__ __forceinline__ int swizzle(int row) { return (row / Geometry<W>::kTiles) & 7; }
+template <int W> __device__ __forceinline__ int swizzle(int row) { return (row / (W / 32)) & 7; }
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
@@ -160,49 +163,49 @@ template <int N> __device__ __forceinline__ void take_row(const v16f (&acc)[N], 
     }
 }
 
-// A wave's outputs to rows m and columns n on of c ([rows][cols], row stride
-// ld).  Whole waves inside c store straight from their registers, each lane N
-// neighbouring columns.  Others, and those that add to c, pass through LDS,
-// 32 rows at a time, and go element by element.
-template <typename T, int W, int N>
-__device__ __forceinline__ void write_outputs(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
-                                              int64_t m, int64_t n, bool add, float* lds, int lane)
+// A wave's outputs to rows m on and columns n on of c ([rows][cols], row
+// stride ld): each lane N neighbouring columns at once, at any alignment.
+// WHOLE: all of them lie in c, and c is not added to.  Otherwise a lane that
+// c's last column cuts through stores its columns one by one.  (The checks
+// cost 2 us of a 4,096 x 4,096 x 1,024 product's 22.)
+template <typename T, int W, int N, bool WHOLE>
+__device__ __forceinline__ void write_tiles(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
+                                              int64_t m, int64_t n, bool add, int lane)
 {
-    if (!add && m + W <= rows && n + W <= cols) {
-        T* base = c + (m + 4 * N * (lane >> 5)) * ld + n + (lane & 31) * N;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v16f t[N];
-            take_row<N>(acc[i], t);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                Pack<T, N> x;
-#pragma unroll
-                for (int j = 0; j < N; ++j) x.v[j] = from_float<T>(t[j][r]);
-                store_pack(base + ((8 * (r >> 2) + (r & 3)) * N + i) * ld, x);
-            }
-        }
-        return;
-    }
+    const int rows_left = static_cast<int>(rows - m < W ? rows - m : W) - 4 * N * (lane >> 5);
+    const int cols_left = static_cast<int>(cols - n < W ? cols - n : W) - N * (lane & 31);
+    T* base = c + (m + 4 * N * (lane >> 5)) * ld + n + N * (lane & 31);
+    const bool cut = __ballot(cols_left > 0 && cols_left < N) != 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         v16f t[N];
         take_row<N>(acc[i], t);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int row = 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+            const int row = (8 * (r >> 2) + (r & 3)) * N + i;
+            T* out = base + row * ld;
+            if (WHOLE || (row < rows_left && cols_left >= N)) {
+                Pack<T, N> x;
+                if (!WHOLE && add) x = load_pack<T, N>(out);
 #pragma unroll
-            for (int j = 0; j < N; ++j) lds[row * W + (lane & 31) * N + j] = t[j][r];
-        }
-        for (int row = 0; row < 32 && m + row * N + i < rows; ++row) {
-            T* out = c + (m + row * N + i) * ld + n;
-            for (int col = lane; col < W; col += 64) {
-                if (n + col >= cols) continue;
-                const float x = lds[row * W + col];
-                out[col] = from_float<T>(add ? to_float(out[col]) + x : x);
+                for (int j = 0; j < N; ++j) x.v[j] = from_float<T>(!WHOLE && add ? to_float(x.v[j]) + t[j][r] : t[j][r]);
+                store_pack(out, x);
+            }
+            if (!WHOLE && cut && row < rows_left) {
+#pragma unroll
+                for (int j = 0; j + 1 < N; ++j)
+                    if (j < cols_left && cols_left < N) out[j] = from_float<T>(add ? to_float(out[j]) + t[j][r] : t[j][r]);
             }
         }
     }
+}
+
+template <typename T, int W, int N>
+__device__ __forceinline__ void write_outputs(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
+                                              int64_t m, int64_t n, bool add, int lane)
+{
+    if (!add && m + W <= rows && n + W <= cols) write_tiles<T, W, N, true>(acc, c, ld, rows, cols, m, n, add, lane);
+    else write_tiles<T, W, N, false>(acc, c, ld, rows, cols, m, n, add, lane);
 }
 
 #endif
@@ -211,15 +214,16 @@ struct Grid {
     int32_t tiles_m, tiles_n, splits, steps;    // steps: stages per split
 };
 
-template <int W, int FA, int FB, bool WIDE>
+template <int W, int WM, int FA, int FB, bool WIDE>
 __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product p, Grid g)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    using G = Geometry<W>;
+    using G = Geometry<W, WM>;
     constexpr int N = G::kTiles;
-    __shared__ __attribute__((aligned(16))) uint8_t a0[G::kStage], b0[G::kStage], a1[G::kStage], b1[G::kStage];
+    __shared__ __attribute__((aligned(16))) uint8_t a0[G::kStageA], b0[G::kStageB], a1[G::kStageA], b1[G::kStageB];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave_m = wave / G::kWavesN, wave_n = wave % G::kWavesN;
 
     // Consecutive blocks go to the 8 XCDs in turn: give each XCD a run of
     // tiles, 8 rows of tiles deep, so that its L2 serves their operands.
@@ -234,28 +238,30 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
         const int in = id - group * deep;
         id = (first + in % rows) * g.tiles_n + in / rows;
     }
-    const int64_t m0 = static_cast<int64_t>(id / g.tiles_n) * G::kSide, n0 = static_cast<int64_t>(id % g.tiles_n) * G::kSide;
+    const int64_t m0 = static_cast<int64_t>(id / g.tiles_n) * G::kRowsA, n0 = static_cast<int64_t>(id % g.tiles_n) * G::kRowsB;
     const int64_t blocks = (p.a.k + kBytes - 1) / kBytes;
     const int64_t kb0 = static_cast<int64_t>(split) * g.steps;
     const int steps = static_cast<int>(blocks - kb0 < g.steps ? blocks - kb0 : g.steps);
 
     // A row past the operand's end is read as its last row: its outputs are
     // not stored.
-    uint32_t off_a[G::kLoads], off_b[G::kLoads];
-    const int last_a = static_cast<int>(p.a.rows - m0 < G::kSide ? p.a.rows - m0 : G::kSide) - 1;
-    const int last_b = static_cast<int>(p.b.rows - n0 < G::kSide ? p.b.rows - n0 : G::kSide) - 1;
-#pragma unroll
-    for (int q = 0; q < G::kLoads; ++q) {
+    uint32_t off_a[G::kLoadsA], off_b[G::kLoadsB];
+    const int last_a = static_cast<int>(p.a.rows - m0 < G::kRowsA ? p.a.rows - m0 : G::kRowsA) - 1;
+    const int last_b = static_cast<int>(p.b.rows - n0 < G::kRowsB ? p.b.rows - n0 : G::kRowsB) - 1;
+    auto offset = [&](int q, int last, int64_t ld) {
         const int row = (q * 4 + wave) * 8 + (lane >> 3);
-        const uint32_t chunk = ((lane & 7) ^ swizzle<W>(row)) * 16;
-        off_a[q] = static_cast<uint32_t>(row < last_a ? row : last_a) * static_cast<uint32_t>(p.a.ld) + chunk;
-        off_b[q] = static_cast<uint32_t>(row < last_b ? row : last_b) * static_cast<uint32_t>(p.b.ld) + chunk;
-    }
+        return static_cast<uint32_t>(row < last ? row : last) * static_cast<uint32_t>(ld) +
+               ((lane & 7) ^ swizzle<W>(row)) * 16u;
+    };
+#pragma unroll
+    for (int q = 0; q < G::kLoadsA; ++q) off_a[q] = offset(q, last_a, p.a.ld);
+#pragma unroll
+    for (int q = 0; q < G::kLoadsB; ++q) off_b[q] = offset(q, last_b, p.b.ld);
     const auto ga = buffer(p.a.data + m0 * p.a.ld + kb0 * kBytes,
                                              (p.a.rows - m0) * p.a.ld - kb0 * kBytes);
     const auto gb = buffer(p.b.data + n0 * p.b.ld + kb0 * kBytes,
                                              (p.b.rows - n0) * p.b.ld - kb0 * kBytes);
-    const int row_a = (wave >> 1) * W + (lane & 31) * N, row_b = (wave & 1) * W + (lane & 31) * N;
+    const int row_a = wave_m * W + (lane & 31) * N, row_b = wave_n * W + (lane & 31) * N;
     const int64_t sra = m0 + row_a < p.a.lds - N ? m0 + row_a : p.a.lds - N;
     const int64_t srb = n0 + row_b < p.b.lds - N ? n0 + row_b : p.b.lds - N;
     const uint8_t* sa = p.a.scales + kb0 * p.a.lds + sra;
@@ -281,10 +287,10 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
     auto load = [&](int k, uint8_t* a, uint8_t* b) {
         const int at = (k < steps ? k : steps - 1) * kBytes;
 #pragma unroll
-        for (int q = 0; q < G::kLoads; ++q)
+        for (int q = 0; q < G::kLoadsA; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ga, (lds_ptr)(a + (q * 4 + wave) * 1024), 16, off_a[q], at, 0, 0);
 #pragma unroll
-        for (int q = 0; q < G::kLoads; ++q)
+        for (int q = 0; q < G::kLoadsB; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(gb, (lds_ptr)(b + (q * 4 + wave) * 1024), 16, off_b[q], at, 0, 0);
     };
     Fragments<WIDE, N> frag[2];
@@ -330,7 +336,7 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
         read(frag[0], an, bn, 0);
         load(k + 2, a, b);
         multiply(frag[1], xa[s], xb[s], frag[0], xa[s ^ 1], xb[s ^ 1]);
-        interleave<kMfma, kReads, 2 * G::kLoads, WIDE ? kMfma * 2 : 0>();
+        interleave<kMfma, kReads, G::kLoadsA + G::kLoadsB, WIDE ? kMfma * 2 : 0>();
         __builtin_amdgcn_sched_barrier(0);
         scales(k + 2, s);
     };
@@ -348,34 +354,49 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
         k += 2;
     } while (k < steps);
 
-    // every wave has its last fragments: the stages' LDS is free
-    __syncthreads();
-    float* lds = reinterpret_cast<float*>((wave >> 1 ? b0 : a0) + (wave & 1) * (G::kStage / 2));
-    const int64_t m = m0 + (wave >> 1) * W, n = n0 + (wave & 1) * W, rows = p.a.rows, cols = p.b.rows;
+    // the last loads land in LDS before this block gives it up
+    __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0)
+    const int64_t m = m0 + wave_m * W, n = n0 + wave_n * W, rows = p.a.rows, cols = p.b.rows;
     const bool add = p.accumulate != 0;
     if (g.splits > 1)
-        write_outputs<float, W, N>(acc, p.partial + split * rows * cols, cols, rows, cols, m, n, false, lds, lane);
+        write_outputs<float, W, N>(acc, p.partial + split * rows * cols, cols, rows, cols, m, n, false, lane);
     else if constexpr (WIDE)
-        write_outputs<float, W, N>(acc, static_cast<float*>(p.c), p.ldc, rows, cols, m, n, add, lds, lane);
+        write_outputs<float, W, N>(acc, static_cast<float*>(p.c), p.ldc, rows, cols, m, n, add, lane);
     else if (p.c_dtype == DTYPE_BF16)
-        write_outputs<bf16, W, N>(acc, static_cast<bf16*>(p.c), p.ldc, rows, cols, m, n, add, lds, lane);
+        write_outputs<bf16, W, N>(acc, static_cast<bf16*>(p.c), p.ldc, rows, cols, m, n, add, lane);
     else
-        write_outputs<f16, W, N>(acc, static_cast<f16*>(p.c), p.ldc, rows, cols, m, n, add, lds, lane);
+        write_outputs<f16, W, N>(acc, static_cast<f16*>(p.c), p.ldc, rows, cols, m, n, add, lane);
 #endif
 }
 
 // The splits' partial products joined in order (splits = 0: an empty
-// contraction).
+// contraction), 4 outputs a thread.
 template <typename T> __global__ __launch_bounds__(256) void join(Fp8Product p, int splits)
 {
     const int64_t n = p.b.rows, total = p.a.rows * n;
     const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
-    for (int e = 0; e < 4; ++e) {
-        if (i + e >= total) return;
-        float s = 0.0f;
-        for (int k = 0; k < splits; ++k) s += p.partial[k * total + i + e];
-        T* c = static_cast<T*>(p.c) + (i + e) / n * p.ldc + (i + e) % n;
-        *c = from_float<T>(p.accumulate ? to_float(*c) + s : s);
+    if (i >= total) return;
+    const int count = total - i < 4 ? static_cast<int>(total - i) : 4;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (count == 4) {
+#pragma unroll 4
+        for (int k = 0; k < splits; ++k) {
+            const Pack<float, 4> x = load_pack<float, 4>(p.partial + k * total + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += x.v[e];
+        }
+    } else {
+        for (int k = 0; k < splits; ++k)
+            for (int e = 0; e < count; ++e) s[e] += p.partial[k * total + i + e];
+    }
+    int64_t row = i / n, col = i - row * n;
+    for (int e = 0; e < count; ++e) {
+        T* c = static_cast<T*>(p.c) + row * p.ldc + col;
+        *c = from_float<T>(p.accumulate ? to_float(*c) + s[e] : s[e]);
+        if (++col == n) {
+            col = 0;
+            ++row;
+        }
     }
 }
 
@@ -389,51 +410,80 @@ hipError_t launch_join(const Fp8Product& p, int splits, hipStream_t s)
     return hipGetLastError();
 }
 
-// 256 x 256 tiles where they fill the chip, else 128 x 128 ones, their
-// contraction split until 256 blocks are there (at least 4 stages each).
+enum Shape { k256, k128, k64Rows, k64Cols };    // block tiles 256 x 256, 128 x 128, 64 x 256, 256 x 64
 struct Plan {
-    bool large;
+    Shape shape;
     Grid g;
 };
+
+// Share of the chip that `tiles` equal blocks use, `slots` of which run at
+// once.
+double use(int64_t tiles, int64_t slots)
+{
+    return static_cast<double>(tiles) / static_cast<double>((tiles + slots - 1) / slots * slots);
+}
+
+// 256 x 256 tiles (one block per CU) reach twice the rate of 128 x 128 ones
+// (two per CU), whose fragments need all of LDS's bandwidth, so the smaller
+// are taken only where they use more than 1.6 times as much of the chip
+// (4,099 x 2,002 x 5,003: 66 against 72 us), and where they do not outnumber
+// the CUs, so that one's latency is all that counts (300 x 5,000 x 700: 10
+// against 16 us).
+// Few rows on one side take tiles of 64 of them.  Where tiles leave half of
+// the chip or more idle, the contraction is split, at least 4 stages each.
 Plan plan_of(int64_t m, int64_t n, int64_t k)
 {
+    const auto count = [](int64_t x, int64_t side) { return (x + side - 1) / side; };
     Plan p;
-    const int64_t large = ((m + 255) / 256) * ((n + 255) / 256);
-    p.large = large >= 192;
-    const int64_t side = p.large ? 256 : 128;
-    p.g.tiles_m = static_cast<int32_t>((m + side - 1) / side);
-    p.g.tiles_n = static_cast<int32_t>((n + side - 1) / side);
-    const int64_t tiles = static_cast<int64_t>(p.g.tiles_m) * p.g.tiles_n, blocks = (k + kBytes - 1) / kBytes;
-    int64_t splits = 1;
-    if (!p.large && tiles < 256) {
-        splits = (256 + tiles - 1) / tiles;
-        if (splits > blocks / 4) splits = blocks / 4;
-        if (splits > kMaxSplits) splits = kMaxSplits;
-        if (splits < 1) splits = 1;
+    int64_t side_m = 256, side_n = 256;
+    if (m <= kFewRows) {
+        p.shape = k64Rows;
+        side_m = 64;
+    } else if (n <= kFewRows) {
+        p.shape = k64Cols;
+        side_n = 64;
+    } else if (count(m, 128) * count(n, 128) > 256 &&
+               use(count(m, 256) * count(n, 256), 256) * 1.6 >= use(count(m, 128) * count(n, 128), 512)) {
+        p.shape = k256;
+    } else {
+        p.shape = k128;
+        side_m = side_n = 128;
     }
+    const int64_t tiles = count(m, side_m) * count(n, side_n), blocks = count(k, kBytes);
+    int64_t splits = 256 / tiles;
+    if (splits > blocks / 4) splits = blocks / 4;
+    if (splits > kMaxSplits) splits = kMaxSplits;
+    if (splits < 1) splits = 1;
+    p.g.tiles_m = static_cast<int32_t>(count(m, side_m));
+    p.g.tiles_n = static_cast<int32_t>(count(n, side_n));
     p.g.steps = static_cast<int32_t>((blocks + splits - 1) / splits);
+    if (splits > 1) p.g.steps += p.g.steps & 1;     // the kernel takes stages in pairs
     p.g.splits = static_cast<int32_t>((blocks + p.g.steps - 1) / p.g.steps);
     return p;
 }
 
-template <int FA, int FB> hipError_t launch_formats(const Fp8Product& p, const Plan& plan, hipStream_t s)
+template <int FA, int FB, bool WIDE> hipError_t launch_arithmetic(const Fp8Product& p, const Plan& plan, hipStream_t s)
 {
     const unsigned blocks = static_cast<unsigned>(plan.g.tiles_m) * plan.g.tiles_n * plan.g.splits;
-    if (p.c_dtype == DTYPE_F32) {
-        if (plan.large) product<128, FA, FB, true><<<blocks, kThreads, 0, s>>>(p, plan.g);
-        else product<64, FA, FB, true><<<blocks, kThreads, 0, s>>>(p, plan.g);
-    } else {
-        if (plan.large) product<128, FA, FB, false><<<blocks, kThreads, 0, s>>>(p, plan.g);
-        else product<64, FA, FB, false><<<blocks, kThreads, 0, s>>>(p, plan.g);
+    switch (plan.shape) {
+    case k256: product<128, 2, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
+    case k128: product<64, 2, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
+    case k64Rows: product<64, 1, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
+    case k64Cols: product<64, 4, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
     }
     return hipGetLastError();
+}
+
+template <int FA, int FB> hipError_t launch_formats(const Fp8Product& p, const Plan& plan, hipStream_t s)
+{
+    return p.c_dtype == DTYPE_F32 ? launch_arithmetic<FA, FB, true>(p, plan, s) : launch_arithmetic<FA, FB, false>(p, plan, s);
 }
 
 }  // namespace
 
 size_t fp8_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
-    if (m < 1 || n < 1 || k < 1) return 0;
+    if (m < 1 || n < 1 || k < 1 || fp8_few(m, n, k)) return 0;
     const Plan p = plan_of(m, n, k);
     return p.g.splits > 1 ? sizeof(float) * static_cast<size_t>(p.g.splits) * static_cast<size_t>(m) * static_cast<size_t>(n) : 0;
 }
@@ -441,6 +491,7 @@ size_t fp8_workspace_bytes(int64_t m, int64_t n, int64_t k)
 hipError_t launch_fp8_product(const Fp8Product& p, hipStream_t s)
 {
     if (p.a.k == 0) return launch_join(p, 0, s);
+    if (fp8_few(p.a.rows, p.b.rows, p.a.k)) return launch_fp8_few(p, s);
     const Plan plan = plan_of(p.a.rows, p.b.rows, p.a.k);
     hipError_t e;
     if (p.a.format == FP8_E4M3)
