@@ -4,7 +4,8 @@ the parameter server turns a fetched theta into its gradient.
 
 Argument marshalling only, as in the package's __init__ (which re-exports
 these names): every step runs in the HIP kernels of libfasgd.so, there is no
-fallback, and no call allocates.  Activations are CUDA (HIP) tensors of one
+fallback, and no call allocates.  Plain arguments are marshalled natively
+(csrc/marshal.cpp), others below, with the same library call.  Activations are CUDA (HIP) tensors of one
 dtype (float32, bfloat16 or float16) of one or two dimensions whose last
 stride is 1 (rows may lie apart); parameters and their gradients are
 contiguous float32 tensors.
@@ -80,6 +81,21 @@ def bind(lib):
     return lib
 
 
+_calls = None     # module _marshal with the client's entry points bound, or what stands in for it
+
+
+def _native():
+    global _calls
+    if _calls is None:
+        from . import _native as package_native
+        m = package_native()
+        if hasattr(m, "CLIENT_ENTRY_POINTS") and isinstance(m.CLIENT_ENTRY_POINTS, tuple):
+            lib = _library()
+            m.bind_client([ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in m.CLIENT_ENTRY_POINTS])
+        _calls = m
+    return _calls
+
+
 def _check(rc: int):
     if rc != 0:
         from . import FasgdError
@@ -136,6 +152,9 @@ def client_dropout(x, out, p: float, seed: int, T: int, client: int, site: int =
     """out = [residual +] dropout(x) with the mask drawn from (seed, T, client,
     site, index); the backward pass is the same call on the gradient, without
     residual.  out may be x or residual."""
+    rc = (_calls or _native()).client_dropout(x, out, p, seed, T, client, site, residual, index_base, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     px, ldx = _matrix(x, "x")
     py, ldy = _matrix(out, "out", x)
     pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x)
@@ -214,6 +233,11 @@ def client_residual_norm_forward(branch, residual, sum_out, normed, stats, *, ki
     gate: None, float32 [cols] (per channel), float32 [rows, 1] (per row) or a matrix like branch.  residual may be
     None.  dropout: None or (p, seed, T, client, site) as client_dropout takes them.  stats: float32 [rows, 4], kept
     for the backward pass."""
+    rc = (_calls or _native()).client_residual_norm_forward(
+        branch, residual, sum_out, normed, stats, kind, w_post, b_post, gate, gate_act, w_pre, b_pre, residual_scale,
+        eps, dropout, index_base, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     op = _norm_op(branch, kind, w_post, b_post, gate, gate_act, w_pre, b_pre, residual_scale, eps, dropout, index_base)
     pb, lb = _matrix(branch, "branch")
     pr, lr = _optional(residual, "residual", branch)
@@ -232,6 +256,11 @@ def client_residual_norm_backward(branch, sum_in, stats, dsum, dnormed, dbranch,
     and of normed (dnormed, or None without w_pre), into dbranch, dresidual (or None; may be dsum), and where given
     dw_post, db_post, dw_pre, db_pre (float32 [cols]) and dgate (like gate).  workspace: uint8,
     client_residual_norm_workspace_bytes(rows, cols) bytes."""
+    rc = (_calls or _native()).client_residual_norm_backward(
+        branch, sum_in, stats, dsum, dnormed, dbranch, dresidual, dw_post, db_post, dgate, dw_pre, db_pre, workspace,
+        kind, w_post, b_post, gate, gate_act, w_pre, b_pre, residual_scale, eps, dropout, index_base, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     import torch
     op = _norm_op(branch, kind, w_post, b_post, gate, gate_act, w_pre, b_pre, residual_scale, eps, dropout, index_base)
     cols = op.cols
@@ -298,6 +327,10 @@ def client_fp8_workspace_bytes(m: int, n: int, k: int) -> int:
 def client_fp8_quantize(x, by_rows=None, by_cols=None, block_rows: int = 1, stream=None) -> None:
     """Quantizes x [rows, cols] into the operand by_rows ([rows, k = cols]) and / or by_cols (the transpose,
     [cols, k = rows]); block_rows = 128 takes one scale per 128 x 128 block (weights)."""
+    rc = (_calls or _native()).client_fp8_quantize(
+        x, None if by_rows is None else by_rows.c, None if by_cols is None else by_cols.c, block_rows, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     px, ldx = _matrix(x, "x")
     rows, cols = _shape(x)
     _check(_library().client_fp8_quantize(px, ldx, rows, cols, _dtype(x, "x"), int(block_rows),
@@ -316,6 +349,9 @@ def _workspace(workspace):
 def client_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out, accumulate: bool = False, workspace=None, stream=None) -> None:
     """out [a.rows, b.rows] = a b^T over their common k (accumulate: added to out).  workspace: uint8,
     client_fp8_workspace_bytes(a.rows, b.rows, k) bytes."""
+    rc = (_calls or _native()).client_fp8_matmul(a.c, b.c, out, accumulate, workspace, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     pc, ldc = _matrix(out, "out")
     if _shape(out) != (a.rows, b.rows):
         raise ValueError(f"out is {tuple(out.shape)}, expected {(a.rows, b.rows)}")
@@ -327,6 +363,9 @@ def client_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out, accumulate: bool = Fals
 def client_fp8_linear(x, w: Fp8Operand, out, workspace=None, stream=None) -> None:
     """out [m, w.rows] = x w^T for x [m, w.k] of out's dtype, quantized in e4m3 on the way.  workspace: uint8,
     client_fp8_workspace_bytes(m, w.rows, w.k) bytes."""
+    rc = (_calls or _native()).client_fp8_linear(x, w.c, out, workspace, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     px, ldx = _matrix(x, "x")
     py, ldy = _matrix(out, "out")
     if out.dtype != x.dtype:

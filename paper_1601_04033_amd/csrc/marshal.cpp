@@ -17,7 +17,7 @@
 #include <stdint.h>
 #include <string.h>
 
-#include "../../include/fasgd.h"
+#include "../../include/fasgd_client.h"
 
 namespace {
 
@@ -42,6 +42,21 @@ struct Entry {
     decltype(&::bfasgd_apply_segments) bfasgd_apply_segments;
 };
 static_assert(sizeof(Entry) == kCount * sizeof(void*), "one pointer per name");
+// and the client's, by the order of kClientNames
+constexpr const char* kClientNames[] = {"client_dropout", "client_residual_norm_forward",
+                                        "client_residual_norm_backward", "client_fp8_quantize", "client_fp8_matmul",
+                                        "client_fp8_linear"};
+constexpr int kClientCount = sizeof kClientNames / sizeof kClientNames[0];
+struct ClientEntry {
+    decltype(&::client_dropout) client_dropout;
+    decltype(&::client_residual_norm_forward) client_residual_norm_forward;
+    decltype(&::client_residual_norm_backward) client_residual_norm_backward;
+    decltype(&::client_fp8_quantize) client_fp8_quantize;
+    decltype(&::client_fp8_matmul) client_fp8_matmul;
+    decltype(&::client_fp8_linear) client_fp8_linear;
+};
+static_assert(sizeof(ClientEntry) == kClientCount * sizeof(void*), "one pointer per name");
+ClientEntry g_client;                 // set by bind_client()
 Entry g_lib;                          // set by bind(), once, before any other call
 PyObject* g_current_stream = nullptr; // callable: the current stream's handle as an int
 
@@ -578,6 +593,294 @@ PyObject* apply_segments(PyObject*, PyObject* const* args, Py_ssize_t n)
     return finish(a, [&] { return g_lib.bfasgd_apply_segments(st, g, seg, S, send, client, ts, s); });
 }
 
+// ---- the client's operators
+
+// A matrix of activations: one or two dimensions, last stride 1.
+struct Matrix {
+    void* p = nullptr;
+    int64_t rows = 0, cols = 0, ld = 0;
+    int32_t dtype = -1;
+    int dim = 0;
+};
+
+struct ClientArgs : Args {
+    Py_buffer operand_view[2] = {};
+    explicit ClientArgs(PyObject* const* args) : Args(args) {}
+    ~ClientArgs()
+    {
+        for (Py_buffer& b : operand_view)
+            if (b.obj) PyBuffer_Release(&b);
+    }
+
+    Matrix matrix(int i)
+    {
+        Matrix m;
+        if (!plain) return m;
+        if (!THPVariable_CheckExact(v[i])) {
+            refuse();
+            return m;
+        }
+        try {
+            const at::Tensor& t = THPVariable_Unpack(v[i]);
+            switch (t.scalar_type()) {
+            case c10::ScalarType::Float: m.dtype = CLIENT_F32; break;
+            case c10::ScalarType::BFloat16: m.dtype = CLIENT_BF16; break;
+            case c10::ScalarType::Half: m.dtype = CLIENT_F16; break;
+            default: break;
+            }
+            m.dim = static_cast<int>(t.dim());
+            if (!t.is_cuda() || m.dtype < 0 || m.dim < 1 || m.dim > 2) {
+                refuse();
+                return m;
+            }
+            m.rows = m.dim == 2 ? t.size(0) : 1;
+            m.cols = t.size(m.dim - 1);
+            if (m.cols > 1 && t.stride(m.dim - 1) != 1) {
+                refuse();
+                return m;
+            }
+            m.ld = m.rows > 1 ? t.stride(0) : m.cols;
+            m.p = t.data_ptr();
+        } catch (...) {
+            refuse();
+        }
+        return m;
+    }
+    // one of the shape and type of `like`; None where it may be absent
+    Matrix matrix_like(int i, const Matrix& like, bool optional = false)
+    {
+        if (!plain || (optional && v[i] == Py_None)) return Matrix{};
+        const Matrix m = matrix(i);
+        if (plain && (m.dtype != like.dtype || m.dim != like.dim || m.rows != like.rows || m.cols != like.cols)) refuse();
+        return m;
+    }
+    // an optional parameter vector
+    float* parameters(int i, int64_t n) { return plain && v[i] != Py_None ? floats(i, n) : nullptr; }
+    double wide_real(PyObject* o)
+    {
+        if (!plain) return 0.0;
+        const double d = PyFloat_AsDouble(o);
+        if (d == -1.0 && PyErr_Occurred()) refuse();
+        return d;
+    }
+    uint64_t seed_of(PyObject* o)
+    {
+        if (!plain) return 0;
+        PyObject* x = PyNumber_Index(o);
+        if (!x) {
+            refuse();
+            return 0;
+        }
+        const uint64_t r = PyLong_AsUnsignedLongLongMask(x);
+        Py_DECREF(x);
+        if (PyErr_Occurred()) refuse();
+        return r;
+    }
+    // an 8-bit operand's struct (a ctypes Structure, by its buffer); None: NULL
+    client_fp8_operand* operand(int i, int which)
+    {
+        if (!plain || v[i] == Py_None) return nullptr;
+        if (PyObject_GetBuffer(v[i], &operand_view[which], PyBUF_WRITABLE) != 0 ||
+            operand_view[which].len != static_cast<Py_ssize_t>(sizeof(client_fp8_operand))) {
+            refuse();
+            return nullptr;
+        }
+        return static_cast<client_fp8_operand*>(operand_view[which].buf);
+    }
+    void* workspace(int i, int64_t* n)
+    {
+        *n = 0;
+        return plain && v[i] != Py_None ? tensor(i, c10::ScalarType::Byte, -1, 0, n) : nullptr;
+    }
+    // gate forms as the binding's general way tells them apart
+    bool gate(int i, const Matrix& like, int32_t* form, void** p, int64_t* ld)
+    {
+        *form = CLIENT_GATE_NONE;
+        *p = nullptr;
+        *ld = 0;
+        if (!plain || v[i] == Py_None) return plain;
+        const Matrix g = matrix(i);
+        if (!plain) return false;
+        const bool same = g.dtype == like.dtype && g.dim == like.dim && g.rows == like.rows && g.cols == like.cols;
+        if (same && (g.dim == 2 || g.dtype != CLIENT_F32)) {
+            *form = CLIENT_GATE_FULL;
+            *ld = g.ld;
+        } else if (g.dtype != CLIENT_F32) {
+            return refuse();
+        } else if (g.dim == 1 && g.cols == like.cols) {
+            *form = CLIENT_GATE_CHANNEL;
+        } else if (g.dim == 2 && g.cols == 1 && g.rows == like.rows && (g.ld == 1 || g.rows == 1)) {
+            *form = CLIENT_GATE_ROW;
+        } else {
+            return refuse();
+        }
+        *p = g.p;
+        return true;
+    }
+    // from `at` on: kind, w_post, b_post, gate, gate_act, w_pre, b_pre, residual_scale, eps, dropout, index_base
+    client_residual_norm norm(int at, const Matrix& x)
+    {
+        client_residual_norm op;
+        memset(&op, 0, sizeof op);
+        op.rows = x.rows;
+        op.cols = x.cols;
+        op.dtype = x.dtype;
+        op.kind = int32(at);
+        op.w_post = parameters(at + 1, x.cols);
+        op.b_post = parameters(at + 2, x.cols);
+        void* g = nullptr;
+        gate(at + 3, x, &op.gate_form, &g, &op.ld_gate);
+        op.gate = g;
+        op.gate_act = int32(at + 4);
+        op.w_pre = parameters(at + 5, x.cols);
+        op.b_pre = parameters(at + 6, x.cols);
+        op.residual_scale = real(at + 7);
+        op.eps = real(at + 8);
+        if (plain && v[at + 9] != Py_None) {
+            PyObject* d = v[at + 9];
+            if (!PyTuple_CheckExact(d) || PyTuple_GET_SIZE(d) != 5) {
+                refuse();
+                return op;
+            }
+            op.p = wide_real(PyTuple_GET_ITEM(d, 0));
+            op.seed = seed_of(PyTuple_GET_ITEM(d, 1));
+            op.T = integer_of(PyTuple_GET_ITEM(d, 2));
+            op.client = narrow(integer_of(PyTuple_GET_ITEM(d, 3)));
+            op.site = narrow(integer_of(PyTuple_GET_ITEM(d, 4)));
+        }
+        op.index_base = int64(at + 10);
+        return op;
+    }
+};
+
+// (x, out, p, seed, T, client, site, residual, index_base, stream)
+PyObject* client_dropout_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 10)) return nullptr;
+    ClientArgs a(args);
+    const Matrix x = a.matrix(0), y = a.matrix_like(1, x), r = a.matrix_like(7, x, true);
+    const double p = a.wide_real(args[2]);
+    const uint64_t seed = a.seed(3);
+    const int64_t T = a.int64(4);
+    const int32_t client = a.int32(5), site = a.int32(6);
+    const int64_t base = a.int64(8);
+    hipStream_t s = a.stream(9);
+    return finish(a, [&] {
+        return g_client.client_dropout(x.p, x.ld, r.p, r.ld, y.p, y.ld, x.rows, x.cols, x.dtype, p, seed, T, client,
+                                       site, base, s);
+    });
+}
+
+// (branch, residual, sum, normed, stats, the operator's 11, stream)
+PyObject* norm_forward_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 17)) return nullptr;
+    ClientArgs a(args);
+    const Matrix x = a.matrix(0), r = a.matrix_like(1, x, true), sum = a.matrix_like(2, x), h = a.matrix_like(3, x, true);
+    float* stats = a.floats(4, 4 * x.rows);
+    const client_residual_norm op = a.norm(5, x);
+    hipStream_t s = a.stream(16);
+    return finish(a, [&] {
+        return g_client.client_residual_norm_forward(&op, x.p, x.ld, r.p, r.ld, sum.p, sum.ld, h.p, h.ld, stats, s);
+    });
+}
+
+// (branch, sum, stats, dsum, dnormed, dbranch, dresidual, dw_post, db_post, dgate, dw_pre, db_pre, workspace, the
+// operator's 11, stream)
+PyObject* norm_backward_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 25)) return nullptr;
+    ClientArgs a(args);
+    const Matrix x = a.matrix(0), sum = a.matrix_like(1, x, true);
+    const float* stats = a.floats(2, 4 * x.rows);
+    const Matrix ds = a.matrix_like(3, x, true), dh = a.matrix_like(4, x, true), dx = a.matrix_like(5, x),
+                 dr = a.matrix_like(6, x, true);
+    float* dwp = a.parameters(7, x.cols);
+    float* dbp = a.parameters(8, x.cols);
+    int32_t form = 0;
+    void* dg = nullptr;
+    int64_t ld_dg = 0;
+    a.gate(9, x, &form, &dg, &ld_dg);
+    float* dwn = a.parameters(10, x.cols);
+    float* dbn = a.parameters(11, x.cols);
+    int64_t ws = 0;
+    void* w = a.workspace(12, &ws);
+    const client_residual_norm op = a.norm(13, x);
+    if (a.plain && dg && form != op.gate_form) a.refuse();
+    hipStream_t s = a.stream(24);
+    return finish(a, [&] {
+        return g_client.client_residual_norm_backward(&op, x.p, x.ld, sum.p, sum.ld, stats, ds.p, ds.ld, dh.p, dh.ld, dx.p,
+                                                      dx.ld, dr.p, dr.ld, dwp, dbp, dg, ld_dg, dwn, dbn, w,
+                                                      static_cast<size_t>(ws), s);
+    });
+}
+
+// (x, by_rows, by_cols, block_rows, stream)
+PyObject* quantize_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 5)) return nullptr;
+    ClientArgs a(args);
+    const Matrix x = a.matrix(0);
+    const client_fp8_operand *r = a.operand(1, 0), *c = a.operand(2, 1);
+    const int32_t block = a.int32(3);
+    hipStream_t s = a.stream(4);
+    return finish(a, [&] { return g_client.client_fp8_quantize(x.p, x.ld, x.rows, x.cols, x.dtype, block, r, c, s); });
+}
+
+// (a, b, out, accumulate, workspace, stream)
+PyObject* matmul_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 6)) return nullptr;
+    ClientArgs a(args);
+    const client_fp8_operand *x = a.operand(0, 0), *y = a.operand(1, 1);
+    const Matrix c = a.matrix(2);
+    if (a.plain && (!x || !y || c.rows != x->rows || c.cols != y->rows || (args[3] != Py_True && args[3] != Py_False)))
+        a.refuse();
+    int64_t ws = 0;
+    void* w = a.workspace(4, &ws);
+    hipStream_t s = a.stream(5);
+    return finish(a, [&] {
+        return g_client.client_fp8_matmul(x, y, c.p, c.ld, c.dtype, args[3] == Py_True, w, static_cast<size_t>(ws), s);
+    });
+}
+
+// (x, w, out, workspace, stream)
+PyObject* linear_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 5)) return nullptr;
+    ClientArgs a(args);
+    const Matrix x = a.matrix(0);
+    const client_fp8_operand* w = a.operand(1, 0);
+    const Matrix y = a.matrix(2);
+    if (a.plain && (!w || x.dtype != y.dtype || x.cols != w->k || y.rows != x.rows || y.cols != w->rows)) a.refuse();
+    int64_t ws = 0;
+    void* p = a.workspace(3, &ws);
+    hipStream_t s = a.stream(4);
+    return finish(a, [&] {
+        return g_client.client_fp8_linear(x.p, x.ld, x.rows, w, y.p, y.ld, x.dtype, p, static_cast<size_t>(ws), s);
+    });
+}
+
+// bind_client(addresses of the entry points in kClientNames' order), after bind()
+PyObject* bind_client(PyObject*, PyObject* list)
+{
+    if (!PyList_Check(list) || PyList_GET_SIZE(list) != kClientCount) {
+        PyErr_SetString(PyExc_ValueError, "_marshal.bind_client: one address per entry point");
+        return nullptr;
+    }
+    void* p[kClientCount];
+    for (int i = 0; i < kClientCount; ++i) {
+        p[i] = PyLong_AsVoidPtr(PyList_GET_ITEM(list, i));
+        if (PyErr_Occurred()) return nullptr;
+        if (!p[i]) {
+            PyErr_SetString(PyExc_ValueError, "_marshal.bind_client: NULL address");
+            return nullptr;
+        }
+    }
+    memcpy(&g_client, p, sizeof g_client);
+    Py_RETURN_NONE;
+}
+
 // bind(addresses of the entry points in kNames' order, current-stream callable)
 PyObject* bind(PyObject*, PyObject* args)
 {
@@ -618,6 +921,13 @@ PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, nullptr},
                           {kNames[9], fast(apply_fetch), METH_FASTCALL, nullptr},
                           {kNames[10], fast(decide_segments), METH_FASTCALL, nullptr},
                           {kNames[11], fast(apply_segments), METH_FASTCALL, nullptr},
+                          {"bind_client", bind_client, METH_O, nullptr},
+                          {kClientNames[0], fast(client_dropout_call), METH_FASTCALL, nullptr},
+                          {kClientNames[1], fast(norm_forward_call), METH_FASTCALL, nullptr},
+                          {kClientNames[2], fast(norm_backward_call), METH_FASTCALL, nullptr},
+                          {kClientNames[3], fast(quantize_call), METH_FASTCALL, nullptr},
+                          {kClientNames[4], fast(matmul_call), METH_FASTCALL, nullptr},
+                          {kClientNames[5], fast(linear_call), METH_FASTCALL, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
@@ -632,6 +942,10 @@ PyMODINIT_FUNC PyInit__marshal()
     if (!names) return nullptr;
     for (int i = 0; i < kCount; ++i) PyTuple_SET_ITEM(names, i, PyUnicode_FromString(kNames[i]));
     if (PyModule_AddObject(m, "ENTRY_POINTS", names) != 0) return nullptr;
+    PyObject* client = PyTuple_New(kClientCount);
+    if (!client) return nullptr;
+    for (int i = 0; i < kClientCount; ++i) PyTuple_SET_ITEM(client, i, PyUnicode_FromString(kClientNames[i]));
+    if (PyModule_AddObject(m, "CLIENT_ENTRY_POINTS", client) != 0) return nullptr;
     // at::Tensor's layout is that torch's alone
     if (PyModule_AddStringConstant(m, "TORCH_VERSION", FASGD_TORCH_VERSION) != 0) return nullptr;
     return m;
