@@ -47,6 +47,19 @@ template <typename T, int N> __device__ __forceinline__ void store_pack(T* p, co
     __builtin_memcpy(p, &r, sizeof r);
 }
 
+// x of this lane and of the lane LANES (16 or 32) away, in some order: what a
+// sum or a maximum over lanes joins, without a pass through LDS.
+struct Pair {
+    float x, y;
+};
+template <int LANES> __device__ __forceinline__ Pair across(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto r = LANES == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false)
+                               : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+
 // Key and counter words of one dropout (include/fasgd_client.h).
 struct DropKey {
     uint32_t key0, key1;        // seed low / high words

@@ -19,7 +19,14 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
     const int64_t n = a.rows * a.cols;
     const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * kChunk;
     if (i >= n) return;
-    int64_t r = i / a.cols, c = i % a.cols;
+    int64_t r, c;
+    if (n <= UINT32_MAX) {      // a 64-bit division costs as much as the draw
+        r = static_cast<uint32_t>(i) / static_cast<uint32_t>(a.cols);
+        c = i - r * a.cols;
+    } else {
+        r = i / a.cols;
+        c = i - r * a.cols;
+    }
     const uint32_t keep = keep_bits(a.key, a.key.chunk_base + i / kChunk);
     if (c + kChunk <= a.cols) {
         Pack<T, kChunk> v = load_pack<T, kChunk>(x + r * a.ldx + c);

@@ -38,11 +38,13 @@ __device__ __forceinline__ v8i join_chunks(const v4i& lo, const v4i& hi)
 // 16 rows x 128 of an operand: lane l holds row l % 16, the 16-byte chunks
 // l / 16 of the block's two halves (both sides agree, so which of the
 // contraction's values these are does not matter).
-__device__ __forceinline__ v8i read_rows(const Fp8View& v, int64_t row, int64_t kb, int lane)
+template <bool STREAM> __device__ __forceinline__ v8i read_rows(const Fp8View& v, int64_t row, int64_t kb, int lane)
 {
     const int64_t r = row + (lane & 15) < v.rows ? row + (lane & 15) : v.rows - 1;
     const uint8_t* p = v.data + r * v.ld + kb * kFp8Block + (lane >> 4) * 16;
-    return join_chunks(*reinterpret_cast<const v4i*>(p), *reinterpret_cast<const v4i*>(p + 64));
+    const v4i* q = reinterpret_cast<const v4i*>(p);
+    if (STREAM) return join_chunks(__builtin_nontemporal_load(q), __builtin_nontemporal_load(q + 4));
+    return join_chunks(q[0], q[4]);
 }
 __device__ __forceinline__ int read_scale(const Fp8View& v, int64_t row, int64_t kb, int lane)
 {
@@ -131,13 +133,13 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
             const int in = k + u * kWaves < blocks ? -1 : 0;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                g.big[u][n] = read_rows(p.big, r0 + n * 16, kb, lane);
+                g.big[u][n] = read_rows<true>(p.big, r0 + n * 16, kb, lane);
                 g.scale_big[u][n] = read_scale(p.big, r0 + n * 16, kb, lane) & in;
             }
             if constexpr (!FUSED) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    g.few[u][m] = read_rows(p.few, m0 + m * 16, kb, lane);
+                    g.few[u][m] = read_rows<false>(p.few, m0 + m * 16, kb, lane);
                     g.scale_few[u][m] = read_scale(p.few, m0 + m * 16, kb, lane) & in;
                 }
             }

@@ -39,10 +39,10 @@ template <int W, int WM> struct Geometry {
 
 #if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources
 
-// The 16-byte chunk of a row that lies in slot s of its 128 LDS bytes.  Rows
-// that one read touches together (kTiles apart) get their chunks in
-// different banks.
-template <int W> __device__ __forceinline__ int swizzle(int row) { return (row / (W / 32)) & 7; }
+// A stage in LDS: the rows that one read touches together, row r of tile i
+// for r = 0 .. 31, are neighbours, and the 16-byte chunk c of a row's 128
+// bytes lies in slot c ^ (r / 2 mod 8), so that 16 lanes meet in no bank.
+__device__ __forceinline__ int slot(int c, int r) { return c ^ (r >> 1 & 7); }
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
@@ -82,7 +82,7 @@ __device__ __forceinline__ void read_one(Fragments<WIDE, N>& f, const uint8_t* a
     constexpr int C = Sub<WIDE>::kChunks;
     const int i = q / (2 * C), rest = q % (2 * C), c = rest % C;
     const uint8_t* p = rest < C ? a + at.row_a : b + at.row_b;
-    const v4i x = *reinterpret_cast<const v4i*>(p + at.chunk[s * C + c] + i * kBytes);
+    const v4i x = *reinterpret_cast<const v4i*>(p + at.chunk[s * C + c] + i * 32 * kBytes);
     if (rest < C) f.a[i][c] = x;
     else f.b[i][c] = x;
 }
@@ -249,9 +249,9 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
     const int last_a = static_cast<int>(p.a.rows - m0 < G::kRowsA ? p.a.rows - m0 : G::kRowsA) - 1;
     const int last_b = static_cast<int>(p.b.rows - n0 < G::kRowsB ? p.b.rows - n0 : G::kRowsB) - 1;
     auto offset = [&](int q, int last, int64_t ld) {
-        const int row = (q * 4 + wave) * 8 + (lane >> 3);
-        return static_cast<uint32_t>(row < last ? row : last) * static_cast<uint32_t>(ld) +
-               ((lane & 7) ^ swizzle<W>(row)) * 16u;
+        const int place = (q * 4 + wave) * 8 + (lane >> 3), r = place % 32;
+        const int row = place / W * W + r * N + place % W / 32;
+        return static_cast<uint32_t>(row < last ? row : last) * static_cast<uint32_t>(ld) + slot(lane & 7, r) * 16u;
     };
 #pragma unroll
     for (int q = 0; q < G::kLoadsA; ++q) off_a[q] = offset(q, last_a, p.a.ld);
@@ -268,10 +268,10 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
     const uint8_t* sb = p.b.scales + kb0 * p.b.lds + srb;
 
     Places places;
-    places.row_a = row_a * kBytes;
-    places.row_b = row_b * kBytes;
+    places.row_a = (wave_m * W + (lane & 31)) * kBytes;
+    places.row_b = (wave_n * W + (lane & 31)) * kBytes;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) places.chunk[c] = ((c * 2 + (lane >> 5)) ^ (lane & 7)) * 16;    // swizzle(row) = lane & 7
+    for (int c = 0; c < 4; ++c) places.chunk[c] = slot(c * 2 + (lane >> 5), lane & 31) * 16;
 
     v16f acc[N][N];
 #pragma unroll

@@ -47,8 +47,14 @@ template <int LANES> __device__ __forceinline__ float lane_sum(float x)
     if constexpr (LANES >= 4) x += dpp<0x4E>(x);        // quad_perm 2 3 0 1
     if constexpr (LANES >= 8) x += dpp<0x141>(x);       // row_half_mirror
     if constexpr (LANES >= 16) x += dpp<0x140>(x);      // row_mirror
-    if constexpr (LANES >= 32) x += __shfl_xor(x, 16);
-    if constexpr (LANES >= 64) x += __shfl_xor(x, 32);
+    if constexpr (LANES >= 32) {
+        const Pair p = across<16>(x);
+        x = p.x + p.y;
+    }
+    if constexpr (LANES >= 64) {
+        const Pair p = across<32>(x);
+        x = p.x + p.y;
+    }
     return x;
 }
 
