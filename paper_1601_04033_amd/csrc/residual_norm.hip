@@ -27,6 +27,7 @@ constexpr int kLoopThreads = 1024;  // threads per row where a row does not fit 
 
 constexpr int kCols = 8;            // columns of a row per thread: one or two 16-byte vectors
 constexpr int kForwardWaves = 6;    // per SIMD, for which the kernels' registers are limited
+constexpr int kForwardGeneralWaves = 5;
 constexpr int kBackwardWaves = 4;
 constexpr int kSubThreads = 512;    // threads of a block whose waves hold whole rows
 
@@ -90,6 +91,33 @@ __device__ __forceinline__ float activate(float g, int act)
     if (act == ACT_SIGMOID) return 1.0f / (1.0f + expf(-g));
     if (act == ACT_TANH) return tanhf(g);
     return g;
+}
+// Activations of V gates in place, the kind of activation decided once.  FAST,
+// for gates of every element in 16-bit types: from the hardware's exponential
+// and reciprocal (an ulp of fp32 each, far below what these gates and sums
+// hold); near 0, tanh is its series, as the quotient would lose what the
+// subtraction cancels.
+template <bool FAST, int V> __device__ __forceinline__ void activate_all(float (&g)[V], int act)
+{
+    constexpr float kLog2e = 1.4426950408889634f;
+    if (act == ACT_SIGMOID) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            g[j] = FAST ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * g[j])) : activate(g[j], ACT_SIGMOID);
+    } else if (act == ACT_TANH) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (!FAST) {
+                g[j] = activate(g[j], ACT_TANH);
+                continue;
+            }
+            const float x = fabsf(g[j]), s = g[j] * g[j];
+            const float t = __builtin_amdgcn_exp2f(-2.0f * kLog2e * x);
+            const float large = __builtin_copysignf((1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), g[j]);
+            const float small = g[j] * fmaf(s, fmaf(s, fmaf(s, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+            g[j] = x < 0.125f ? small : large;
+        }
+    }
 }
 // the derivative, from the activation's value
 __device__ __forceinline__ float slope(float a, int act)
@@ -228,6 +256,25 @@ __device__ __forceinline__ void row_keep(const NormArgs& a, const Place<T, SUB>&
 #pragma unroll
     for (int v = 0; v < kVecs<T>; ++v) keep[v] = ~0u;
     if (!a.drop) return;
+    if constexpr (kVec<T> == 8 && (SUB == 0 || SUB == 64)) {
+        // A wave's lanes hold neighbouring runs of 8, which begin `off` into
+        // a chunk of the draws: a lane's run ends in its right neighbour's
+        // first chunk, and only the last lane's in one that no lane has drawn,
+        // which the scalar unit draws.
+        const int64_t first = row * a.cols + at.column(0);
+        const uint64_t chunk = static_cast<uint64_t>(a.key.chunk_base) + static_cast<uint64_t>(first >> 3);
+        const uint32_t mine = keep_bits(a.key, chunk);
+        const int off = __builtin_amdgcn_readfirstlane(static_cast<int>(first & 7));
+        keep[0] = mine;
+        if (off == 0) return;
+        const uint32_t low = __builtin_amdgcn_readlane(static_cast<uint32_t>(chunk), 63);
+        const uint32_t high = __builtin_amdgcn_readlane(static_cast<uint32_t>(chunk >> 32), 63);
+        const uint32_t last = keep_bits(a.key, (static_cast<uint64_t>(high) << 32 | low) + 1);
+        uint32_t next = __shfl_down(mine, 1);
+        if ((threadIdx.x & 63) == 63) next = last;
+        keep[0] = (mine << 8 | next) >> (8 - off);
+        return;
+    }
 #pragma unroll
     for (int v = 0; v < kVecs<T>; ++v)
         if (at.column(v) < cols) keep[v] = keep_run<kVec<T>>(a.key, row * a.cols + at.column(v));
@@ -243,7 +290,7 @@ __device__ __forceinline__ void row_keep(const NormArgs& a, const Place<T, SUB>&
 // ---- forward
 
 template <typename T, int SUB, int MAXT, bool GENERAL>
-__global__ __launch_bounds__(MAXT, MAXT == 1024 || GENERAL ? kBackwardWaves : kForwardWaves) void norm_forward(NormArgs a)
+__global__ __launch_bounds__(MAXT, GENERAL ? kForwardGeneralWaves : kForwardWaves) void norm_forward(NormArgs a)
 {
     constexpr int V = kVec<T>, NV = kVecs<T>;
     constexpr int kPost = 0, kPre = 1, kPostBias = 2, kPreBias = 3;
@@ -260,8 +307,7 @@ __global__ __launch_bounds__(MAXT, MAXT == 1024 || GENERAL ? kBackwardWaves : kF
         for (int j = 0; j < V; ++j) f[j] = 1.0f;
         if (a.gate_form == GATE_CHANNEL) {
             load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) f[j] = activate(f[j], a.gate_act);
+            activate_all<false>(f, a.gate_act);
         }
         const float scale = a.drop ? a.key.scale : 1.0f;
         load_params<V>(a.w_post, c, a.cols, 1.0f, x);
@@ -316,8 +362,12 @@ __global__ __launch_bounds__(MAXT, MAXT == 1024 || GENERAL ? kBackwardWaves : kF
             for (int j = 0; j < V; ++j)
                 d[v][j] = GENERAL ? fmaf(d[v][j] * k, w[j], b[j] * row_gate) : d[v][j] * k * w[j];
             if (GENERAL && a.gate_form == GATE_FULL) {
+                float f[V];
 #pragma unroll
-                for (int j = 0; j < V; ++j) d[v][j] *= activate(to_float(g[v].v[j]), a.gate_act);
+                for (int j = 0; j < V; ++j) f[j] = to_float(g[v].v[j]);
+                activate_all<sizeof(T) == 2>(f, a.gate_act);
+#pragma unroll
+                for (int j = 0; j < V; ++j) d[v][j] *= f[j];
             }
             Pack<T, V> out;
 #pragma unroll
@@ -376,8 +426,9 @@ __global__ __launch_bounds__(MAXT, SUB && GENERAL ? 2 : kBackwardWaves) void nor
         if (a.gate_form == GATE_CHANNEL) {
             float f[V];
             load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, f);
+            activate_all<false>(f, a.gate_act);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] *= activate(f[j], a.gate_act);
+            for (int j = 0; j < V; ++j) x[j] *= f[j];
         }
         params.set(kPost, v, at, x);
         load_params<V>(a.w_pre, c, a.cols, 1.0f, x);
@@ -475,11 +526,24 @@ __global__ __launch_bounds__(MAXT, SUB && GENERAL ? 2 : kBackwardWaves) void nor
             params.get(kPost, v, at, w);
             if constexpr (GENERAL) params.get(kPostBias, v, at, b);
             if (GENERAL && a.gate_form == GATE_FULL) {
+                float f[V], z[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float f = activate(to_float(g[v].v[j]), a.gate_act);
-                    out.v[j] = from_float<T>(ds[v][j] * fmaf(xh[v][j], w[j], b[j]) * slope(f, a.gate_act));
-                    ds[v][j] *= f;
+                    f[j] = to_float(g[v].v[j]);
+                    z[j] = ds[v][j] * fmaf(xh[v][j], w[j], b[j]);
+                }
+                activate_all<sizeof(T) == 2>(f, a.gate_act);
+                if (a.gate_act == ACT_SIGMOID) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) z[j] *= slope(f[j], ACT_SIGMOID);
+                } else if (a.gate_act == ACT_TANH) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) z[j] *= slope(f[j], ACT_TANH);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    out.v[j] = from_float<T>(z[j]);
+                    ds[v][j] *= f[j];
                 }
                 store_cols<T, V>(static_cast<T*>(a.dgate) + row * a.ld_dgate, c, cols, out);
             } else if (a.gate_form == GATE_ROW) {
@@ -774,7 +838,7 @@ void launch_kernel(const NormArgs& a, int threads, bool backward, hipStream_t s)
     const int64_t rpb = SUB ? kSubThreads / (SUB ? SUB : 1) : 1;
     const int64_t groups = (a.rows + rpb - 1) / rpb;
     if (!backward) {
-        const int64_t most = resident_blocks(GENERAL ? kBackwardWaves : kForwardWaves, a.cols);
+        const int64_t most = resident_blocks(GENERAL ? kForwardGeneralWaves : kForwardWaves, a.cols);
         norm_forward<T, SUB, MAXT, GENERAL><<<static_cast<unsigned>(groups < most ? groups : most), threads, 0, s>>>(a);
     } else {
         const int blocks = static_cast<int>(backward_blocks(groups, a.cols));
