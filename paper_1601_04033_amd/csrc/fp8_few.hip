@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
         v8i big[kAhead][NT], few[kAhead][kFew];
         int scale_big[kAhead][NT], scale_few[kAhead][kFew];
     };
-    // A block past the last is the last again, with scales of 2^-127: products of 0.
+    // A block past the last is the last again, with scales of 2^-127 each way: products of 0 in fp32.
     auto load = [&](Group& g, int k) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
                 const int kb = k + u * kWaves < blocks ? k + u * kWaves : blocks - 1;
                 const uint8_t* q = h.data + held_row * h.stride + kb * kFp8Block + (lane >> 4) * 16;
                 few[0] = join_chunks(*reinterpret_cast<const v4i*>(q), *reinterpret_cast<const v4i*>(q + 64));
-                scale_few[0] = h.scales[kb * 16 + held_row];
+                scale_few[0] = k + u * kWaves < blocks ? h.scales[kb * 16 + held_row] : 0;
             } else {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {

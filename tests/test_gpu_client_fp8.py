@@ -315,3 +315,23 @@ def test_rejections():
         fa.client_fp8_linear(torch.zeros(4, 128, device="cuda"), w, out)
     torch.cuda.synchronize()
     assert not out.any()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("m, n, k", [(1, 40, 128), (3, 9000, 300), (16, 50, 1200), (40, 300, 700)])
+def test_smallest_scales(dtype, m, n, k):
+    """Weights whose blocks have the smallest scale there is: what fills a wave's last group of blocks weighs nothing
+    even beside them.  Powers of two, so the products are exact."""
+    import torch
+    gpu()
+    g = torch.Generator().manual_seed(m + n)
+    x = torch.exp2(torch.randint(96, 100, (m, k), generator=g).float())
+    w = torch.exp2(-torch.randint(124, 126, (n, k), generator=g).float())
+    b = fa.client_fp8_operand(n, k)
+    fa.client_fp8_quantize(w.cuda(), b, block_rows=128)
+    assert int(b.scales[:, :n].max()) == 1
+    out = torch.empty(m, n, device="cuda", dtype=getattr(torch, dtype))
+    ws = torch.empty(fa.client_fp8_workspace_bytes(m, n, k), device="cuda", dtype=torch.uint8)
+    fa.client_fp8_linear(x.to(out.dtype).cuda(), b, out, workspace=ws)
+    want = x.double() @ w.double().t()
+    assert torch.equal(out.cpu(), want.to(torch.float32).to(out.dtype))
