@@ -556,6 +556,14 @@ __global__ __launch_bounds__(MAXT, SUB && GENERAL ? 2 : kBackwardWaves) void nor
                     out.v[j] = from_float<T>(z[j]);
                     ds[v][j] *= f[j];
                 }
+                if (a.drop) {
+                    // nor does the gate of what is dropped, were it infinite or NaN
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        out.v[j] = from_float<T>(kept(z[j], keep[v], V - 1 - j));
+                        ds[v][j] = kept(ds[v][j], keep[v], V - 1 - j);
+                    }
+                }
                 store_cols<T, V>(static_cast<T*>(a.dgate) + row * a.ld_dgate, c, cols, out);
             } else if (a.gate_form == GATE_ROW) {
 #pragma unroll
@@ -760,32 +768,32 @@ template <typename T> __global__ __launch_bounds__(kLoopThreads) void norm_backw
         const float m0 = two[0] * a.inv_cols, m1 = a.layer ? two[1] * a.inv_cols : 0.0f;
         float row_gate = 1.0f;
         if (a.gate_form == GATE_ROW) row_gate = activate(static_cast<const float*>(a.gate)[row], a.gate_act);
-        // ds, du and the normed branch value of one element
-        auto element = [&](int c, float& ds, float& du, float& xh1, float& xa) {
+        // ds, du, the normed branch value and the gate of one element; what is
+        // dropped takes no part, were it or its own gate infinite or NaN
+        auto element = [&](int c, float& ds, float& du, float& xh1, float& xa, float& g) {
             ds = a.dsum ? to_float(static_cast<const T*>(a.dsum)[row * a.ld_dsum + c]) : 0.0f;
             if (a.w_pre) {
                 const float xh = (to_float(s[c]) - st[2]) * st[3];
                 ds = fmaf(st[3], to_float(dh[c]) * a.w_pre[c] - m1 - xh * m0, ds);
             }
             du = ds;
+            g = row_gate;
+            if (a.gate_form == GATE_CHANNEL) g = activate(static_cast<const float*>(a.gate)[c], a.gate_act);
+            if (a.gate_form == GATE_FULL)
+                g = activate(to_float(static_cast<const T*>(a.gate)[row * a.ld_gate + c]), a.gate_act);
             xa = xh1 = (to_float(x[c]) - st[0]) * st[1];
             if (a.drop) {
                 const uint32_t keep = keep_run<1>(a.key, row * a.cols + c);
                 du = kept(du * a.key.scale, keep, 0);
                 xa = kept(xa, keep, 0);
+                if (a.gate_form == GATE_FULL) g = kept(g, keep, 0);
             }
-        };
-        auto gate_of = [&](int c) {
-            if (a.gate_form == GATE_CHANNEL) return activate(static_cast<const float*>(a.gate)[c], a.gate_act);
-            if (a.gate_form == GATE_FULL)
-                return activate(to_float(static_cast<const T*>(a.gate)[row * a.ld_gate + c]), a.gate_act);
-            return row_gate;
         };
         float three[2] = {0.0f, 0.0f}, dg_row[1] = {0.0f};
         for (int c = threadIdx.x; c < a.cols; c += kLoopThreads) {
-            float ds, du, xh, xa;
-            element(c, ds, du, xh, xa);
-            const float w = a.w_post ? a.w_post[c] : 1.0f, g = gate_of(c);
+            float ds, du, xh, xa, g;
+            element(c, ds, du, xh, xa, g);
+            const float w = a.w_post ? a.w_post[c] : 1.0f;
             const float z = fmaf(xa, w, a.b_post ? a.b_post[c] : 0.0f);
             if (a.gate_form == GATE_ROW) dg_row[0] = fmaf(du, z, dg_row[0]);
             const float own = a.gate_form == GATE_CHANNEL ? du : du * g;
@@ -810,9 +818,9 @@ template <typename T> __global__ __launch_bounds__(kLoopThreads) void norm_backw
         const float k0 = a.w_post ? three[0] * a.inv_cols : 0.0f;
         const float k1 = a.w_post && a.layer ? three[1] * a.inv_cols : 0.0f;
         for (int c = threadIdx.x; c < a.cols; c += kLoopThreads) {
-            float ds, du, xh, xa;
-            element(c, ds, du, xh, xa);
-            const float w = a.w_post ? a.w_post[c] : 1.0f, g = gate_of(c);
+            float ds, du, xh, xa, g;
+            element(c, ds, du, xh, xa, g);
+            const float w = a.w_post ? a.w_post[c] : 1.0f;
             const float z = fmaf(xa, w, a.b_post ? a.b_post[c] : 0.0f);
             if (a.dresidual) static_cast<T*>(a.dresidual)[row * a.ld_dresidual + c] = from_float<T>(a.rho * ds);
             if (a.gate_form == GATE_FULL)

@@ -311,3 +311,33 @@ def test_other_stream_and_graph():
         want, hw, _ = pr.forward()
         torch.cuda.synchronize()
         assert torch.equal(t2, want) and torch.equal(h2, hw)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("act", ["identity", "sigmoid", "tanh"])
+@pytest.mark.parametrize("cols, post", [(40, True), (520, False), (520, True), (5003, True), (9000, True), (9000, False)])
+def test_gates_of_what_is_dropped(dtype, act, cols, post):
+    """A gate of every element may hold anything where the element is dropped: the results are those of a 0 there."""
+    import torch
+    gpu()
+    pr = Problem(5, cols, dtype, True, "full", act, 0.5, False, post=post)
+    dropped = torch.from_numpy(pr.m == 0).cuda()
+    pr.gate[dropped] = 0.0
+    total, h, stats = pr.forward()
+    dsum, dnormed = pr.matrix(0.1), pr.matrix(0.1)
+    ws = torch.empty(fa.client_residual_norm_workspace_bytes(5, cols), device="cuda", dtype=torch.uint8)
+
+    def backward():
+        out = [torch.empty_like(pr.branch) for _ in range(3)] + [torch.empty(cols, device="cuda") for _ in range(2)]
+        fa.client_residual_norm_backward(pr.branch, total, stats, dsum, dnormed, out[0], out[1], dgate=out[2],
+                                         dw_post=out[3] if post else None, dw_pre=out[4], workspace=ws, **pr.opts)
+        return out if post else out[:3] + out[4:]
+
+    want = backward()
+    assert all(torch.isfinite(t).all() for t in want)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        pr.gate[dropped] = bad
+        t2, h2, _ = pr.forward()
+        assert torch.equal(t2, total) and torch.equal(h2, h)
+        for a, b in zip(backward(), want):
+            assert torch.equal(a, b)
