@@ -158,7 +158,7 @@ fasgd_status client_residual_norm_backward(const client_residual_norm* op, const
  * A product needs data to be 16-byte aligned, ld a multiple of 128 and at
  * least k rounded up to one (the values past k must be 0), scales 4-byte
  * aligned and lds a multiple of 4 of at least rows.  k and ld are at most
- * 2^23.
+ * 2^23, rows 2^27.
  */
 typedef enum client_fp8_format {
     CLIENT_FP8_E4M3 = 0,

@@ -126,6 +126,8 @@ fasgd_status norm_setup(const client_residual_norm* op, fasgd::NormArgs& a)
 
 constexpr int64_t kMaxK = int64_t(1) << 23;    // of an operand: 256 rows of it stay within 32-bit offsets
 
+constexpr int64_t kMaxOperandRows = int64_t(1) << 27;   // every product's launch stays below 2^32 threads
+
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // An 8-bit operand; its arrays are needed where it holds anything.
@@ -134,7 +136,8 @@ fasgd_status check_operand(const char* name, const client_fp8_operand* op, fasgd
     if (!op) return fail(FASGD_ERR_NULL, "%s is NULL", name);
     if (op->format != CLIENT_FP8_E4M3 && op->format != CLIENT_FP8_E5M2)
         return fail(FASGD_ERR_ARG, "%s: format = %d is not a client_fp8_format value", name, op->format);
-    if (op->rows < 0 || op->rows > kMaxElements) return fail(FASGD_ERR_ARG, "%s: rows = %lld is not in [0, 2^40]", name, (long long)op->rows);
+    if (op->rows < 0 || op->rows > kMaxOperandRows)
+        return fail(FASGD_ERR_ARG, "%s: rows = %lld is not in [0, 2^27]", name, (long long)op->rows);
     if (op->k < 0 || op->k > kMaxK) return fail(FASGD_ERR_ARG, "%s: k = %lld is not in [0, 2^23]", name, (long long)op->k);
     v = fasgd::Fp8View{op->data, op->scales, op->rows, op->k, op->ld, op->lds, op->format};
     if (op->rows == 0 || op->k == 0) return FASGD_OK;

@@ -19,8 +19,11 @@ struct DropoutArgs {
     void* y;
     int64_t ldx, ldr, ldy;
     int64_t rows, cols;
+    int64_t first;          // element that a launch begins at
     DropKey key;
 };
+// A launch may have fewer than 2^32 threads: larger work goes in several.
+constexpr int64_t kLaunchBlocks = int64_t(1) << 23;
 hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s);
 
 enum : int { GATE_NONE = 0, GATE_CHANNEL = 1, GATE_ROW = 2, GATE_FULL = 3 };
@@ -76,6 +79,7 @@ struct QuantizeArgs {
     const void* x;
     int64_t ldx, rows, cols;
     Fp8View row, col;
+    int64_t first;          // block that a launch begins at (rows alone)
     int32_t whole;
 };
 hipError_t launch_quantize(const QuantizeArgs& a, int dtype, hipStream_t s);

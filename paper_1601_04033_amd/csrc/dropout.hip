@@ -17,7 +17,7 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
     const T* res = static_cast<const T*>(a.residual);
     T* y = static_cast<T*>(a.y);
     const int64_t n = a.rows * a.cols;
-    const int64_t i = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * kChunk;
+    const int64_t i = a.first + (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * kChunk;
     if (i >= n) return;
     int64_t r, c;
     if (n <= UINT32_MAX) {      // a 64-bit division costs as much as the draw
@@ -54,14 +54,21 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
 
 }  // namespace
 
-hipError_t launch_dropout(const DropoutArgs& a, int dtype, hipStream_t s)
+hipError_t launch_dropout(const DropoutArgs& args, int dtype, hipStream_t s)
 {
-    const int64_t chunks = (a.rows * a.cols + kChunk - 1) / kChunk;
-    const unsigned blocks = static_cast<unsigned>((chunks + kBlock - 1) / kBlock);
-    if (dtype == DTYPE_F32) dropout<float><<<blocks, kBlock, 0, s>>>(a);
-    else if (dtype == DTYPE_BF16) dropout<bf16><<<blocks, kBlock, 0, s>>>(a);
-    else dropout<f16><<<blocks, kBlock, 0, s>>>(a);
-    return hipGetLastError();
+    DropoutArgs a = args;
+    constexpr int64_t kElements = int64_t(kBlock) * kChunk;
+    const int64_t blocks = (a.rows * a.cols + kElements - 1) / kElements;
+    hipError_t e = hipSuccess;
+    for (int64_t b = 0; b < blocks && e == hipSuccess; b += kLaunchBlocks) {
+        a.first = b * kElements;
+        const unsigned n = static_cast<unsigned>(blocks - b < kLaunchBlocks ? blocks - b : kLaunchBlocks);
+        if (dtype == DTYPE_F32) dropout<float><<<n, kBlock, 0, s>>>(a);
+        else if (dtype == DTYPE_BF16) dropout<bf16><<<n, kBlock, 0, s>>>(a);
+        else dropout<f16><<<n, kBlock, 0, s>>>(a);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace fasgd

@@ -374,28 +374,29 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
 template <typename T> __global__ __launch_bounds__(256) void join(Fp8Product p, int splits)
 {
     const int64_t n = p.b.rows, total = p.a.rows * n;
-    const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
-    if (i >= total) return;
-    const int count = total - i < 4 ? static_cast<int>(total - i) : 4;
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (count == 4) {
+    for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4; i < total;
+         i += static_cast<int64_t>(gridDim.x) * 1024) {
+        const int count = total - i < 4 ? static_cast<int>(total - i) : 4;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (count == 4) {
 #pragma unroll 4
-        for (int k = 0; k < splits; ++k) {
-            const Pack<float, 4> x = load_pack<float, 4>(p.partial + k * total + i);
+            for (int k = 0; k < splits; ++k) {
+                const Pack<float, 4> x = load_pack<float, 4>(p.partial + k * total + i);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[e] += x.v[e];
+                for (int e = 0; e < 4; ++e) s[e] += x.v[e];
+            }
+        } else {
+            for (int k = 0; k < splits; ++k)
+                for (int e = 0; e < count; ++e) s[e] += p.partial[k * total + i + e];
         }
-    } else {
-        for (int k = 0; k < splits; ++k)
-            for (int e = 0; e < count; ++e) s[e] += p.partial[k * total + i + e];
-    }
-    int64_t row = i / n, col = i - row * n;
-    for (int e = 0; e < count; ++e) {
-        T* c = static_cast<T*>(p.c) + row * p.ldc + col;
-        *c = from_float<T>(p.accumulate ? to_float(*c) + s[e] : s[e]);
-        if (++col == n) {
-            col = 0;
-            ++row;
+        int64_t row = i / n, col = i - row * n;
+        for (int e = 0; e < count; ++e) {
+            T* c = static_cast<T*>(p.c) + row * p.ldc + col;
+            *c = from_float<T>(p.accumulate ? to_float(*c) + s[e] : s[e]);
+            if (++col == n) {
+                col = 0;
+                ++row;
+            }
         }
     }
 }
@@ -403,7 +404,7 @@ template <typename T> __global__ __launch_bounds__(256) void join(Fp8Product p, 
 hipError_t launch_join(const Fp8Product& p, int splits, hipStream_t s)
 {
     const int64_t quads = (p.a.rows * p.b.rows + 3) / 4;
-    const unsigned blocks = static_cast<unsigned>((quads + 255) / 256);
+    const unsigned blocks = static_cast<unsigned>((quads + 255) / 256 < kLaunchBlocks ? (quads + 255) / 256 : kLaunchBlocks);
     if (p.c_dtype == DTYPE_F32) join<float><<<blocks, 256, 0, s>>>(p, splits);
     else if (p.c_dtype == DTYPE_BF16) join<bf16><<<blocks, 256, 0, s>>>(p, splits);
     else join<f16><<<blocks, 256, 0, s>>>(p, splits);

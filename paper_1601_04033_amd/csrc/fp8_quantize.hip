@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void quantize_rows(QuantizeArgs a)
 {
     const int lane = threadIdx.x & 15;
     const int64_t blocks = (a.cols + kTile - 1) / kTile;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4);
+    const int64_t i = a.first + static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4);
     if (i >= a.rows * blocks) return;
     const int64_t r = i / blocks, kb = i % blocks, c = kb * kTile + lane * 8;
     const Pack<T, 8> p = load8(static_cast<const T*>(a.x) + r * a.ldx, c, a.cols);
@@ -258,11 +258,19 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 ? 4 : 6) void quantize_tile(Qua
 template <typename T, int FORMAT> hipError_t launch_format(const QuantizeArgs& a, hipStream_t s)
 {
     const int64_t tiles_c = (a.cols + kTile - 1) / kTile, tiles_r = (a.rows + kTile - 1) / kTile;
-    if (!a.col.data && !a.whole)
-        quantize_rows<T, FORMAT><<<static_cast<unsigned>((a.rows * tiles_c + 15) / 16), 256, 0, s>>>(a);
-    else
+    if (a.col.data || a.whole) {
         quantize_tile<T, FORMAT><<<static_cast<unsigned>(tiles_c * tiles_r), 512, 0, s>>>(a);
-    return hipGetLastError();
+        return hipGetLastError();
+    }
+    QuantizeArgs q = a;
+    const int64_t blocks = (a.rows * tiles_c + 15) / 16;
+    hipError_t e = hipSuccess;
+    for (int64_t b = 0; b < blocks && e == hipSuccess; b += kLaunchBlocks) {
+        q.first = b * 16;
+        quantize_rows<T, FORMAT><<<static_cast<unsigned>(blocks - b < kLaunchBlocks ? blocks - b : kLaunchBlocks), 256, 0, s>>>(q);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 template <typename T> hipError_t launch_type(const QuantizeArgs& a, int format, hipStream_t s)

@@ -163,3 +163,18 @@ def test_other_stream():
     fa.client_dropout(x, b, 0.5, 1, 2, 3, stream=s)
     s.synchronize()
     assert torch.equal(a, b)
+
+
+def test_more_elements_than_a_launch():
+    """A matrix of more elements (2^35 and three rows) than the threads of one launch cover, 64 GB."""
+    import torch
+    gpu()
+    rows, cols = 2 ** 20 + 3, 2 ** 15
+    x = torch.ones(rows, cols, device="cuda", dtype=torch.bfloat16)
+    fa.client_dropout(x, x, 0.5, 77, 5, 3, site=1)
+    for first in (0, 2 ** 18, 2 ** 19 - 1, 2 ** 19, 2 ** 20 - 1, rows - 1):
+        part = torch.ones(1, cols, device="cuda", dtype=torch.bfloat16)
+        fa.client_dropout(part, part, 0.5, 77, 5, 3, site=1, index_base=first * cols)
+        assert torch.equal(x[first], part[0]), first
+    want = ref.keep_mask(1, cols, 0.5, 77, 5, 3, 1, (rows - 1) * cols)
+    assert np.array_equal(x[rows - 1].cpu().float().numpy() != 0, want[0])
