@@ -30,27 +30,45 @@ struct Few {
     int32_t accumulate;
 };
 
-__device__ __forceinline__ v8i join_chunks(const v4i& lo, const v4i& hi)
-{
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-}
+#if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources
 
-// 16 rows x 128 of an operand: lane l holds row l % 16, the 16-byte chunks
-// l / 16 of the block's two halves (both sides agree, so which of the
-// contraction's values these are does not matter).
-template <bool STREAM> __device__ __forceinline__ v8i read_rows(const Fp8View& v, int64_t row, int64_t kb, int lane)
-{
-    const int64_t r = row + (lane & 15) < v.rows ? row + (lane & 15) : v.rows - 1;
-    const uint8_t* p = v.data + r * v.ld + kb * kFp8Block + (lane >> 4) * 16;
-    const v4i* q = reinterpret_cast<const v4i*>(p);
-    if (STREAM) return join_chunks(__builtin_nontemporal_load(q), __builtin_nontemporal_load(q + 4));
-    return join_chunks(q[0], q[4]);
-}
-__device__ __forceinline__ int read_scale(const Fp8View& v, int64_t row, int64_t kb, int lane)
-{
-    const int64_t r = row + (lane & 15) < v.rows ? row + (lane & 15) : v.rows - 1;
-    return v.scales[kb * v.lds + r];
-}
+// Rows of an operand from `row` on, 16 to a tile: lane l holds row l % 16 of
+// a tile, and of a block of 128 the 16-byte chunks l / 16 of its two halves
+// (both sides agree, so which of the contraction's values these are does not
+// matter).  A row past the operand's end reads as 0.  Through buffers a load's
+// address costs one scalar addition, and no register that a load under way
+// still needs.
+struct Rows {
+    __amdgpu_buffer_rsrc_t data;
+    const uint8_t* scales;
+    int64_t lds, scales_left;
+    uint32_t ld, at;
+    int lane;
+    __device__ Rows(const Fp8View& v, int64_t row, int lane_)
+        : data(buffer(v.data + row * v.ld, (v.rows - row) * v.ld)), scales(v.scales + row), lds(v.lds),
+          scales_left(v.lds - row), ld(static_cast<uint32_t>(v.ld)),
+          at((lane_ & 15) * static_cast<uint32_t>(v.ld) + (lane_ >> 4) * 16), lane(lane_)
+    {
+    }
+    template <bool STREAM> __device__ v8i read(int tile, int kb) const
+    {
+        constexpr int kOnce = STREAM ? 2 : 0;   // non-temporal
+        const uint32_t p = at + tile * 16 * ld;
+        const auto lo = __builtin_amdgcn_raw_buffer_load_b128(data, p, kb * kFp8Block, kOnce);
+        const auto hi = __builtin_amdgcn_raw_buffer_load_b128(data, p + 64, kb * kFp8Block, kOnce);
+        return join_chunks(__builtin_bit_cast(v4i, lo), __builtin_bit_cast(v4i, hi));
+    }
+    // the lane's row's scale with its three neighbours', and the scale alone:
+    // a byte by itself would be widened, and so waited for, where the loop's
+    // next loads begin
+    __device__ uint32_t read_scale(int tile, int kb) const
+    {
+        return __builtin_amdgcn_raw_buffer_load_b32(buffer(scales + kb * lds, scales_left), tile * 16 + (lane & 12), 0, 0);
+    }
+    __device__ int scale(uint32_t four) const { return four >> (lane & 3) * 8 & 0xff; }
+};
+
+#endif
 
 // Activations in LDS: rows of k rounded up to 128 and 16 bytes (so that 16
 // rows lie in different banks), then the scales, 16 to a block of 128.
@@ -107,11 +125,12 @@ template <int FORMAT> __device__ __forceinline__ void widen_rows(const v8i& f, i
 template <typename X, bool FUSED, bool WIDE, int FBIG, int FFEW, int MT, int NT>
 __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_stride)
 {
+#if defined(__HIP_DEVICE_COMPILE__)
     // blocks of 128 loaded while as many are multiplied, within 128 registers
-    constexpr int kAhead = NT * MT >= 4 ? 1 : 4 / (NT * MT);
+    constexpr int kAhead = (FUSED ? 4 : 2) / (NT * MT);
     extern __shared__ __attribute__((aligned(16))) uint8_t dynamic[];
     __shared__ __attribute__((aligned(16))) float sums[kWaves][NT][MT][64][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t r0 = static_cast<int64_t>(blockIdx.x) * (16 * NT), m0 = static_cast<int64_t>(blockIdx.y) * (16 * MT);
     const int blocks = static_cast<int>((p.big.k + kFp8Block - 1) / kFp8Block);
     v4f acc[NT][MT];
@@ -123,27 +142,30 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
     constexpr int kFew = FUSED ? 1 : MT;
     struct Group {
         v8i big[kAhead][NT], few[kAhead][kFew];
-        int scale_big[kAhead][NT], scale_few[kAhead][kFew];
+        uint32_t scale_big[kAhead][NT], scale_few[kAhead][kFew];
     };
-    // A block past the last is the last again, with scales of 2^-127 each way: products of 0 in fp32.
+    const Rows big(p.big, r0, lane), few_rows(FUSED ? p.big : p.few, FUSED ? r0 : m0, lane);
+    // A block past the last is loaded as the last one and not multiplied:
+    // with the same loads on every way the waits are for what is needed.
     auto load = [&](Group& g, int k) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int kb = k + u * kWaves < blocks ? k + u * kWaves : blocks - 1;
-            const int in = k + u * kWaves < blocks ? -1 : 0;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                g.big[u][n] = read_rows<true>(p.big, r0 + n * 16, kb, lane);
-                g.scale_big[u][n] = read_scale(p.big, r0 + n * 16, kb, lane) & in;
+                g.scale_big[u][n] = big.read_scale(n, kb);
+                g.big[u][n] = big.read<true>(n, kb);
             }
             if constexpr (!FUSED) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    g.few[u][m] = read_rows<false>(p.few, m0 + m * 16, kb, lane);
-                    g.scale_few[u][m] = read_scale(p.few, m0 + m * 16, kb, lane) & in;
+                    g.scale_few[u][m] = few_rows.read_scale(m, kb);
+                    g.few[u][m] = few_rows.read<false>(m, kb);
                 }
             }
         }
+        // the compiler would put a scale's load where it is used, and wait there for all loads
+        __builtin_amdgcn_sched_barrier(0);
     };
     Held h;
     h.data = dynamic;
@@ -153,24 +175,27 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
     auto multiply = [&](const Group& g, int k) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
+            const int kb = k + u * kWaves;
+            if (kb >= blocks) break;
             v8i few[MT];
-            int scale_few[MT];
+            int scale_few[MT], scale_big[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) scale_big[n] = big.scale(g.scale_big[u][n]);
             if constexpr (FUSED) {
-                const int kb = k + u * kWaves < blocks ? k + u * kWaves : blocks - 1;
                 const uint8_t* q = h.data + held_row * h.stride + kb * kFp8Block + (lane >> 4) * 16;
                 few[0] = join_chunks(*reinterpret_cast<const v4i*>(q), *reinterpret_cast<const v4i*>(q + 64));
-                scale_few[0] = k + u * kWaves < blocks ? h.scales[kb * 16 + held_row] : 0;
+                scale_few[0] = h.scales[kb * 16 + held_row];
             } else {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     few[m] = g.few[u][m];
-                    scale_few[m] = g.scale_few[u][m];
+                    scale_few[m] = few_rows.scale(g.scale_few[u][m]);
                 }
             }
             if constexpr (WIDE) {
                 v8bf wb[NT][4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) widen_rows<FBIG>(g.big[u][n], g.scale_big[u][n], wb[n]);
+                for (int n = 0; n < NT; ++n) widen_rows<FBIG>(g.big[u][n], scale_big[n], wb[n]);
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     v8bf wf[4];
@@ -187,12 +212,14 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
 #pragma unroll
                     for (int m = 0; m < MT; ++m)
                         acc[n][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                            g.big[u][n], few[m], acc[n][m], FBIG, FFEW, 0, g.scale_big[u][n], 0, scale_few[m]);
+                            g.big[u][n], few[m], acc[n][m], FBIG, FFEW, 0, scale_big[n], 0, scale_few[m]);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
     };
     Group g[2];
     constexpr int kStep = kWaves * kAhead;
+    const bool all = blocks <= kStep;   // one group of each wave holds all of the contraction
     load(g[0], wave);
     if constexpr (FUSED) {
         hold<X>(p, h, blocks);
@@ -201,7 +228,8 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     }
-    for (int k = wave; k < blocks; k += 2 * kStep) {
+    if (all) multiply(g[0], wave);
+    for (int k = wave; !all && k < blocks; k += 2 * kStep) {
         load(g[1], k + kStep);
         multiply(g[0], k);
         if (k + kStep >= blocks) break;
@@ -233,6 +261,7 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
             *c = from_float<f16>(p.accumulate ? to_float(*c) + s : s);
         }
     }
+#endif
 }
 
 // 32 rows a block where that still gives every CU one, else 16.
@@ -272,12 +301,20 @@ template <typename X> hipError_t launch_fused(const Few& p, hipStream_t s)
 
 }  // namespace
 
-// Beyond 16 rows, blocks of 16 x 32 outputs read (16 + 32) k bytes each from
-// the caches: taken up to 48 MB, about 6 us.
+// Beyond 16 rows, where these blocks of 16 x 32 outputs are estimated to take
+// no more than 9.5 us, about what the tiles of fp8_product.hip take for so
+// little: 3.2 us for each round of 512 blocks, and a block's reads of a block
+// of 128 at 0.0034 us a row (500 x 500 x 500 5 against 7 to 10 us, 64 x 1,000
+// x 3,000 8 against 10 to 12; but 1,000 x 784 x 128 12 against 7 to 9, 32 x
+// 1,000 x 16,000 24 against 13 to 17).
 bool fp8_few(int64_t m, int64_t n, int64_t k)
 {
     const int64_t few = m < n ? m : n, big = m < n ? n : m;
-    return few <= 16 || ((big + 15) / 16) * ((few + 31) / 32) * 48 * k <= int64_t(48) << 20;
+    if (few <= 16) return true;
+    const int64_t blocks = ((big + 15) / 16) * ((few + 31) / 32), rows = 16 + (few < 32 ? few : 32);
+    const double per_cu = blocks > 256 ? static_cast<double>(blocks) / 256 : 1.0;
+    return 3.2 * static_cast<double>((blocks + 511) / 512) +
+               0.0034 * static_cast<double>(rows * ((k + kFp8Block - 1) / kFp8Block)) * per_cu <= 9.5;
 }
 
 bool fp8_linear_few(int64_t m, int64_t k) { return m <= 16 && held_bytes(m, k) <= 48 * 1024; }

@@ -25,6 +25,11 @@ __device__ __forceinline__ int block_exponent(float amax, int fmax_exponent)
 }
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
 
+__device__ __forceinline__ v8i join_chunks(const v4i& lo, const v4i& hi)
+{
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // |x|, 0 for what is not finite
 __device__ __forceinline__ float finite_abs(float x)
 {
@@ -65,6 +70,17 @@ __device__ __forceinline__ float max_of_16(float x)
     x = fmaxf(x, dpp_move<0x141>(x));   // row_half_mirror
     return fmaxf(x, dpp_move<0x140>(x));    // row_mirror
 }
+
+#if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources
+// A buffer of the bytes from p on, as many of `bytes` as 32 bits can say;
+// what is read past its end is 0.
+__device__ __forceinline__ auto buffer(const uint8_t* p, int64_t bytes)
+{
+    constexpr int kRaw = 0x00020000;    // raw buffer, 32-bit data
+    const uint32_t n = bytes < 0xffffffffll ? static_cast<uint32_t>(bytes) : 0xffffffffu;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, static_cast<int>(n), kRaw);
+}
+#endif
 
 // 8 values (dwords lo and hi) times 2^(scale - 127), as bf16: exact.
 template <int FORMAT> __device__ __forceinline__ v8bf widen(int lo, int hi, float scale)

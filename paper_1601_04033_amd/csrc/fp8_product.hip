@@ -46,15 +46,6 @@ __device__ __forceinline__ int slot(int c, int r) { return c ^ (r >> 1 & 7); }
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
-// A buffer of the bytes from p on (all of `bytes` that 32 bits can say; the
-// offsets used stay below 2^31 + 2^23).
-__device__ __forceinline__ auto buffer(const uint8_t* p, int64_t bytes)
-{
-    constexpr int kRaw = 0x00020000;    // raw buffer, 32-bit data
-    const uint32_t n = bytes < 0xffffffffll ? static_cast<uint32_t>(bytes) : 0xffffffffu;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, static_cast<int>(n), kRaw);
-}
-
 // A stage is worked through in sub-steps of 1,024 matrix cycles per wave (at
 // W = 128): 64 of the contraction in the 8-bit instruction, 32 in bf16.  A
 // sub-step's fragments (lane l: row l % 32 of a tile, the 16-byte chunks of
@@ -85,11 +76,6 @@ __device__ __forceinline__ void read_one(Fragments<WIDE, N>& f, const uint8_t* a
     const v4i x = *reinterpret_cast<const v4i*>(p + at.chunk[s * C + c] + i * 32 * kBytes);
     if (rest < C) f.a[i][c] = x;
     else f.b[i][c] = x;
-}
-
-__device__ __forceinline__ v8i join_chunks(const v4i& lo, const v4i& hi)
-{
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // byte i of packed scales as the power of two it stands for
@@ -133,22 +119,26 @@ template <int N> __device__ __forceinline__ void multiply_wide(v16f (&acc)[N][N]
 // Orders of the instructions of a sub-step for the compiler's scheduler:
 // between two matrix instructions go one LDS read, the loads of the stage
 // after next, and the conversions of what is multiplied next.
-template <int MFMA, int READS, int LOADS, int VALU> __device__ __forceinline__ void interleave()
+template <int MFMA, int READS, int LOADS, int VALU, int I = 0> __device__ __forceinline__ void interleave()
 {
     constexpr int kMfma = 0x8, kDsRead = 0x100, kVmem = 0x20, kValu = 0x2;
-#pragma unroll
-    for (int i = 0; i < MFMA; ++i) {
-        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-        if (i * READS / MFMA != (i + 1) * READS / MFMA) __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
-        if (i * LOADS / MFMA != (i + 1) * LOADS / MFMA) __builtin_amdgcn_sched_group_barrier(kVmem, LOADS > MFMA ? 2 : 1, 0);
-        if (VALU) __builtin_amdgcn_sched_group_barrier(kValu, VALU / MFMA, 0);
-    }
+    constexpr int kReads = (I + 1) * READS / MFMA - I * READS / MFMA, kLoads = (I + 1) * LOADS / MFMA - I * LOADS / MFMA;
+    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(kDsRead, kReads, 0);
+    if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(kVmem, kLoads, 0);
+    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(kValu, VALU / MFMA, 0);
+    if constexpr (I + 1 < MFMA) interleave<MFMA, READS, LOADS, VALU, I + 1>();
 }
 
-template <int N> __device__ __forceinline__ int load_scales(const uint8_t* p)
+// A lane's N neighbouring scales, the first in byte 0.  p: as many bytes on,
+// but no further than 4 before the scales' end (N = 3: then `shift` bits before them).
+template <int N> __device__ __forceinline__ int load_scales(const uint8_t* p, int shift)
 {
     if constexpr (N == 4) return *reinterpret_cast<const int*>(p);
-    else return *reinterpret_cast<const uint16_t*>(p);
+    if constexpr (N == 2) return *reinterpret_cast<const uint16_t*>(p);
+    uint32_t x;
+    __builtin_memcpy(&x, p, sizeof x);
+    return static_cast<int>(x >> shift);
 }
 
 // One row of tiles in vector registers.  Accumulators stay in the accumulation
@@ -215,7 +205,7 @@ struct Grid {
 };
 
 template <int W, int WM, int FA, int FB, bool WIDE>
-__global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product p, Grid g)
+__global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void product(Fp8Product p, Grid g)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using G = Geometry<W, WM>;
@@ -262,8 +252,14 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
     const auto gb = buffer(p.b.data + n0 * p.b.ld + kb0 * kBytes,
                                              (p.b.rows - n0) * p.b.ld - kb0 * kBytes);
     const int row_a = wave_m * W + (lane & 31) * N, row_b = wave_n * W + (lane & 31) * N;
-    const int64_t sra = m0 + row_a < p.a.lds - N ? m0 + row_a : p.a.lds - N;
-    const int64_t srb = n0 + row_b < p.b.lds - N ? n0 + row_b : p.b.lds - N;
+    constexpr int kSpan = N == 3 ? 4 : N;   // bytes that a lane's scales are read from
+    auto scale_place = [&](int64_t row, int64_t lds, int& shift) {
+        const int64_t at = row < lds - kSpan ? row : lds - kSpan;
+        shift = row - at < 3 ? static_cast<int>(row - at) * 8 : 24;
+        return at;
+    };
+    int shift_a, shift_b;
+    const int64_t sra = scale_place(m0 + row_a, p.a.lds, shift_a), srb = scale_place(n0 + row_b, p.b.lds, shift_b);
     const uint8_t* sa = p.a.scales + kb0 * p.a.lds + sra;
     const uint8_t* sb = p.b.scales + kb0 * p.b.lds + srb;
 
@@ -315,8 +311,8 @@ __global__ __launch_bounds__(kThreads, W == 128 ? 1 : 2) void product(Fp8Product
     auto scales = [&](int k, int s) {
         const int64_t at = k < steps ? k : steps - 1;
         const int in = k < steps ? -1 : 0;
-        xa[s] = load_scales<N>(sa + at * p.a.lds) & in;
-        xb[s] = load_scales<N>(sb + at * p.b.lds) & in;
+        xa[s] = load_scales<N>(sa + at * p.a.lds, shift_a) & in;
+        xb[s] = load_scales<N>(sb + at * p.b.lds, shift_b) & in;
     };
     // Stage k lies in (a, b), stage k + 1 in (an, bn) or on its way there, and
     // frag[0] holds stage k's first sub-step.
@@ -411,55 +407,78 @@ hipError_t launch_join(const Fp8Product& p, int splits, hipStream_t s)
     return hipGetLastError();
 }
 
-enum Shape { k256, k128, k64Rows, k64Cols };    // block tiles 256 x 256, 128 x 128, 64 x 256, 256 x 64
+enum Shape { k256, k192, k128, k64Rows, k64Cols };  // block tiles 256 x 256, 192 x 192, 128 x 128, 64 x 256, 256 x 64
 struct Plan {
     Shape shape;
     Grid g;
 };
 
-// Share of the chip that `tiles` equal blocks use, `slots` of which run at
-// once.
-double use(int64_t tiles, int64_t slots)
+// Microseconds of a square tile's blocks, measured at 8,192 x 8,192 x 4,096
+// and where one round of blocks or less is all there is: of a stage with as
+// many blocks on a CU as fit (of 128 x 128 two, of the others one), of a
+// stage of a 128 x 128 tile alone on its CU, and of what a tile costs besides
+// its stages.  The larger tile has the higher rate (8,192 x 8,192 x 4,096:
+// 245, 333 and 267 us with 256, 192 and 128), the smaller ones waste less of
+// a product's edges and of the last round (4,099 x 2,002 x 5,003: 70, 57 and
+// 72 us; 2,500 x 2,500 x 2,500: 39, 35 and 24).
+struct Rate {
+    Shape shape;
+    int side;
+    double stage, alone, besides;
+};
+constexpr Rate kRates[2][3] = {
+    {{k256, 256, 1.65, 1.65, 8.0}, {k192, 192, 1.30, 1.30, 6.0}, {k128, 128, 1.00, 0.68, 4.0}},
+    {{k256, 256, 3.20, 3.20, 8.0}, {k192, 192, 2.10, 2.10, 6.0}, {k128, 128, 1.80, 1.15, 4.0}}};  // fp32 outputs
+
+int64_t count(int64_t x, int64_t side) { return (x + side - 1) / side; }
+
+double time_of(const Rate& r, int64_t tiles, int64_t stages)
 {
-    return static_cast<double>(tiles) / static_cast<double>((tiles + slots - 1) / slots * slots);
+    const int64_t slots = r.side == 128 ? 512 : 256, full = tiles / slots, rest = tiles % slots;
+    const double last = rest == 0 ? 0.0 : (rest <= 256 ? r.alone : r.stage) * static_cast<double>(stages) + r.besides;
+    return static_cast<double>(full) * (r.stage * static_cast<double>(stages) + r.besides) + last;
 }
 
-// 256 x 256 tiles (one block per CU) reach twice the rate of 128 x 128 ones
-// (two per CU), whose fragments need all of LDS's bandwidth, so the smaller
-// are taken only where they use more than 1.6 times as much of the chip
-// (4,099 x 2,002 x 5,003: 66 against 72 us), and where they do not outnumber
-// the CUs, so that one's latency is all that counts (300 x 5,000 x 700: 10
-// against 16 us).
-// Few rows on one side take tiles of 64 of them.  Where tiles leave half of
-// the chip or more idle, the contraction is split, at least 4 stages each.
-Plan plan_of(int64_t m, int64_t n, int64_t k)
+// The square tile that takes the least time, or tiles of 64 rows where one
+// side has no more.  Where tiles leave half of the chip or more idle, the
+// contraction is split, at least 4 stages each.
+Plan plan_of(int64_t m, int64_t n, int64_t k, bool wide)
 {
-    const auto count = [](int64_t x, int64_t side) { return (x + side - 1) / side; };
+    const int64_t blocks = count(k, kBytes);
+    const auto splits_of = [&](int64_t tiles) {
+        int64_t s = 256 / tiles;
+        if (s > blocks / 4) s = blocks / 4;
+        if (s > kMaxSplits) s = kMaxSplits;
+        return s < 1 ? 1 : s;
+    };
     Plan p;
-    int64_t side_m = 256, side_n = 256;
+    int64_t side_m = 64, side_n = 256;
     if (m <= kFewRows) {
         p.shape = k64Rows;
-        side_m = 64;
     } else if (n <= kFewRows) {
         p.shape = k64Cols;
+        side_m = 256;
         side_n = 64;
-    } else if (count(m, 128) * count(n, 128) > 256 &&
-               use(count(m, 256) * count(n, 256), 256) * 1.6 >= use(count(m, 128) * count(n, 128), 512)) {
-        p.shape = k256;
     } else {
-        p.shape = k128;
-        side_m = side_n = 128;
+        double best = 0.0;
+        for (const Rate& r : kRates[wide]) {
+            const int64_t tiles = count(m, r.side) * count(n, r.side), s = splits_of(tiles);
+            double t = time_of(r, tiles * s, count(blocks, s));
+            // the parts are written and read again, at about 4 TB/s, by one launch more
+            if (s > 1) t += 3.0 + 8.0 * static_cast<double>(s) * static_cast<double>(m) * static_cast<double>(n) / 4e6;
+            if (best == 0.0 || t < best) {
+                best = t;
+                p.shape = r.shape;
+                side_m = side_n = r.side;
+            }
+        }
     }
-    const int64_t tiles = count(m, side_m) * count(n, side_n), blocks = count(k, kBytes);
-    int64_t splits = 256 / tiles;
-    if (splits > blocks / 4) splits = blocks / 4;
-    if (splits > kMaxSplits) splits = kMaxSplits;
-    if (splits < 1) splits = 1;
+    const int64_t splits = splits_of(count(m, side_m) * count(n, side_n));
     p.g.tiles_m = static_cast<int32_t>(count(m, side_m));
     p.g.tiles_n = static_cast<int32_t>(count(n, side_n));
-    p.g.steps = static_cast<int32_t>((blocks + splits - 1) / splits);
+    p.g.steps = static_cast<int32_t>(count(blocks, splits));
     if (splits > 1) p.g.steps += p.g.steps & 1;     // the kernel takes stages in pairs
-    p.g.splits = static_cast<int32_t>((blocks + p.g.steps - 1) / p.g.steps);
+    p.g.splits = static_cast<int32_t>(count(blocks, p.g.steps));
     return p;
 }
 
@@ -468,6 +487,7 @@ template <int FA, int FB, bool WIDE> hipError_t launch_arithmetic(const Fp8Produ
     const unsigned blocks = static_cast<unsigned>(plan.g.tiles_m) * plan.g.tiles_n * plan.g.splits;
     switch (plan.shape) {
     case k256: product<128, 2, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
+    case k192: product<96, 2, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
     case k128: product<64, 2, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
     case k64Rows: product<64, 1, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
     case k64Cols: product<64, 4, FA, FB, WIDE><<<blocks, kThreads, 0, s>>>(p, plan.g); break;
@@ -485,15 +505,19 @@ template <int FA, int FB> hipError_t launch_formats(const Fp8Product& p, const P
 size_t fp8_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
     if (m < 1 || n < 1 || k < 1 || fp8_few(m, n, k)) return 0;
-    const Plan p = plan_of(m, n, k);
-    return p.g.splits > 1 ? sizeof(float) * static_cast<size_t>(p.g.splits) * static_cast<size_t>(m) * static_cast<size_t>(n) : 0;
+    int splits = 1;
+    for (const bool wide : {false, true}) {
+        const int planned = plan_of(m, n, k, wide).g.splits;
+        if (planned > splits) splits = planned;
+    }
+    return splits > 1 ? sizeof(float) * static_cast<size_t>(splits) * static_cast<size_t>(m) * static_cast<size_t>(n) : 0;
 }
 
 hipError_t launch_fp8_product(const Fp8Product& p, hipStream_t s)
 {
     if (p.a.k == 0) return launch_join(p, 0, s);
     if (fp8_few(p.a.rows, p.b.rows, p.a.k)) return launch_fp8_few(p, s);
-    const Plan plan = plan_of(p.a.rows, p.b.rows, p.a.k);
+    const Plan plan = plan_of(p.a.rows, p.b.rows, p.a.k, p.c_dtype == DTYPE_F32);
     hipError_t e;
     if (p.a.format == FP8_E4M3)
         e = p.b.format == FP8_E4M3 ? launch_formats<0, 0>(p, plan, s) : launch_formats<0, 1>(p, plan, s);
