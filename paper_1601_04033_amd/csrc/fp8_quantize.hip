@@ -135,8 +135,17 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 ? 4 : 6) void quantize_tile(Qua
 #pragma unroll
         for (int i = 0; i < R; ++i) p[i] = load_pack<T, 8>(x + (r0 + i) * a.ldx + c0);
     } else {
+        // a row past the end is read as the last one, so that a thread's loads are under way together
+        const bool whole = c0 + 8 <= a.cols;
+        if (whole) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) p[i] = load_pack<T, 8>(x + (r0 + i < a.rows ? r0 + i : a.rows - 1) * a.ldx + c0);
+        }
+#pragma unroll
         for (int i = 0; i < R; ++i) {
-            if (r0 + i < a.rows) {
+            const bool in = r0 + i < a.rows;
+            if (whole && in) continue;
+            if (!whole && in && c0 < a.cols) {
                 p[i] = load8(x + (r0 + i) * a.ldx, c0, a.cols);
             } else {
 #pragma unroll
