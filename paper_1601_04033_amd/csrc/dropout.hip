@@ -9,7 +9,8 @@ constexpr int kChunk = 8;
 
 // One chunk of 8 consecutive matrix elements per thread: one Philox call and
 // one wide access each way.  A chunk that crosses a row's end (rows of a
-// length that is no multiple of 8) goes element by element.
+// length that is no multiple of 8) goes element by element.  Rows without
+// gaps are one row.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
 {
@@ -19,8 +20,9 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
     const int64_t n = a.rows * a.cols;
     const int64_t i = a.first + (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) * kChunk;
     if (i >= n) return;
-    int64_t r, c;
-    if (n <= UINT32_MAX) {      // a 64-bit division costs as much as the draw
+    int64_t r = 0, c = i;
+    if (a.rows == 1) {          // one row, or rows without gaps: nothing to divide
+    } else if (n <= UINT32_MAX) {      // a 64-bit division costs as much as the draw
         r = static_cast<uint32_t>(i) / static_cast<uint32_t>(a.cols);
         c = i - r * a.cols;
     } else {
@@ -41,6 +43,25 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
         store_pack(y + r * a.ldy + c, v);
         return;
     }
+    if (a.cols >= kChunk) {     // at most one row ends here: the loads are under way together
+        float f[kChunk];
+        const T* xr = x + r * a.ldx + c;
+        const T* rr = res + r * a.ldr + c;
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            const bool next = c + e >= a.cols, in = i + e < n;
+            f[e] = in ? to_float(xr[next ? a.ldx - a.cols + e : e]) : 0.0f;
+        }
+        T* yr = y + r * a.ldy + c;
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            const bool next = c + e >= a.cols, in = i + e < n;
+            f[e] = kept(f[e] * a.key.scale, keep, kChunk - 1 - e);
+            if (res) f[e] += in ? to_float(rr[next ? a.ldr - a.cols + e : e]) : 0.0f;
+            if (in) yr[next ? a.ldy - a.cols + e : e] = from_float<T>(f[e]);
+        }
+        return;
+    }
     for (int e = 0; e < kChunk && i + e < n; ++e) {
         float f = kept(to_float(x[r * a.ldx + c]) * a.key.scale, keep, kChunk - 1 - e);
         if (res) f += to_float(res[r * a.ldr + c]);
@@ -57,6 +78,10 @@ __global__ __launch_bounds__(kBlock) void dropout(DropoutArgs a)
 hipError_t launch_dropout(const DropoutArgs& args, int dtype, hipStream_t s)
 {
     DropoutArgs a = args;
+    if (a.ldx == a.cols && a.ldy == a.cols && (!a.residual || a.ldr == a.cols)) {
+        a.cols *= a.rows;
+        a.rows = 1;
+    }
     constexpr int64_t kElements = int64_t(kBlock) * kChunk;
     const int64_t blocks = (a.rows * a.cols + kElements - 1) / kElements;
     hipError_t e = hipSuccess;
