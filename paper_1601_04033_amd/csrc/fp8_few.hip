@@ -7,11 +7,12 @@
 // rows, its 8 waves take the contraction's blocks of 128 in turn and read
 // fragments straight from memory (16 rows of 128 bytes: whole lines), each
 // value once; the few rows come from the caches.  The waves' sums are joined
-// through LDS, so one launch writes the result.
-// Up to 16 rows of unquantized activations (48 KB once quantized) are
-// quantized on the way: every block does it again, into LDS, while its first
-// loads of the larger operand are under way, which costs less than a launch
-// before this one.
+// through LDS, so one launch writes the result.  1 x 4,096 x 16,384 (67 MB):
+// 16.0 us, 4.2 TB/s, of which about 4 are the launch and x's quantization;
+// 128 x 784 x 1,000: 3.7 us.
+// Few unquantized activations (128 blocks of 128) are quantized on the way:
+// every block does it again, into LDS, while its first loads of the larger
+// operand are under way, which costs less than a launch before this one.
 #include "fp8_math.hpp"
 
 namespace fasgd {
@@ -39,6 +40,7 @@ struct Few {
 // address costs one scalar addition, and no register that a load under way
 // still needs.
 struct Rows {
+    static constexpr uint32_t kOutside = 0xf0000000u;
     __amdgpu_buffer_rsrc_t data;
     const uint8_t* scales;
     int64_t lds, scales_left;
@@ -50,10 +52,10 @@ struct Rows {
           at((lane_ & 15) * static_cast<uint32_t>(v.ld) + (lane_ >> 4) * 16), lane(lane_)
     {
     }
-    template <bool STREAM> __device__ v8i read(int tile, int kb) const
+    template <bool STREAM> __device__ v8i read(int tile, int kb, bool in) const
     {
         constexpr int kOnce = STREAM ? 2 : 0;   // non-temporal
-        const uint32_t p = at + tile * 16 * ld;
+        const uint32_t p = in ? at + tile * 16 * ld : kOutside;
         const auto lo = __builtin_amdgcn_raw_buffer_load_b128(data, p, kb * kFp8Block, kOnce);
         const auto hi = __builtin_amdgcn_raw_buffer_load_b128(data, p + 64, kb * kFp8Block, kOnce);
         return join_chunks(__builtin_bit_cast(v4i, lo), __builtin_bit_cast(v4i, hi));
@@ -61,9 +63,9 @@ struct Rows {
     // the lane's row's scale with its three neighbours', and the scale alone:
     // a byte by itself would be widened, and so waited for, where the loop's
     // next loads begin
-    __device__ uint32_t read_scale(int tile, int kb) const
+    __device__ uint32_t read_scale(int tile, int kb, bool in) const
     {
-        return __builtin_amdgcn_raw_buffer_load_b32(buffer(scales + kb * lds, scales_left), tile * 16 + (lane & 12), 0, 0);
+        return __builtin_amdgcn_raw_buffer_load_b32(buffer(scales + kb * lds, scales_left), in ? tile * 16 + (lane & 12) : kOutside, 0, 0);
     }
     __device__ int scale(uint32_t four) const { return four >> (lane & 3) * 8 & 0xff; }
 };
@@ -83,17 +85,29 @@ inline size_t held_bytes(int64_t rows, int64_t k)
     return static_cast<size_t>(rows) * held_stride(k) + static_cast<size_t>((k + kFp8Block - 1) / kFp8Block) * 16;
 }
 
-// x quantized in e4m3 into LDS, 16 threads to a block of a row.
-template <typename T> __device__ __forceinline__ void hold(const Few& p, const Held& h, int blocks)
+// x quantized in e4m3 into LDS, 16 threads to a block of a row.  `first` is
+// what a thread takes of the first blocks, loaded before anything else: 8
+// elements, used where the row's end does not cut them.
+// Whole registers until then: taken apart where they are loaded, they would be
+// waited for there.
+template <typename T> using Words = Pack<uint32_t, 2 * sizeof(T)>;
+template <typename T> __device__ __forceinline__ Words<T> load_x(const Few& p, int i, int blocks)
+{
+    const int r = i / blocks, c = i % blocks * kFp8Block + (threadIdx.x & 15) * 8, k = static_cast<int>(p.few.k);
+    Words<T> w;
+    if (k >= 8) __builtin_memcpy(&w, static_cast<const T*>(p.x) + r * p.ldx + (c < k - 8 ? c : k - 8), sizeof w);
+    return w;
+}
+template <typename T>
+__device__ __forceinline__ void hold(const Few& p, const Held& h, int blocks, const Words<T>& first)
 {
     const int lane = threadIdx.x & 15, rows = static_cast<int>(p.few.rows), k = static_cast<int>(p.few.k);
-    for (int i = threadIdx.x >> 4; i < rows * blocks; i += kThreads / 16) {
-        const int r = i / blocks, kb = i % blocks, c = kb * kFp8Block + lane * 8;
-        const T* x = static_cast<const T*>(p.x) + r * p.ldx;
+    auto item = [&](int i, const Words<T>& w) {
         Pack<T, 8> q;
-        if (c + 8 <= k) {
-            q = load_pack<T, 8>(x + c);
-        } else {
+        __builtin_memcpy(&q, &w, sizeof q);
+        const int r = i / blocks, kb = i % blocks, c = kb * kFp8Block + lane * 8;
+        if (c + 8 > k) {
+            const T* x = static_cast<const T*>(p.x) + r * p.ldx;
 #pragma unroll
             for (int j = 0; j < 8; ++j) q.v[j] = c + j < k ? x[c + j] : from_float<T>(0.0f);
         }
@@ -110,7 +124,10 @@ template <typename T> __device__ __forceinline__ void hold(const Few& p, const H
         out.y = pack4<FP8_E4M3>(v[4], v[5], v[6], v[7], s);
         *reinterpret_cast<uint2*>(h.data + r * h.stride + c) = out;
         if (lane == 0) h.scales[kb * 16 + r] = static_cast<uint8_t>(e + 127);
-    }
+    };
+    int i = threadIdx.x >> 4;
+    if (i < rows * blocks) item(i, first);      // apart from the rest, whose loads are waited for with all others
+    for (i += kThreads / 16; i < rows * blocks; i += kThreads / 16) item(i, load_x<T>(p, i, blocks));
 }
 
 template <int FORMAT> __device__ __forceinline__ void widen_rows(const v8i& f, int scale, v8bf (&w)[4])
@@ -145,22 +162,25 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
         uint32_t scale_big[kAhead][NT], scale_few[kAhead][kFew];
     };
     const Rows big(p.big, r0, lane), few_rows(FUSED ? p.big : p.few, FUSED ? r0 : m0, lane);
-    // A block past the last is loaded as the last one and not multiplied:
-    // with the same loads on every way the waits are for what is needed.
+    // A block past the last is loaded from outside the buffers, which moves
+    // nothing (read as the last block it cost as much again: 1 x 4,096 x 16,384
+    // 22 against 16 us), and not multiplied: with the same loads on every way
+    // the waits are for what is needed.
     auto load = [&](Group& g, int k) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int kb = k + u * kWaves < blocks ? k + u * kWaves : blocks - 1;
+            const bool in = k + u * kWaves < blocks;
+            const int kb = in ? k + u * kWaves : 0;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                g.scale_big[u][n] = big.read_scale(n, kb);
-                g.big[u][n] = big.read<true>(n, kb);
+                g.scale_big[u][n] = big.read_scale(n, kb, in);
+                g.big[u][n] = big.read<true>(n, kb, in);
             }
             if constexpr (!FUSED) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    g.scale_few[u][m] = few_rows.read_scale(m, kb);
-                    g.few[u][m] = few_rows.read<false>(m, kb);
+                    g.scale_few[u][m] = few_rows.read_scale(m, kb, in);
+                    g.few[u][m] = few_rows.read<false>(m, kb, in);
                 }
             }
         }
@@ -219,22 +239,33 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
     };
     Group g[2];
     constexpr int kStep = kWaves * kAhead;
-    const bool all = blocks <= kStep;   // one group of each wave holds all of the contraction
-    load(g[0], wave);
+    auto run = [&] {    // with g[0] and g[1] under way
+        for (int k = wave; k < blocks; k += 2 * kStep) {
+            multiply(g[0], k);
+            load(g[0], k + 2 * kStep);
+            if (k + kStep >= blocks) break;
+            multiply(g[1], k + kStep);
+            load(g[1], k + 3 * kStep);
+        }
+    };
     if constexpr (FUSED) {
-        hold<X>(p, h, blocks);
+        const int i = threadIdx.x >> 4, last = static_cast<int>(p.few.rows) * blocks - 1;
+        const Words<X> first = load_x<X>(p, i < last ? i : last, blocks);
+        load(g[0], wave);
+        load(g[1], wave + kStep);
+        hold<X>(p, h, blocks, first);
         // only LDS has to be there: the loads above stay under way
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-    }
-    if (all) multiply(g[0], wave);
-    for (int k = wave; !all && k < blocks; k += 2 * kStep) {
-        load(g[1], k + kStep);
-        multiply(g[0], k);
-        if (k + kStep >= blocks) break;
-        load(g[0], k + 2 * kStep);
-        multiply(g[1], k + kStep);
+        run();
+    } else if (blocks <= kStep) {   // one group of each wave holds all of the contraction
+        load(g[0], wave);
+        multiply(g[0], wave);
+    } else {
+        load(g[0], wave);
+        load(g[1], wave + kStep);
+        run();
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -317,7 +348,10 @@ bool fp8_few(int64_t m, int64_t n, int64_t k)
                0.0034 * static_cast<double>(rows * ((k + kFp8Block - 1) / kFp8Block)) * per_cu <= 9.5;
 }
 
-bool fp8_linear_few(int64_t m, int64_t k) { return m <= 16 && held_bytes(m, k) <= 48 * 1024; }
+// Each 32 blocks of x take a turn of a block's threads: beyond 4 turns a launch
+// of their own costs less (16 x 2,048 x 16,384: 12 against 16 us, 12 x 2,000 x
+// 8,192: 8.4 against 9.9).
+bool fp8_linear_few(int64_t m, int64_t k) { return m <= 16 && m * ((k + kFp8Block - 1) / kFp8Block) <= 128; }
 
 hipError_t launch_fp8_few(const Fp8Product& q, hipStream_t s)
 {

@@ -18,11 +18,11 @@
 // registers, written once per block and joined in a fixed order by a second
 // small kernel.
 //
-// Measured at 16,384 x 4,096 bf16, rms, channel gate, dropout: forward 121 us
-// (4.4 TB/s; 108 without dropout), backward 160 us (6 matrices: 5.0 TB/s),
+// Measured at 16,384 x 4,096 bf16, rms, channel gate, dropout: forward 111 us
+// (4.8 TB/s; 103 without dropout), backward 160 us (6 matrices: 5.0 TB/s),
 // column sums 6 us; fp32 forward 201 us (5.3 TB/s).  The vector unit is busy
 // two thirds of the forward pass.  Biases and full gates cost most (2,053 x
-// 5,003 fp16: 55 and 70 us): their registers leave room for two rows a CU
+// 5,003 fp16: 52 and 70 us): their registers leave room for two rows a CU
 // forward and one backward, too few to hide a row's reductions.
 #include "client_kernels.hpp"
 
