@@ -335,3 +335,41 @@ def test_smallest_scales(dtype, m, n, k):
     fa.client_fp8_linear(x.to(out.dtype).cuda(), b, out, workspace=ws)
     want = x.double() @ w.double().t()
     assert torch.equal(out.cpu(), want.to(torch.float32).to(out.dtype))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("fmt_a, fmt_b", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")])
+@pytest.mark.parametrize("m, n, k", [(4099, 2002, 2600), (4097, 2001, 2049), (2975, 2897, 1537)])
+def test_tiles_whose_rows_end_within_a_scale_word(dtype, fmt_a, fmt_b, m, n, k):
+    """Products of a little more than a round of 128 x 128 tiles, which larger tiles take: rows that end 1, 2 or 3 into
+    a lane's scales."""
+    import torch
+    gpu()
+    a, b, want = _integers(m, n, k, dtype, fmt_a, fmt_b)
+    out = torch.full_like(want, 7.0)
+    ws = torch.empty(fa.client_fp8_workspace_bytes(m, n, k), device="cuda", dtype=torch.uint8).fill_(255)
+    fa.client_fp8_matmul(a, b, out, workspace=ws)
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("m", [1, 3, 16, 17])
+@pytest.mark.parametrize("k", [1, 5, 7, 8, 9, 120, 127, 129, 135, 1030])
+def test_linear_of_short_and_cut_rows(dtype, m, k):
+    """Rows shorter than a vector, and rows whose end cuts one, between other values; weights are powers of two and
+    activations small integers, so the results are exact."""
+    import torch
+    gpu()
+    g = torch.Generator().manual_seed(m * 1000 + k)
+    buf = torch.full((m * (k + 5) + 3,), float("nan"), dtype=getattr(torch, dtype))
+    x = buf[3:].view(m, k + 5)[:, :k]
+    x.copy_(torch.randint(-3, 4, (m, k), generator=g))
+    w = torch.exp2(torch.randint(-2, 3, (50, k), generator=g).float())
+    d = buf.cuda()
+    b = fa.client_fp8_operand(50, k)
+    fa.client_fp8_quantize(w.cuda(), b, block_rows=128)
+    out = torch.empty(m, 50, device="cuda", dtype=d.dtype)
+    ws = torch.empty(fa.client_fp8_workspace_bytes(m, 50, k), device="cuda", dtype=torch.uint8)
+    fa.client_fp8_linear(d[3:].view(m, k + 5)[:, :k], b, out, workspace=ws)
+    want = x.double() @ w.double().t()
+    assert torch.equal(out.cpu(), want.to(torch.float32).to(out.dtype))
