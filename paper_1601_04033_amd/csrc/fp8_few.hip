@@ -8,7 +8,8 @@
 // fragments straight from memory (16 rows of 128 bytes: whole lines), each
 // value once; the few rows come from the caches.  The waves' sums are joined
 // through LDS, so one launch writes the result.  1 x 4,096 x 16,384 (67 MB):
-// 16.0 us, 4.2 TB/s, of which about 4 are the launch and x's quantization;
+// 15.3 us, 4.4 TB/s, of which about 4 are the launch and x's quantization; 1 x
+// 14,592 x 12,032 (176 MB): 34 us, 5.2 TB/s;
 // 128 x 784 x 1,000: 3.7 us.
 // Few unquantized activations (128 blocks of 128) are quantized on the way:
 // every block does it again, into LDS, while its first loads of the larger
@@ -52,12 +53,12 @@ struct Rows {
           at((lane_ & 15) * static_cast<uint32_t>(v.ld) + (lane_ >> 4) * 16), lane(lane_)
     {
     }
-    template <bool STREAM> __device__ v8i read(int tile, int kb, bool in) const
+    // (Non-temporal loads were slower: 1 x 14,592 x 12,032 46 against 34 us.)
+    __device__ v8i read(int tile, int kb, bool in) const
     {
-        constexpr int kOnce = STREAM ? 2 : 0;   // non-temporal
         const uint32_t p = in ? at + tile * 16 * ld : kOutside;
-        const auto lo = __builtin_amdgcn_raw_buffer_load_b128(data, p, kb * kFp8Block, kOnce);
-        const auto hi = __builtin_amdgcn_raw_buffer_load_b128(data, p + 64, kb * kFp8Block, kOnce);
+        const auto lo = __builtin_amdgcn_raw_buffer_load_b128(data, p, kb * kFp8Block, 0);
+        const auto hi = __builtin_amdgcn_raw_buffer_load_b128(data, p + 64, kb * kFp8Block, 0);
         return join_chunks(__builtin_bit_cast(v4i, lo), __builtin_bit_cast(v4i, hi));
     }
     // the lane's row's scale with its three neighbours', and the scale alone:
@@ -174,13 +175,13 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 g.scale_big[u][n] = big.read_scale(n, kb, in);
-                g.big[u][n] = big.read<true>(n, kb, in);
+                g.big[u][n] = big.read(n, kb, in);
             }
             if constexpr (!FUSED) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
                     g.scale_few[u][m] = few_rows.read_scale(m, kb, in);
-                    g.few[u][m] = few_rows.read<false>(m, kb, in);
+                    g.few[u][m] = few_rows.read(m, kb, in);
                 }
             }
         }
