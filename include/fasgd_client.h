@@ -211,8 +211,9 @@ fasgd_status client_fp8_matmul(const client_fp8_operand* a, const client_fp8_ope
  * y = x W^T for activations x ([m][w->k] of dtype, not quantized before) and
  * weights held as an operand, as serving and evaluation need it: x is
  * quantized in e4m3 as client_fp8_quantize does with block_rows = 1, then
- * multiplied.  y is [m][w->rows] of dtype.  workspace:
- * client_fp8_workspace_bytes(m, w->rows, w->k) bytes, as above.
+ * multiplied.  y is [m][w->rows] of dtype, m at most 2^27 as an operand's
+ * rows are.  workspace: client_fp8_workspace_bytes(m, w->rows, w->k) bytes,
+ * as above.
  */
 fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const client_fp8_operand* w, void* y,
                                int64_t ldy, int32_t dtype, void* workspace, size_t workspace_bytes,

@@ -363,6 +363,7 @@ fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const clie
     FASGD_TRY(check_operand("w", w, p.b));
     FASGD_TRY(check_shape(m, w->rows, dtype));
     FASGD_TRY(check_shape(m, w->k, dtype));
+    if (m > kMaxOperandRows) return fail(FASGD_ERR_ARG, "m = %lld is not in [0, 2^27]", (long long)m);
     if (m == 0 || w->rows == 0) return ok();
     FASGD_TRY(check_matrix("y", y, ldy, m, w->rows, dtype));
     if (w->k > 0) {

@@ -1,0 +1,31 @@
+"""Limits of the client's calls, checked on the host: what is beyond them is
+rejected before anything is enqueued (so these calls never touch a device)."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+import paper_1601_04033_amd as fa
+from paper_1601_04033_amd import client
+
+ARG = 2
+BUF = np.zeros(64, np.float32)
+P = (BUF.ctypes.data + 15) & ~15       # stands in for device memory: no call below reaches a launch
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(fa.LIB_PATH):
+        from paper_1601_04033_amd import _build
+        _build.build()
+    return client.bind(fa.load_library())
+
+
+@pytest.mark.parametrize("m, n, k", [(2 ** 27 + 1, 1, 1), (2 ** 28, 16, 128), (2 ** 30, 1, 100)])
+def test_linear_takes_as_many_rows_as_an_operand(lib, m, n, k):
+    """From 2^28 rows on, a narrow layer's product would be a launch of 2^32 threads, behind a quantization that is
+    already enqueued."""
+    w = client.client_fp8_operand_struct(P, P, n, k, -(-k // 128) * 128, -(-n // 4) * 4, 0)
+    assert lib.client_fp8_linear(P, k, m, ctypes.byref(w), P, n, 1, P, 2 ** 62, None) == ARG
+    assert b"m = " in lib.fasgd_last_error()
