@@ -678,11 +678,11 @@ __global__ __launch_bounds__(MAXT, SUB && GENERAL ? 2 : kBackwardWaves) void nor
 // The column sums of `blocks` blocks joined: each of the block's 16 waves
 // takes every 16th, and the waves' sums are added in order, so the order is
 // fixed.  blockIdx.y: the norm after the block, or the one before the next.
-__global__ __launch_bounds__(1024) void norm_columns(NormArgs a, int blocks, int bias)
+__global__ __launch_bounds__(1024) void norm_columns(NormArgs a, int blocks, int bias, int first)
 {
     __shared__ float part[2][16][64];
     const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, pre = blockIdx.y;
-    const int c = blockIdx.x * 64 + lane;
+    const int c = first + blockIdx.x * 64 + lane;
     float s[2] = {0.0f, 0.0f};
     if (c < a.cols) {
         const float* p = a.partial + static_cast<int64_t>(pre) * blocks * a.cols + c;
@@ -717,9 +717,16 @@ __global__ __launch_bounds__(1024) void norm_columns(NormArgs a, int blocks, int
     if (a.db_post) a.db_post[c] = f * s[1];
 }
 
+// 16 threads a column and norm, so a launch takes 2^26 columns of the 2^30
+// that there may be: it may have fewer than 2^32 threads.
 void launch_columns(const NormArgs& a, int blocks, int bias, hipStream_t s)
 {
-    norm_columns<<<dim3((a.cols + 63) / 64, a.w_pre ? 2 : 1), 1024, 0, s>>>(a, blocks, bias);
+    constexpr int kColumns = 1 << 26;
+    for (int first = 0; first < a.cols; first += kColumns) {
+        const int n = a.cols - first < kColumns ? a.cols - first : kColumns;
+        norm_columns<<<dim3((n + 63) / 64, a.w_pre ? 2 : 1), 1024, 0, s>>>(a, blocks, bias, first);
+        if (hipPeekAtLastError() != hipSuccess) return;     // the launcher's caller takes it
+    }
 }
 
 // ---- rows too long for the registers: the same sums with the row read again
