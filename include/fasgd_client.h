@@ -165,6 +165,9 @@ typedef enum client_fp8_format {
     CLIENT_FP8_E5M2 = 1
 } client_fp8_format;
 
+/* added to the output's type: a choice of client_fp8_matmul and client_fp8_linear */
+enum { CLIENT_FP8_SHORT_SUMS = 0x100 };
+
 typedef struct client_fp8_operand {
     uint8_t* data;              /* [rows][ld] */
     uint8_t* scales;            /* [ceil(k / 128)][lds], an exponent + 127 each */
@@ -195,9 +198,17 @@ fasgd_status client_fp8_quantize(const void* x, int64_t ldx, int64_t rows, int64
  * what c holds), [a->rows][b->rows] of c_dtype, for two operands of one k.
  * A linear layer y = x W^T is the product of x and W; its input gradient
  * that of dy and W transposed, its weight gradient that of dy transposed and
- * x transposed.  Sums are fp32 and rounded once.  Where few outputs leave
- * most of the chip idle, the contraction is split and its parts joined in
- * order through the workspace, so the result is the same run to run.
+ * x transposed.  Sums are fp32 and rounded once (values below 2^-126 are held
+ * to 2^-133).
+ * c_dtype CLIENT_BF16 or CLIENT_F16 with CLIENT_FP8_SHORT_SUMS added to it
+ * takes the matrix instruction of 8-bit values, at twice the rate: each 8
+ * consecutive products of a sum, from a multiple of 8 on, are then cut off
+ * below 2^-13 of the largest of them before they go into the fp32 sum, an
+ * error of up to 7 x 2^-13 of that product for each 8, whatever the sum of
+ * them is.
+ * Where few outputs leave most of the chip idle, the contraction is split and
+ * its parts joined in order through the workspace, so the result is the same
+ * run to run.
  * workspace: client_fp8_workspace_bytes(a->rows, b->rows, k) bytes of device
  * scratch, 16-byte aligned, contents irrelevant (the same size serves
  * client_fp8_linear, which also holds its quantized x there).
@@ -211,9 +222,9 @@ fasgd_status client_fp8_matmul(const client_fp8_operand* a, const client_fp8_ope
  * y = x W^T for activations x ([m][w->k] of dtype, not quantized before) and
  * weights held as an operand, as serving and evaluation need it: x is
  * quantized in e4m3 as client_fp8_quantize does with block_rows = 1, then
- * multiplied.  y is [m][w->rows] of dtype, m at most 2^27 as an operand's
- * rows are.  workspace: client_fp8_workspace_bytes(m, w->rows, w->k) bytes,
- * as above.
+ * multiplied, with the same sums (short ones by the same flag in dtype).  y
+ * is [m][w->rows] of dtype, m at most 2^27 as an operand's rows are.
+ * workspace: client_fp8_workspace_bytes(m, w->rows, w->k) bytes, as above.
  */
 fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const client_fp8_operand* w, void* y,
                                int64_t ldy, int32_t dtype, void* workspace, size_t workspace_bytes,

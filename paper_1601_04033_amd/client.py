@@ -21,6 +21,7 @@ CLIENT_ABI_FUNCTIONS = ("client_dropout", "client_residual_norm_workspace_bytes"
 
 FP8_E4M3 = 0
 FP8_E5M2 = 1
+_FP8_SHORT_SUMS = 0x100
 
 NORM_RMS = 0
 NORM_LAYER = 1
@@ -346,24 +347,30 @@ def _workspace(workspace):
     return _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel()
 
 
-def client_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out, accumulate: bool = False, workspace=None, stream=None) -> None:
+def _output_type(out, short_sums):
+    return _dtype(out, "out") | (_FP8_SHORT_SUMS if short_sums else 0)
+
+
+def client_fp8_matmul(a: Fp8Operand, b: Fp8Operand, out, accumulate: bool = False, workspace=None, stream=None,
+                      short_sums: bool = False) -> None:
     """out [a.rows, b.rows] = a b^T over their common k (accumulate: added to out).  workspace: uint8,
-    client_fp8_workspace_bytes(a.rows, b.rows, k) bytes."""
-    rc = (_calls or _native()).client_fp8_matmul(a.c, b.c, out, accumulate, workspace, stream)
+    client_fp8_workspace_bytes(a.rows, b.rows, k) bytes.  Sums are fp32; short_sums (out bfloat16 or float16) takes the
+    8-bit matrix instruction at twice the rate, which cuts each 8 products off below 2^-13 of the largest of them."""
+    rc = (_calls or _native()).client_fp8_matmul(a.c, b.c, out, accumulate, workspace, stream, short_sums)
     if rc is not None:
         return _check(rc) if rc else None
     pc, ldc = _matrix(out, "out")
     if _shape(out) != (a.rows, b.rows):
         raise ValueError(f"out is {tuple(out.shape)}, expected {(a.rows, b.rows)}")
     pw, nw = _workspace(workspace)
-    _check(_library().client_fp8_matmul(ctypes.byref(a.c), ctypes.byref(b.c), pc, ldc, _dtype(out, "out"),
+    _check(_library().client_fp8_matmul(ctypes.byref(a.c), ctypes.byref(b.c), pc, ldc, _output_type(out, short_sums),
                                         1 if accumulate else 0, pw, nw, _stream(stream)))
 
 
-def client_fp8_linear(x, w: Fp8Operand, out, workspace=None, stream=None) -> None:
+def client_fp8_linear(x, w: Fp8Operand, out, workspace=None, stream=None, short_sums: bool = False) -> None:
     """out [m, w.rows] = x w^T for x [m, w.k] of out's dtype, quantized in e4m3 on the way.  workspace: uint8,
-    client_fp8_workspace_bytes(m, w.rows, w.k) bytes."""
-    rc = (_calls or _native()).client_fp8_linear(x, w.c, out, workspace, stream)
+    client_fp8_workspace_bytes(m, w.rows, w.k) bytes.  short_sums as in client_fp8_matmul."""
+    rc = (_calls or _native()).client_fp8_linear(x, w.c, out, workspace, stream, short_sums)
     if rc is not None:
         return _check(rc) if rc else None
     px, ldx = _matrix(x, "x")
@@ -374,5 +381,5 @@ def client_fp8_linear(x, w: Fp8Operand, out, workspace=None, stream=None) -> Non
     if k != w.k or _shape(out) != (m, w.rows):
         raise ValueError(f"x {tuple(x.shape)} and out {tuple(out.shape)} do not fit weights [{w.rows}, {w.k}]")
     pw, nw = _workspace(workspace)
-    _check(_library().client_fp8_linear(px, ldx, m, ctypes.byref(w.c), py, ldy, _dtype(x, "x"), pw, nw,
+    _check(_library().client_fp8_linear(px, ldx, m, ctypes.byref(w.c), py, ldy, _output_type(out, short_sums), pw, nw,
                                         _stream(stream)))

@@ -163,6 +163,15 @@ fasgd_status check_workspace(const void* workspace, size_t bytes, size_t need)
     return FASGD_OK;
 }
 
+// Takes the choice of short sums out of an output's type.
+fasgd_status take_short_sums(int32_t& dtype, int32_t& short_sums)
+{
+    short_sums = (dtype & CLIENT_FP8_SHORT_SUMS) != 0;
+    dtype &= ~CLIENT_FP8_SHORT_SUMS;
+    if (short_sums && dtype == CLIENT_F32) return fail(FASGD_ERR_ARG, "short sums are of 16-bit outputs");
+    return FASGD_OK;
+}
+
 // client_fp8_linear's quantized x at the front of its workspace.
 size_t linear_operand_bytes(int64_t m, int64_t k)
 {
@@ -335,6 +344,7 @@ fasgd_status client_fp8_matmul(const client_fp8_operand* a, const client_fp8_ope
 {
     fasgd::Fp8Product p;
     memset(&p, 0, sizeof p);
+    FASGD_TRY(take_short_sums(c_dtype, p.short_sums));
     FASGD_TRY(check_operand("a", a, p.a));
     FASGD_TRY(check_operand("b", b, p.b));
     if (a->k != b->k)
@@ -360,6 +370,7 @@ fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const clie
 {
     fasgd::Fp8Product p;
     memset(&p, 0, sizeof p);
+    FASGD_TRY(take_short_sums(dtype, p.short_sums));
     FASGD_TRY(check_operand("w", w, p.b));
     FASGD_TRY(check_shape(m, w->rows, dtype));
     FASGD_TRY(check_shape(m, w->k, dtype));

@@ -91,6 +91,7 @@ struct Fp8Product {
     int64_t ldc;
     int32_t c_dtype;
     int32_t accumulate;
+    int32_t short_sums;     // 16-bit c: each 8 products to 2^-13 of the largest
     float* partial;         // [splits][m][n], unused with one split
 };
 // Products that read their operands straight into registers: launch_fp8_few,

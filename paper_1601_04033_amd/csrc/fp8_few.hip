@@ -325,9 +325,8 @@ template <bool WIDE> hipError_t launch_formats(const Few& p, hipStream_t s)
     return p.few.format == FP8_E4M3 ? launch_few_rows<WIDE, 1, 0>(p, s) : launch_few_rows<WIDE, 1, 1>(p, s);
 }
 
-template <typename X> hipError_t launch_fused(const Few& p, hipStream_t s)
+template <typename X, bool WIDE> hipError_t launch_fused(const Few& p, hipStream_t s)
 {
-    constexpr bool WIDE = sizeof(X) == 4;
     return p.big.format == FP8_E4M3 ? launch_rows<X, true, WIDE, 0, 0, 1>(p, s) : launch_rows<X, true, WIDE, 1, 0, 1>(p, s);
 }
 
@@ -367,15 +366,15 @@ hipError_t launch_fp8_few(const Fp8Product& q, hipStream_t s)
     p.stride_few = b_few ? 1 : q.ldc;
     p.c_dtype = q.c_dtype;
     p.accumulate = q.accumulate;
-    return q.c_dtype == DTYPE_F32 ? launch_formats<true>(p, s) : launch_formats<false>(p, s);
+    return q.short_sums ? launch_formats<false>(p, s) : launch_formats<true>(p, s);
 }
 
 hipError_t launch_fp8_linear_few(const void* x, int64_t ldx, const Fp8Product& q, hipStream_t s)
 {
     const Few p{q.b, q.a, x, ldx, q.c, 1, q.ldc, q.c_dtype, 0};
-    if (q.c_dtype == DTYPE_F32) return launch_fused<float>(p, s);
-    if (q.c_dtype == DTYPE_BF16) return launch_fused<bf16>(p, s);
-    return launch_fused<f16>(p, s);
+    if (q.c_dtype == DTYPE_F32) return launch_fused<float, true>(p, s);
+    if (q.short_sums) return q.c_dtype == DTYPE_BF16 ? launch_fused<bf16, false>(p, s) : launch_fused<f16, false>(p, s);
+    return q.c_dtype == DTYPE_BF16 ? launch_fused<bf16, true>(p, s) : launch_fused<f16, true>(p, s);
 }
 
 }  // namespace fasgd

@@ -692,6 +692,14 @@ struct ClientArgs : Args {
         *n = 0;
         return plain && v[i] != Py_None ? tensor(i, c10::ScalarType::Byte, -1, 0, n) : nullptr;
     }
+    // a truth value
+    bool truth(int i)
+    {
+        if (v[i] != Py_True && v[i] != Py_False) refuse();
+        return v[i] == Py_True;
+    }
+    // the type of a product's output, with the choice of short sums
+    int32_t output_type(const Matrix& m, int i) { return truth(i) ? m.dtype | CLIENT_FP8_SHORT_SUMS : m.dtype; }
     // gate forms as the binding's general way tells them apart
     bool gate(int i, const Matrix& like, int32_t* form, void** p, int64_t* ld)
     {
@@ -827,37 +835,39 @@ PyObject* quantize_call(PyObject*, PyObject* const* args, Py_ssize_t n)
     return finish(a, [&] { return g_client.client_fp8_quantize(x.p, x.ld, x.rows, x.cols, x.dtype, block, r, c, s); });
 }
 
-// (a, b, out, accumulate, workspace, stream)
+// (a, b, out, accumulate, workspace, stream, short sums)
 PyObject* matmul_call(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    if (!arity(n, 6)) return nullptr;
+    if (!arity(n, 7)) return nullptr;
     ClientArgs a(args);
     const client_fp8_operand *x = a.operand(0, 0), *y = a.operand(1, 1);
     const Matrix c = a.matrix(2);
-    if (a.plain && (!x || !y || c.rows != x->rows || c.cols != y->rows || (args[3] != Py_True && args[3] != Py_False)))
-        a.refuse();
+    if (a.plain && (!x || !y || c.rows != x->rows || c.cols != y->rows)) a.refuse();
+    const bool add = a.truth(3);
+    const int32_t type = a.output_type(c, 6);
     int64_t ws = 0;
     void* w = a.workspace(4, &ws);
     hipStream_t s = a.stream(5);
     return finish(a, [&] {
-        return g_client.client_fp8_matmul(x, y, c.p, c.ld, c.dtype, args[3] == Py_True, w, static_cast<size_t>(ws), s);
+        return g_client.client_fp8_matmul(x, y, c.p, c.ld, type, add, w, static_cast<size_t>(ws), s);
     });
 }
 
-// (x, w, out, workspace, stream)
+// (x, w, out, workspace, stream, short sums)
 PyObject* linear_call(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
-    if (!arity(n, 5)) return nullptr;
+    if (!arity(n, 6)) return nullptr;
     ClientArgs a(args);
     const Matrix x = a.matrix(0);
     const client_fp8_operand* w = a.operand(1, 0);
     const Matrix y = a.matrix(2);
     if (a.plain && (!w || x.dtype != y.dtype || x.cols != w->k || y.rows != x.rows || y.cols != w->rows)) a.refuse();
+    const int32_t type = a.output_type(y, 5);
     int64_t ws = 0;
     void* p = a.workspace(3, &ws);
     hipStream_t s = a.stream(4);
     return finish(a, [&] {
-        return g_client.client_fp8_linear(x.p, x.ld, x.rows, w, y.p, y.ld, x.dtype, p, static_cast<size_t>(ws), s);
+        return g_client.client_fp8_linear(x.p, x.ld, x.rows, w, y.p, y.ld, type, p, static_cast<size_t>(ws), s);
     });
 }
 

@@ -29,3 +29,17 @@ def test_linear_takes_as_many_rows_as_an_operand(lib, m, n, k):
     w = client.client_fp8_operand_struct(P, P, n, k, -(-k // 128) * 128, -(-n // 4) * 4, 0)
     assert lib.client_fp8_linear(P, k, m, ctypes.byref(w), P, n, 1, P, 2 ** 62, None) == ARG
     assert b"m = " in lib.fasgd_last_error()
+
+
+def test_short_sums_are_of_16_bit_outputs(lib):
+    """The flag in an output's type: taken with the 16-bit types, rejected with fp32 and with what is no type."""
+    a = client.client_fp8_operand_struct(P, P, 4, 100, 128, 4, 0)
+    ref = ctypes.byref(a)
+    for dtype, text in ((0x100, b"short sums"), (0x103, b"dtype"), (0x201, b"dtype"), (-1, b"dtype")):
+        assert lib.client_fp8_matmul(ref, ref, P, 4, dtype, 0, P, 1 << 20, None) == ARG
+        assert text in lib.fasgd_last_error()
+        assert lib.client_fp8_linear(P, 100, 4, ref, P, 4, dtype, P, 1 << 20, None) == ARG
+        assert text in lib.fasgd_last_error()
+    for dtype in (0x101, 0x102):        # as far as the next check
+        assert lib.client_fp8_matmul(ref, ref, P, 3, dtype, 0, P, 1 << 20, None) == ARG
+        assert b"row stride" in lib.fasgd_last_error()
