@@ -22,7 +22,7 @@
 // (4.8 TB/s; 103 without dropout), backward 160 us (6 matrices: 5.0 TB/s),
 // column sums 6 us; fp32 forward 201 us (5.3 TB/s).  The vector unit is busy
 // two thirds of the forward pass.  Biases and full gates cost most (2,053 x
-// 5,003 fp16: 52 and 70 us): their registers leave room for two rows a CU
+// 5,003 fp16: 59 and 77 us): their registers leave room for two rows a CU
 // forward and one backward, too few to hide a row's reductions.
 #include "client_kernels.hpp"
 
@@ -102,31 +102,17 @@ __device__ __forceinline__ float activate(float g, int act)
     if (act == ACT_TANH) return tanhf(g);
     return g;
 }
-// Activations of V gates in place, the kind of activation decided once.  FAST,
-// for gates of every element in 16-bit types: from the hardware's exponential
-// and reciprocal (an ulp of fp32 each, far below what these gates and sums
-// hold); near 0, tanh is its series, as the quotient would lose what the
-// subtraction cancels.
-template <bool FAST, int V> __device__ __forceinline__ void activate_all(float (&g)[V], int act)
+// Activations of V gates in place, the kind of activation decided once.  (From
+// the hardware's exponential and reciprocal alone a sigmoid is 30 ulps of fp32
+// off at a gate of -40; it took 2,053 x 5,003 fp16 from 142 to 127 us.)
+template <int V> __device__ __forceinline__ void activate_all(float (&g)[V], int act)
 {
-    constexpr float kLog2e = 1.4426950408889634f;
     if (act == ACT_SIGMOID) {
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            g[j] = FAST ? __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * g[j])) : activate(g[j], ACT_SIGMOID);
+        for (int j = 0; j < V; ++j) g[j] = activate(g[j], ACT_SIGMOID);
     } else if (act == ACT_TANH) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if (!FAST) {
-                g[j] = activate(g[j], ACT_TANH);
-                continue;
-            }
-            const float x = fabsf(g[j]), s = g[j] * g[j];
-            const float t = __builtin_amdgcn_exp2f(-2.0f * kLog2e * x);
-            const float large = __builtin_copysignf((1.0f - t) * __builtin_amdgcn_rcpf(1.0f + t), g[j]);
-            const float small = g[j] * fmaf(s, fmaf(s, fmaf(s, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-            g[j] = x < 0.125f ? small : large;
-        }
+        for (int j = 0; j < V; ++j) g[j] = activate(g[j], ACT_TANH);
     }
 }
 // the derivative, from the activation's value
@@ -336,7 +322,7 @@ __global__ __launch_bounds__(MAXT, GENERAL ? kForwardGeneralWaves : kForwardWave
         for (int j = 0; j < V; ++j) f[j] = 1.0f;
         if (a.gate_form == GATE_CHANNEL) {
             load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, f);
-            activate_all<false>(f, a.gate_act);
+            activate_all(f, a.gate_act);
         }
         const float scale = a.drop ? a.key.scale : 1.0f;
         load_params<V>(a.w_post, c, a.cols, 1.0f, x);
@@ -394,7 +380,7 @@ __global__ __launch_bounds__(MAXT, GENERAL ? kForwardGeneralWaves : kForwardWave
                 float f[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) f[j] = to_float(g[v].v[j]);
-                activate_all<sizeof(T) == 2>(f, a.gate_act);
+                activate_all(f, a.gate_act);
 #pragma unroll
                 for (int j = 0; j < V; ++j) d[v][j] *= f[j];
             }
@@ -482,7 +468,7 @@ __global__ __launch_bounds__(MAXT, SUB && GENERAL ? 2 : kBackwardWaves) void nor
         if (a.gate_form == GATE_CHANNEL) {
             float f[V];
             load_params<V>(static_cast<const float*>(a.gate), c, a.cols, 0.0f, f);
-            activate_all<false>(f, a.gate_act);
+            activate_all(f, a.gate_act);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] *= f[j];
         }
@@ -572,7 +558,7 @@ __global__ __launch_bounds__(MAXT, SUB && GENERAL ? 2 : kBackwardWaves) void nor
                     f[j] = to_float(g[v].v[j]);
                     z[j] = ds[v][j] * fmaf(xh[v][j], w[j], b[j]);
                 }
-                activate_all<sizeof(T) == 2>(f, a.gate_act);
+                activate_all(f, a.gate_act);
                 if (a.gate_act == ACT_SIGMOID) {
 #pragma unroll
                     for (int j = 0; j < V; ++j) z[j] *= slope(f[j], ACT_SIGMOID);
