@@ -100,9 +100,12 @@ struct Fp8Product {
 constexpr int64_t kFewRows = 64;
 bool fp8_few(int64_t m, int64_t n, int64_t k);
 bool fp8_linear_few(int64_t m, int64_t k);
+int fp8_few_splits(int64_t m, int64_t n, int64_t k);     // of a product that fp8_few takes
 hipError_t launch_fp8_few(const Fp8Product& p, hipStream_t s);
 hipError_t launch_fp8_linear_few(const void* x, int64_t ldx, const Fp8Product& q, hipStream_t s);
 size_t fp8_workspace_bytes(int64_t m, int64_t n, int64_t k);
 hipError_t launch_fp8_product(const Fp8Product& p, hipStream_t s);
+// c from the splits' products in the workspace, added in order.
+hipError_t launch_fp8_join(const Fp8Product& p, int splits, hipStream_t s);
 
 }  // namespace fasgd

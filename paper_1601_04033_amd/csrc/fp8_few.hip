@@ -7,13 +7,17 @@
 // rows, its 8 waves take the contraction's blocks of 128 in turn and read
 // fragments straight from memory (16 rows of 128 bytes: whole lines), each
 // value once; the few rows come from the caches.  The waves' sums are joined
-// through LDS, so one launch writes the result.  1 x 4,096 x 16,384 (67 MB):
+// through LDS, so one launch writes the result, unless the larger operand's
+// rows are too few for the CUs and long: then blocks take parts of the
+// contraction, joined in order by a second launch.  1 x 4,096 x 16,384 (67 MB):
 // 15.3 us, 4.4 TB/s, of which about 4 are the launch and x's quantization; 1 x
 // 14,592 x 12,032 (176 MB): 34 us, 5.2 TB/s;
 // 128 x 784 x 1,000: 3.7 us.
 // Few unquantized activations (128 blocks of 128) are quantized on the way:
 // every block does it again, into LDS, while its first loads of the larger
 // operand are under way, which costs less than a launch before this one.
+#include <string.h>
+
 #include "fp8_math.hpp"
 
 namespace fasgd {
@@ -30,6 +34,8 @@ struct Few {
     int64_t stride_big, stride_few;
     int32_t c_dtype;
     int32_t accumulate;
+    int32_t steps;          // blocks of 128 a split takes
+    int64_t part;           // elements between the splits' products (0: one split)
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources
@@ -40,6 +46,7 @@ struct Few {
 // matter).  A row past the operand's end reads as 0.  Through buffers a load's
 // address costs one scalar addition, and no register that a load under way
 // still needs.
+// Of the contraction the blocks from kb0 on.
 struct Rows {
     static constexpr uint32_t kOutside = 0xf0000000u;
     __amdgpu_buffer_rsrc_t data;
@@ -47,9 +54,9 @@ struct Rows {
     int64_t lds, scales_left;
     uint32_t ld, at;
     int lane;
-    __device__ Rows(const Fp8View& v, int64_t row, int lane_)
-        : data(buffer(v.data + row * v.ld, (v.rows - row) * v.ld)), scales(v.scales + row), lds(v.lds),
-          scales_left(v.lds - row), ld(static_cast<uint32_t>(v.ld)),
+    __device__ Rows(const Fp8View& v, int64_t row, int64_t kb0, int lane_)
+        : data(buffer(v.data + row * v.ld + kb0 * kFp8Block, (v.rows - row) * v.ld - kb0 * kFp8Block)),
+          scales(v.scales + kb0 * v.lds + row), lds(v.lds), scales_left(v.lds - row), ld(static_cast<uint32_t>(v.ld)),
           at((lane_ & 15) * static_cast<uint32_t>(v.ld) + (lane_ >> 4) * 16), lane(lane_)
     {
     }
@@ -150,7 +157,13 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
     __shared__ __attribute__((aligned(16))) float sums[kWaves][NT][MT][64][4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t r0 = static_cast<int64_t>(blockIdx.x) * (16 * NT), m0 = static_cast<int64_t>(blockIdx.y) * (16 * MT);
-    const int blocks = static_cast<int>((p.big.k + kFp8Block - 1) / kFp8Block);
+    const int kb0 = blockIdx.z * p.steps, left = static_cast<int>((p.big.k + kFp8Block - 1) / kFp8Block) - kb0;
+    const int blocks = left < p.steps ? left : p.steps;
+    if constexpr (FUSED) {      // of x the columns of these blocks
+        p.x = static_cast<const X*>(p.x) + static_cast<int64_t>(kb0) * kFp8Block;
+        const int64_t k = p.few.k - static_cast<int64_t>(kb0) * kFp8Block, most = static_cast<int64_t>(blocks) * kFp8Block;
+        p.few.k = k < most ? k : most;
+    }
     v4f acc[NT][MT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -162,7 +175,7 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
         v8i big[kAhead][NT], few[kAhead][kFew];
         uint32_t scale_big[kAhead][NT], scale_few[kAhead][kFew];
     };
-    const Rows big(p.big, r0, lane), few_rows(FUSED ? p.big : p.few, FUSED ? r0 : m0, lane);
+    const Rows big(p.big, r0, kb0, lane), few_rows(FUSED ? p.big : p.few, FUSED ? r0 : m0, kb0, lane);
     // A block past the last is loaded from outside the buffers, which moves
     // nothing (read as the last block it cost as much again: 1 x 4,096 x 16,384
     // 22 against 16 us), and not multiplied: with the same loads on every way
@@ -283,7 +296,7 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
         if (row >= p.big.rows || col >= p.few.rows) continue;
         const int64_t at = row * p.stride_big + col * p.stride_few;
         if (p.c_dtype == DTYPE_F32) {
-            float* c = static_cast<float*>(p.c) + at;
+            float* c = static_cast<float*>(p.c) + blockIdx.z * p.part + at;
             *c = p.accumulate ? *c + s : s;
         } else if (p.c_dtype == DTYPE_BF16) {
             bf16* c = static_cast<bf16*>(p.c) + at;
@@ -297,18 +310,21 @@ __global__ __launch_bounds__(kThreads, 4) void product_few(Few p, int held_strid
 }
 
 // 32 rows a block where that still gives every CU one, else 16.
+constexpr int64_t kRowsFor32 = 256 * 32;
 template <typename X, bool FUSED, bool WIDE, int FBIG, int FFEW, int MT>
 hipError_t launch_rows(const Few& p, hipStream_t s)
 {
-    const size_t lds = FUSED ? held_bytes(p.few.rows, p.few.k) : 0;
-    const int stride = FUSED ? held_stride(p.few.k) : 0;
+    const int64_t blocks = (p.few.k + kFp8Block - 1) / kFp8Block, held = blocks < p.steps ? blocks : p.steps;
+    const size_t lds = FUSED ? held_bytes(p.few.rows, held * kFp8Block) : 0;
+    const int stride = FUSED ? held_stride(held * kFp8Block) : 0;
+    const unsigned splits = static_cast<unsigned>((blocks + p.steps - 1) / p.steps);
     const unsigned along = static_cast<unsigned>((p.few.rows + 16 * MT - 1) / (16 * MT));
-    if (MT == 1 && p.big.rows >= 256 * 32)
+    if (MT == 1 && p.big.rows >= kRowsFor32)
         product_few<X, FUSED, WIDE, FBIG, FFEW, MT, MT == 1 ? 2 : 1>
-            <<<dim3(static_cast<unsigned>((p.big.rows + 31) / 32), along), kThreads, lds, s>>>(p, stride);
+            <<<dim3(static_cast<unsigned>((p.big.rows + 31) / 32), along, splits), kThreads, lds, s>>>(p, stride);
     else
         product_few<X, FUSED, WIDE, FBIG, FFEW, MT, 1>
-            <<<dim3(static_cast<unsigned>((p.big.rows + 15) / 16), along), kThreads, lds, s>>>(p, stride);
+            <<<dim3(static_cast<unsigned>((p.big.rows + 15) / 16), along, splits), kThreads, lds, s>>>(p, stride);
     return hipGetLastError();
 }
 
@@ -353,28 +369,75 @@ bool fp8_few(int64_t m, int64_t n, int64_t k)
 // 8,192: 8.4 against 9.9).
 bool fp8_linear_few(int64_t m, int64_t k) { return m <= 16 && m * ((k + kFp8Block - 1) / kFp8Block) <= 128; }
 
+// Splits of the contraction of a product of up to 16 rows, whose blocks alone
+// may leave most of the CUs idle: by the estimate above and that of the join,
+// 4 us and 0.15 for each part (unsplit and split, fp32 out: 10 x 1,000 x 65,536
+// 52 and 19 us, 16 x 16 x 2^20 904 and 24, 10 x 1,000 x 8,192 9.3 and 7.0; one
+// token through 256 x 16,384 bf16 12.9 and 7.4; 10 x 4,096 x 16,384 stays at
+// 19, two parts take 23).
+int fp8_few_splits(int64_t m, int64_t n, int64_t k)
+{
+    const int64_t few = m < n ? m : n, big = m < n ? n : m;
+    if (few < 1 || few > 16) return 1;
+    const int64_t rows = big >= kRowsFor32 ? 32 : 16, wide = (big + rows - 1) / rows, blocks = (k + kFp8Block - 1) / kFp8Block;
+    int best = 1;
+    double least = 0.0;
+    for (int s = 1; s <= 64 && (s == 1 || wide * s <= 512); s *= 2) {
+        const double per_cu = wide * s > 256 ? static_cast<double>(wide * s) / 256 : 1.0;
+        const double t = 0.0034 * static_cast<double>((rows + 16) * ((blocks + s - 1) / s)) * per_cu + (s > 1 ? 4.0 + 0.15 * s : 0.0);
+        if (s == 1 || t < least) {
+            least = t;
+            best = s;
+        }
+    }
+    const int64_t steps = (blocks + best - 1) / best;       // so that no split is empty
+    return static_cast<int>((blocks + steps - 1) / steps);
+}
+
+namespace {
+
+// The product as the kernel takes it, big the larger operand.  Splits leave
+// their fp32 products in q's workspace.
+Few few_of(const Fp8Product& q, const Fp8View& big, const Fp8View& few, bool big_is_a, int splits)
+{
+    const int64_t blocks = (q.a.k + kFp8Block - 1) / kFp8Block;
+    Few p;
+    memset(&p, 0, sizeof p);
+    p.big = big;
+    p.few = few;
+    const int64_t ldc = splits > 1 ? q.b.rows : q.ldc;
+    p.c = splits > 1 ? q.partial : q.c;
+    p.stride_big = big_is_a ? ldc : 1;
+    p.stride_few = big_is_a ? 1 : ldc;
+    p.c_dtype = splits > 1 ? static_cast<int32_t>(DTYPE_F32) : q.c_dtype;
+    p.accumulate = splits > 1 ? 0 : q.accumulate;
+    p.steps = static_cast<int32_t>((blocks + splits - 1) / splits);
+    p.part = splits > 1 ? q.a.rows * q.b.rows : 0;
+    return p;
+}
+
+}  // namespace
+
 hipError_t launch_fp8_few(const Fp8Product& q, hipStream_t s)
 {
-    Few p;
+    const int splits = fp8_few_splits(q.a.rows, q.b.rows, q.a.k);
     const bool b_few = q.b.rows <= q.a.rows;
-    p.big = b_few ? q.a : q.b;
-    p.few = b_few ? q.b : q.a;
-    p.x = nullptr;
-    p.ldx = 0;
-    p.c = q.c;
-    p.stride_big = b_few ? q.ldc : 1;
-    p.stride_few = b_few ? 1 : q.ldc;
-    p.c_dtype = q.c_dtype;
-    p.accumulate = q.accumulate;
-    return q.short_sums ? launch_formats<false>(p, s) : launch_formats<true>(p, s);
+    const Few p = b_few ? few_of(q, q.a, q.b, true, splits) : few_of(q, q.b, q.a, false, splits);
+    const hipError_t e = q.short_sums ? launch_formats<false>(p, s) : launch_formats<true>(p, s);
+    return e == hipSuccess && splits > 1 ? launch_fp8_join(q, splits, s) : e;
 }
 
 hipError_t launch_fp8_linear_few(const void* x, int64_t ldx, const Fp8Product& q, hipStream_t s)
 {
-    const Few p{q.b, q.a, x, ldx, q.c, 1, q.ldc, q.c_dtype, 0};
-    if (q.c_dtype == DTYPE_F32) return launch_fused<float, true>(p, s);
-    if (q.short_sums) return q.c_dtype == DTYPE_BF16 ? launch_fused<bf16, false>(p, s) : launch_fused<f16, false>(p, s);
-    return q.c_dtype == DTYPE_BF16 ? launch_fused<bf16, true>(p, s) : launch_fused<f16, true>(p, s);
+    const int splits = fp8_few_splits(q.a.rows, q.b.rows, q.a.k);
+    Few p = few_of(q, q.b, q.a, false, splits);
+    p.x = x;
+    p.ldx = ldx;
+    hipError_t e;
+    if (q.c_dtype == DTYPE_F32) e = launch_fused<float, true>(p, s);
+    else if (q.c_dtype == DTYPE_BF16) e = q.short_sums ? launch_fused<bf16, false>(p, s) : launch_fused<bf16, true>(p, s);
+    else e = q.short_sums ? launch_fused<f16, false>(p, s) : launch_fused<f16, true>(p, s);
+    return e == hipSuccess && splits > 1 ? launch_fp8_join(q, splits, s) : e;
 }
 
 }  // namespace fasgd

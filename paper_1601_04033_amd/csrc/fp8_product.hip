@@ -405,16 +405,6 @@ template <typename T> __global__ __launch_bounds__(256) void join(Fp8Product p, 
     }
 }
 
-hipError_t launch_join(const Fp8Product& p, int splits, hipStream_t s)
-{
-    const int64_t quads = (p.a.rows * p.b.rows + 3) / 4;
-    const unsigned blocks = static_cast<unsigned>((quads + 255) / 256 < kLaunchBlocks ? (quads + 255) / 256 : kLaunchBlocks);
-    if (p.c_dtype == DTYPE_F32) join<float><<<blocks, 256, 0, s>>>(p, splits);
-    else if (p.c_dtype == DTYPE_BF16) join<bf16><<<blocks, 256, 0, s>>>(p, splits);
-    else join<f16><<<blocks, 256, 0, s>>>(p, splits);
-    return hipGetLastError();
-}
-
 enum Shape { k256, k192, k128, k64Rows, k64Cols };  // block tiles 256 x 256, 192 x 192, 128 x 128, 64 x 256, 256 x 64
 struct Plan {
     Shape shape;
@@ -510,20 +500,34 @@ template <int FA, int FB> hipError_t launch_formats(const Fp8Product& p, const P
 
 }  // namespace
 
+hipError_t launch_fp8_join(const Fp8Product& p, int splits, hipStream_t s)
+{
+    const int64_t quads = (p.a.rows * p.b.rows + 3) / 4;
+    const unsigned blocks = static_cast<unsigned>((quads + 255) / 256 < kLaunchBlocks ? (quads + 255) / 256 : kLaunchBlocks);
+    if (p.c_dtype == DTYPE_F32) join<float><<<blocks, 256, 0, s>>>(p, splits);
+    else if (p.c_dtype == DTYPE_BF16) join<bf16><<<blocks, 256, 0, s>>>(p, splits);
+    else join<f16><<<blocks, 256, 0, s>>>(p, splits);
+    return hipGetLastError();
+}
+
 size_t fp8_workspace_bytes(int64_t m, int64_t n, int64_t k)
 {
-    if (m < 1 || n < 1 || k < 1 || fp8_few(m, n, k)) return 0;
+    if (m < 1 || n < 1 || k < 1) return 0;
     int splits = 1;
-    for (const bool wide : {false, true}) {
-        const int planned = plan_of(m, n, k, wide).g.splits;
-        if (planned > splits) splits = planned;
+    if (fp8_few(m, n, k)) {
+        splits = fp8_few_splits(m, n, k);
+    } else {
+        for (const bool wide : {false, true}) {
+            const int planned = plan_of(m, n, k, wide).g.splits;
+            if (planned > splits) splits = planned;
+        }
     }
     return splits > 1 ? sizeof(float) * static_cast<size_t>(splits) * static_cast<size_t>(m) * static_cast<size_t>(n) : 0;
 }
 
 hipError_t launch_fp8_product(const Fp8Product& p, hipStream_t s)
 {
-    if (p.a.k == 0) return launch_join(p, 0, s);
+    if (p.a.k == 0) return launch_fp8_join(p, 0, s);
     if (fp8_few(p.a.rows, p.b.rows, p.a.k)) return launch_fp8_few(p, s);
     const Plan plan = plan_of(p.a.rows, p.b.rows, p.a.k, !p.short_sums);
     hipError_t e;
@@ -531,7 +535,7 @@ hipError_t launch_fp8_product(const Fp8Product& p, hipStream_t s)
         e = p.b.format == FP8_E4M3 ? launch_formats<0, 0>(p, plan, s) : launch_formats<0, 1>(p, plan, s);
     else
         e = p.b.format == FP8_E4M3 ? launch_formats<1, 0>(p, plan, s) : launch_formats<1, 1>(p, plan, s);
-    if (e == hipSuccess && plan.g.splits > 1) e = launch_join(p, plan.g.splits, s);
+    if (e == hipSuccess && plan.g.splits > 1) e = launch_fp8_join(p, plan.g.splits, s);
     return e;
 }
 

@@ -43,3 +43,11 @@ def test_short_sums_are_of_16_bit_outputs(lib):
     for dtype in (0x101, 0x102):        # as far as the next check
         assert lib.client_fp8_matmul(ref, ref, P, 3, dtype, 0, P, 1 << 20, None) == ARG
         assert b"row stride" in lib.fasgd_last_error()
+
+
+@pytest.mark.parametrize("m, n, k", [(10, 1000, 65_536), (1000, 10, 65_536), (16, 16, 2 ** 20), (1, 256, 16_384)])
+def test_long_contractions_of_few_outputs_are_split(lib, m, n, k):
+    """Where 16 rows a block leave most of the 256 CUs idle, the workspace has room for parts of the contraction."""
+    x = m * k + k // 128 * m
+    assert fa.client_fp8_workspace_bytes(m, n, k) - x >= 4 * 4 * m * n
+    assert fa.client_fp8_workspace_bytes(16, 9000, k) - 16 * k - k // 128 * 16 < 4 * 4 * 16 * 9000
