@@ -348,6 +348,8 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void product(Fp8Product 
     scales(0, 0);
     load(1, a1, b1);
     scales(1, 1);
+    // every wave's part of the first stage has arrived
+    __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0)
     __syncthreads();
     read(frag[0], a0, b0, 0);
     if constexpr (WIDE) widen_half<FA, FB, N>(wide[0], frag[0], 0, xa[0], xb[0]);
