@@ -60,6 +60,12 @@ template <int LANES> __device__ __forceinline__ Pair across(float x)
     return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 
+// x of the lane that CTRL (a data-parallel primitive's code) names.
+template <int CTRL> __device__ __forceinline__ float dpp(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+
 // Key and counter words of one dropout (include/fasgd_client.h).
 struct DropKey {
     uint32_t key0, key1;        // seed low / high words

@@ -57,18 +57,13 @@ template <int FORMAT> __device__ __forceinline__ uint32_t pack4(float x0, float 
     return static_cast<uint32_t>(v);
 }
 
-// Where a lane's neighbours `CTRL` away stand (data-parallel primitives).
-template <int CTRL> __device__ __forceinline__ float dpp_move(float x)
-{
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
-}
 // Largest value of each group of 16 lanes, in all of them.
 __device__ __forceinline__ float max_of_16(float x)
 {
-    x = fmaxf(x, dpp_move<0xB1>(x));    // quad_perm 1 0 3 2
-    x = fmaxf(x, dpp_move<0x4E>(x));    // quad_perm 2 3 0 1
-    x = fmaxf(x, dpp_move<0x141>(x));   // row_half_mirror
-    return fmaxf(x, dpp_move<0x140>(x));    // row_mirror
+    x = fmaxf(x, dpp<0xB1>(x));    // quad_perm 1 0 3 2
+    x = fmaxf(x, dpp<0x4E>(x));    // quad_perm 2 3 0 1
+    x = fmaxf(x, dpp<0x141>(x));   // row_half_mirror
+    return fmaxf(x, dpp<0x140>(x));    // row_mirror
 }
 
 #if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources

@@ -46,11 +46,6 @@ template <typename T> constexpr int kVecs = kCols / kVec<T>;
 
 // ---- sums over the lanes of a row
 
-template <int CTRL> __device__ __forceinline__ float dpp(float x)
-{
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
-}
-
 // Sum over groups of LANES consecutive lanes, in every lane of the group.
 template <int LANES> __device__ __forceinline__ float lane_sum(float x)
 {
