@@ -2,7 +2,7 @@
 //
 // Bound by memory: one read and one write an element, and the ten rounds of
 // Philox for each 8 elements fit beside them.  16,384 x 4,096: fp16 41 us, 6.6
-// TB/s; bf16 with a residual 68 us, 5.9 TB/s.
+// TB/s; bf16 with a residual 70 us, 5.7 TB/s.
 #include "client_kernels.hpp"
 
 namespace fasgd {

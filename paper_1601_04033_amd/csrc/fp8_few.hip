@@ -10,9 +10,9 @@
 // through LDS, so one launch writes the result, unless the larger operand's
 // rows are too few for the CUs and long: then blocks take parts of the
 // contraction, joined in order by a second launch.  1 x 4,096 x 16,384 (67 MB):
-// 15.3 us, 4.4 TB/s, of which about 4 are the launch and x's quantization; 1 x
-// 14,592 x 12,032 (176 MB): 34 us, 5.2 TB/s;
-// 128 x 784 x 1,000: 3.7 us.
+// 17.2 us, 3.9 TB/s, with weights that are in no cache (a ring of layers), 15.8
+// where one layer follows itself, of which about 4 are the launch and x's
+// quantization; 1 x 14,592 x 12,032 (176 MB): 39 and 34 us, 4.5 and 5.1 TB/s.
 // Few unquantized activations (128 blocks of 128) are quantized on the way:
 // every block does it again, into LDS, while its first loads of the larger
 // operand are under way, which costs less than a launch before this one.
@@ -60,7 +60,8 @@ struct Rows {
           at((lane_ & 15) * static_cast<uint32_t>(v.ld) + (lane_ >> 4) * 16), lane(lane_)
     {
     }
-    // (Non-temporal loads were slower: 1 x 14,592 x 12,032 46 against 34 us.)
+    // (Non-temporal loads were slower, with the weights in the last-level cache
+    // and in none: 1 x 14,592 x 12,032 46 against 34 and 48 against 39 us.)
     __device__ v8i read(int tile, int kb, bool in) const
     {
         const uint32_t p = in ? at + tile * 16 * ld : kOutside;

@@ -17,10 +17,10 @@
 //     about 3e-5 of c's size, a hundredth of c's rounding to bf16 and a
 //     seventh of fp16's.
 //
-// Bound by the matrix instructions where tiles fill the chip: 8,192 x 8,192 x
-// 4,096 in 411 us (full sums, 1,340 TFLOP/s, where the library's bf16 product
-// reaches 1,450 at 8,192^3) and 219 us (short sums, 2,510, its 8-bit product
-// 2,970).  Below, by whole rounds of tiles and about 8 us of launch, first
+// Bound by the matrix instructions where tiles fill the chip: 8,192^3 with
+// bf16 outputs in 746 us (full sums, 1,470 TFLOP/s; the library's bf16 product
+// 1,450) and 377 us (short sums, 2,920; the library's 8-bit product 2,970); fp32
+// outputs 780 us.  Below, by whole rounds of tiles and about 8 us of launch, first
 // loads and last stores.
 #include "fp8_math.hpp"
 
@@ -165,7 +165,7 @@ template <int N> __device__ __forceinline__ void take_row(const v16f (&acc)[N], 
 // stride ld): each lane N neighbouring columns at once, at any alignment.
 // WHOLE: all of them lie in c, and c is not added to.  Otherwise a lane that
 // c's last column cuts through stores its columns one by one.  (The checks
-// cost 2 us of a 4,096 x 4,096 x 1,024 product's 22.)
+// cost 2 us of a 4,096 x 4,096 x 1,024 product's 22 with short sums.)
 template <typename T, int W, int N, bool WHOLE>
 __device__ __forceinline__ void write_tiles(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
                                               int64_t m, int64_t n, bool add, int lane)
@@ -413,14 +413,15 @@ struct Plan {
     Grid g;
 };
 
-// Microseconds of a square tile's blocks, measured at 8,192 x 8,192 x 4,096
-// and where one round of blocks or less is all there is: of a stage with as
-// many blocks on a CU as fit (of 128 x 128 two, of the others one), of a
-// stage of a 128 x 128 tile alone on its CU, and of what a tile costs besides
-// its stages.  The larger tile has the higher rate (8,192 x 8,192 x 4,096:
-// 245, 333 and 267 us with 256, 192 and 128), the smaller ones waste less of
-// a product's edges and of the last round (4,099 x 2,002 x 5,003: 70, 57 and
-// 72 us; 2,500 x 2,500 x 2,500: 39, 35 and 24).
+// Microseconds of a square tile's blocks: of a stage with as many blocks on a
+// CU as fit (of 128 x 128 two, of the others one), of a stage of a 128 x 128
+// tile alone on its CU, and of what a tile costs besides its stages.  The
+// choice goes by their ratios: 8,192 x 8,192 x 4,096 takes a sixth less than
+// they say with all three.  The larger tile has the higher rate (there 205, 322
+// and 247 us with 256, 192 and 128, short sums; 390, 524 and 440 with full
+// ones), the smaller ones waste less of a product's edges and of the last round
+// (4,099 x 2,002 x 5,003: 65, 55 and 70, full 116, 88 and 110; 2,500 x 2,500 x
+// 2,500: 38, 33 and 23, full 51, 49 and 36).
 struct Rate {
     Shape shape;
     int side;

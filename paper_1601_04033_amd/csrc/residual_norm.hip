@@ -18,9 +18,9 @@
 // registers, written once per block and joined in a fixed order by a second
 // small kernel.
 //
-// Measured at 16,384 x 4,096 bf16, rms, channel gate, dropout: forward 111 us
-// (4.8 TB/s; 103 without dropout), backward 160 us (6 matrices: 5.0 TB/s),
-// column sums 6 us; fp32 forward 201 us (5.3 TB/s).  The vector unit is busy
+// Measured at 16,384 x 4,096 bf16, rms, channel gate, dropout: forward 109 us
+// (4.9 TB/s; 103 without dropout), backward 157 us (6 matrices: 5.1 TB/s),
+// column sums 6 us; fp32 205 and 313 us (5.2 TB/s).  The vector unit is busy
 // two thirds of the forward pass.  Biases and full gates cost most (2,053 x
 // 5,003 fp16: 59 and 77 us): their registers leave room for two rows a CU
 // forward and one backward, too few to hide a row's reductions.

@@ -152,3 +152,26 @@ def test_short_sums_are_refused_for_fp32_and_marshalled_alike(both):  # noqa: F8
         assert not out.any()
         return [y, z]
     _same(both(f))
+
+
+@pytest.mark.parametrize("dtype", SIXTEEN[:1] + ["float32"])
+@pytest.mark.parametrize("m, n, k", [(1, 40, 128), (3, 100, 3000), (27, 4100, 300), (300, 513, 640)])
+def test_values_below_the_normal_range(dtype, m, n, k):
+    """Powers of two from 2^-133 on in blocks of the smallest scale, beside values near 2^-117: held, and counted."""
+    import torch
+    gpu()
+    g = torch.Generator(device="cuda").manual_seed(m + n + k)
+    a, b = fa.client_fp8_operand(m, k), fa.client_fp8_operand(n, k)
+    x = torch.zeros(m, k, device="cuda")
+    x[:, 5] = 1.0
+    fa.client_fp8_quantize(x, a)
+    a.scales[:, :m] = 127 + 96
+    q = torch.exp2(torch.randint(-7, 9, (n, k), device="cuda", generator=g).float())
+    b.data.zero_()
+    b.data[:, :k] = q.to(torch.float8_e4m3fn).view(torch.uint8)
+    b.scales.fill_(1)
+    want = (_held(a)[0] @ _held(b)[0].T)
+    out = torch.full((m, n), 7.0, device="cuda", dtype=getattr(torch, dtype))
+    ws = torch.empty(fa.client_fp8_workspace_bytes(m, n, k), device="cuda", dtype=torch.uint8).fill_(255)
+    fa.client_fp8_matmul(a, b, out, workspace=ws)
+    assert np.array_equal(out.double().cpu().numpy(), want)
