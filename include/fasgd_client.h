@@ -230,6 +230,88 @@ fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const clie
                                int64_t ldy, int32_t dtype, void* workspace, size_t workspace_bytes,
                                hipStream_t stream);
 
+/*
+ * Losses over a large vocabulary: where a client's gradient begins.
+ *   z_rj = logit_scale x_r . w_j,  lse_r = log sum_j exp z_rj,
+ *   p_rj = exp(z_rj - lse_r)
+ * for activations x [rows][cols] and class weights w [vocab][cols] of one
+ * dtype.  The logits are never kept: the forward pass keeps statistics of
+ * them, the backward pass computes them again for a piece of the vocabulary
+ * at a time.  Sums, statistics and losses are fp32; fp32 activations and
+ * weights go into the matrix products as three bf16 terms each (24 bits).
+ * A row that is left out costs nothing, its results are 0, and what it holds
+ * reaches no result, be it NaN.
+ * rows <= 2^20, cols in [1, 2^16], vocab in [1, 2^30]; logit_scale finite, > 0.
+ */
+typedef struct client_vocab_head {
+    int64_t rows, cols, vocab;
+    int32_t dtype;              /* client_dtype of x and w */
+    float logit_scale;
+    const void* x;
+    int64_t ld_x;
+    const void* w;
+    int64_t ld_w;
+} client_vocab_head;
+
+/*
+ * Device scratch of the calls below, 16-byte aligned, contents irrelevant:
+ * for a forward call, or (backward != 0) for a backward one.  Calls that may
+ * overlap need one each.  0 for sizes out of range.
+ */
+size_t client_vocab_workspace_bytes(int64_t rows, int64_t cols, int64_t vocab, int32_t dtype, int32_t backward);
+
+/*
+ * Softmax cross entropy.  With a row's target t:
+ *   loss_r = lse_r - (1 - smoothing) z_rt - smoothing / vocab sum_j z_rj
+ *            + z_loss lse_r^2
+ * loss, lse and picked (z_rt; the backward pass reads the last two) are fp32
+ * [rows].  A target outside [0, vocab) leaves its row out.
+ */
+fasgd_status client_vocab_loss_forward(const client_vocab_head* op, const int64_t* targets, float smoothing, float z_loss,
+                                       float* loss, float* lse, float* picked, void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream);
+
+/*
+ * The gradients of sum_r grad_scale dloss_r loss_r (dloss fp32 [rows], NULL:
+ * ones):
+ *   dz_rj = grad_scale dloss_r ((1 + 2 z_loss lse_r) p_rj - smoothing / vocab
+ *                               - (1 - smoothing) [j = t])
+ *   dx = logit_scale dz w (dtype),  dw = logit_scale dz^T x (dw_dtype:
+ *   CLIENT_F32 or dtype; accumulate != 0: added to what dw holds).
+ * Either may be NULL.  dx may not be x, nor dw be w.  In the products dz has
+ * 16 bits (bf16; fp16 22) for an fp32 dw, and the type's own precision for a
+ * dx or dw of 16 bits, but for its entries at the targets, which dx takes in
+ * fp32.  Sums are taken in a fixed order.
+ */
+fasgd_status client_vocab_loss_backward(const client_vocab_head* op, const int64_t* targets, float smoothing, float z_loss,
+                                        const float* lse, const float* picked, const float* dloss, float grad_scale,
+                                        void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, int32_t dw_dtype,
+                                        int32_t accumulate, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Distillation from a teacher's top logits.  Each row has `entries` (1 to
+ * 1024) classes, index [rows][entries], with the teacher's logits, teacher
+ * [rows][entries] of dtype.  An entry whose class is outside [0, vocab) or
+ * whose logit is -infinity is left out; a row without entries is left out.
+ *   q_k = exp(teacher_scale teacher_k - teacher_lse_r), or, with teacher_lse
+ *   NULL, the softmax of teacher_scale teacher_k over the row's entries
+ *   loss_r = sum_k q_k (log q_k - z_{r, index_k} + lse_r)
+ *   dz_rj  = grad_scale dloss_r (p_rj sum_k q_k - sum_{k: index_k = j} q_k)
+ * picked, fp32 [rows][entries], is z at the entries.  A temperature T is
+ * logit_scale = teacher_scale = 1 / T.  The rest is as above; a class may
+ * stand in a row more than once.
+ */
+fasgd_status client_vocab_distill_forward(const client_vocab_head* op, const int64_t* index, const void* teacher,
+                                          int32_t entries, float teacher_scale, const float* teacher_lse, float* loss,
+                                          float* lse, float* picked, void* workspace, size_t workspace_bytes,
+                                          hipStream_t stream);
+fasgd_status client_vocab_distill_backward(const client_vocab_head* op, const int64_t* index, const void* teacher,
+                                           int32_t entries, float teacher_scale, const float* teacher_lse,
+                                           const float* lse, const float* picked, const float* dloss, float grad_scale,
+                                           void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, int32_t dw_dtype,
+                                           int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                           hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -680,4 +680,6 @@ from .client import (CLIENT_ABI_FUNCTIONS, FP8_E4M3, FP8_E5M2, GATE_IDENTITY, GA
                      GATE_TANH, NORM_LAYER, NORM_RMS, Fp8Operand, client_dropout, client_fp8_linear,
                      client_fp8_matmul, client_fp8_operand, client_fp8_quantize, client_fp8_workspace_bytes,
                      client_residual_norm_backward, client_residual_norm_forward,
-                     client_residual_norm_workspace_bytes)
+                     client_residual_norm_workspace_bytes,
+                     client_vocab_distill_backward, client_vocab_distill_forward, client_vocab_head,
+                     client_vocab_loss_backward, client_vocab_loss_forward, client_vocab_workspace_bytes)

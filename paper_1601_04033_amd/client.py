@@ -1,6 +1,7 @@
 """Binding of the client's operators (include/fasgd_client.h): dropout, the
 residual norm between blocks and 8-bit matrix products, with which a client of
-the parameter server turns a fetched theta into its gradient.
+the parameter server turns a fetched theta into its gradient, and the losses over
+a large vocabulary where that gradient begins.
 
 Argument marshalling only, as in the package's __init__ (which re-exports
 these names): every step runs in the HIP kernels of libfasgd.so, there is no
@@ -17,7 +18,9 @@ import ctypes
 # every function include/fasgd_client.h declares
 CLIENT_ABI_FUNCTIONS = ("client_dropout", "client_residual_norm_workspace_bytes", "client_residual_norm_forward",
                         "client_residual_norm_backward", "client_fp8_workspace_bytes", "client_fp8_quantize",
-                        "client_fp8_matmul", "client_fp8_linear")
+                        "client_fp8_matmul", "client_fp8_linear", "client_vocab_workspace_bytes",
+                        "client_vocab_loss_forward", "client_vocab_loss_backward", "client_vocab_distill_forward",
+                        "client_vocab_distill_backward")
 
 FP8_E4M3 = 0
 FP8_E5M2 = 1
@@ -49,6 +52,13 @@ class client_fp8_operand_struct(ctypes.Structure):
                 ("k", ctypes.c_int64), ("ld", ctypes.c_int64), ("lds", ctypes.c_int64), ("format", ctypes.c_int32)]
 
 
+class client_vocab_head(ctypes.Structure):
+    """Mirror of the C struct client_vocab_head."""
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("logit_scale", ctypes.c_float), ("x", ctypes.c_void_p),
+                ("ld_x", ctypes.c_int64), ("w", ctypes.c_void_p), ("ld_w", ctypes.c_int64)]
+
+
 _DTYPES = None
 _lib = None
 
@@ -77,6 +87,14 @@ def bind(lib):
     lib.client_fp8_quantize.argtypes = [P, i64, i64, i64, i32, i32, O, O, P]
     lib.client_fp8_matmul.argtypes = [O, O, P, i64, i32, i32, P, sz, P]
     lib.client_fp8_linear.argtypes = [P, i64, i64, O, P, i64, i32, P, sz, P]
+    f = ctypes.c_float
+    H = ctypes.POINTER(client_vocab_head)
+    grads = [P, P, P, f, P, i64, P, i64, i32, i32, P, sz, P]
+    lib.client_vocab_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.client_vocab_loss_forward.argtypes = [H, P, f, f, P, P, P, P, sz, P]
+    lib.client_vocab_loss_backward.argtypes = [H, P, f, f, *grads]
+    lib.client_vocab_distill_forward.argtypes = [H, P, P, i32, f, P, P, P, P, P, sz, P]
+    lib.client_vocab_distill_backward.argtypes = [H, P, P, i32, f, P, *grads]
     for name in CLIENT_ABI_FUNCTIONS:
         getattr(lib, name).restype = sz if name.endswith("_bytes") else ctypes.c_int
     return lib
@@ -383,3 +401,125 @@ def client_fp8_linear(x, w: Fp8Operand, out, workspace=None, stream=None, short_
     pw, nw = _workspace(workspace)
     _check(_library().client_fp8_linear(px, ldx, m, ctypes.byref(w.c), py, ldy, _output_type(out, short_sums), pw, nw,
                                         _stream(stream)))
+
+
+def client_vocab_workspace_bytes(rows: int, cols: int, vocab: int, dtype, backward: bool = True) -> int:
+    """Bytes of workspace of the losses over a vocabulary, for activations [rows, cols] of a torch dtype: of a backward
+    call, or of a forward one."""
+    import torch
+    return int(_library().client_vocab_workspace_bytes(int(rows), int(cols), int(vocab),
+                                                       _dtype(torch.empty(0, dtype=dtype), "x"), 1 if backward else 0))
+
+
+def _indices(t, name, shape):
+    """Pointer of a contiguous int64 tensor."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype != torch.int64 or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous int64 tensor")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {shape}")
+    return t.data_ptr()
+
+
+def _head(x, w, logit_scale):
+    op = client_vocab_head()
+    op.x, op.ld_x = _matrix(x, "x")
+    op.w, op.ld_w = _matrix(w, "w")
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w must have two dimensions")
+    if w.dtype != x.dtype:
+        raise TypeError(f"w is {w.dtype}, expected {x.dtype}")
+    op.rows, op.cols = x.shape
+    op.vocab = w.shape[0]
+    if w.shape[1] != op.cols:
+        raise ValueError(f"x {tuple(x.shape)} does not fit weights {tuple(w.shape)}")
+    op.dtype, op.logit_scale = _dtype(x, "x"), logit_scale
+    return op
+
+
+def _gradients(x, w, dx, dw, dloss, grad_scale, accumulate):
+    import torch
+    px, lx = _optional(dx, "dx", x)
+    pw, lw, kind = None, 0, 0
+    if dw is not None:
+        if dw.dtype not in (torch.float32, w.dtype):
+            raise TypeError(f"dw is {dw.dtype}, expected float32 or {w.dtype}")
+        if dw.shape != w.shape:
+            raise ValueError(f"dw is {tuple(dw.shape)}, expected {tuple(w.shape)}")
+        pw, lw = _matrix(dw, "dw")
+        kind = _dtype(dw, "dw")
+    return _vector(dloss, "dloss", x.shape[0]), grad_scale, px, lx, pw, lw, kind, 1 if accumulate else 0
+
+
+def _teacher(x, index, teacher, teacher_lse):
+    import torch
+    if not isinstance(index, torch.Tensor) or index.dim() != 2:
+        raise ValueError("index must have two dimensions, [rows, entries]")
+    shape = (x.shape[0], index.shape[1])
+    pi = _indices(index, "index", shape)
+    _matrix(teacher, "teacher")
+    if teacher.dtype != x.dtype or not teacher.is_contiguous():
+        raise TypeError(f"teacher must be a contiguous {x.dtype} tensor")
+    if tuple(teacher.shape) != shape:
+        raise ValueError(f"teacher is {tuple(teacher.shape)}, expected {shape}")
+    return pi, teacher.data_ptr(), shape[1], _vector(teacher_lse, "teacher_lse", shape[0])
+
+
+def client_vocab_loss_forward(x, w, targets, loss, lse, picked, *, smoothing: float = 0.0, z_loss: float = 0.0,
+                              logit_scale: float = 1.0, workspace=None, stream=None) -> None:
+    """Softmax cross entropy of the logits logit_scale x w^T for x [rows, cols] and class weights w [vocab, cols]:
+    loss, lse and picked (the targets' logits), float32 [rows].  targets: int64 [rows]; one outside [0, vocab) leaves
+    its row out.  workspace: uint8, client_vocab_workspace_bytes(rows, cols, vocab, dtype, backward=False) bytes."""
+    op = _head(x, w, logit_scale)
+    n = op.rows
+    pw, nw = _workspace(workspace)
+    _check(_library().client_vocab_loss_forward(
+        ctypes.byref(op), _indices(targets, "targets", (n,)), smoothing, z_loss, _vector(loss, "loss", n),
+        _vector(lse, "lse", n), _vector(picked, "picked", n), pw, nw, _stream(stream)))
+
+
+def client_vocab_loss_backward(x, w, targets, lse, picked, dx, dw, *, dloss=None, grad_scale: float = 1.0,
+                               accumulate: bool = False, smoothing: float = 0.0, z_loss: float = 0.0,
+                               logit_scale: float = 1.0, workspace=None, stream=None) -> None:
+    """The gradients of sum(grad_scale dloss loss) (dloss float32 [rows] or None for ones) of
+    client_vocab_loss_forward (same keyword arguments, its lse and picked): dx like x or None, dw [vocab, cols] float32
+    or of w's dtype (accumulate: added to) or None.  workspace: client_vocab_workspace_bytes(rows, cols, vocab, dtype)
+    bytes."""
+    op = _head(x, w, logit_scale)
+    n = op.rows
+    pw, nw = _workspace(workspace)
+    _check(_library().client_vocab_loss_backward(
+        ctypes.byref(op), _indices(targets, "targets", (n,)), smoothing, z_loss, _vector(lse, "lse", n),
+        _vector(picked, "picked", n), *_gradients(x, w, dx, dw, dloss, grad_scale, accumulate), pw, nw,
+        _stream(stream)))
+
+
+def client_vocab_distill_forward(x, w, index, teacher, loss, lse, picked, *, teacher_scale: float = 1.0,
+                                 teacher_lse=None, logit_scale: float = 1.0, workspace=None, stream=None) -> None:
+    """Divergence from a teacher's top logits, teacher [rows, entries] of x's dtype at the classes index (int64), to
+    the softmax of logit_scale x w^T: loss and lse float32 [rows], picked float32 [rows, entries] (the logits at the
+    entries).  An entry outside [0, vocab) is left out.  teacher_lse: float32 [rows], the teacher's log-sum-exp over
+    its whole vocabulary; None takes the softmax of the row's entries.  workspace as client_vocab_loss_forward."""
+    op = _head(x, w, logit_scale)
+    n = op.rows
+    pi, pt, k, pl = _teacher(x, index, teacher, teacher_lse)
+    pw, nw = _workspace(workspace)
+    _check(_library().client_vocab_distill_forward(
+        ctypes.byref(op), pi, pt, k, teacher_scale, pl, _vector(loss, "loss", n), _vector(lse, "lse", n),
+        _vector(picked, "picked", n * k), pw, nw, _stream(stream)))
+
+
+def client_vocab_distill_backward(x, w, index, teacher, lse, picked, dx, dw, *, dloss=None, grad_scale: float = 1.0,
+                                  accumulate: bool = False, teacher_scale: float = 1.0, teacher_lse=None,
+                                  logit_scale: float = 1.0, workspace=None, stream=None) -> None:
+    """The gradients of client_vocab_distill_forward (same keyword arguments, its lse and picked), as
+    client_vocab_loss_backward gives them."""
+    op = _head(x, w, logit_scale)
+    n = op.rows
+    pi, pt, k, pl = _teacher(x, index, teacher, teacher_lse)
+    pw, nw = _workspace(workspace)
+    _check(_library().client_vocab_distill_backward(
+        ctypes.byref(op), pi, pt, k, teacher_scale, pl, _vector(lse, "lse", n), _vector(picked, "picked", n * k),
+        *_gradients(x, w, dx, dw, dloss, grad_scale, accumulate), pw, nw, _stream(stream)))

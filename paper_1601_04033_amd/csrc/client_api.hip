@@ -5,6 +5,7 @@
 
 #include "../../include/fasgd_client.h"
 #include "client_kernels.hpp"
+#include "vocab_kernels.hpp"
 #include "status.hpp"
 
 static_assert(CLIENT_F32 == fasgd::DTYPE_F32 && CLIENT_BF16 == fasgd::DTYPE_BF16 && CLIENT_F16 == fasgd::DTYPE_F16,
@@ -128,6 +129,10 @@ constexpr int64_t kMaxK = int64_t(1) << 23;    // of an operand: 256 rows of it 
 
 constexpr int64_t kMaxOperandRows = int64_t(1) << 27;   // every product's launch stays below 2^32 threads
 
+constexpr int64_t kMaxVocabRows = int64_t(1) << 20;     // 256 rows of any operand stay within 32-bit offsets
+constexpr int64_t kMaxVocabCols = int64_t(1) << 16;
+constexpr int64_t kMaxVocab = int64_t(1) << 30;
+
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // An 8-bit operand; its arrays are needed where it holds anything.
@@ -176,6 +181,119 @@ fasgd_status take_short_sums(int32_t& dtype, int32_t& short_sums)
 size_t linear_operand_bytes(int64_t m, int64_t k)
 {
     return static_cast<size_t>(round_up(m * round_up(k, 128) + round_up(k, 128) / 128 * round_up(m, 4), 256));
+}
+
+// What the losses over a vocabulary share.
+fasgd_status vocab_setup(const client_vocab_head* op, fasgd::VocabArgs& a)
+{
+    memset(&a, 0, sizeof a);
+    if (!op) return fail(FASGD_ERR_NULL, "the head's description is NULL");
+    if (op->dtype != CLIENT_F32 && op->dtype != CLIENT_BF16 && op->dtype != CLIENT_F16)
+        return fail(FASGD_ERR_ARG, "dtype = %d is not a client_dtype value", op->dtype);
+    if (op->rows < 0 || op->rows > kMaxVocabRows)
+        return fail(FASGD_ERR_ARG, "rows = %lld is not in [0, 2^20]", (long long)op->rows);
+    if (op->cols < 1 || op->cols > kMaxVocabCols)
+        return fail(FASGD_ERR_ARG, "cols = %lld is not in [1, 2^16]", (long long)op->cols);
+    if (op->vocab < 1 || op->vocab > kMaxVocab)
+        return fail(FASGD_ERR_ARG, "vocab = %lld is not in [1, 2^30]", (long long)op->vocab);
+    FASGD_TRY(check_shape(op->vocab, op->cols, op->dtype));
+    if (!(isfinite(op->logit_scale) && op->logit_scale > 0.0f)) return fail(FASGD_ERR_ARG, "logit_scale must be finite and > 0");
+    a.rows = op->rows;
+    a.cols = op->cols;
+    a.vocab = op->vocab;
+    a.dtype = op->dtype;
+    a.scale = op->logit_scale;
+    a.x = op->x;
+    a.w = op->w;
+    a.ldx = op->ld_x;
+    a.ldw = op->ld_w;
+    return FASGD_OK;
+}
+
+fasgd_status vocab_inputs(const fasgd::VocabArgs& a, const char* index, const float* lse, const float* picked)
+{
+    FASGD_TRY(check_matrix("x", a.x, a.ldx, a.rows, a.cols, a.dtype));
+    FASGD_TRY(check_matrix("w", a.w, a.ldw, a.vocab, a.cols, a.dtype));
+    if (!a.index) return fail(FASGD_ERR_NULL, "%s is NULL", index);
+    if (!aligned(a.index, 8)) return fail(FASGD_ERR_ALIGN, "%s is not 8-byte aligned", index);
+    FASGD_TRY(check_vector("lse", lse, true));
+    return check_vector("picked", picked, true);
+}
+
+fasgd_status vocab_smoothing(fasgd::VocabArgs& a, float smoothing, float z_loss)
+{
+    if (!(smoothing >= 0.0f && smoothing <= 1.0f)) return fail(FASGD_ERR_ARG, "smoothing must be in [0, 1]");
+    if (!isfinite(z_loss)) return fail(FASGD_ERR_ARG, "z_loss must be finite");
+    a.entries = 1;
+    a.smoothing = smoothing;
+    a.z_loss = z_loss;
+    return FASGD_OK;
+}
+
+fasgd_status vocab_teacher(fasgd::VocabArgs& a, int32_t entries, float teacher_scale)
+{
+    if (entries < 1 || entries > fasgd::kMostEntries)
+        return fail(FASGD_ERR_ARG, "entries = %d is not in [1, %d]", entries, fasgd::kMostEntries);
+    if (!(isfinite(teacher_scale) && teacher_scale > 0.0f)) return fail(FASGD_ERR_ARG, "teacher_scale must be finite and > 0");
+    a.entries = entries;
+    a.teacher_scale = teacher_scale;
+    return FASGD_OK;
+}
+
+fasgd_status vocab_teacher_inputs(const fasgd::VocabArgs& a)
+{
+    if (!a.teacher) return fail(FASGD_ERR_NULL, "teacher is NULL");
+    if (!aligned(a.teacher, fasgd::dtype_size(a.dtype)))
+        return fail(FASGD_ERR_ALIGN, "teacher is not %zu-byte aligned", fasgd::dtype_size(a.dtype));
+    return check_vector("teacher_lse", a.teacher_lse, false);
+}
+
+fasgd_status vocab_forward(fasgd::VocabArgs& a, float* loss, float* lse, float* picked, void* workspace, size_t bytes,
+                           hipStream_t stream, const char* name)
+{
+    FASGD_TRY(check_vector("loss", loss, true));
+    FASGD_TRY(check_workspace(workspace, bytes, fasgd::vocab_workspace_bytes(a.rows, a.cols, a.vocab, a.dtype, false)));
+    a.loss = loss;
+    a.lse = lse;
+    a.picked = picked;
+    a.workspace = workspace;
+    const hipError_t e = fasgd::launch_vocab_forward(a, stream);
+    if (e != hipSuccess) return hip_fail(e, name);
+    return ok();
+}
+
+fasgd_status vocab_gradients(fasgd::VocabArgs& a, const float* dloss, float grad_scale, void* dx, int64_t ld_dx, void* dw,
+                             int64_t ld_dw, int32_t dw_dtype, int32_t accumulate)
+{
+    if (!isfinite(grad_scale)) return fail(FASGD_ERR_ARG, "grad_scale must be finite");
+    if (dw_dtype != CLIENT_F32 && dw_dtype != a.dtype)
+        return fail(FASGD_ERR_ARG, "dw_dtype = %d is neither CLIENT_F32 nor dtype = %d", dw_dtype, a.dtype);
+    if (dw) FASGD_TRY(check_matrix("dw", dw, ld_dw, a.vocab, a.cols, dw_dtype));
+    if (dx && a.rows > 0) FASGD_TRY(check_matrix("dx", dx, ld_dx, a.rows, a.cols, a.dtype));
+    FASGD_TRY(check_vector("dloss", dloss, false));
+    a.dloss = dloss;
+    a.grad_scale = grad_scale;
+    a.dx = dx;
+    a.dw = dw;
+    a.lddx = ld_dx;
+    a.lddw = ld_dw;
+    a.dw_dtype = dw_dtype;
+    a.accumulate = accumulate != 0;
+    return FASGD_OK;
+}
+
+fasgd_status vocab_backward(fasgd::VocabArgs& a, const float* lse, const float* picked, void* workspace, size_t bytes,
+                            hipStream_t stream, const char* name)
+{
+    if (!a.dx && !a.dw) return ok();
+    if (a.rows > 0)
+        FASGD_TRY(check_workspace(workspace, bytes, fasgd::vocab_workspace_bytes(a.rows, a.cols, a.vocab, a.dtype, true)));
+    a.lse = const_cast<float*>(lse);
+    a.picked = const_cast<float*>(picked);
+    a.workspace = workspace;
+    const hipError_t e = fasgd::launch_vocab_backward(a, stream);
+    if (e != hipSuccess) return hip_fail(e, name);
+    return ok();
 }
 
 }  // namespace
@@ -405,6 +523,79 @@ fasgd_status client_fp8_linear(const void* x, int64_t ldx, int64_t m, const clie
     if (e == hipSuccess && !few) e = fasgd::launch_fp8_product(p, stream);
     if (e != hipSuccess) return hip_fail(e, "client_fp8_linear");
     return ok();
+}
+
+size_t client_vocab_workspace_bytes(int64_t rows, int64_t cols, int64_t vocab, int32_t dtype, int32_t backward)
+{
+    if (rows < 1 || rows > kMaxVocabRows || cols < 1 || cols > kMaxVocabCols || vocab < 1 || vocab > kMaxVocab ||
+        dtype < CLIENT_F32 || dtype > CLIENT_F16)
+        return 0;
+    return fasgd::vocab_workspace_bytes(rows, cols, vocab, dtype, backward != 0);
+}
+
+fasgd_status client_vocab_loss_forward(const client_vocab_head* op, const int64_t* targets, float smoothing, float z_loss,
+                                       float* loss, float* lse, float* picked, void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream)
+{
+    fasgd::VocabArgs a;
+    FASGD_TRY(vocab_setup(op, a));
+    FASGD_TRY(vocab_smoothing(a, smoothing, z_loss));
+    if (a.rows == 0) return ok();
+    a.index = targets;
+    FASGD_TRY(vocab_inputs(a, "targets", lse, picked));
+    return vocab_forward(a, loss, lse, picked, workspace, workspace_bytes, stream, "client_vocab_loss_forward");
+}
+
+fasgd_status client_vocab_loss_backward(const client_vocab_head* op, const int64_t* targets, float smoothing, float z_loss,
+                                        const float* lse, const float* picked, const float* dloss, float grad_scale,
+                                        void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, int32_t dw_dtype,
+                                        int32_t accumulate, void* workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    fasgd::VocabArgs a;
+    FASGD_TRY(vocab_setup(op, a));
+    FASGD_TRY(vocab_smoothing(a, smoothing, z_loss));
+    FASGD_TRY(vocab_gradients(a, dloss, grad_scale, dx, ld_dx, dw, ld_dw, dw_dtype, accumulate));
+    a.index = targets;
+    if (a.rows > 0) FASGD_TRY(vocab_inputs(a, "targets", lse, picked));
+    return vocab_backward(a, lse, picked, workspace, workspace_bytes, stream, "client_vocab_loss_backward");
+}
+
+fasgd_status client_vocab_distill_forward(const client_vocab_head* op, const int64_t* index, const void* teacher,
+                                          int32_t entries, float teacher_scale, const float* teacher_lse, float* loss,
+                                          float* lse, float* picked, void* workspace, size_t workspace_bytes,
+                                          hipStream_t stream)
+{
+    fasgd::VocabArgs a;
+    FASGD_TRY(vocab_setup(op, a));
+    FASGD_TRY(vocab_teacher(a, entries, teacher_scale));
+    if (a.rows == 0) return ok();
+    a.index = index;
+    a.teacher = teacher;
+    a.teacher_lse = teacher_lse;
+    FASGD_TRY(vocab_inputs(a, "index", lse, picked));
+    FASGD_TRY(vocab_teacher_inputs(a));
+    return vocab_forward(a, loss, lse, picked, workspace, workspace_bytes, stream, "client_vocab_distill_forward");
+}
+
+fasgd_status client_vocab_distill_backward(const client_vocab_head* op, const int64_t* index, const void* teacher,
+                                           int32_t entries, float teacher_scale, const float* teacher_lse,
+                                           const float* lse, const float* picked, const float* dloss, float grad_scale,
+                                           void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, int32_t dw_dtype,
+                                           int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                           hipStream_t stream)
+{
+    fasgd::VocabArgs a;
+    FASGD_TRY(vocab_setup(op, a));
+    FASGD_TRY(vocab_teacher(a, entries, teacher_scale));
+    FASGD_TRY(vocab_gradients(a, dloss, grad_scale, dx, ld_dx, dw, ld_dw, dw_dtype, accumulate));
+    a.index = index;
+    a.teacher = teacher;
+    a.teacher_lse = teacher_lse;
+    if (a.rows > 0) {
+        FASGD_TRY(vocab_inputs(a, "index", lse, picked));
+        FASGD_TRY(vocab_teacher_inputs(a));
+    }
+    return vocab_backward(a, lse, picked, workspace, workspace_bytes, stream, "client_vocab_distill_backward");
 }
 
 }  // extern "C"

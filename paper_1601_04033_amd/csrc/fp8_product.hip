@@ -22,37 +22,15 @@
 // 1,450) and 377 us (short sums, 2,920; the library's 8-bit product 2,970); fp32
 // outputs 780 us.  Below, by whole rounds of tiles and about 8 us of launch, first
 // loads and last stores.
-#include "fp8_math.hpp"
+#include "tiles.hpp"
 
 namespace fasgd {
 namespace {
 
-constexpr int kThreads = 256;       // 4 waves
-constexpr int kBytes = kFp8Block;   // contraction per stage: one scale each way
+static_assert(kBytes == kFp8Block, "a stage holds one scale each way");
 constexpr int kMaxSplits = 16;
 
-// A wave owns W x W outputs as (W/32)^2 matrix tiles, and WM of the block's 4
-// waves stand along a's rows.  Row r of tile i is the wave's row
-// (W/32) r + i, so a lane's scales for its tiles are neighbouring bytes (one
-// load; the instruction picks the byte) and its outputs are neighbouring
-// columns.
-template <int W, int WM> struct Geometry {
-    static constexpr int kTiles = W / 32;
-    static constexpr int kWavesN = 4 / WM;
-    static constexpr int kRowsA = W * WM, kRowsB = W * kWavesN;             // block tile
-    static constexpr int kStageA = kRowsA * kBytes, kStageB = kRowsB * kBytes;  // LDS bytes of a stage
-    static constexpr int kLoadsA = kStageA / (kThreads * 16);               // 16-byte loads per thread
-    static constexpr int kLoadsB = kStageB / (kThreads * 16);
-};
-
 #if defined(__HIP_DEVICE_COMPILE__)     // the host pass does not know buffer resources
-
-// A stage in LDS: the rows that one read touches together, row r of tile i
-// for r = 0 .. 31, are neighbours, and the 16-byte chunk c of a row's 128
-// bytes lies in slot c ^ (r / 2 mod 8), so that 16 lanes meet in no bank.
-__device__ __forceinline__ int slot(int c, int r) { return c ^ (r >> 1 & 7); }
-
-typedef __attribute__((address_space(3))) void* lds_ptr;
 
 // A stage is worked through in sub-steps of 1,024 matrix cycles per wave (at
 // W = 128): 64 of the contraction with short sums, 32 with full ones.  A
@@ -124,20 +102,6 @@ template <int N> __device__ __forceinline__ void multiply_wide(v16f (&acc)[N][N]
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w.a[i], w.b[j], acc[i][j], 0, 0, 0);
 }
 
-// Orders of the instructions of a sub-step for the compiler's scheduler:
-// between two matrix instructions go one LDS read, the loads of the stage
-// after next, and the conversions of what is multiplied next.
-template <int MFMA, int READS, int LOADS, int VALU, int I = 0> __device__ __forceinline__ void interleave()
-{
-    constexpr int kMfma = 0x8, kDsRead = 0x100, kVmem = 0x20, kValu = 0x2;
-    constexpr int kReads = (I + 1) * READS / MFMA - I * READS / MFMA, kLoads = (I + 1) * LOADS / MFMA - I * LOADS / MFMA;
-    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-    if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(kDsRead, kReads, 0);
-    if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(kVmem, kLoads, 0);
-    if constexpr (VALU > 0) __builtin_amdgcn_sched_group_barrier(kValu, VALU / MFMA, 0);
-    if constexpr (I + 1 < MFMA) interleave<MFMA, READS, LOADS, VALU, I + 1>();
-}
-
 // A lane's N neighbouring scales, the first in byte 0.  p: as many bytes on,
 // but no further than 4 before the scales' end (N = 3: then `shift` bits before them).
 template <int N> __device__ __forceinline__ int load_scales(const uint8_t* p, int shift)
@@ -147,63 +111,6 @@ template <int N> __device__ __forceinline__ int load_scales(const uint8_t* p, in
     uint32_t x;
     __builtin_memcpy(&x, p, sizeof x);
     return static_cast<int>(x >> shift);
-}
-
-// One row of tiles in vector registers.  Accumulators stay in the accumulation
-// registers until here: without this the compiler wants all of them where
-// the conversions below can read them, and has no room.
-template <int N> __device__ __forceinline__ void take_row(const v16f (&acc)[N], v16f (&t)[N])
-{
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        t[j] = acc[j];
-        asm volatile("" : "+v"(t[j]));
-    }
-}
-
-// A wave's outputs to rows m on and columns n on of c ([rows][cols], row
-// stride ld): each lane N neighbouring columns at once, at any alignment.
-// WHOLE: all of them lie in c, and c is not added to.  Otherwise a lane that
-// c's last column cuts through stores its columns one by one.  (The checks
-// cost 2 us of a 4,096 x 4,096 x 1,024 product's 22 with short sums.)
-template <typename T, int W, int N, bool WHOLE>
-__device__ __forceinline__ void write_tiles(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
-                                              int64_t m, int64_t n, bool add, int lane)
-{
-    const int rows_left = static_cast<int>(rows - m < W ? rows - m : W) - 4 * N * (lane >> 5);
-    const int cols_left = static_cast<int>(cols - n < W ? cols - n : W) - N * (lane & 31);
-    T* base = c + (m + 4 * N * (lane >> 5)) * ld + n + N * (lane & 31);
-    const bool cut = __ballot(cols_left > 0 && cols_left < N) != 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v16f t[N];
-        take_row<N>(acc[i], t);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = (8 * (r >> 2) + (r & 3)) * N + i;
-            T* out = base + row * ld;
-            if (WHOLE || (row < rows_left && cols_left >= N)) {
-                Pack<T, N> x;
-                if (!WHOLE && add) x = load_pack<T, N>(out);
-#pragma unroll
-                for (int j = 0; j < N; ++j) x.v[j] = from_float<T>(!WHOLE && add ? to_float(x.v[j]) + t[j][r] : t[j][r]);
-                store_pack(out, x);
-            }
-            if (!WHOLE && cut && row < rows_left) {
-#pragma unroll
-                for (int j = 0; j + 1 < N; ++j)
-                    if (j < cols_left && cols_left < N) out[j] = from_float<T>(add ? to_float(out[j]) + t[j][r] : t[j][r]);
-            }
-        }
-    }
-}
-
-template <typename T, int W, int N>
-__device__ __forceinline__ void write_outputs(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
-                                              int64_t m, int64_t n, bool add, int lane)
-{
-    if (!add && m + W <= rows && n + W <= cols) write_tiles<T, W, N, true>(acc, c, ld, rows, cols, m, n, add, lane);
-    else write_tiles<T, W, N, false>(acc, c, ld, rows, cols, m, n, add, lane);
 }
 
 #endif
@@ -223,19 +130,9 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void product(Fp8Product 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_m = wave / G::kWavesN, wave_n = wave % G::kWavesN;
 
-    // Consecutive blocks go to the 8 XCDs in turn: give each XCD a run of
-    // tiles, 8 rows of tiles deep, so that its L2 serves their operands.
     const int tiles = g.tiles_m * g.tiles_n;
-    int id = blockIdx.x % tiles;
+    const int id = tile_of(blockIdx.x % tiles, g.tiles_m, g.tiles_n);
     const int split = blockIdx.x / tiles;
-    {
-        const int xcd = id & 7, each = tiles >> 3, extra = tiles & 7;
-        id = xcd * each + (xcd < extra ? xcd : extra) + (id >> 3);
-        const int deep = 8 * g.tiles_n, group = id / deep, first = group * 8;
-        const int rows = g.tiles_m - first < 8 ? g.tiles_m - first : 8;
-        const int in = id - group * deep;
-        id = (first + in % rows) * g.tiles_n + in / rows;
-    }
     const int64_t m0 = static_cast<int64_t>(id / g.tiles_n) * G::kRowsA, n0 = static_cast<int64_t>(id % g.tiles_n) * G::kRowsB;
     const int64_t blocks = (p.a.k + kBytes - 1) / kBytes;
     const int64_t kb0 = static_cast<int64_t>(split) * g.steps;

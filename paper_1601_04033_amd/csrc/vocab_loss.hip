@@ -1,0 +1,756 @@
+// The losses over a large vocabulary: softmax cross entropy and the divergence
+// from a teacher's top logits, forward and backward (include/fasgd_client.h).
+//
+// Rows that take part are gathered first, so that the others cost nothing and
+// whatever they hold reaches no result.  Forward, the logits' product keeps
+// statistics of its tiles alone (vocab_product.hip), which are joined here in
+// order.  Backward, a piece of the vocabulary at a time: its logits again, their
+// gradient dz as 16-bit terms in the workspace, then dz W, added up over the
+// pieces, and dz^T x, whole for the piece's classes.
+//
+// The entries that a row is held to (its target, a teacher's classes) are the
+// largest of dz, with p - q cancelling.  They are computed here from the
+// picked logits, put into dz^T in place of what the tile wrote, and left out
+// of dz: dx takes them in fp32, times the rows of W, at the end.
+#include <float.h>
+
+#include "vocab_kernels.hpp"
+
+namespace fasgd {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kWaves = kBlock / 64;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+__device__ __forceinline__ float wave_max(float x)
+{
+    for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+__device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---- entries
+
+__device__ __forceinline__ float teacher_logit(const VocabArgs& a, int64_t at)
+{
+    if (a.dtype == DTYPE_F32) return static_cast<const float*>(a.teacher)[at];
+    if (a.dtype == DTYPE_BF16) return to_float(static_cast<const bf16*>(a.teacher)[at]);
+    return to_float(static_cast<const f16*>(a.teacher)[at]);
+}
+
+// Whether entry `at` of the index counts: a class of the vocabulary, to which
+// the teacher gives any weight.
+__device__ __forceinline__ bool counts(const VocabArgs& a, int64_t at)
+{
+    const int64_t i = a.index[at];
+    return i >= 0 && i < a.vocab && !(a.teacher && teacher_logit(a, at) == -INFINITY);
+}
+
+// A row's teacher: weights are exp(s_t t - top) by.  A whole wave's work.
+struct Teacher {
+    float top, by;
+};
+__device__ __forceinline__ Teacher teacher_of(const VocabArgs& a, int64_t row, int lane)
+{
+    if (!a.teacher) return Teacher{0.0f, 1.0f - a.smoothing};
+    if (a.teacher_lse) return Teacher{a.teacher_lse[row], 1.0f};
+    float top = -INFINITY, sum = 0.0f;
+    for (int k = lane; k < a.entries; k += 64)
+        if (counts(a, row * a.entries + k)) top = fmaxf(top, teacher_logit(a, row * a.entries + k) * a.teacher_scale);
+    const float all = wave_max(top);
+    for (int k = lane; k < a.entries; k += 64)
+        if (counts(a, row * a.entries + k))
+            sum += power((teacher_logit(a, row * a.entries + k) * a.teacher_scale - all) * kLog2e);
+    return Teacher{all, 1.0f / wave_sum(sum)};
+}
+// log of the weight before `by`, for an entry that counts
+__device__ __forceinline__ float log_weight(const VocabArgs& a, const Teacher& t, int64_t at)
+{
+    return a.teacher ? teacher_logit(a, at) * a.teacher_scale - t.top : 0.0f;
+}
+__device__ __forceinline__ float weight(const VocabArgs& a, const Teacher& t, int64_t at)
+{
+    return power(log_weight(a, t, at) * kLog2e) * t.by;
+}
+
+// dz at entry k of a row, for the first of those that name a class (the
+// weights of the same class add up); false for the others.
+__device__ __forceinline__ bool entry_gradient(const VocabArgs& a, const VocabRow& row, const Teacher& t, int64_t r,
+                                               int k, float* dz)
+{
+    const int64_t base = r * a.entries;
+    if (!counts(a, base + k)) return false;
+    const int64_t i = a.index[base + k];
+    float q = 0.0f;
+    if (a.entries == 1) {
+        q = weight(a, t, base);
+    } else {
+        for (int j = 0; j < a.entries; ++j) {
+            if (a.index[base + j] != i || !counts(a, base + j)) continue;
+            if (j < k) return false;
+            q += weight(a, t, base + j);
+        }
+    }
+    const float p = power(__builtin_fmaf(a.picked[base + k], kLog2e, -row.l));
+    *dz = __builtin_fmaf(row.f, p, -row.b) - row.g * q;
+    return true;
+}
+
+// ---- rows that take part
+
+// used[r]; what a forward call says of rows that take no part.
+__global__ __launch_bounds__(kBlock) void mark_rows(VocabArgs a, int32_t* used, uint32_t* largest)
+{
+    if (blockIdx.x == 0 && threadIdx.x == 0) *largest = 0;
+    const int lanes = a.entries == 1 ? 1 : 64;
+    const int64_t r = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) / lanes;
+    const int lane = threadIdx.x % lanes;
+    if (r >= a.rows) return;
+    bool any = false;
+    for (int k = lane; k < a.entries; k += lanes) any |= counts(a, r * a.entries + k);
+    if (lanes > 1) any = __ballot(any) != 0;
+    if (lane == 0) used[r] = any;
+    if (any || !a.loss) return;
+    if (lane == 0) a.loss[r] = a.lse[r] = 0.0f;
+    for (int k = lane; k < a.entries; k += lanes) a.picked[r * a.entries + k] = 0.0f;
+}
+
+// list: the rows that take part, in order; place: where in it a row is, or -1.
+__global__ __launch_bounds__(1024) void gather_rows(const int32_t* used, int64_t rows, int32_t* list, int32_t* place,
+                                                    int32_t* active)
+{
+    __shared__ int waves[16];
+    __shared__ int base;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x == 0) base = 0;
+    for (int64_t at = 0; at < rows; at += 1024) {
+        const int64_t r = at + threadIdx.x;
+        const bool in = r < rows && used[r] != 0;
+        const unsigned long long votes = __ballot(in);
+        if (lane == 0) waves[wave] = __popcll(votes);
+        __syncthreads();
+        int before = base, all = base;
+        for (int w = 0; w < 16; ++w) {
+            before += w < wave ? waves[w] : 0;
+            all += waves[w];
+        }
+        const int here = before + __popcll(votes & ((1ull << lane) - 1));
+        if (in) list[here] = static_cast<int32_t>(r);
+        if (r < rows) place[r] = in ? here : -1;
+        __syncthreads();
+        if (threadIdx.x == 0) base = all;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *active = base;
+}
+
+// ---- operands
+
+// A matrix as the products read it: by_rows [row][terms][cols_padded] and / or
+// by_cols [column][terms][rows_padded], zeros in the padding.  list: its rows are these of src (as many as `active` says).
+struct LayOut {
+    const void* src;
+    int64_t ld, rows, cols;
+    const int32_t *list, *active;
+    uint16_t *by_rows, *by_cols;
+    int64_t cols_padded, rows_padded;
+};
+
+// fp32 in three bf16 terms: the first two cut off, so that none exceeds the
+// value, the last rounded.
+__device__ __forceinline__ void terms_of(float x, uint16_t (&t)[3])
+{
+    const uint32_t hi = __float_as_uint(x) & 0xffff0000u;
+    const float r = x - __uint_as_float(hi);
+    const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
+    t[0] = static_cast<uint16_t>(hi >> 16);
+    t[1] = static_cast<uint16_t>(mid >> 16);
+    t[2] = from_float<bf16>(r - __uint_as_float(mid)).bits;
+}
+
+// 64 x 64 elements a block, 16 of a row a thread.
+template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_out(LayOut a)
+{
+    __shared__ uint16_t turned[TERMS][64][72];
+    const int64_t rows = a.active ? *a.active : a.rows;
+    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64, c0 = static_cast<int64_t>(blockIdx.y) * 64;
+    if (r0 >= (rows + kVocabTile - 1) / kVocabTile * kVocabTile) return;
+    const int row = threadIdx.x >> 2, part = threadIdx.x & 3;
+    const int64_t r = r0 + row, c = c0 + part * 16;
+    T x[16];
+    for (int e = 0; e < 16; ++e) x[e] = from_float<T>(0.0f);
+    if (r < rows) {
+        const T* src = static_cast<const T*>(a.src) + (a.list ? a.list[r] : r) * a.ld + c;
+        if (c + 16 <= a.cols) {
+            const Pack<T, 16> p = load_pack<T, 16>(src);
+            for (int e = 0; e < 16; ++e) x[e] = p.v[e];
+        } else {
+            for (int e = 0; e < 16; ++e)
+                if (c + e < a.cols) x[e] = src[e];
+        }
+    }
+    Pack<uint16_t, 16> t[TERMS];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        if constexpr (TERMS == 1) {
+            t[0].v[e] = __builtin_bit_cast(uint16_t, x[e]);
+        } else {
+            uint16_t s[3];
+            terms_of(x[e], s);
+            for (int i = 0; i < TERMS; ++i) t[i].v[e] = s[i];
+        }
+    }
+    if (a.by_rows) {
+#pragma unroll
+        for (int i = 0; i < TERMS; ++i) store_pack(a.by_rows + (r * TERMS + i) * a.cols_padded + c, t[i]);
+    }
+    if (!a.by_cols) return;
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) turned[i][part * 16 + e][row] = t[i].v[e];
+    __syncthreads();
+    const int64_t col = c0 + row;
+    if (col >= a.cols) return;
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i)
+        store_pack(a.by_cols + (col * TERMS + i) * a.rows_padded + r0 + part * 16, load_pack<uint16_t, 16>(&turned[i][row][part * 16]));
+}
+
+// ---- forward
+
+// The logits at the entries: a wave for each.
+template <typename T> __global__ __launch_bounds__(kBlock) void pick(VocabArgs a, const int32_t* list, const int32_t* active)
+{
+    const int64_t all = static_cast<int64_t>(*active) * a.entries;
+    const int lane = threadIdx.x & 63;
+    for (int64_t w = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6); w < all;
+         w += static_cast<int64_t>(gridDim.x) * kWaves) {
+        const int64_t r = list[w / a.entries], at = r * a.entries + w % a.entries;
+        float sum = 0.0f;
+        if (counts(a, at)) {
+            const T* x = static_cast<const T*>(a.x) + r * a.ldx;
+            const T* c = static_cast<const T*>(a.w) + a.index[at] * a.ldw;
+            int64_t k = lane * 8;
+            for (; k + 8 <= a.cols; k += 512) {
+                const Pack<T, 8> p = load_pack<T, 8>(x + k), q = load_pack<T, 8>(c + k);
+                for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(to_float(p.v[e]), to_float(q.v[e]), sum);
+            }
+            for (; k < a.cols; ++k) {       // the lane whose 8 the row's end cuts
+                sum = __builtin_fmaf(to_float(x[k]), to_float(c[k]), sum);
+            }
+            sum = wave_sum(sum) * a.scale;
+        }
+        if (lane == 0) a.picked[at] = sum;
+    }
+}
+
+// Rows' losses from the statistics of their logits: 8 rows a block, the slots
+// in 32 parts, joined in order.
+__global__ __launch_bounds__(kBlock) void finish(VocabArgs a, const int32_t* list, const int32_t* active, const float2* partial,
+                                                 const float* partial_sum, int64_t slots, int64_t padded)
+{
+    __shared__ float2 part[32][8];
+    __shared__ float part_sum[32][8];
+    __shared__ float lse_of[8], mean_of[8];
+    const int64_t n = *active, first = static_cast<int64_t>(blockIdx.x) * 8;
+    if (first >= n) return;
+    const int at = threadIdx.x & 7, slice = threadIdx.x >> 3;
+    float top = -FLT_MAX, sum = 0.0f, all = 0.0f;
+#pragma unroll 4
+    for (int64_t s = slice; s < slots; s += 32) {
+        const float2 x = partial[s * padded + first + at];
+        const float next = fmaxf(top, x.x);
+        sum = sum * power(top - next) + x.y * power(x.x - next);
+        top = next;
+        if (partial_sum) all += partial_sum[s * padded + first + at];
+    }
+    part[slice][at] = make_float2(top, sum);
+    part_sum[slice][at] = all;
+    __syncthreads();
+    if (threadIdx.x < 8) {
+        top = -FLT_MAX;
+        for (int s = 0; s < 32; ++s) top = fmaxf(top, part[s][at].x);
+        sum = all = 0.0f;
+        for (int s = 0; s < 32; ++s) {
+            sum += part[s][at].y * power(part[s][at].x - top);
+            all += part_sum[s][at];
+        }
+        lse_of[at] = __builtin_fmaf(top, kLn2, logf(sum));
+        mean_of[at] = all * a.scale / static_cast<float>(a.vocab);
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 63;
+    for (int i = threadIdx.x >> 6; i < 8 && first + i < n; i += kWaves) {
+        const int64_t r = list[first + i];
+        const float lse = lse_of[i];
+        float loss = 0.0f;
+        if (!a.teacher) {
+            if (lane == 0)
+                loss = lse - (1.0f - a.smoothing) * a.picked[r] - a.smoothing * mean_of[i] + a.z_loss * lse * lse;
+        } else {
+            const Teacher t = teacher_of(a, r, lane);
+            const float log_by = logf(t.by);
+            for (int k = lane; k < a.entries; k += 64)
+                if (counts(a, r * a.entries + k)) {
+                    const float lw = log_weight(a, t, r * a.entries + k), q = power(lw * kLog2e) * t.by;
+                    loss += q == 0.0f ? 0.0f : q * (lw + log_by - (a.picked[r * a.entries + k] - lse));
+                }
+            loss = wave_sum(loss);
+        }
+        if (lane == 0) {
+            a.loss[r] = loss;
+            a.lse[r] = lse;
+        }
+    }
+}
+
+// ---- backward
+
+// Coefficients of the rows that take part (a wave each), zeros for the rows
+// that fill up the last tile; the largest coefficient.
+__global__ __launch_bounds__(kBlock) void coefficients(VocabArgs a, const int32_t* list, const int32_t* active, VocabRow* row,
+                                                       float2* teacher, uint32_t* largest)
+{
+    const int lane = threadIdx.x & 63, n = *active;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    if (at >= (n + kVocabTile - 1) / kVocabTile * kVocabTile) return;
+    VocabRow c = {0.0f, 0.0f, 0.0f, 0.0f};
+    Teacher t = {0.0f, 0.0f};
+    if (at < n) {
+        const int64_t r = list[at];
+        t = teacher_of(a, r, lane);
+        const float lse = a.lse[r];
+        c.g = a.grad_scale * (a.dloss ? a.dloss[r] : 1.0f);
+        c.l = lse * kLog2e;
+        float most = 0.0f;
+        if (!a.teacher) {
+            c.f = c.g * (1.0f + 2.0f * a.z_loss * lse);
+            c.b = c.g * (a.smoothing / static_cast<float>(a.vocab));
+            most = fabsf(c.g);
+        } else {
+            float q = 0.0f;
+            for (int k = lane; k < a.entries; k += 64)
+                if (counts(a, r * a.entries + k)) q += weight(a, t, r * a.entries + k);
+            q = wave_sum(q);
+            c.f = c.g * q;
+            most = fabsf(c.f);
+        }
+        most += fabsf(c.f) + fabsf(c.b);
+        if (lane == 0) atomicMax(largest, __float_as_uint(most));      // the same in any order
+    }
+    if (lane == 0) {
+        row[at] = c;
+        teacher[at] = make_float2(t.top, t.by);
+    }
+}
+
+struct Gradient {
+    const VocabRow* row;
+    const float2* teacher;
+    const int32_t *list, *place, *active;
+    const uint32_t* largest;
+    uint16_t *dz, *dzt;
+    int32_t dz_terms, dzt_terms;
+    int64_t first, classes, padded;
+    int64_t count;          // classes of the piece
+    const float* sums;      // [splits][padded][cols_padded]: dz W without the entries
+    int32_t splits;
+    int64_t cols_padded;
+};
+
+// The entries of a piece's classes: into dz^T, and out of dz.  A wave a row.
+template <typename T> __global__ __launch_bounds__(kBlock) void place_entries(VocabArgs a, Gradient g)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    if (at >= *g.active) return;
+    const int64_t r = g.list[at];
+    const VocabRow row = g.row[at];
+    const Teacher t = {g.teacher[at].x, g.teacher[at].y};
+    const float up = term_scale<T>(*g.largest);
+    for (int k = lane; k < a.entries; k += 64) {
+        const int64_t i = a.index[r * a.entries + k] - g.first;
+        float x;
+        if (i < 0 || i >= g.count || !entry_gradient(a, row, t, r, k, &x)) continue;
+        x *= up;
+        for (int j = 0; j < g.dz_terms; ++j) g.dz[(at * g.dz_terms + j) * g.classes + i] = 0;
+        for (int j = 0; j < g.dzt_terms; ++j) {
+            const T term = from_float<T>(x);
+            x -= to_float(term);
+            g.dzt[(i * g.dzt_terms + j) * g.padded + at] = __builtin_bit_cast(uint16_t, term);
+        }
+    }
+}
+
+// dx of a row: the products' sums and the entries', times the logits' scale.
+template <typename T, typename TERM> __global__ __launch_bounds__(kBlock) void finish_dx(VocabArgs a, Gradient g)
+{
+    __shared__ float value[kMostEntries];
+    __shared__ int64_t of[kMostEntries];
+    __shared__ int entries;
+    const int64_t r = blockIdx.x;
+    const int32_t at = g.place[r];
+    T* out = static_cast<T*>(a.dx) + r * a.lddx;
+    if (at < 0) {
+        for (int64_t c = threadIdx.x; c < a.cols; c += kBlock) out[c] = from_float<T>(0.0f);
+        return;
+    }
+    if (threadIdx.x < 64) {     // the entries in order
+        const int lane = threadIdx.x;
+        const VocabRow row = g.row[at];
+        const Teacher t = {g.teacher[at].x, g.teacher[at].y};
+        int n = 0;
+        for (int k0 = 0; k0 < a.entries; k0 += 64) {
+            const int k = k0 + lane;
+            float x = 0.0f;
+            const bool in = k < a.entries && entry_gradient(a, row, t, r, k, &x);
+            const unsigned long long votes = __ballot(in);
+            if (in) {
+                const int here = n + __popcll(votes & ((1ull << lane) - 1));
+                value[here] = x;
+                of[here] = a.index[r * a.entries + k] * a.ldw;
+            }
+            n += __popcll(votes);
+        }
+        if (lane == 0) entries = n;
+    }
+    __syncthreads();
+    const int n = entries;
+    const float by = a.scale / term_scale<TERM>(*g.largest);
+    const T* w = static_cast<const T*>(a.w);
+    for (int64_t c = threadIdx.x * 4; c < a.cols; c += kBlock * 4) {
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, own[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < g.splits; ++s) {
+            const Pack<float, 4> p = load_pack<float, 4>(g.sums + (s * g.padded + at) * g.cols_padded + c);
+            for (int e = 0; e < 4; ++e) sum[e] += p.v[e];
+        }
+        if (c + 4 <= a.cols) {
+#pragma unroll 4
+            for (int k = 0; k < n; ++k) {
+                const Pack<T, 4> p = load_pack<T, 4>(w + of[k] + c);
+                for (int e = 0; e < 4; ++e) own[e] = __builtin_fmaf(value[k], to_float(p.v[e]), own[e]);
+            }
+        } else {
+            for (int k = 0; k < n; ++k)
+                for (int e = 0; e < 4 && c + e < a.cols; ++e) own[e] = __builtin_fmaf(value[k], to_float(w[of[k] + c + e]), own[e]);
+        }
+        for (int e = 0; e < 4 && c + e < a.cols; ++e) out[c + e] = from_float<T>(__builtin_fmaf(sum[e], by, own[e] * a.scale));
+    }
+}
+
+// dW of no rows.
+template <typename T> __global__ __launch_bounds__(kBlock) void clear(T* c, int64_t ld, int64_t rows, int64_t cols)
+{
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int64_t i = threadIdx.x; i < cols; i += kBlock) c[r * ld + i] = from_float<T>(0.0f);
+}
+
+// ---- the host's side
+
+// Where things lie in the workspace, in bytes.
+struct Layout {
+    int terms;
+    int64_t padded, cols_padded, piece, pieces, slots;
+    int wave;               // of the statistics
+    int splits;             // of dz W
+    int64_t used, list, place, scalars, row, teacher, x, xt, w, wt, dz, dzt, sums, partial, partial_sum, bytes;
+};
+
+// Bytes of a piece's gradient, and its part of W: pieces are large enough to
+// fill the chip with tiles several times over, small beside the card's memory.
+constexpr int64_t kPieceBytes = int64_t(1) << 30;
+
+Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool backward)
+{
+    Layout l = {};
+    l.terms = vocab_terms(dtype);
+    l.padded = round_up(rows, kVocabTile);
+    l.cols_padded = round_up(cols, 128);
+    const int dzt_terms = l.terms == 1 ? 2 : 3;
+    const int64_t each = 2 * (l.padded * (l.terms + dzt_terms) + 2 * l.cols_padded * l.terms);
+    int64_t most = kPieceBytes / each / kVocabTile * kVocabTile;
+    if (most < 2048) most = 2048;
+    if (most > int64_t(1) << 20) most = int64_t(1) << 20;
+    l.pieces = (vocab + most - 1) / most;
+    l.piece = round_up((vocab + l.pieces - 1) / l.pieces, kVocabTile);
+    l.pieces = (vocab + l.piece - 1) / l.piece;
+    l.wave = vocab_wave(l.piece, rows);
+    l.slots = (vocab + l.wave - 1) / l.wave;
+    l.splits = vocab_splits(rows, cols, l.piece / 64 * (l.terms == 3 ? 6 : 1));
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at = round_up(at + bytes, 256);
+        return here;
+    };
+    l.used = take(4 * rows);
+    l.list = take(4 * rows);
+    l.place = take(4 * rows);
+    l.scalars = take(256);      // rows that take part; the largest coefficient
+    l.x = take(2 * l.terms * l.padded * l.cols_padded);
+    l.w = take(2 * l.terms * l.piece * l.cols_padded);
+    if (backward) {
+        l.row = take(sizeof(VocabRow) * l.padded);
+        l.teacher = take(sizeof(float2) * l.padded);
+        l.xt = take(2 * l.terms * l.padded * cols);
+        l.wt = take(2 * l.terms * l.piece * cols);
+        l.dz = take(2 * l.terms * l.padded * l.piece);
+        l.dzt = take(2 * dzt_terms * l.padded * l.piece);
+        l.sums = take(4 * l.splits * l.padded * l.cols_padded);
+    } else {
+        l.partial = take(8 * l.slots * l.padded);
+        l.partial_sum = take(4 * l.slots * l.padded);
+    }
+    l.bytes = at;
+    return l;
+}
+
+// Whether the products can read W where it lies.
+bool in_place(const VocabArgs& a)
+{
+    return a.dtype != DTYPE_F32 && a.cols % 128 == 0 && a.ldw % 8 == 0 && a.ldw <= (int64_t(1) << 21) &&
+           (reinterpret_cast<uintptr_t>(a.w) & 15) == 0;
+}
+
+hipError_t launch_lay_out(const LayOut& l, int dtype, int64_t rows, int64_t cols, hipStream_t s)
+{
+    const dim3 grid(static_cast<unsigned>(round_up(rows, kVocabTile) / 64), static_cast<unsigned>(round_up(cols, 128) / 64));
+    if (dtype == DTYPE_F32) lay_out<float, 3><<<grid, kBlock, 0, s>>>(l);
+    else lay_out<bf16, 1><<<grid, kBlock, 0, s>>>(l);       // bits of either 16-bit type
+    return hipGetLastError();
+}
+
+#define VOCAB_TRY(call)                              \
+    do {                                             \
+        const hipError_t try_error = (call);         \
+        if (try_error != hipSuccess) return try_error; \
+    } while (0)
+
+struct Plan {
+    Layout l;
+    int32_t *used, *list, *place, *active;
+    uint32_t* largest;
+    uint8_t* base;
+    bool w_in_place;
+    template <typename T> T* at(int64_t offset) const { return reinterpret_cast<T*>(base + offset); }
+};
+
+// Rows that take part, and x as an operand (backward: transposed too).
+hipError_t begin(const VocabArgs& a, bool backward, Plan& p, hipStream_t s)
+{
+    p.l = layout_of(a.rows, a.cols, a.vocab, a.dtype, backward);
+    p.base = static_cast<uint8_t*>(a.workspace);
+    p.used = p.at<int32_t>(p.l.used);
+    p.list = p.at<int32_t>(p.l.list);
+    p.place = p.at<int32_t>(p.l.place);
+    p.active = p.at<int32_t>(p.l.scalars);
+    p.largest = p.at<uint32_t>(p.l.scalars + 4);
+    p.w_in_place = in_place(a);
+    const int64_t threads = a.rows * (a.entries == 1 ? 1 : 64);
+    mark_rows<<<static_cast<unsigned>((threads + kBlock - 1) / kBlock), kBlock, 0, s>>>(a, p.used, p.largest);
+    VOCAB_TRY(hipGetLastError());
+    gather_rows<<<1, 1024, 0, s>>>(p.used, a.rows, p.list, p.place, p.active);
+    VOCAB_TRY(hipGetLastError());
+    LayOut x = {};
+    x.src = a.x;
+    x.ld = a.ldx;
+    x.rows = a.rows;
+    x.cols = a.cols;
+    x.list = p.list;
+    x.active = p.active;
+    x.by_rows = p.at<uint16_t>(p.l.x);
+    x.by_cols = backward && a.dw ? p.at<uint16_t>(p.l.xt) : nullptr;
+    x.cols_padded = p.l.cols_padded;
+    x.rows_padded = p.l.padded;
+    return launch_lay_out(x, a.dtype, a.rows, a.cols, s);
+}
+
+constexpr uint32_t kPairsA = 0 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 2 << 10;   // of three terms each: those above 2^-24
+constexpr uint32_t kPairsB = 0 | 1 << 2 | 0 << 4 | 1 << 6 | 2 << 8 | 0 << 10;
+
+// The logits of classes first .. first + n - 1: W as an operand where it cannot
+// be read in place (and transposed, for dx), and the product's two sides.
+hipError_t piece_of(const VocabArgs& a, const Plan& p, int64_t first, int64_t n, bool transposed, VocabProduct& q, hipStream_t s)
+{
+    const Layout& l = p.l;
+    const int64_t size = static_cast<int64_t>(dtype_size(a.dtype));
+    const uint8_t* w = static_cast<const uint8_t*>(a.w) + first * a.ldw * size;
+    if (!p.w_in_place || transposed) {
+        LayOut o = {};
+        o.src = w;
+        o.ld = a.ldw;
+        o.rows = n;
+        o.cols = a.cols;
+        o.by_rows = p.w_in_place ? nullptr : p.at<uint16_t>(l.w);
+        o.by_cols = transposed ? p.at<uint16_t>(l.wt) : nullptr;
+        o.cols_padded = l.cols_padded;
+        o.rows_padded = l.piece;
+        VOCAB_TRY(launch_lay_out(o, a.dtype, n, a.cols, s));
+    }
+    q = VocabProduct{};
+    q.a.data = p.w_in_place ? w : p.at<uint8_t>(l.w);
+    q.a.ld = p.w_in_place ? a.ldw * size : 2 * l.terms * l.cols_padded;
+    q.a.rows = static_cast<int32_t>(n);
+    q.a.plane = q.b.plane = static_cast<int32_t>(2 * l.cols_padded);
+    q.b.data = p.at<uint8_t>(l.x);
+    q.b.ld = 2 * l.terms * l.cols_padded;
+    q.active = p.active;
+    q.rows_b_active = 1;
+    q.blocks = static_cast<int32_t>(l.cols_padded / 64);
+    q.terms = l.terms == 3 ? 6 : 1;
+    q.terms_a = l.terms == 3 ? kPairsA : 0;
+    q.terms_b = l.terms == 3 ? kPairsB : 0;
+    q.splits = 1;
+    q.f16 = a.dtype == DTYPE_F16;
+    q.scale_log2e = a.scale * kLog2e;
+    q.first = first;
+    q.padded = l.padded;
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t vocab_workspace_bytes(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool backward)
+{
+    return static_cast<size_t>(layout_of(rows, cols, vocab, dtype, backward).bytes);
+}
+
+hipError_t launch_vocab_forward(const VocabArgs& a, hipStream_t s)
+{
+    Plan p;
+    VOCAB_TRY(begin(a, false, p, s));
+    const Layout& l = p.l;
+    for (int64_t first = 0; first < a.vocab; first += l.piece) {
+        const int64_t n = a.vocab - first < l.piece ? a.vocab - first : l.piece;
+        VocabProduct q;
+        VOCAB_TRY(piece_of(a, p, first, n, false, q, s));
+        q.wave = l.wave;
+        q.partial = p.at<float2>(l.partial);
+        q.partial_sum = a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr;
+        VOCAB_TRY(launch_vocab_product(VOCAB_STATISTICS, q, n, a.rows, s));
+    }
+    const int64_t waves = a.rows * a.entries, blocks = (waves + kWaves - 1) / kWaves;
+    const unsigned picks = static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20);
+    if (a.dtype == DTYPE_F32) pick<float><<<picks, kBlock, 0, s>>>(a, p.list, p.active);
+    else if (a.dtype == DTYPE_BF16) pick<bf16><<<picks, kBlock, 0, s>>>(a, p.list, p.active);
+    else pick<f16><<<picks, kBlock, 0, s>>>(a, p.list, p.active);
+    VOCAB_TRY(hipGetLastError());
+    finish<<<static_cast<unsigned>((a.rows + 7) / 8), kBlock, 0, s>>>(a, p.list, p.active, p.at<float2>(l.partial),
+                                                                      a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr,
+                                                                      l.slots, l.padded);
+    return hipGetLastError();
+}
+
+hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
+{
+    if (a.rows == 0) {
+        if (!a.dw || a.accumulate) return hipSuccess;
+        const unsigned blocks = static_cast<unsigned>(a.vocab < (1 << 16) ? a.vocab : 1 << 16);
+        if (a.dw_dtype == DTYPE_F32) clear<float><<<blocks, kBlock, 0, s>>>(static_cast<float*>(a.dw), a.lddw, a.vocab, a.cols);
+        else clear<bf16><<<blocks, kBlock, 0, s>>>(static_cast<bf16*>(a.dw), a.lddw, a.vocab, a.cols);
+        return hipGetLastError();
+    }
+    Plan p;
+    VOCAB_TRY(begin(a, true, p, s));
+    const Layout& l = p.l;
+    Gradient g = {};
+    g.row = p.at<VocabRow>(l.row);
+    g.teacher = p.at<float2>(l.teacher);
+    g.list = p.list;
+    g.place = p.place;
+    g.active = p.active;
+    g.largest = p.largest;
+    g.dz = p.at<uint16_t>(l.dz);
+    g.dzt = p.at<uint16_t>(l.dzt);
+    // an fp32 dw takes two terms of a 16-bit type's dz (22 or 16 bits), a 16-bit one takes one
+    g.dz_terms = a.dx ? l.terms : 0;
+    g.dzt_terms = !a.dw ? 0 : (l.terms == 3 ? 3 : (a.dw_dtype == DTYPE_F32 ? 2 : 1));
+    g.classes = l.piece;
+    g.padded = l.padded;
+    g.sums = p.at<float>(l.sums);
+    g.splits = l.splits;
+    g.cols_padded = l.cols_padded;
+    const unsigned row_waves = static_cast<unsigned>((l.padded + kWaves - 1) / kWaves);
+    coefficients<<<row_waves, kBlock, 0, s>>>(a, p.list, p.active, p.at<VocabRow>(l.row), p.at<float2>(l.teacher), p.largest);
+    VOCAB_TRY(hipGetLastError());
+    for (int64_t first = 0; first < a.vocab; first += l.piece) {
+        const int64_t n = a.vocab - first < l.piece ? a.vocab - first : l.piece;
+        VocabProduct q;
+        VOCAB_TRY(piece_of(a, p, first, n, a.dx != nullptr, q, s));
+        q.wave = vocab_wave(n, a.rows);
+        q.row = g.row;
+        q.largest = p.largest;
+        q.dz = g.dz;
+        q.dzt = g.dzt;
+        q.dz_terms = g.dz_terms;
+        q.dzt_terms = g.dzt_terms;
+        q.classes = g.classes;
+        VOCAB_TRY(launch_vocab_product(VOCAB_GRADIENT, q, n, a.rows, s));
+        g.first = first;
+        g.count = n;
+        if (a.dtype == DTYPE_F16) place_entries<f16><<<row_waves, kBlock, 0, s>>>(a, g);
+        else place_entries<bf16><<<row_waves, kBlock, 0, s>>>(a, g);
+        VOCAB_TRY(hipGetLastError());
+        VocabProduct c = {};
+        c.active = p.active;
+        c.f16 = q.f16;
+        c.largest = p.largest;
+        if (a.dx) {
+            c.a = VocabOperand{p.at<uint8_t>(l.dz), 2 * l.terms * l.piece, 0, static_cast<int32_t>(2 * l.piece)};
+            c.b = VocabOperand{p.at<uint8_t>(l.wt), 2 * l.terms * l.piece, static_cast<int32_t>(a.cols), static_cast<int32_t>(2 * l.piece)};
+            c.rows_a_active = 1;
+            c.blocks = static_cast<int32_t>(round_up(n, 128) / 64);
+            c.terms = q.terms;
+            c.terms_a = q.terms_a;
+            c.terms_b = q.terms_b;
+            c.wave = vocab_wave(a.rows, a.cols);
+            c.splits = l.splits;
+            c.c = p.at<float>(l.sums);
+            c.ldc = l.cols_padded;
+            c.split_stride = l.padded * l.cols_padded;
+            c.c_dtype = DTYPE_F32;
+            c.add = first > 0;
+            c.by = 1.0f;
+            c.largest = nullptr;
+            VOCAB_TRY(launch_vocab_product(VOCAB_STORE, c, a.rows, a.cols, s));
+        }
+        if (a.dw) {
+            c.a = VocabOperand{p.at<uint8_t>(l.dzt), 2 * g.dzt_terms * l.padded, static_cast<int32_t>(n), static_cast<int32_t>(2 * l.padded)};
+            c.b = VocabOperand{p.at<uint8_t>(l.xt), 2 * l.terms * l.padded, static_cast<int32_t>(a.cols), static_cast<int32_t>(2 * l.padded)};
+            c.rows_a_active = 0;
+            c.k_active = 1;
+            c.blocks = static_cast<int32_t>(l.padded / 64);
+            c.terms = l.terms == 3 ? 6 : g.dzt_terms;
+            c.terms_a = l.terms == 3 ? kPairsA : 1 << 2;    // both terms of dz, the one of x
+            c.terms_b = l.terms == 3 ? kPairsB : 0;
+            c.wave = vocab_wave(n, a.cols);
+            c.splits = 1;
+            c.c = static_cast<uint8_t*>(a.dw) + first * a.lddw * static_cast<int64_t>(dtype_size(a.dw_dtype));
+            c.ldc = a.lddw;
+            c.c_dtype = a.dw_dtype;
+            c.add = a.accumulate;
+            c.by = a.scale;
+            c.largest = p.largest;
+            VOCAB_TRY(launch_vocab_product(VOCAB_STORE, c, n, a.cols, s));
+        }
+    }
+    if (a.dx) {
+        const unsigned rows = static_cast<unsigned>(a.rows);
+        if (a.dtype == DTYPE_F32) finish_dx<float, bf16><<<rows, kBlock, 0, s>>>(a, g);
+        else if (a.dtype == DTYPE_BF16) finish_dx<bf16, bf16><<<rows, kBlock, 0, s>>>(a, g);
+        else finish_dx<f16, f16><<<rows, kBlock, 0, s>>>(a, g);
+        VOCAB_TRY(hipGetLastError());
+    }
+    return hipSuccess;
+}
+
+}  // namespace fasgd
