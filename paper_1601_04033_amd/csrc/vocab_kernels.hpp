@@ -80,7 +80,8 @@ struct VocabProduct {
     // VOCAB_GRADIENT, same operands
     const VocabRow* row;    // [padded]
     const uint32_t* largest;        // of the rows' coefficients, as bits (fp16 terms are scaled by it)
-    uint16_t *dz, *dzt;     // [padded][dz_terms][classes] and [classes][dzt_terms][padded]
+    uint16_t *dz, *dzt;     // rows of [dz_terms][classes] and of [dzt_terms][padded], ld_dz and ld_dzt values apart
+    int64_t ld_dz, ld_dzt;
     int32_t dz_terms, dzt_terms;    // 0: not wanted
     int64_t classes;        // padded to 256
     // VOCAB_STORE: c[split] (+)= by a b^T, by divided by the gradient's scale
@@ -91,10 +92,13 @@ struct VocabProduct {
 };
 
 constexpr int64_t kVocabTile = 256;     // classes and rows are padded to this
-// Side of a wave's tile for an m x n product (128: blocks of 256 x 256 where
-// they fill most of the chip, else 64), and the parts its contraction goes in.
-int vocab_wave(int64_t m, int64_t n);
-int vocab_splits(int64_t m, int64_t n, int64_t stages);
+// How an m x n product over `stages` of 64 (times the pairs of terms) goes:
+// side of a wave's tile (128: blocks of 256 x 256; or 64), parts of the contraction.
+struct VocabPlan {
+    int wave, splits;
+};
+constexpr int kVocabSplits = 16;
+VocabPlan vocab_plan(int64_t m, int64_t n, int64_t stages, int most_splits);
 hipError_t launch_vocab_product(int what, const VocabProduct& p, int64_t m, int64_t n, hipStream_t s);
 
 // What a gradient's terms are multiplied by: 1 in bf16; in fp16, whose range

@@ -154,14 +154,15 @@ __global__ __launch_bounds__(1024) void gather_rows(const int32_t* used, int64_t
 
 // ---- operands
 
-// A matrix as the products read it: by_rows [row][terms][cols_padded] and / or
-// by_cols [column][terms][rows_padded], zeros in the padding.  list: its rows are these of src (as many as `active` says).
+// A matrix as the products read it: by_rows, rows of [terms][cols_padded], and /
+// or by_cols, columns of [terms][rows_padded], zeros in the padding.  list: its
+// rows are these of src (as many as `active` says).
 struct LayOut {
     const void* src;
     int64_t ld, rows, cols;
     const int32_t *list, *active;
     uint16_t *by_rows, *by_cols;
-    int64_t cols_padded, rows_padded;
+    int64_t cols_padded, ld_rows, rows_padded, ld_cols;
 };
 
 // fp32 in three bf16 terms: the first two cut off, so that none exceeds the
@@ -210,7 +211,7 @@ template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_o
     }
     if (a.by_rows) {
 #pragma unroll
-        for (int i = 0; i < TERMS; ++i) store_pack(a.by_rows + (r * TERMS + i) * a.cols_padded + c, t[i]);
+        for (int i = 0; i < TERMS; ++i) store_pack(a.by_rows + r * a.ld_rows + i * a.cols_padded + c, t[i]);
     }
     if (!a.by_cols) return;
 #pragma unroll
@@ -222,7 +223,7 @@ template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_o
     if (col >= a.cols) return;
 #pragma unroll
     for (int i = 0; i < TERMS; ++i)
-        store_pack(a.by_cols + (col * TERMS + i) * a.rows_padded + r0 + part * 16, load_pack<uint16_t, 16>(&turned[i][row][part * 16]));
+        store_pack(a.by_cols + col * a.ld_cols + i * a.rows_padded + r0 + part * 16, load_pack<uint16_t, 16>(&turned[i][row][part * 16]));
 }
 
 // ---- forward
@@ -360,7 +361,7 @@ struct Gradient {
     const uint32_t* largest;
     uint16_t *dz, *dzt;
     int32_t dz_terms, dzt_terms;
-    int64_t first, classes, padded;
+    int64_t first, classes, padded, ld_dz, ld_dzt;
     int64_t count;          // classes of the piece
     const float* sums;      // [splits][padded][cols_padded]: dz W without the entries
     int32_t splits;
@@ -382,11 +383,11 @@ template <typename T> __global__ __launch_bounds__(kBlock) void place_entries(Vo
         float x;
         if (i < 0 || i >= g.count || !entry_gradient(a, row, t, r, k, &x)) continue;
         x *= up;
-        for (int j = 0; j < g.dz_terms; ++j) g.dz[(at * g.dz_terms + j) * g.classes + i] = 0;
+        for (int j = 0; j < g.dz_terms; ++j) g.dz[at * g.ld_dz + j * g.classes + i] = 0;
         for (int j = 0; j < g.dzt_terms; ++j) {
             const T term = from_float<T>(x);
             x -= to_float(term);
-            g.dzt[(i * g.dzt_terms + j) * g.padded + at] = __builtin_bit_cast(uint16_t, term);
+            g.dzt[i * g.ld_dzt + j * g.padded + at] = __builtin_bit_cast(uint16_t, term);
         }
     }
 }
@@ -460,14 +461,19 @@ template <typename T> __global__ __launch_bounds__(kBlock) void clear(T* c, int6
 struct Layout {
     int terms;
     int64_t padded, cols_padded, piece, pieces, slots;
-    int wave;               // of the statistics
-    int splits;             // of dz W
+    int64_t ld_cols, ld_rows, ld_piece;     // values between rows of terms along the columns, the rows, a piece's classes
+    VocabPlan logits, dx, dw;
     int64_t used, list, place, scalars, row, teacher, x, xt, w, wt, dz, dzt, sums, partial, partial_sum, bytes;
 };
 
 // Bytes of a piece's gradient, and its part of W: pieces are large enough to
 // fill the chip with tiles several times over, small beside the card's memory.
 constexpr int64_t kPieceBytes = int64_t(1) << 30;
+
+// Values between rows of n: an odd number of 512 bytes, so that the rows of a
+// tile, which are read together, spread over L2's channels (8,192 x 4,096 x
+// 16,384: rows 32 KB apart 855 us, 512 bytes more 822, 256 more 957).
+int64_t apart(int64_t n) { return ((n + 255) / 256 | 1) * 256; }
 
 Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool backward)
 {
@@ -483,9 +489,14 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool back
     l.pieces = (vocab + most - 1) / most;
     l.piece = round_up((vocab + l.pieces - 1) / l.pieces, kVocabTile);
     l.pieces = (vocab + l.piece - 1) / l.piece;
-    l.wave = vocab_wave(l.piece, rows);
-    l.slots = (vocab + l.wave - 1) / l.wave;
-    l.splits = vocab_splits(rows, cols, l.piece / 64 * (l.terms == 3 ? 6 : 1));
+    const int64_t pairs = l.terms == 3 ? 6 : 1;
+    l.logits = vocab_plan(l.piece, rows, l.cols_padded / 64 * pairs, 1);
+    l.dx = vocab_plan(rows, cols, l.piece / 64 * pairs, kVocabSplits);
+    l.dw = vocab_plan(l.piece, cols, l.padded / 64 * (l.terms == 3 ? 6 : 2), 1);
+    l.slots = (vocab + l.logits.wave - 1) / l.logits.wave;
+    l.ld_cols = apart(l.terms * l.cols_padded);
+    l.ld_rows = apart(l.terms * l.padded);
+    l.ld_piece = apart(l.terms * l.piece);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
@@ -496,16 +507,16 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool back
     l.list = take(4 * rows);
     l.place = take(4 * rows);
     l.scalars = take(256);      // rows that take part; the largest coefficient
-    l.x = take(2 * l.terms * l.padded * l.cols_padded);
-    l.w = take(2 * l.terms * l.piece * l.cols_padded);
+    l.x = take(2 * l.padded * l.ld_cols);
+    l.w = take(2 * l.piece * l.ld_cols);
     if (backward) {
         l.row = take(sizeof(VocabRow) * l.padded);
         l.teacher = take(sizeof(float2) * l.padded);
-        l.xt = take(2 * l.terms * l.padded * cols);
-        l.wt = take(2 * l.terms * l.piece * cols);
-        l.dz = take(2 * l.terms * l.padded * l.piece);
-        l.dzt = take(2 * dzt_terms * l.padded * l.piece);
-        l.sums = take(4 * l.splits * l.padded * l.cols_padded);
+        l.xt = take(2 * cols * l.ld_rows);
+        l.wt = take(2 * cols * l.ld_piece);
+        l.dz = take(2 * l.padded * l.ld_piece);
+        l.dzt = take(2 * l.piece * apart(dzt_terms * l.padded));
+        l.sums = take(4 * l.dx.splits * l.padded * l.cols_padded);
     } else {
         l.partial = take(8 * l.slots * l.padded);
         l.partial_sum = take(4 * l.slots * l.padded);
@@ -570,12 +581,15 @@ hipError_t begin(const VocabArgs& a, bool backward, Plan& p, hipStream_t s)
     x.by_rows = p.at<uint16_t>(p.l.x);
     x.by_cols = backward && a.dw ? p.at<uint16_t>(p.l.xt) : nullptr;
     x.cols_padded = p.l.cols_padded;
+    x.ld_rows = p.l.ld_cols;
     x.rows_padded = p.l.padded;
+    x.ld_cols = p.l.ld_rows;
     return launch_lay_out(x, a.dtype, a.rows, a.cols, s);
 }
 
-constexpr uint32_t kPairsA = 0 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 2 << 10;   // of three terms each: those above 2^-24
-constexpr uint32_t kPairsB = 0 | 1 << 2 | 0 << 4 | 1 << 6 | 2 << 8 | 0 << 10;
+// Pairs of three terms each, those above 2^-24, the smallest first.
+constexpr uint32_t kPairsA = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
+constexpr uint32_t kPairsB = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 
 // The logits of classes first .. first + n - 1: W as an operand where it cannot
 // be read in place (and transposed, for dx), and the product's two sides.
@@ -593,16 +607,18 @@ hipError_t piece_of(const VocabArgs& a, const Plan& p, int64_t first, int64_t n,
         o.by_rows = p.w_in_place ? nullptr : p.at<uint16_t>(l.w);
         o.by_cols = transposed ? p.at<uint16_t>(l.wt) : nullptr;
         o.cols_padded = l.cols_padded;
+        o.ld_rows = l.ld_cols;
         o.rows_padded = l.piece;
+        o.ld_cols = l.ld_piece;
         VOCAB_TRY(launch_lay_out(o, a.dtype, n, a.cols, s));
     }
     q = VocabProduct{};
     q.a.data = p.w_in_place ? w : p.at<uint8_t>(l.w);
-    q.a.ld = p.w_in_place ? a.ldw * size : 2 * l.terms * l.cols_padded;
+    q.a.ld = p.w_in_place ? a.ldw * size : 2 * l.ld_cols;
     q.a.rows = static_cast<int32_t>(n);
     q.a.plane = q.b.plane = static_cast<int32_t>(2 * l.cols_padded);
     q.b.data = p.at<uint8_t>(l.x);
-    q.b.ld = 2 * l.terms * l.cols_padded;
+    q.b.ld = 2 * l.ld_cols;
     q.active = p.active;
     q.rows_b_active = 1;
     q.blocks = static_cast<int32_t>(l.cols_padded / 64);
@@ -633,7 +649,7 @@ hipError_t launch_vocab_forward(const VocabArgs& a, hipStream_t s)
         const int64_t n = a.vocab - first < l.piece ? a.vocab - first : l.piece;
         VocabProduct q;
         VOCAB_TRY(piece_of(a, p, first, n, false, q, s));
-        q.wave = l.wave;
+        q.wave = l.logits.wave;
         q.partial = p.at<float2>(l.partial);
         q.partial_sum = a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr;
         VOCAB_TRY(launch_vocab_product(VOCAB_STATISTICS, q, n, a.rows, s));
@@ -676,8 +692,10 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
     g.dzt_terms = !a.dw ? 0 : (l.terms == 3 ? 3 : (a.dw_dtype == DTYPE_F32 ? 2 : 1));
     g.classes = l.piece;
     g.padded = l.padded;
+    g.ld_dz = l.ld_piece;
+    g.ld_dzt = apart(g.dzt_terms * l.padded);
     g.sums = p.at<float>(l.sums);
-    g.splits = l.splits;
+    g.splits = l.dx.splits;
     g.cols_padded = l.cols_padded;
     const unsigned row_waves = static_cast<unsigned>((l.padded + kWaves - 1) / kWaves);
     coefficients<<<row_waves, kBlock, 0, s>>>(a, p.list, p.active, p.at<VocabRow>(l.row), p.at<float2>(l.teacher), p.largest);
@@ -686,7 +704,7 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
         const int64_t n = a.vocab - first < l.piece ? a.vocab - first : l.piece;
         VocabProduct q;
         VOCAB_TRY(piece_of(a, p, first, n, a.dx != nullptr, q, s));
-        q.wave = vocab_wave(n, a.rows);
+        q.wave = l.logits.wave;
         q.row = g.row;
         q.largest = p.largest;
         q.dz = g.dz;
@@ -694,6 +712,8 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
         q.dz_terms = g.dz_terms;
         q.dzt_terms = g.dzt_terms;
         q.classes = g.classes;
+        q.ld_dz = g.ld_dz;
+        q.ld_dzt = g.ld_dzt;
         VOCAB_TRY(launch_vocab_product(VOCAB_GRADIENT, q, n, a.rows, s));
         g.first = first;
         g.count = n;
@@ -705,15 +725,15 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
         c.f16 = q.f16;
         c.largest = p.largest;
         if (a.dx) {
-            c.a = VocabOperand{p.at<uint8_t>(l.dz), 2 * l.terms * l.piece, 0, static_cast<int32_t>(2 * l.piece)};
-            c.b = VocabOperand{p.at<uint8_t>(l.wt), 2 * l.terms * l.piece, static_cast<int32_t>(a.cols), static_cast<int32_t>(2 * l.piece)};
+            c.a = VocabOperand{p.at<uint8_t>(l.dz), 2 * l.ld_piece, 0, static_cast<int32_t>(2 * l.piece)};
+            c.b = VocabOperand{p.at<uint8_t>(l.wt), 2 * l.ld_piece, static_cast<int32_t>(a.cols), static_cast<int32_t>(2 * l.piece)};
             c.rows_a_active = 1;
             c.blocks = static_cast<int32_t>(round_up(n, 128) / 64);
             c.terms = q.terms;
             c.terms_a = q.terms_a;
             c.terms_b = q.terms_b;
-            c.wave = vocab_wave(a.rows, a.cols);
-            c.splits = l.splits;
+            c.wave = l.dx.wave;
+            c.splits = l.dx.splits;
             c.c = p.at<float>(l.sums);
             c.ldc = l.cols_padded;
             c.split_stride = l.padded * l.cols_padded;
@@ -724,15 +744,15 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
             VOCAB_TRY(launch_vocab_product(VOCAB_STORE, c, a.rows, a.cols, s));
         }
         if (a.dw) {
-            c.a = VocabOperand{p.at<uint8_t>(l.dzt), 2 * g.dzt_terms * l.padded, static_cast<int32_t>(n), static_cast<int32_t>(2 * l.padded)};
-            c.b = VocabOperand{p.at<uint8_t>(l.xt), 2 * l.terms * l.padded, static_cast<int32_t>(a.cols), static_cast<int32_t>(2 * l.padded)};
+            c.a = VocabOperand{p.at<uint8_t>(l.dzt), 2 * g.ld_dzt, static_cast<int32_t>(n), static_cast<int32_t>(2 * l.padded)};
+            c.b = VocabOperand{p.at<uint8_t>(l.xt), 2 * l.ld_rows, static_cast<int32_t>(a.cols), static_cast<int32_t>(2 * l.padded)};
             c.rows_a_active = 0;
             c.k_active = 1;
             c.blocks = static_cast<int32_t>(l.padded / 64);
             c.terms = l.terms == 3 ? 6 : g.dzt_terms;
-            c.terms_a = l.terms == 3 ? kPairsA : 1 << 2;    // both terms of dz, the one of x
+            c.terms_a = l.terms == 3 ? kPairsA : (g.dzt_terms == 2 ? 1 : 0);    // the second term of dz, then the first
             c.terms_b = l.terms == 3 ? kPairsB : 0;
-            c.wave = vocab_wave(n, a.cols);
+            c.wave = l.dw.wave;
             c.splits = 1;
             c.c = static_cast<uint8_t*>(a.dw) + first * a.lddw * static_cast<int64_t>(dtype_size(a.dw_dtype));
             c.ldc = a.lddw;

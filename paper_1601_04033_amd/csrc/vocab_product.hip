@@ -22,8 +22,6 @@ namespace {
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
-constexpr int kMaxSplits = 16;
-
 #if defined(__HIP_DEVICE_COMPILE__)
 
 template <typename T> __device__ __forceinline__ v16f mfma(const v4i& a, const v4i& b, const v16f& c);
@@ -125,8 +123,8 @@ __device__ __forceinline__ void gradient(const v16f (&acc)[N][N], const VocabPro
         b[j] = row.b * up;
     }
     const int terms = p.dz_terms > p.dzt_terms ? p.dz_terms : p.dzt_terms;
-    uint16_t* dz = p.dz + (n + N * (lane & 31)) * p.dz_terms * p.classes + m;
-    uint16_t* dzt = p.dzt + m * p.dzt_terms * p.padded + n + N * (lane & 31);
+    uint16_t* dz = p.dz + (n + N * (lane & 31)) * p.ld_dz + m;
+    uint16_t* dzt = p.dzt + m * p.ld_dzt + n + N * (lane & 31);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int first = 4 * N * (2 * q + (lane >> 5));    // of the 4 N classes
@@ -157,7 +155,7 @@ __device__ __forceinline__ void gradient(const v16f (&acc)[N][N], const VocabPro
                     Pack<uint16_t, N> x;
 #pragma unroll
                     for (int j = 0; j < N; ++j) x.v[j] = w[k][j];
-                    store_pack(dzt + ((first + k) * static_cast<int64_t>(p.dzt_terms) + t) * p.padded, x);
+                    store_pack(dzt + (first + k) * p.ld_dzt + t * p.padded, x);
                 }
             }
             if (t < p.dz_terms) {
@@ -166,11 +164,25 @@ __device__ __forceinline__ void gradient(const v16f (&acc)[N][N], const VocabPro
                     Pack<uint16_t, 4 * N> x;
 #pragma unroll
                     for (int k = 0; k < 4 * N; ++k) x.v[k] = w[k][j];
-                    store_pack(dz + (static_cast<int64_t>(j) * p.dz_terms + t) * p.classes + first, x);
+                    store_pack(dz + j * p.ld_dz + t * p.classes + first, x);
                 }
             }
         }
     }
+}
+
+// Order of a sub-step's instructions for the compiler's scheduler: between
+// matrix instructions go the LDS reads, in the first half, so that they have
+// arrived at its end, and the loads.
+template <int MFMA, int READS, int LOADS, int I = 0> __device__ __forceinline__ void order()
+{
+    constexpr int kMfma = 0x8, kDsRead = 0x100, kVmem = 0x20, kHalf = MFMA / 2;
+    constexpr int kReads = I < kHalf ? (I + 1) * READS / kHalf - I * READS / kHalf : 0;
+    constexpr int kLoads = (I + 1) * LOADS / MFMA - I * LOADS / MFMA;
+    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(kDsRead, kReads, 0);
+    if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(kVmem, kLoads, 0);
+    if constexpr (I + 1 < MFMA) order<MFMA, READS, LOADS, I + 1>();
 }
 
 #endif
@@ -236,22 +248,33 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-    // Loads go on from stage to stage: the pairs of terms of a block of the
-    // contraction, then the next block.  Past the last stage it is loaded again.
+    // Loads go on from stage to stage, a pair of terms over the contraction and
+    // then the next pair.  Past the last it is loaded again.  The pairs come
+    // with the smallest first: the matrix instruction aligns its 16 products
+    // with the sum and cuts off what lies 3 bits below the sum's last, so the
+    // large sums are to be met as few times as there are blocks (fp32, 1,024
+    // rows: dx off by 3.3e-6 with a block's pairs together, 1.4e-6 so).
     int at = 0, pair = 0;
-    auto load = [&](uint8_t* a, uint8_t* b) {
-        const int at_a = at + static_cast<int>(p.terms_a >> (2 * pair) & 3u) * p.a.plane;
-        const int at_b = at + static_cast<int>(p.terms_b >> (2 * pair) & 3u) * p.b.plane;
-#pragma unroll
-        for (int q = 0; q < G::kLoadsA; ++q)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ga, (lds_ptr)(a + (q * 4 + wave) * 1024), 16, off_a[q], at_a, 0, 0);
-#pragma unroll
-        for (int q = 0; q < G::kLoadsB; ++q)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(gb, (lds_ptr)(b + (q * 4 + wave) * 1024), 16, off_b[q], at_b, 0, 0);
-        if (pair + 1 < p.terms) ++pair;
-        else if (at + kBytes < own_blocks * kBytes) {
+    constexpr int kLoads = G::kLoadsA + G::kLoadsB;
+    constexpr int kFirst = kLoads / 2;
+    int at_a, at_b;
+    auto next = [&]() {
+        at_a = at + static_cast<int>(p.terms_a >> (2 * pair) & 3u) * p.a.plane;
+        at_b = at + static_cast<int>(p.terms_b >> (2 * pair) & 3u) * p.b.plane;
+        if (at + kBytes < own_blocks * kBytes) {
             at += kBytes;
-            pair = 0;
+        } else if (pair + 1 < p.terms) {
+            ++pair;
+            at = 0;
+        }
+    };
+    auto load = [&](uint8_t* a, uint8_t* b, int from, int to) {
+#pragma unroll
+        for (int q = from; q < to; ++q) {
+            if (q < G::kLoadsA)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ga, (lds_ptr)(a + (q * 4 + wave) * 1024), 16, off_a[q], at_a, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(gb, (lds_ptr)(b + ((q - G::kLoadsA) * 4 + wave) * 1024), 16, off_b[q - G::kLoadsA], at_b, 0, 0);
         }
     };
     v4i fa[2][N], fb[2][N];
@@ -274,24 +297,31 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
 #pragma unroll
         for (int u = 0; u < 3; ++u) {
             read((u + 1) & 1, a, b, u + 1);
+            if (u == 0) load(an, bn, kFirst, kLoads);
             multiply(u & 1);
-            interleave<N * N, 2 * N, 0, 0>();
+            if (u == 0) order<N * N, 2 * N, kLoads - kFirst>();
+            else order<N * N, 2 * N, 0>();
             __builtin_amdgcn_sched_barrier(0);
         }
         // The next stage has arrived and every wave holds the rest of this one
-        // in registers: its LDS is free for the stage after next.
+        // in registers: its LDS is free for the stage after next.  Its loads go
+        // over two sub-steps: at once they are more than the CU takes in while
+        // one is multiplied (8,192 x 16,384 x 4,096 906 against 850 us).
         __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
+        next();
         read(0, an, bn, 0);
-        load(a, b);
+        load(a, b, 0, kFirst);
         multiply(1);
-        interleave<N * N, 2 * N, G::kLoadsA + G::kLoadsB, 0>();
+        order<N * N, 2 * N, kFirst>();
         __builtin_amdgcn_sched_barrier(0);
     };
     if (steps > 0) {
-        load(a0, b0);
-        load(a1, b1);
+        next();
+        load(a0, b0, 0, kLoads);
+        next();
+        load(a1, b1, 0, kFirst);
         __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0)
         __syncthreads();
         read(0, a0, b0, 0);
@@ -342,15 +372,32 @@ template <typename T, int W> hipError_t launch_what(int what, const VocabProduct
 
 }  // namespace
 
-int vocab_wave(int64_t m, int64_t n) { return count(m, 256) * count(n, 256) >= 192 ? 128 : 64; }
-
-int vocab_splits(int64_t m, int64_t n, int64_t stages)
+// Microseconds of a tile's blocks: of a stage with as many blocks on a CU as
+// fit (of 128 x 128 two, of 256 x 256 one), of a stage of a 128 x 128 tile
+// alone on its CU, and of what a tile costs besides (256 tiles of 256 x 256 over
+// 4,096 take 104 us, over 1,024 32; of 128 x 128 47 and 13; 512 of those 62 and
+// 18; stores add 4 to 8).  A split contraction's parts are read again, at
+// about 4 TB/s.
+VocabPlan vocab_plan(int64_t m, int64_t n, int64_t stages, int most_splits)
 {
-    const int64_t side = 2 * vocab_wave(m, n), tiles = count(m, side) * count(n, side);
-    int64_t s = 256 / tiles;
-    if (s > stages / 8) s = stages / 8;
-    if (s > kMaxSplits) s = kMaxSplits;
-    return s < 1 ? 1 : static_cast<int>(s);
+    VocabPlan best = {64, 1};
+    double least = 0.0;
+    for (const int wave : {128, 64}) {
+        const int64_t tiles = count(m, 2 * wave) * count(n, 2 * wave);
+        const double stage = wave == 128 ? 1.5 : 0.9, alone = wave == 128 ? 1.5 : 0.72, besides = wave == 128 ? 12.0 : 6.0;
+        for (int s = 1; s <= most_splits && s <= stages; ++s) {
+            const int64_t blocks = tiles * s, slots = wave == 128 ? 256 : 512, rest = blocks % slots;
+            const double each = static_cast<double>(count(stages, s));
+            double t = static_cast<double>(blocks / slots) * (stage * each + besides);
+            if (rest > 0) t += (rest <= 256 ? alone : stage) * each + besides;
+            if (s > 1) t += 4.0 * s * static_cast<double>(m) * static_cast<double>(n) / 4e6;
+            if (least == 0.0 || t < least) {
+                least = t;
+                best = VocabPlan{wave, s};
+            }
+        }
+    }
+    return best;
 }
 
 hipError_t launch_vocab_product(int what, const VocabProduct& p, int64_t m, int64_t n, hipStream_t s)
