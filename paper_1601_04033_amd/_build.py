@@ -13,7 +13,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfasgd.so")
 SOURCES = ["fasgd_api.hip", "dense.hip", "bfasgd.hip", "segments.hip", "pushes.hip", "selfcheck.hip", "anchor.hip",
            "client_api.hip", "dropout.hip", "residual_norm.hip",
-           "fp8_quantize.hip", "fp8_product.hip", "fp8_few.hip", "vocab_product.hip", "vocab_loss.hip"]
+           "fp8_quantize.hip", "fp8_product.hip", "fp8_few.hip", "vocab_product.hip", "vocab_loss.hip",
+           "vocab_direct.hip"]
 
 MARSHAL = os.path.join(PKG, "_marshal.so")
 

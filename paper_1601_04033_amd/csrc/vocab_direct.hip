@@ -1,0 +1,565 @@
+// The losses over a large vocabulary for few rows and for small problems: x, W
+// and the gradients as they lie, without gathering, laying out or 16-bit terms.
+//
+// A few rows against a large vocabulary are bound by reading W (twice forward
+// and backward, and once more for dx) and writing dW; a small problem by its
+// chain of launches.  So there are two a pass or three, the matrix instruction
+// takes operands from global memory straight into registers (16 x 16 tiles:
+// 16-bit types as they are, fp32 by the fp32 instruction), and the gradient of
+// the logits is held in fp32.
+#include <float.h>
+
+#include "fp8_math.hpp"
+#include "vocab_rows.hpp"
+
+namespace fasgd {
+namespace {
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+
+// ---- logits: 16 rows by 16 classes at a time
+
+// A block's 8 waves each take a part of the contraction and keep the rows' part
+// of x in registers; W goes by, 16 classes a group.  The parts' sums meet in LDS,
+// where a wave each joins a group's, in order.
+constexpr int kLogitThreads = 512, kLogitWaves = 8;
+
+struct Direct {
+    int64_t groups_each;    // groups of 16 classes a block
+    int64_t padded;         // rows to a multiple of 16
+    float2* partial;        // [gridDim.x][padded]
+    float* partial_sum;
+    float *dz, *dzt;        // fp32 [rows][vocab], [vocab][padded]
+    int32_t* used;          // [padded]
+};
+
+// 16 bytes of a lane: what it holds of an operand's row per step of 64 bytes a row.
+template <typename T> struct Chunk {
+    static constexpr int kValues = 16 / sizeof(T);      // per lane
+    static constexpr int kStep = 4 * kValues;           // per row
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+
+__device__ __forceinline__ v4f tile(const bf16*, const v4i& a, const v4i& b, const v4f& c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f tile(const f16*, const v4i& a, const v4i& b, const v4f& c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f tile(const float*, const v4i& a, const v4i& b, v4f c)
+{
+    const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+    return c;
+}
+
+// 16 bytes from value k on of a row of `cols`; zeros past its end.
+template <typename T> __device__ __forceinline__ v4i load_chunk(const T* row, int k, int cols)
+{
+    Pack<T, Chunk<T>::kValues> p;
+    if (k + Chunk<T>::kValues <= cols) {
+        p = load_pack<T, Chunk<T>::kValues>(row + k);
+    } else {
+#pragma unroll
+        for (int e = 0; e < Chunk<T>::kValues; ++e) p.v[e] = k + e < cols ? row[k + e] : from_float<T>(0.0f);
+    }
+    return __builtin_bit_cast(v4i, p);
+}
+
+#endif
+
+// NK: steps of a wave at most.  GRADIENT: dz of the rows, else their statistics
+// and the picked logits.
+template <typename T, int NK, bool GRADIENT>
+__global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int kBatch = 8;       // groups between two meetings of the waves
+    constexpr int kLoads = NK < 8 ? NK : 8, kParts = NK / kLoads;       // of a group: loads in flight, times
+    constexpr int kSequence = kParts == 1 ? 2 : kParts;                 // loads with a buffer each of two
+    __shared__ v4f part[kLogitWaves][kBatch][64];
+    __shared__ float table[16][kBatch * 16 + 4];
+    __shared__ float2 stat[kLogitWaves][16];
+    __shared__ float stat_sum[kLogitWaves][16];
+    __shared__ VocabRow coefficient[16];
+    __shared__ Teacher teachers[16];
+    __shared__ int used[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t r0 = static_cast<int64_t>(blockIdx.y) * 16;
+    const int cols = static_cast<int>(a.cols);
+    const int rows = a.rows - r0 < 16 ? static_cast<int>(a.rows - r0) : 16;
+
+    // Which rows take part, and their coefficients: two rows a wave.
+    for (int i = wave * 2; i < wave * 2 + 2; ++i) {
+        const int64_t r = r0 + i;
+        bool any = false;
+        if (i < rows)
+            for (int k = lane; k < a.entries; k += 64) any |= counts(a, r * a.entries + k);
+        any = __ballot(any) != 0;
+        VocabRow c = {0.0f, 0.0f, 0.0f, 0.0f};
+        Teacher t = {0.0f, 0.0f};
+        if (GRADIENT && any) {
+            t = teacher_of(a, r, lane);
+            c = coefficients_of(a, r, t, lane);
+        }
+        if (lane == 0) {
+            used[i] = any;
+            coefficient[i] = c;
+            teachers[i] = t;
+            if (GRADIENT && blockIdx.x == 0) d.used[r] = any;
+        }
+    }
+    __syncthreads();
+
+    const int steps = (cols + Chunk<T>::kStep - 1) / Chunk<T>::kStep, each = (steps + kLogitWaves - 1) / kLogitWaves;
+    const int first = wave * each;
+    const int own = steps - first < each ? (steps - first < 0 ? 0 : steps - first) : each;     // <= NK
+    const int k0 = first * Chunk<T>::kStep + (lane >> 4) * Chunk<T>::kValues;
+    // the steps whose 64 bytes all lie within the rows
+    const int whole = cols / Chunk<T>::kStep - first;
+
+    v4i x[NK];
+    {
+        const int i = lane & 15;
+        const bool in = i < rows && used[i] != 0;
+        const T* row = static_cast<const T*>(a.x) + (r0 + (in ? i : 0)) * a.ldx;
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+            x[s] = v4i{0, 0, 0, 0};
+            if (s < own && in) x[s] = load_chunk<T>(row, k0 + s * Chunk<T>::kStep, cols);
+        }
+    }
+    const int64_t groups = (a.vocab + 15) / 16, g0 = static_cast<int64_t>(blockIdx.x) * d.groups_each;
+    const int64_t g1 = g0 + d.groups_each < groups ? g0 + d.groups_each : groups;
+
+    v4i w[2][kLoads];
+    auto load = [&](int buffer, int64_t group, int at) {
+        const int64_t c = group * 16 + (lane & 15);
+        const T* row = static_cast<const T*>(a.w) + (c < a.vocab ? c : a.vocab - 1) * a.ldw;
+#pragma unroll
+        for (int s = 0; s < kLoads; ++s) {
+            const int step = at * kLoads + s;
+            if (step < whole && step < own) w[buffer][s] = __builtin_bit_cast(v4i, load_pack<T, Chunk<T>::kValues>(row + k0 + step * Chunk<T>::kStep));
+            else if (step < own) w[buffer][s] = load_chunk<T>(row, k0 + step * Chunk<T>::kStep, cols);
+            else w[buffer][s] = v4i{0, 0, 0, 0};
+        }
+    };
+    const float c = a.scale * kLog2e;
+    float top = -FLT_MAX, sum = 0.0f, all = 0.0f;      // of this lane's row and the classes it sees
+    v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (g0 < g1) load(0, g0, 0);
+    for (int64_t b0 = g0; b0 < g1; b0 += kBatch) {
+        const int batch = static_cast<int>(g1 - b0 < kBatch ? g1 - b0 : kBatch);
+        for (int g = 0; g < batch; g += kParts == 1 ? 2 : 1) {
+#pragma unroll
+            for (int s = 0; s < kSequence; ++s) {
+                const int here = kParts == 1 ? g + s : g, at = kParts == 1 ? 0 : s;
+                // the next loads: of this group's rest, or of the next group
+                const bool last = kParts == 1 || s + 1 == kParts;
+                const int64_t next = b0 + here + (last ? 1 : 0);
+                if (next < g1) load((s + 1) & 1, next, last ? 0 : s + 1);
+                if (here < batch) {
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) acc = tile(static_cast<const T*>(nullptr), w[s & 1][i], x[at * kLoads + i], acc);
+                    if (last) {
+                        part[wave][here][lane] = acc;
+                        acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        if (wave < batch) {     // a group each: lane l has row l % 16 and classes 4 (l / 16) on
+            v4f z = part[0][wave][lane];
+#pragma unroll
+            for (int i = 1; i < kLogitWaves; ++i) z += part[i][wave][lane];
+            const int64_t first_class = (b0 + wave) * 16 + 4 * (lane >> 4);
+            const int left = a.vocab - first_class < 4 ? static_cast<int>(a.vocab - first_class) : 4;
+            if (GRADIENT) {
+                const VocabRow row = coefficient[lane & 15];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    table[lane & 15][wave * 16 + 4 * (lane >> 4) + e] =
+                        used[lane & 15] ? __builtin_fmaf(row.f, power(__builtin_fmaf(z[e], c, -row.l)), -row.b) : 0.0f;
+            } else {
+                float most = -FLT_MAX;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    table[lane & 15][wave * 16 + 4 * (lane >> 4) + e] = z[e];
+                    all += e < left ? z[e] : 0.0f;
+                    most = e < left ? fmaxf(most, z[e] * c) : most;
+                }
+                const float next = fmaxf(top, most);
+                sum *= power(top - next);
+                top = next;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += e < left ? power(__builtin_fmaf(z[e], c, -top)) : 0.0f;
+            }
+        }
+        __syncthreads();
+        // The entries among the batch's classes.
+        for (int at = threadIdx.x; at < rows * a.entries; at += kLogitThreads) {
+            const int i = at / a.entries, k = at - i * a.entries;
+            const int64_t here = (r0 + i) * a.entries + k, cls = a.index[here] - b0 * 16;
+            if (cls < 0 || cls >= batch * 16 || !counts(a, here)) continue;
+            if (GRADIENT) {
+                float z;
+                if (entry_gradient(a, coefficient[i], teachers[i], r0 + i, k, &z)) table[i][cls] = z;
+            } else {
+                a.picked[here] = table[i][cls] * a.scale;
+            }
+        }
+        if (GRADIENT) {
+            __syncthreads();
+            const int64_t c0 = b0 * 16;
+            const int n = a.vocab - c0 < batch * 16 ? static_cast<int>(a.vocab - c0) : batch * 16;
+            if (d.dz)
+                for (int at = threadIdx.x; at < rows * kBatch * 16; at += kLogitThreads) {
+                    const int i = at / (kBatch * 16), k = at % (kBatch * 16);
+                    if (k < n) d.dz[(r0 + i) * a.vocab + c0 + k] = table[i][k];
+                }
+            if (d.dzt)
+                for (int at = threadIdx.x; at < n * 16; at += kLogitThreads) d.dzt[(c0 + at / 16) * d.padded + r0 + at % 16] = table[at % 16][at / 16];
+        }
+        __syncthreads();
+    }
+    if (GRADIENT) return;
+    // statistics: the lanes of a row, then the waves, in order
+    const float most = larger_of(top, 16), m2 = larger_of(most, 32);
+    sum *= power(top - m2);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    all += __shfl_xor(all, 16);
+    all += __shfl_xor(all, 32);
+    if (lane < 16) {
+        stat[wave][lane] = make_float2(m2, sum);
+        stat_sum[wave][lane] = all;
+    }
+    __syncthreads();
+    if (threadIdx.x < 16) {
+        float m = -FLT_MAX, s = 0.0f, t = 0.0f;
+        for (int i = 0; i < kLogitWaves; ++i) m = fmaxf(m, stat[i][threadIdx.x].x);
+        for (int i = 0; i < kLogitWaves; ++i) {
+            s += stat[i][threadIdx.x].y * power(stat[i][threadIdx.x].x - m);
+            t += stat_sum[i][threadIdx.x];
+        }
+        d.partial[blockIdx.x * d.padded + r0 + threadIdx.x] = make_float2(m, s);
+        if (d.partial_sum) d.partial_sum[blockIdx.x * d.padded + r0 + threadIdx.x] = t;
+    }
+#endif
+}
+
+// ---- dx and dW: c[r][n] = sum_k a[k][r] b[k][n], both along k
+
+// A wave owns 16 rows and 128 columns: lane l holds b's columns 8 (l % 16) on of
+// row l / 16 of each 4 of k, and so 8 neighbouring columns of 4 rows of c.
+struct Thin {
+    const float* a;         // [k][lda]
+    int64_t lda, ldb, rows, cols, k, k_each;        // k_each: of a split, a multiple of 4
+    const void* b;
+    const int32_t* used_k;  // b's rows that take part (NULL: all)
+    void* c;                // one split: the output; else fp32 [split][rows padded to 16][cols padded to 128]
+    int64_t ldc;
+    const int32_t* used_r;  // rows of c that take part, zeros for the others (NULL: all)
+    float by;
+    int32_t add, splits, row_tiles;     // row_tiles: that a wave goes through
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+// 8 values of a row from column n on; zeros past its end.
+template <typename T> __device__ __forceinline__ Pack<T, 8> load_eight(const T* row, int64_t n, int64_t cols)
+{
+    if (n + 8 <= cols) return load_pack<T, 8>(row + n);
+    Pack<T, 8> p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p.v[e] = n + e < cols ? row[n + e] : from_float<T>(0.0f);
+    return p;
+}
+#endif
+
+// HELD: k is at most 16, b's values stay in registers over the row tiles.
+template <typename T, typename OUT, bool HELD> __global__ __launch_bounds__(256) void thin(Thin p)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int lane = threadIdx.x & 63;
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) * 128 + 8 * (lane & 15);
+    if (n - 8 * (lane & 15) >= p.cols) return;
+    const int64_t k0 = blockIdx.z * p.k_each, k1 = k0 + p.k_each < p.k ? k0 + p.k_each : p.k;
+    auto take_b = [&](int64_t k) {
+        if (k < k1 && (!p.used_k || p.used_k[k])) return load_eight<T>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
+        Pack<T, 8> v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.v[e] = from_float<T>(0.0f);
+        return v;
+    };
+    Pack<T, 8> held[HELD ? 4 : 1];
+    if constexpr (HELD) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) held[s] = take_b(k0 + 4 * s + (lane >> 4));
+    }
+    for (int t = 0; t < p.row_tiles; ++t) {
+        const int64_t r0 = (static_cast<int64_t>(blockIdx.y) * p.row_tiles + t) * 16, r = r0 + (lane & 15);
+        if (r0 >= p.rows) return;
+        v4f acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        auto take_a = [&](int64_t k) { return k < k1 && r < p.rows ? p.a[k * p.lda + r] : 0.0f; };
+        auto multiply = [&](float x, const Pack<T, 8>& v) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, to_float(v.v[e]), acc[e], 0, 0, 0);
+        };
+        if constexpr (HELD) {
+            float x[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) x[s] = take_a(k0 + 4 * s + (lane >> 4));
+#pragma unroll
+            for (int s = 0; s < 4; ++s) multiply(x[s], held[s]);
+        } else {
+            constexpr int kFlight = 8;      // loads on their way at once
+            for (int64_t kb = k0; kb < k1; kb += 4 * kFlight) {
+                float x[kFlight];
+                Pack<T, 8> v[kFlight];
+#pragma unroll
+                for (int s = 0; s < kFlight; ++s) {
+                    x[s] = take_a(kb + 4 * s + (lane >> 4));
+                    v[s] = take_b(kb + 4 * s + (lane >> 4));
+                }
+#pragma unroll
+                for (int s = 0; s < kFlight; ++s) multiply(x[s], v[s]);
+            }
+        }
+        if (p.splits > 1) {
+            float* out = static_cast<float*>(p.c) + (blockIdx.z * ((p.rows + 15) / 16 * 16) + r0) * p.ldc + n;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                Pack<float, 8> o;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o.v[e] = acc[e][i];
+                store_pack(out + (4 * (lane >> 4) + i) * p.ldc, o);
+            }
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = r0 + 4 * (lane >> 4) + i;
+            if (row >= p.rows) continue;
+            const bool in = !p.used_r || p.used_r[row];
+            OUT* out = static_cast<OUT*>(p.c) + row * p.ldc + n;
+            if (n + 8 <= p.cols) {
+                Pack<OUT, 8> o;
+                if (p.add) o = load_pack<OUT, 8>(out);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float v = in ? acc[e][i] * p.by : 0.0f;
+                    o.v[e] = from_float<OUT>(p.add ? to_float(o.v[e]) + v : v);
+                }
+                store_pack(out, o);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (n + e < p.cols) {
+                        const float v = in ? acc[e][i] * p.by : 0.0f;
+                        out[e] = from_float<OUT>(p.add ? to_float(out[e]) + v : v);
+                    }
+            }
+        }
+    }
+#endif
+}
+
+// dx from the splits' parts, in order: 4 columns a thread.
+template <typename T> __global__ __launch_bounds__(256) void join(Thin p, T* out, int64_t ld, const int32_t* used)
+{
+    const int64_t r = blockIdx.y, n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (n >= p.cols) return;
+    const float* c = static_cast<const float*>(p.c) + r * p.ldc + n;
+    const int64_t apart = (p.rows + 15) / 16 * 16 * p.ldc;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 8
+    for (int k = 0; k < p.splits; ++k) {
+        const Pack<float, 4> x = load_pack<float, 4>(c + k * apart);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += x.v[e];
+    }
+    const bool in = used[r] != 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (n + e < p.cols) out[r * ld + n + e] = from_float<T>(in ? s[e] * p.by : 0.0f);
+}
+
+int64_t count(int64_t x, int64_t side) { return (x + side - 1) / side; }
+
+// ---- the host's side
+
+struct Layout {
+    int64_t padded, cols_padded, groups_each, blocks;
+    int splits;
+    int64_t k_each;
+    int64_t used, dz, dzt, sums, partial, partial_sum, bytes;
+};
+
+Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, bool backward)
+{
+    Layout l = {};
+    l.padded = count(rows, 16) * 16;
+    l.cols_padded = count(cols, 128) * 128;
+    // about two blocks a CU in all, each with whole groups of classes
+    const int64_t groups = count(vocab, 16), row_tiles = l.padded / 16;
+    l.groups_each = count(groups * row_tiles, 512);
+    if (row_tiles == 1 && groups > 512) l.groups_each = count(groups, 256);
+    l.blocks = count(groups, l.groups_each);
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at = (at + bytes + 255) / 256 * 256;
+        return here;
+    };
+    l.used = take(4 * l.padded);
+    if (backward) {
+        // dx: waves for 16 rows x 128 columns, the classes split to make about 2,048 of them
+        const int64_t waves = row_tiles * l.cols_padded / 128;
+        int64_t s = 2048 / waves;
+        if (s > count(vocab, 32)) s = count(vocab, 32);
+        if (s < 1) s = 1;
+        l.k_each = count(count(vocab, s), 4) * 4;
+        l.splits = static_cast<int>(count(vocab, l.k_each));
+        l.dz = take(4 * rows * vocab);
+        l.dzt = take(4 * l.padded * vocab);
+        l.sums = take(l.splits > 1 ? 4 * l.splits * l.padded * l.cols_padded : 0);
+    } else {
+        l.partial = take(8 * l.blocks * l.padded);
+        l.partial_sum = take(4 * l.blocks * l.padded);
+    }
+    l.bytes = at;
+    return l;
+}
+
+template <typename T, bool GRADIENT> hipError_t launch_logits(const VocabArgs& a, const Direct& d, int64_t blocks, hipStream_t s)
+{
+    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(d.padded / 16));
+    const int64_t each = count(count(a.cols, 64 / static_cast<int64_t>(sizeof(T))), kLogitWaves);
+    if (each <= 2) logits<T, 2, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
+    else if (each <= 8) logits<T, 8, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
+    else if (each <= 16) logits<T, 16, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
+    else logits<T, 32, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
+    return hipGetLastError();
+}
+
+template <bool GRADIENT> hipError_t launch_logits_of(const VocabArgs& a, const Direct& d, int64_t blocks, hipStream_t s)
+{
+    if (a.dtype == DTYPE_F32) return launch_logits<float, GRADIENT>(a, d, blocks, s);
+    if (a.dtype == DTYPE_BF16) return launch_logits<bf16, GRADIENT>(a, d, blocks, s);
+    return launch_logits<f16, GRADIENT>(a, d, blocks, s);
+}
+
+template <typename T, typename OUT> void launch_thin(const Thin& p, hipStream_t s)
+{
+    const dim3 grid(static_cast<unsigned>(count(p.cols, 512)), static_cast<unsigned>(count(count(p.rows, 16), p.row_tiles)),
+                    static_cast<unsigned>(p.splits));
+    if (p.k <= 16) thin<T, OUT, true><<<grid, 256, 0, s>>>(p);
+    else thin<T, OUT, false><<<grid, 256, 0, s>>>(p);
+}
+
+template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, uint8_t* base, hipStream_t s)
+{
+    const int32_t* used = reinterpret_cast<int32_t*>(base + l.used);
+    if (a.dx) {
+        Thin p = {};
+        p.a = reinterpret_cast<float*>(base + l.dzt);
+        p.lda = l.padded;
+        p.b = a.w;
+        p.ldb = a.ldw;
+        p.rows = a.rows;
+        p.cols = a.cols;
+        p.k = a.vocab;
+        p.k_each = l.k_each;
+        p.splits = l.splits;
+        p.row_tiles = 1;
+        p.by = a.scale;
+        p.c = l.splits > 1 ? base + l.sums : static_cast<uint8_t*>(a.dx);
+        p.ldc = l.splits > 1 ? l.cols_padded : a.lddx;
+        p.used_r = used;
+        launch_thin<T, T>(p, s);
+        VOCAB_TRY(hipGetLastError());
+        if (l.splits > 1) {
+            const dim3 grid(static_cast<unsigned>(count(a.cols, 1024)), static_cast<unsigned>(a.rows));
+            join<T><<<grid, 256, 0, s>>>(p, static_cast<T*>(a.dx), a.lddx, used);
+            VOCAB_TRY(hipGetLastError());
+        }
+    }
+    if (a.dw) {
+        Thin p = {};
+        p.a = reinterpret_cast<float*>(base + l.dz);
+        p.lda = a.vocab;
+        p.b = a.x;
+        p.ldb = a.ldx;
+        p.rows = a.vocab;
+        p.cols = a.cols;
+        p.k = a.rows;
+        p.k_each = l.padded;
+        p.splits = 1;
+        p.used_k = used;
+        p.by = a.scale;
+        p.add = a.accumulate;
+        p.c = a.dw;
+        p.ldc = a.lddw;
+        // a wave's row tiles: so many that about 8,192 waves are left
+        const int64_t tiles = count(a.vocab, 16), waves = tiles * count(a.cols, 128);
+        const int64_t each = waves / 8192, least = count(tiles, 32768);     // blocks along y
+        p.row_tiles = static_cast<int32_t>(each < least ? least : each);
+        if (a.dw_dtype == DTYPE_F32) launch_thin<T, float>(p, s);
+        else launch_thin<T, T>(p, s);
+        VOCAB_TRY(hipGetLastError());
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+// 16 rows, or small sums, with a row of W in the registers of 8 waves.
+bool vocab_direct(int64_t rows, int64_t cols, int64_t vocab, int dtype)
+{
+    if (cols * static_cast<int64_t>(dtype_size(dtype)) > 16384) return false;
+    return (rows <= 16 && rows * vocab <= (int64_t(1) << 26)) || (rows <= 1024 && rows * vocab <= (int64_t(1) << 24) && rows * vocab * cols <= (int64_t(1) << 28));
+}
+
+size_t vocab_direct_bytes(int64_t rows, int64_t cols, int64_t vocab, bool backward)
+{
+    return static_cast<size_t>(layout_of(rows, cols, vocab, backward).bytes);
+}
+
+hipError_t launch_vocab_direct_forward(const VocabArgs& a, hipStream_t s)
+{
+    const Layout l = layout_of(a.rows, a.cols, a.vocab, false);
+    uint8_t* base = static_cast<uint8_t*>(a.workspace);
+    Direct d = {};
+    d.groups_each = l.groups_each;
+    d.padded = l.padded;
+    d.partial = reinterpret_cast<float2*>(base + l.partial);
+    d.partial_sum = a.smoothing != 0.0f ? reinterpret_cast<float*>(base + l.partial_sum) : nullptr;
+    VOCAB_TRY(launch_logits_of<false>(a, d, l.blocks, s));
+    finish<<<static_cast<unsigned>(count(a.rows, 8)), kBlock, 0, s>>>(a, nullptr, nullptr, d.partial, d.partial_sum, l.blocks, l.padded);
+    return hipGetLastError();
+}
+
+hipError_t launch_vocab_direct_backward(const VocabArgs& a, hipStream_t s)
+{
+    const Layout l = layout_of(a.rows, a.cols, a.vocab, true);
+    uint8_t* base = static_cast<uint8_t*>(a.workspace);
+    Direct d = {};
+    d.groups_each = l.groups_each;
+    d.padded = l.padded;
+    d.used = reinterpret_cast<int32_t*>(base + l.used);
+    d.dz = a.dw ? reinterpret_cast<float*>(base + l.dz) : nullptr;
+    d.dzt = a.dx ? reinterpret_cast<float*>(base + l.dzt) : nullptr;
+    VOCAB_TRY(launch_logits_of<true>(a, d, l.blocks, s));
+    if (a.dtype == DTYPE_F32) return backward<float>(a, l, base, s);
+    if (a.dtype == DTYPE_BF16) return backward<bf16>(a, l, base, s);
+    return backward<f16>(a, l, base, s);
+}
+
+}  // namespace fasgd

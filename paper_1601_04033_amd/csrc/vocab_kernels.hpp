@@ -40,6 +40,12 @@ size_t vocab_workspace_bytes(int64_t rows, int64_t cols, int64_t vocab, int dtyp
 hipError_t launch_vocab_forward(const VocabArgs& a, hipStream_t s);
 hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s);
 
+// Few rows, and small problems, without operands laid out (vocab_direct.hip).
+bool vocab_direct(int64_t rows, int64_t cols, int64_t vocab, int dtype);
+size_t vocab_direct_bytes(int64_t rows, int64_t cols, int64_t vocab, bool backward);
+hipError_t launch_vocab_direct_forward(const VocabArgs& a, hipStream_t s);
+hipError_t launch_vocab_direct_backward(const VocabArgs& a, hipStream_t s);
+
 // ---- the products (vocab_product.hip)
 
 // An operand: rows of 16-bit terms, each term's values along the contraction

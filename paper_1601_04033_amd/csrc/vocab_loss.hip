@@ -12,97 +12,12 @@
 // largest of dz, with p - q cancelling.  They are computed here from the
 // picked logits, put into dz^T in place of what the tile wrote, and left out
 // of dz: dx takes them in fp32, times the rows of W, at the end.
-#include <float.h>
-
-#include "vocab_kernels.hpp"
+#include "vocab_rows.hpp"
 
 namespace fasgd {
 namespace {
 
-constexpr int kBlock = 256;
-constexpr int kWaves = kBlock / 64;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-
-__device__ __forceinline__ float wave_sum(float x)
-{
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    return x;
-}
-__device__ __forceinline__ float wave_max(float x)
-{
-    for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
-}
-__device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// ---- entries
-
-__device__ __forceinline__ float teacher_logit(const VocabArgs& a, int64_t at)
-{
-    if (a.dtype == DTYPE_F32) return static_cast<const float*>(a.teacher)[at];
-    if (a.dtype == DTYPE_BF16) return to_float(static_cast<const bf16*>(a.teacher)[at]);
-    return to_float(static_cast<const f16*>(a.teacher)[at]);
-}
-
-// Whether entry `at` of the index counts: a class of the vocabulary, to which
-// the teacher gives any weight.
-__device__ __forceinline__ bool counts(const VocabArgs& a, int64_t at)
-{
-    const int64_t i = a.index[at];
-    return i >= 0 && i < a.vocab && !(a.teacher && teacher_logit(a, at) == -INFINITY);
-}
-
-// A row's teacher: weights are exp(s_t t - top) by.  A whole wave's work.
-struct Teacher {
-    float top, by;
-};
-__device__ __forceinline__ Teacher teacher_of(const VocabArgs& a, int64_t row, int lane)
-{
-    if (!a.teacher) return Teacher{0.0f, 1.0f - a.smoothing};
-    if (a.teacher_lse) return Teacher{a.teacher_lse[row], 1.0f};
-    float top = -INFINITY, sum = 0.0f;
-    for (int k = lane; k < a.entries; k += 64)
-        if (counts(a, row * a.entries + k)) top = fmaxf(top, teacher_logit(a, row * a.entries + k) * a.teacher_scale);
-    const float all = wave_max(top);
-    for (int k = lane; k < a.entries; k += 64)
-        if (counts(a, row * a.entries + k))
-            sum += power((teacher_logit(a, row * a.entries + k) * a.teacher_scale - all) * kLog2e);
-    return Teacher{all, 1.0f / wave_sum(sum)};
-}
-// log of the weight before `by`, for an entry that counts
-__device__ __forceinline__ float log_weight(const VocabArgs& a, const Teacher& t, int64_t at)
-{
-    return a.teacher ? teacher_logit(a, at) * a.teacher_scale - t.top : 0.0f;
-}
-__device__ __forceinline__ float weight(const VocabArgs& a, const Teacher& t, int64_t at)
-{
-    return power(log_weight(a, t, at) * kLog2e) * t.by;
-}
-
-// dz at entry k of a row, for the first of those that name a class (the
-// weights of the same class add up); false for the others.
-__device__ __forceinline__ bool entry_gradient(const VocabArgs& a, const VocabRow& row, const Teacher& t, int64_t r,
-                                               int k, float* dz)
-{
-    const int64_t base = r * a.entries;
-    if (!counts(a, base + k)) return false;
-    const int64_t i = a.index[base + k];
-    float q = 0.0f;
-    if (a.entries == 1) {
-        q = weight(a, t, base);
-    } else {
-        for (int j = 0; j < a.entries; ++j) {
-            if (a.index[base + j] != i || !counts(a, base + j)) continue;
-            if (j < k) return false;
-            q += weight(a, t, base + j);
-        }
-    }
-    const float p = power(__builtin_fmaf(a.picked[base + k], kLog2e, -row.l));
-    *dz = __builtin_fmaf(row.f, p, -row.b) - row.g * q;
-    return true;
-}
 
 // ---- rows that take part
 
@@ -254,66 +169,6 @@ template <typename T> __global__ __launch_bounds__(kBlock) void pick(VocabArgs a
     }
 }
 
-// Rows' losses from the statistics of their logits: 8 rows a block, the slots
-// in 32 parts, joined in order.
-__global__ __launch_bounds__(kBlock) void finish(VocabArgs a, const int32_t* list, const int32_t* active, const float2* partial,
-                                                 const float* partial_sum, int64_t slots, int64_t padded)
-{
-    __shared__ float2 part[32][8];
-    __shared__ float part_sum[32][8];
-    __shared__ float lse_of[8], mean_of[8];
-    const int64_t n = *active, first = static_cast<int64_t>(blockIdx.x) * 8;
-    if (first >= n) return;
-    const int at = threadIdx.x & 7, slice = threadIdx.x >> 3;
-    float top = -FLT_MAX, sum = 0.0f, all = 0.0f;
-#pragma unroll 4
-    for (int64_t s = slice; s < slots; s += 32) {
-        const float2 x = partial[s * padded + first + at];
-        const float next = fmaxf(top, x.x);
-        sum = sum * power(top - next) + x.y * power(x.x - next);
-        top = next;
-        if (partial_sum) all += partial_sum[s * padded + first + at];
-    }
-    part[slice][at] = make_float2(top, sum);
-    part_sum[slice][at] = all;
-    __syncthreads();
-    if (threadIdx.x < 8) {
-        top = -FLT_MAX;
-        for (int s = 0; s < 32; ++s) top = fmaxf(top, part[s][at].x);
-        sum = all = 0.0f;
-        for (int s = 0; s < 32; ++s) {
-            sum += part[s][at].y * power(part[s][at].x - top);
-            all += part_sum[s][at];
-        }
-        lse_of[at] = __builtin_fmaf(top, kLn2, logf(sum));
-        mean_of[at] = all * a.scale / static_cast<float>(a.vocab);
-    }
-    __syncthreads();
-    const int lane = threadIdx.x & 63;
-    for (int i = threadIdx.x >> 6; i < 8 && first + i < n; i += kWaves) {
-        const int64_t r = list[first + i];
-        const float lse = lse_of[i];
-        float loss = 0.0f;
-        if (!a.teacher) {
-            if (lane == 0)
-                loss = lse - (1.0f - a.smoothing) * a.picked[r] - a.smoothing * mean_of[i] + a.z_loss * lse * lse;
-        } else {
-            const Teacher t = teacher_of(a, r, lane);
-            const float log_by = logf(t.by);
-            for (int k = lane; k < a.entries; k += 64)
-                if (counts(a, r * a.entries + k)) {
-                    const float lw = log_weight(a, t, r * a.entries + k), q = power(lw * kLog2e) * t.by;
-                    loss += q == 0.0f ? 0.0f : q * (lw + log_by - (a.picked[r * a.entries + k] - lse));
-                }
-            loss = wave_sum(loss);
-        }
-        if (lane == 0) {
-            a.loss[r] = loss;
-            a.lse[r] = lse;
-        }
-    }
-}
-
 // ---- backward
 
 // Coefficients of the rows that take part (a wave each), zeros for the rows
@@ -329,22 +184,8 @@ __global__ __launch_bounds__(kBlock) void coefficients(VocabArgs a, const int32_
     if (at < n) {
         const int64_t r = list[at];
         t = teacher_of(a, r, lane);
-        const float lse = a.lse[r];
-        c.g = a.grad_scale * (a.dloss ? a.dloss[r] : 1.0f);
-        c.l = lse * kLog2e;
-        float most = 0.0f;
-        if (!a.teacher) {
-            c.f = c.g * (1.0f + 2.0f * a.z_loss * lse);
-            c.b = c.g * (a.smoothing / static_cast<float>(a.vocab));
-            most = fabsf(c.g);
-        } else {
-            float q = 0.0f;
-            for (int k = lane; k < a.entries; k += 64)
-                if (counts(a, r * a.entries + k)) q += weight(a, t, r * a.entries + k);
-            q = wave_sum(q);
-            c.f = c.g * q;
-            most = fabsf(c.f);
-        }
+        c = coefficients_of(a, r, t, lane);
+        float most = fabsf(a.teacher ? c.f : c.g);
         most += fabsf(c.f) + fabsf(c.b);
         if (lane == 0) atomicMax(largest, __float_as_uint(most));      // the same in any order
     }
@@ -540,12 +381,6 @@ hipError_t launch_lay_out(const LayOut& l, int dtype, int64_t rows, int64_t cols
     return hipGetLastError();
 }
 
-#define VOCAB_TRY(call)                              \
-    do {                                             \
-        const hipError_t try_error = (call);         \
-        if (try_error != hipSuccess) return try_error; \
-    } while (0)
-
 struct Plan {
     Layout l;
     int32_t *used, *list, *place, *active;
@@ -637,11 +472,13 @@ hipError_t piece_of(const VocabArgs& a, const Plan& p, int64_t first, int64_t n,
 
 size_t vocab_workspace_bytes(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool backward)
 {
+    if (vocab_direct(rows, cols, vocab, dtype)) return vocab_direct_bytes(rows, cols, vocab, backward);
     return static_cast<size_t>(layout_of(rows, cols, vocab, dtype, backward).bytes);
 }
 
 hipError_t launch_vocab_forward(const VocabArgs& a, hipStream_t s)
 {
+    if (vocab_direct(a.rows, a.cols, a.vocab, a.dtype)) return launch_vocab_direct_forward(a, s);
     Plan p;
     VOCAB_TRY(begin(a, false, p, s));
     const Layout& l = p.l;
@@ -675,6 +512,7 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
         else clear<bf16><<<blocks, kBlock, 0, s>>>(static_cast<bf16*>(a.dw), a.lddw, a.vocab, a.cols);
         return hipGetLastError();
     }
+    if (vocab_direct(a.rows, a.cols, a.vocab, a.dtype)) return launch_vocab_direct_backward(a, s);
     Plan p;
     VOCAB_TRY(begin(a, true, p, s));
     const Layout& l = p.l;

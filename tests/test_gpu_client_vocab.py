@@ -101,7 +101,9 @@ def check(c, whole=False, dw=torch.float32, **kw):
 
 
 SIZES = [(1, 1, 1), (1, 8, 2), (3, 5, 7), (1, 128, 300), (2, 127, 129), (17, 64, 1000), (128, 1000, 10), (130, 129, 257),
-         (255, 200, 511), (300, 384, 1025), (64, 1544, 2003)]
+         (255, 200, 511), (300, 384, 1025), (64, 1544, 2003), (16, 4096, 3000), (15, 4000, 4099), (33, 2048, 2100),
+         # beyond what goes without laid out operands
+         (1025, 1, 1), (1030, 5, 7), (1100, 130, 33), (1, 8200, 3), (5, 8193, 70), (130, 8320, 257), (1300, 127, 1000)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -111,7 +113,8 @@ def test_loss(dtype, m, d, V):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("m, d, V, K", [(1, 4, 3, 1), (5, 33, 70, 2), (70, 128, 300, 64), (129, 257, 1030, 65), (33, 64, 5, 130)])
+@pytest.mark.parametrize("m, d, V, K", [(1, 4, 3, 1), (5, 33, 70, 2), (70, 128, 300, 64), (129, 257, 1030, 65), (33, 64, 5, 130),
+                                        (16, 4096, 3001, 64), (1030, 40, 90, 7), (1100, 128, 300, 66), (20, 8200, 130, 20)])
 @pytest.mark.parametrize("whole", [False, True])
 def test_distill(dtype, m, d, V, K, whole):
     """Classes stand in a row more than once; K beyond a wave; more entries than classes."""
@@ -122,7 +125,7 @@ def test_distill(dtype, m, d, V, K, whole):
 @pytest.mark.parametrize("kind", ["loss", "distill"])
 def test_rows_left_out_and_gaps(dtype, kind):
     """NaN in the rows that are left out, between rows and in unused entries reaches nothing."""
-    for m, d, V, gaps in ((200, 72, 333, 5), (513, 136, 520, 8)):
+    for m, d, V, gaps in ((200, 72, 333, 5), (14, 129, 520, 3), (1200, 136, 520, 8), (1100, 256, 300, 8), (40, 8200, 99, 1)):
         c = Case(dtype, m, d, V, 9 if kind == "distill" else 0, out=0.4, gaps=gaps, short=kind == "distill")
         loss, lse, picked, dx, dw = check(c, whole=True)
         left = ~reference(c, True).used
@@ -134,30 +137,34 @@ def test_rows_left_out_and_gaps(dtype, kind):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("kind", ["loss", "distill"])
 def test_every_row_left_out(dtype, kind):
-    c = Case(dtype, 70, 96, 130, 4 if kind == "distill" else 0, out=1.1)
-    loss, lse, picked = forward(c)
-    dx, dw = backward(c, lse, picked)
-    for t in (loss, lse, picked, dx, dw):
-        assert (t == 0).all()
+    for m in (7, 70, 1030):
+        c = Case(dtype, m, 96, 130, 4 if kind == "distill" else 0, out=1.1)
+        loss, lse, picked = forward(c)
+        dx, dw = backward(c, lse, picked)
+        for t in (loss, lse, picked, dx, dw):
+            assert (t == 0).all()
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_options_of_the_loss(dtype):
-    c = Case(dtype, 90, 160, 700, out=0.2)
+@pytest.mark.parametrize("m", [90, 1100])
+def test_options_of_the_loss(dtype, m):
+    c = Case(dtype, m, 160, 700, out=0.2)
     check(c, smoothing=0.1, z_loss=1e-3, logit_scale=0.5, grad_scale=3.0)
     check(c, smoothing=1.0)
     check(c, z_loss=0.1, dw=c.dt)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_options_of_the_distillation(dtype):
-    c = Case(dtype, 90, 160, 700, 20, out=0.2, short=True)
+@pytest.mark.parametrize("m", [90, 1100])
+def test_options_of_the_distillation(dtype, m):
+    c = Case(dtype, m, 160, 700, 20, out=0.2, short=True)
     check(c, False, logit_scale=0.5, teacher_scale=0.25, grad_scale=4.0, dw=c.dt)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_one_gradient_alone_and_accumulation(dtype):
-    c = Case(dtype, 60, 100, 300)
+@pytest.mark.parametrize("m", [12, 60, 1100])
+def test_one_gradient_alone_and_accumulation(dtype, m):
+    c = Case(dtype, m, 100, 300)
     loss, lse, picked, dx, dw = check(c)
     only_x, none = backward(c, lse, picked, dw=None)
     none2, only_w = backward(c, lse, picked, dx=False)
@@ -224,8 +231,9 @@ def test_gradient_is_the_loss_s_slope(kind):
         assert abs(slope - want) <= bound + 2.0 ** -18 * abs(value[0]) / h, (float(slope), float(want), float(bound))
 
 
-def test_on_another_stream_and_captured():
-    c = Case("bf16", 100, 256, 900, out=0.2)
+@pytest.mark.parametrize("m", [100, 1100])
+def test_on_another_stream_and_captured(m):
+    c = Case("bf16", m, 256, 900, out=0.2)
     want = check(c)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
