@@ -88,12 +88,43 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
     __shared__ VocabRow coefficient[16];
     __shared__ Teacher teachers[16];
     __shared__ int used[16];
+    constexpr int kHeld = 2048;
+    __shared__ int32_t cls[kHeld];
+    __shared__ float weights[GRADIENT ? kHeld : 1], total[GRADIENT ? kHeld : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t r0 = static_cast<int64_t>(blockIdx.y) * 16;
     const int cols = static_cast<int>(a.cols);
     const int rows = a.rows - r0 < 16 ? static_cast<int>(a.rows - r0) : 16;
 
-    // Which rows take part, and their coefficients: two rows a wave.
+    const int steps = (cols + Chunk<T>::kStep - 1) / Chunk<T>::kStep, each = (steps + kLogitWaves - 1) / kLogitWaves;
+    const int first = wave * each;
+    const int own = steps - first < each ? (steps - first < 0 ? 0 : steps - first) : each;     // <= NK
+    const int k0 = first * Chunk<T>::kStep + (lane >> 4) * Chunk<T>::kValues;
+    // the steps whose 64 bytes all lie within the rows
+    const int whole = cols / Chunk<T>::kStep - first;
+
+    v4i x[NK];
+    {
+        const int i = lane & 15;
+        const T* row = static_cast<const T*>(a.x) + (r0 + (i < rows ? i : 0)) * a.ldx;
+#pragma unroll
+        for (int s = 0; s < NK; ++s) {
+            if (s < whole && s < own) x[s] = __builtin_bit_cast(v4i, load_pack<T, Chunk<T>::kValues>(row + k0 + s * Chunk<T>::kStep));
+            else if (s < own) x[s] = load_chunk<T>(row, k0 + s * Chunk<T>::kStep, cols);
+            else x[s] = v4i{0, 0, 0, 0};
+        }
+    }
+
+    // The entries: their classes (-1: left out) and, backward, their weights, in
+    // LDS where they fit; which rows take part, and their coefficients, two rows
+    // a wave.
+    const int entries = rows * a.entries;
+    const bool held = entries <= kHeld;
+    if (held)
+        for (int at = threadIdx.x; at < entries; at += kLogitThreads) {
+            const int64_t here = r0 * a.entries + at;
+            cls[at] = counts(a, here) ? static_cast<int32_t>(a.index[here]) : -1;
+        }
     for (int i = wave * 2; i < wave * 2 + 2; ++i) {
         const int64_t r = r0 + i;
         bool any = false;
@@ -106,6 +137,8 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
             t = teacher_of(a, r, lane);
             c = coefficients_of(a, r, t, lane);
         }
+        if (GRADIENT && held && i < rows)
+            for (int k = lane; k < a.entries; k += 64) weights[i * a.entries + k] = any ? weight(a, t, r * a.entries + k) : 0.0f;
         if (lane == 0) {
             used[i] = any;
             coefficient[i] = c;
@@ -114,24 +147,28 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
         }
     }
     __syncthreads();
-
-    const int steps = (cols + Chunk<T>::kStep - 1) / Chunk<T>::kStep, each = (steps + kLogitWaves - 1) / kLogitWaves;
-    const int first = wave * each;
-    const int own = steps - first < each ? (steps - first < 0 ? 0 : steps - first) : each;     // <= NK
-    const int k0 = first * Chunk<T>::kStep + (lane >> 4) * Chunk<T>::kValues;
-    // the steps whose 64 bytes all lie within the rows
-    const int whole = cols / Chunk<T>::kStep - first;
-
-    v4i x[NK];
-    {
-        const int i = lane & 15;
-        const bool in = i < rows && used[i] != 0;
-        const T* row = static_cast<const T*>(a.x) + (r0 + (in ? i : 0)) * a.ldx;
+    if (used[lane & 15] == 0) {     // what a row that is left out holds reaches nothing
 #pragma unroll
-        for (int s = 0; s < NK; ++s) {
-            x[s] = v4i{0, 0, 0, 0};
-            if (s < own && in) x[s] = load_chunk<T>(row, k0 + s * Chunk<T>::kStep, cols);
+        for (int s = 0; s < NK; ++s) x[s] = v4i{0, 0, 0, 0};
+    }
+    if (GRADIENT && held && a.entries > 1) {    // weights of one class of a row add up at its first entry
+        for (int at = threadIdx.x; at < entries; at += kLogitThreads) {
+            const int base = at / a.entries * a.entries, mine = cls[at];
+            float q = 0.0f;
+            bool later = false;
+            for (int j = base; j < base + a.entries; ++j) {
+                const bool same = cls[j] == mine;
+                q += same ? weights[j] : 0.0f;
+                later |= same && j < at;
+            }
+            total[at] = later ? -1.0f : q;
         }
+        __syncthreads();
+        for (int at = threadIdx.x; at < entries; at += kLogitThreads) {
+            weights[at] = total[at];
+            if (total[at] < 0.0f) cls[at] = -1;
+        }
+        __syncthreads();
     }
     const int64_t groups = (a.vocab + 15) / 16, g0 = static_cast<int64_t>(blockIdx.x) * d.groups_each;
     const int64_t g1 = g0 + d.groups_each < groups ? g0 + d.groups_each : groups;
@@ -202,15 +239,18 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
         }
         __syncthreads();
         // The entries among the batch's classes.
-        for (int at = threadIdx.x; at < rows * a.entries; at += kLogitThreads) {
-            const int i = at / a.entries, k = at - i * a.entries;
-            const int64_t here = (r0 + i) * a.entries + k, cls = a.index[here] - b0 * 16;
-            if (cls < 0 || cls >= batch * 16 || !counts(a, here)) continue;
-            if (GRADIENT) {
-                float z;
-                if (entry_gradient(a, coefficient[i], teachers[i], r0 + i, k, &z)) table[i][cls] = z;
+        for (int at = threadIdx.x; at < entries; at += kLogitThreads) {
+            if (held && cls[at] < 0) continue;
+            const int64_t here = r0 * a.entries + at, c0 = (held ? cls[at] : a.index[here]) - b0 * 16;
+            if (c0 < 0 || c0 >= batch * 16 || (!held && !counts(a, here))) continue;
+            const int i = at / a.entries;
+            if (!GRADIENT) {
+                a.picked[here] = table[i][c0] * a.scale;
+            } else if (held) {
+                table[i][c0] = entry_value(coefficient[i], a.picked[here], weights[at]);
             } else {
-                a.picked[here] = table[i][cls] * a.scale;
+                float z;
+                if (entry_gradient(a, coefficient[i], teachers[i], r0 + i, at - i * a.entries, &z)) table[i][c0] = z;
             }
         }
         if (GRADIENT) {
@@ -266,7 +306,7 @@ struct Thin {
     int64_t ldc;
     const int32_t* used_r;  // rows of c that take part, zeros for the others (NULL: all)
     float by;
-    int32_t add, splits, row_tiles;     // row_tiles: that a wave goes through
+    int32_t add, splits, row_tiles;     // row_tiles: that a wave goes through (k of at most 16)
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -281,92 +321,144 @@ template <typename T> __device__ __forceinline__ Pack<T, 8> load_eight(const T* 
 }
 #endif
 
-// HELD: k is at most 16, b's values stay in registers over the row tiles.
-template <typename T, typename OUT, bool HELD> __global__ __launch_bounds__(256) void thin(Thin p)
+// Rows 4 (lane / 16) + i of a tile, the lane's 8 columns.
+template <typename OUT> __device__ __forceinline__ void store_eight(const Thin& p, int64_t row, int64_t n, const float (&v)[8])
+{
+    if (row >= p.rows) return;
+    const bool in = !p.used_r || p.used_r[row];
+    OUT* out = static_cast<OUT*>(p.c) + row * p.ldc + n;
+    Pack<OUT, 8> o;
+    if (n + 8 <= p.cols) {
+        if (p.add) o = load_pack<OUT, 8>(out);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = in ? v[e] * p.by : 0.0f;
+            o.v[e] = from_float<OUT>(p.add ? to_float(o.v[e]) + x : x);
+        }
+        store_pack(out, o);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (n + e < p.cols) {
+            const float x = in ? v[e] * p.by : 0.0f;
+            out[e] = from_float<OUT>(p.add ? to_float(out[e]) + x : x);
+        }
+}
+
+// k of at most 16: b's values stay in registers, the row tiles go by.  Bound by
+// the stores of c.
+template <typename T, typename OUT> __global__ __launch_bounds__(256) void thin_short(Thin p)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int lane = threadIdx.x & 63;
-    const int64_t n = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) * 128 + 8 * (lane & 15);
-    if (n - 8 * (lane & 15) >= p.cols) return;
-    const int64_t k0 = blockIdx.z * p.k_each, k1 = k0 + p.k_each < p.k ? k0 + p.k_each : p.k;
-    auto take_b = [&](int64_t k) {
-        if (k < k1 && (!p.used_k || p.used_k[k])) return load_eight<T>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
+    const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) * 128, n = n0 + 8 * (lane & 15);
+    if (n0 >= p.cols) return;
+    float held[4][8];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const int64_t k = 4 * s + (lane >> 4);
         Pack<T, 8> v;
+        const bool in = k < p.k && (!p.used_k || p.used_k[k]);
+        if (in) v = load_eight<T>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.v[e] = from_float<T>(0.0f);
-        return v;
-    };
-    Pack<T, 8> held[HELD ? 4 : 1];
-    if constexpr (HELD) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) held[s] = take_b(k0 + 4 * s + (lane >> 4));
+        for (int e = 0; e < 8; ++e) held[s][e] = in ? to_float(v.v[e]) : 0.0f;
     }
+    const int64_t t0 = static_cast<int64_t>(blockIdx.y) * p.row_tiles;
+    const float* at = p.a + (lane >> 4) * p.lda + (lane & 15);
+    auto take_a = [&](int64_t r0, float (&x)[4]) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            x[s] = 4 * s + (lane >> 4) < p.k && r0 + (lane & 15) < p.rows ? at[4 * s * p.lda + r0] : 0.0f;
+    };
+    float x[4];
+    take_a(t0 * 16, x);
     for (int t = 0; t < p.row_tiles; ++t) {
-        const int64_t r0 = (static_cast<int64_t>(blockIdx.y) * p.row_tiles + t) * 16, r = r0 + (lane & 15);
+        const int64_t r0 = (t0 + t) * 16;
         if (r0 >= p.rows) return;
+        float next[4];
+        take_a(r0 + 16, next);
         v4f acc[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-        auto take_a = [&](int64_t k) { return k < k1 && r < p.rows ? p.a[k * p.lda + r] : 0.0f; };
-        auto multiply = [&](float x, const Pack<T, 8>& v) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, to_float(v.v[e]), acc[e], 0, 0, 0);
-        };
-        if constexpr (HELD) {
-            float x[4];
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-            for (int s = 0; s < 4; ++s) x[s] = take_a(k0 + 4 * s + (lane >> 4));
-#pragma unroll
-            for (int s = 0; s < 4; ++s) multiply(x[s], held[s]);
-        } else {
-            constexpr int kFlight = 8;      // loads on their way at once
-            for (int64_t kb = k0; kb < k1; kb += 4 * kFlight) {
-                float x[kFlight];
-                Pack<T, 8> v[kFlight];
-#pragma unroll
-                for (int s = 0; s < kFlight; ++s) {
-                    x[s] = take_a(kb + 4 * s + (lane >> 4));
-                    v[s] = take_b(kb + 4 * s + (lane >> 4));
-                }
-#pragma unroll
-                for (int s = 0; s < kFlight; ++s) multiply(x[s], v[s]);
-            }
-        }
-        if (p.splits > 1) {
-            float* out = static_cast<float*>(p.c) + (blockIdx.z * ((p.rows + 15) / 16 * 16) + r0) * p.ldc + n;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                Pack<float, 8> o;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o.v[e] = acc[e][i];
-                store_pack(out + (4 * (lane >> 4) + i) * p.ldc, o);
-            }
-            continue;
-        }
+            for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], held[s][e], acc[e], 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t row = r0 + 4 * (lane >> 4) + i;
-            if (row >= p.rows) continue;
-            const bool in = !p.used_r || p.used_r[row];
-            OUT* out = static_cast<OUT*>(p.c) + row * p.ldc + n;
-            if (n + 8 <= p.cols) {
-                Pack<OUT, 8> o;
-                if (p.add) o = load_pack<OUT, 8>(out);
+            float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = in ? acc[e][i] * p.by : 0.0f;
-                    o.v[e] = from_float<OUT>(p.add ? to_float(o.v[e]) + v : v);
-                }
-                store_pack(out, o);
-            } else {
+            for (int e = 0; e < 8; ++e) v[e] = acc[e][i];
+            store_eight<OUT>(p, r0 + 4 * (lane >> 4) + i, n, v);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[s] = next[s];
+    }
+#endif
+}
+
+// Any k: a block's 4 waves take 32 of it in turn and join their sums in order.
+template <typename T, typename OUT> __global__ __launch_bounds__(256) void thin_long(Thin p)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ v4f part[4][8][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 128, n = n0 + 8 * (lane & 15);
+    const int64_t r0 = static_cast<int64_t>(blockIdx.y) * 16, r = r0 + (lane & 15);
+    const int64_t k0 = blockIdx.z * p.k_each, k1 = k0 + p.k_each < p.k ? k0 + p.k_each : p.k;
+    constexpr int kFlight = 8;      // loads on their way at once, of 4 of k each
+    constexpr int64_t kStep = 4 * kFlight;
+    v4f acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    const float* a = p.a + (r < p.rows ? r : r0);
+    const T* b = static_cast<const T*>(p.b) + (n0 + 128 <= p.cols ? n : 0);
+    for (int64_t kb = k0 + wave * kStep; kb < k1; kb += 4 * kStep) {
+        float x[kFlight];
+        Pack<T, 8> v[kFlight];
+        const int64_t k = kb + (lane >> 4);
+        if (kb + kStep <= k1 && n0 + 128 <= p.cols) {
+            int in[kFlight];
+#pragma unroll
+            for (int s = 0; s < kFlight; ++s) {
+                x[s] = a[(k + 4 * s) * p.lda];
+                v[s] = load_pack<T, 8>(b + (k + 4 * s) * p.ldb);
+                in[s] = p.used_k ? p.used_k[k + 4 * s] : 1;
+            }
+#pragma unroll
+            for (int s = 0; s < kFlight; ++s)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (n + e < p.cols) {
-                        const float v = in ? acc[e][i] * p.by : 0.0f;
-                        out[e] = from_float<OUT>(p.add ? to_float(out[e]) + v : v);
-                    }
+                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], in[s] ? to_float(v[s].v[e]) : 0.0f, acc[e], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int s = 0; s < kFlight; ++s) {
+                const bool in = k + 4 * s < k1 && (!p.used_k || p.used_k[k + 4 * s]);
+                x[s] = in ? a[(k + 4 * s) * p.lda] : 0.0f;
+                if (in) v[s] = load_eight<T>(static_cast<const T*>(p.b) + (k + 4 * s) * p.ldb, n, p.cols);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], in ? to_float(v[s].v[e]) : 0.0f, acc[e], 0, 0, 0);
             }
         }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[wave][e][lane] = acc[e];
+    __syncthreads();
+    // a wave each: rows 4 (lane / 16) + wave
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = part[0][e][lane][wave] + part[1][e][lane][wave] + part[2][e][lane][wave] + part[3][e][lane][wave];
+    const int64_t row = r0 + 4 * (lane >> 4) + wave;
+    if (p.splits > 1) {
+        Pack<float, 8> o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o.v[e] = v[e];
+        store_pack(static_cast<float*>(p.c) + (blockIdx.z * ((p.rows + 15) / 16 * 16) + row) * p.ldc + n, o);
+    } else {
+        store_eight<OUT>(p, row, n, v);
     }
 #endif
 }
@@ -407,10 +499,9 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, bool backward)
     Layout l = {};
     l.padded = count(rows, 16) * 16;
     l.cols_padded = count(cols, 128) * 128;
-    // about two blocks a CU in all, each with whole groups of classes
+    // a block a CU
     const int64_t groups = count(vocab, 16), row_tiles = l.padded / 16;
-    l.groups_each = count(groups * row_tiles, 512);
-    if (row_tiles == 1 && groups > 512) l.groups_each = count(groups, 256);
+    l.groups_each = count(groups * row_tiles, 256);
     l.blocks = count(groups, l.groups_each);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -420,10 +511,10 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, bool backward)
     };
     l.used = take(4 * l.padded);
     if (backward) {
-        // dx: waves for 16 rows x 128 columns, the classes split to make about 2,048 of them
-        const int64_t waves = row_tiles * l.cols_padded / 128;
-        int64_t s = 2048 / waves;
-        if (s > count(vocab, 32)) s = count(vocab, 32);
+        // dx: blocks for 16 rows x 128 columns, the classes split to make about 768 of them
+        const int64_t blocks = row_tiles * l.cols_padded / 128;
+        int64_t s = 768 / blocks;
+        if (s > count(vocab, 256)) s = count(vocab, 256);
         if (s < 1) s = 1;
         l.k_each = count(count(vocab, s), 4) * 4;
         l.splits = static_cast<int>(count(vocab, l.k_each));
@@ -458,10 +549,12 @@ template <bool GRADIENT> hipError_t launch_logits_of(const VocabArgs& a, const D
 
 template <typename T, typename OUT> void launch_thin(const Thin& p, hipStream_t s)
 {
-    const dim3 grid(static_cast<unsigned>(count(p.cols, 512)), static_cast<unsigned>(count(count(p.rows, 16), p.row_tiles)),
-                    static_cast<unsigned>(p.splits));
-    if (p.k <= 16) thin<T, OUT, true><<<grid, 256, 0, s>>>(p);
-    else thin<T, OUT, false><<<grid, 256, 0, s>>>(p);
+    const unsigned tiles = static_cast<unsigned>(count(count(p.rows, 16), p.row_tiles));
+    if (p.k <= 16) {
+        thin_short<T, OUT><<<dim3(static_cast<unsigned>(count(p.cols, 512)), tiles), 256, 0, s>>>(p);
+    } else {
+        thin_long<T, OUT><<<dim3(static_cast<unsigned>(count(p.cols, 128)), tiles, static_cast<unsigned>(p.splits)), 256, 0, s>>>(p);
+    }
 }
 
 template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, uint8_t* base, hipStream_t s)
@@ -507,9 +600,9 @@ template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, u
         p.add = a.accumulate;
         p.c = a.dw;
         p.ldc = a.lddw;
-        // a wave's row tiles: so many that about 8,192 waves are left
+        // k of at most 16: so many row tiles a wave that about 8,192 waves are left
         const int64_t tiles = count(a.vocab, 16), waves = tiles * count(a.cols, 128);
-        const int64_t each = waves / 8192, least = count(tiles, 32768);     // blocks along y
+        const int64_t each = a.rows <= 16 ? waves / 8192 : 1, least = count(tiles, 32768);     // blocks along y
         p.row_tiles = static_cast<int32_t>(each < least ? least : each);
         if (a.dw_dtype == DTYPE_F32) launch_thin<T, float>(p, s);
         else launch_thin<T, T>(p, s);

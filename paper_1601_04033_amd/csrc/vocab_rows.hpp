@@ -78,6 +78,13 @@ __device__ __forceinline__ float weight(const VocabArgs& a, const Teacher& t, in
     return power(log_weight(a, t, at) * kLog2e) * t.by;
 }
 
+// dz at a class with logit `picked` and weight q.
+__device__ __forceinline__ float entry_value(const VocabRow& row, float picked, float q)
+{
+    const float p = power(__builtin_fmaf(picked, kLog2e, -row.l));
+    return __builtin_fmaf(row.f, p, -row.b) - row.g * q;
+}
+
 // dz at entry k of a row, for the first of those that name a class (the
 // weights of the same class add up); false for the others.
 __device__ __forceinline__ bool entry_gradient(const VocabArgs& a, const VocabRow& row, const Teacher& t, int64_t r,
@@ -96,8 +103,7 @@ __device__ __forceinline__ bool entry_gradient(const VocabArgs& a, const VocabRo
             q += weight(a, t, base + j);
         }
     }
-    const float p = power(__builtin_fmaf(a.picked[base + k], kLog2e, -row.l));
-    *dz = __builtin_fmaf(row.f, p, -row.b) - row.g * q;
+    *dz = entry_value(row, a.picked[base + k], q);
     return true;
 }
 
