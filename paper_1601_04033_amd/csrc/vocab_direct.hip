@@ -295,8 +295,8 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
 
 // ---- dx and dW: c[r][n] = sum_k a[k][r] b[k][n], both along k
 
-// A wave owns 16 rows and 128 columns: lane l holds b's columns 8 (l % 16) on of
-// row l / 16 of each 4 of k, and so 8 neighbouring columns of 4 rows of c.
+// A wave owns 16 rows and 128 columns: lane l holds 8 columns of b at row l / 16
+// of each 4 of k, and so the same columns of 4 rows of c.
 struct Thin {
     const float* a;         // [k][lda]
     int64_t lda, ldb, rows, cols, k, k_each;        // k_each: of a split, a multiple of 4
@@ -307,31 +307,32 @@ struct Thin {
     const int32_t* used_r;  // rows of c that take part, zeros for the others (NULL: all)
     float by;
     int32_t add, splits, row_tiles;     // row_tiles: that a wave goes through (k of at most 16)
+    int32_t column_blocks, row_blocks;
+    int64_t blocks;         // in all; 0: not wanted
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
-// 8 values of a row from column n on; zeros past its end.
-template <typename T> __device__ __forceinline__ Pack<T, 8> load_eight(const T* row, int64_t n, int64_t cols)
+// N values of a row from column n on; zeros past its end.
+template <typename T, int N> __device__ __forceinline__ Pack<T, N> load_values(const T* row, int64_t n, int64_t cols)
 {
-    if (n + 8 <= cols) return load_pack<T, 8>(row + n);
-    Pack<T, 8> p;
+    if (n + N <= cols) return load_pack<T, N>(row + n);
+    Pack<T, N> p;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p.v[e] = n + e < cols ? row[n + e] : from_float<T>(0.0f);
+    for (int e = 0; e < N; ++e) p.v[e] = n + e < cols ? row[n + e] : from_float<T>(0.0f);
     return p;
 }
-#endif
 
-// Rows 4 (lane / 16) + i of a tile, the lane's 8 columns.
-template <typename OUT> __device__ __forceinline__ void store_eight(const Thin& p, int64_t row, int64_t n, const float (&v)[8])
+// N values to row `row` of c, from column n on.
+template <typename OUT, int N> __device__ __forceinline__ void store_values(const Thin& p, int64_t row, int64_t n, const float (&v)[N])
 {
     if (row >= p.rows) return;
     const bool in = !p.used_r || p.used_r[row];
     OUT* out = static_cast<OUT*>(p.c) + row * p.ldc + n;
-    Pack<OUT, 8> o;
-    if (n + 8 <= p.cols) {
-        if (p.add) o = load_pack<OUT, 8>(out);
+    Pack<OUT, N> o;
+    if (n + N <= p.cols) {
+        if (p.add) o = load_pack<OUT, N>(out);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
             const float x = in ? v[e] * p.by : 0.0f;
             o.v[e] = from_float<OUT>(p.add ? to_float(o.v[e]) + x : x);
         }
@@ -339,32 +340,38 @@ template <typename OUT> __device__ __forceinline__ void store_eight(const Thin& 
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < N; ++e)
         if (n + e < p.cols) {
             const float x = in ? v[e] * p.by : 0.0f;
             out[e] = from_float<OUT>(p.add ? to_float(out[e]) + x : x);
         }
 }
+#endif
+
+#if defined(__HIP_DEVICE_COMPILE__)
 
 // k of at most 16: b's values stay in registers, the row tiles go by.  Bound by
-// the stores of c.
-template <typename T, typename OUT> __global__ __launch_bounds__(256) void thin_short(Thin p)
+// the stores of c, so a lane's columns are 4 neighbours in each half of the
+// wave's 128: 16 lanes store 256 bytes.
+template <typename T, typename OUT> __device__ __forceinline__ void thin_short(const Thin& p, int column_block, int64_t row_block)
 {
-#if defined(__HIP_DEVICE_COMPILE__)
     const int lane = threadIdx.x & 63;
-    const int64_t n0 = (static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) * 128, n = n0 + 8 * (lane & 15);
+    const int64_t n0 = (static_cast<int64_t>(column_block) * 4 + (threadIdx.x >> 6)) * 128, n = n0 + 4 * (lane & 15);
     if (n0 >= p.cols) return;
     float held[4][8];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
         const int64_t k = 4 * s + (lane >> 4);
-        Pack<T, 8> v;
         const bool in = k < p.k && (!p.used_k || p.used_k[k]);
-        if (in) v = load_eight<T>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
+        Pack<T, 4> v[2];
+        if (in) {
+            v[0] = load_values<T, 4>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
+            v[1] = load_values<T, 4>(static_cast<const T*>(p.b) + k * p.ldb, n + 64, p.cols);
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) held[s][e] = in ? to_float(v.v[e]) : 0.0f;
+        for (int e = 0; e < 8; ++e) held[s][e] = in ? to_float(v[e >> 2].v[e & 3]) : 0.0f;
     }
-    const int64_t t0 = static_cast<int64_t>(blockIdx.y) * p.row_tiles;
+    const int64_t t0 = row_block * p.row_tiles;
     const float* at = p.a + (lane >> 4) * p.lda + (lane & 15);
     auto take_a = [&](int64_t r0, float (&x)[4]) {
 #pragma unroll
@@ -373,7 +380,9 @@ template <typename T, typename OUT> __global__ __launch_bounds__(256) void thin_
     };
     float x[4];
     take_a(t0 * 16, x);
-    for (int t = 0; t < p.row_tiles; ++t) {
+    const bool plain = n0 + 128 <= p.cols && !p.used_r && !p.add;     // nothing to look at per store
+    OUT* out = static_cast<OUT*>(p.c) + (t0 * 16 + 4 * (lane >> 4)) * p.ldc + n;
+    for (int t = 0; t < p.row_tiles; ++t, out += 16 * p.ldc) {
         const int64_t r0 = (t0 + t) * 16;
         if (r0 >= p.rows) return;
         float next[4];
@@ -385,62 +394,102 @@ template <typename T, typename OUT> __global__ __launch_bounds__(256) void thin_
         for (int s = 0; s < 4; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], held[s][e], acc[e], 0, 0, 0);
+        if (plain && r0 + 16 <= p.rows) {
+            OUT* at_row = out;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float v[8];
+            for (int i = 0; i < 4; ++i, at_row += p.ldc)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = acc[e][i];
-            store_eight<OUT>(p, r0 + 4 * (lane >> 4) + i, n, v);
+                for (int h = 0; h < 2; ++h) {
+                    Pack<OUT, 4> o;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o.v[e] = from_float<OUT>(acc[4 * h + e][i] * p.by);
+                    store_pack(at_row + 64 * h, o);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = acc[4 * h + e][i];
+                    store_values<OUT, 4>(p, r0 + 4 * (lane >> 4) + i, n + 64 * h, v);
+                }
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) x[s] = next[s];
     }
-#endif
 }
 
-// Any k: a block's 4 waves take 32 of it in turn and join their sums in order.
-template <typename T, typename OUT> __global__ __launch_bounds__(256) void thin_long(Thin p)
+// Any k: a block's 4 waves take 16 of it in turn and join their sums in order.
+// A lane has 8 neighbouring columns.
+// MASK: used_k is there.
+template <typename T, typename OUT, bool MASK>
+__device__ __forceinline__ void thin_long(const Thin& p, v4f (&part)[4][8][64], int column_block, int64_t row_block, int split)
 {
-#if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ v4f part[4][8][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 128, n = n0 + 8 * (lane & 15);
-    const int64_t r0 = static_cast<int64_t>(blockIdx.y) * 16, r = r0 + (lane & 15);
-    const int64_t k0 = blockIdx.z * p.k_each, k1 = k0 + p.k_each < p.k ? k0 + p.k_each : p.k;
+    const int64_t n0 = static_cast<int64_t>(column_block) * 128, n = n0 + 8 * (lane & 15);
+    const int64_t r0 = row_block * 16, r = r0 + (lane & 15);
+    const int64_t k0 = split * p.k_each, k1 = k0 + p.k_each < p.k ? k0 + p.k_each : p.k;
     constexpr int kFlight = 8;      // loads on their way at once, of 4 of k each
     constexpr int64_t kStep = 4 * kFlight;
     v4f acc[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     const float* a = p.a + (r < p.rows ? r : r0);
-    const T* b = static_cast<const T*>(p.b) + (n0 + 128 <= p.cols ? n : 0);
-    for (int64_t kb = k0 + wave * kStep; kb < k1; kb += 4 * kStep) {
+    struct Loads {
         float x[kFlight];
         Pack<T, 8> v[kFlight];
-        const int64_t k = kb + (lane >> 4);
-        if (kb + kStep <= k1 && n0 + 128 <= p.cols) {
-            int in[kFlight];
+        int in[kFlight];
+    };
+    auto multiply = [&](const Loads& l) {
+#pragma unroll
+        for (int s = 0; s < kFlight; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(l.x[s], l.in[s] ? to_float(l.v[s].v[e]) : 0.0f, acc[e], 0, 0, 0);
+    };
+    int64_t kb = k0 + wave * kStep;
+    if (n0 + 128 <= p.cols) {       // whole steps, the next on its way while one is multiplied
+        const T* b = static_cast<const T*>(p.b) + n;
+        auto load = [&](Loads& l) {
+            const int64_t k = kb + (lane >> 4);
 #pragma unroll
             for (int s = 0; s < kFlight; ++s) {
-                x[s] = a[(k + 4 * s) * p.lda];
-                v[s] = load_pack<T, 8>(b + (k + 4 * s) * p.ldb);
-                in[s] = p.used_k ? p.used_k[k + 4 * s] : 1;
+                l.x[s] = a[(k + 4 * s) * p.lda];
+                l.v[s] = load_pack<T, 8>(b + (k + 4 * s) * p.ldb);
+                l.in[s] = MASK ? p.used_k[k + 4 * s] : 1;
             }
-#pragma unroll
-            for (int s = 0; s < kFlight; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], in[s] ? to_float(v[s].v[e]) : 0.0f, acc[e], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int s = 0; s < kFlight; ++s) {
-                const bool in = k + 4 * s < k1 && (!p.used_k || p.used_k[k + 4 * s]);
-                x[s] = in ? a[(k + 4 * s) * p.lda] : 0.0f;
-                if (in) v[s] = load_eight<T>(static_cast<const T*>(p.b) + (k + 4 * s) * p.ldb, n, p.cols);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], in ? to_float(v[s].v[e]) : 0.0f, acc[e], 0, 0, 0);
+            kb += 4 * kStep;
+        };
+        Loads l0, l1;
+        if (kb + kStep <= k1) {
+            load(l0);
+            while (true) {
+                if (kb + kStep > k1) {
+                    multiply(l0);
+                    break;
+                }
+                load(l1);
+                multiply(l0);
+                if (kb + kStep > k1) {
+                    multiply(l1);
+                    break;
+                }
+                load(l0);
+                multiply(l1);
             }
+        }
+    }
+    for (; kb < k1; kb += 4 * kStep) {      // what is cut by the end of k or of the columns
+        for (int s = 0; s < kFlight; ++s) {
+            const int64_t k = kb + 4 * s + (lane >> 4);
+            const bool in = k < k1 && (!MASK || p.used_k[k]);
+            const float x = in ? a[k * p.lda] : 0.0f;
+            Pack<T, 8> v;
+            if (in) v = load_values<T, 8>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, in ? to_float(v.v[e]) : 0.0f, acc[e], 0, 0, 0);
         }
     }
 #pragma unroll
@@ -456,10 +505,56 @@ template <typename T, typename OUT> __global__ __launch_bounds__(256) void thin_
         Pack<float, 8> o;
 #pragma unroll
         for (int e = 0; e < 8; ++e) o.v[e] = v[e];
-        store_pack(static_cast<float*>(p.c) + (blockIdx.z * ((p.rows + 15) / 16 * 16) + row) * p.ldc + n, o);
+        store_pack(static_cast<float*>(p.c) + (split * ((p.rows + 15) / 16 * 16) + row) * p.ldc + n, o);
     } else {
-        store_eight<OUT>(p, row, n, v);
+        store_values<OUT, 8>(p, row, n, v);
     }
+}
+
+// A block of a product of long k among all of its blocks.
+template <typename T, typename OUT, bool MASK>
+__device__ __forceinline__ void long_block(const Thin& p, v4f (&part)[4][8][64], int id)
+{
+    const int rest = id / p.column_blocks;
+    thin_long<T, OUT, MASK>(p, part, id % p.column_blocks, rest % p.row_blocks, rest / p.row_blocks);
+}
+
+// Consecutive blocks go to the 8 XCDs in turn: give each XCD a run of them, so
+// that its L2 sees whole rows.  (A column block of each row alone lies in a few
+// of its channels.)
+__device__ __forceinline__ int64_t in_runs(int64_t all)
+{
+    const int64_t each = all >> 3, extra = all & 7, xcd = blockIdx.x & 7;
+    return xcd * each + (xcd < extra ? xcd : extra) + (blockIdx.x >> 3);
+}
+
+#endif
+
+// dW of a few rows; dx of a few classes.
+template <typename T, typename OUT> __global__ __launch_bounds__(256, 3) void short_product(Thin p)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int64_t id = in_runs(p.blocks);
+    thin_short<T, OUT>(p, static_cast<int>(id % p.column_blocks), id / p.column_blocks);
+#endif
+}
+
+template <typename T, typename OUT, bool MASK> __global__ __launch_bounds__(256, 2) void long_product(Thin p)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ v4f part[4][8][64];
+    long_block<T, OUT, MASK>(p, part, static_cast<int>(in_runs(p.blocks)));
+#endif
+}
+
+// Both of a small problem in one launch, dx's blocks first.
+template <typename T, typename OUT> __global__ __launch_bounds__(256, 2) void long_products(Thin dx, Thin dw)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ v4f part[4][8][64];
+    const int id = blockIdx.x;
+    if (id < dx.blocks) long_block<T, T, false>(dx, part, id);
+    else long_block<T, OUT, true>(dw, part, id - static_cast<int>(dx.blocks));
 #endif
 }
 
@@ -511,9 +606,9 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, bool backward)
     };
     l.used = take(4 * l.padded);
     if (backward) {
-        // dx: blocks for 16 rows x 128 columns, the classes split to make about 768 of them
+        // dx: blocks for 16 rows x 128 columns, the classes split to make about 512 of them
         const int64_t blocks = row_tiles * l.cols_padded / 128;
-        int64_t s = 768 / blocks;
+        int64_t s = 512 / blocks;
         if (s > count(vocab, 256)) s = count(vocab, 256);
         if (s < 1) s = 1;
         l.k_each = count(count(vocab, s), 4) * 4;
@@ -547,65 +642,75 @@ template <bool GRADIENT> hipError_t launch_logits_of(const VocabArgs& a, const D
     return launch_logits<f16, GRADIENT>(a, d, blocks, s);
 }
 
-template <typename T, typename OUT> void launch_thin(const Thin& p, hipStream_t s)
+void set_blocks(Thin& p)
 {
-    const unsigned tiles = static_cast<unsigned>(count(count(p.rows, 16), p.row_tiles));
-    if (p.k <= 16) {
-        thin_short<T, OUT><<<dim3(static_cast<unsigned>(count(p.cols, 512)), tiles), 256, 0, s>>>(p);
-    } else {
-        thin_long<T, OUT><<<dim3(static_cast<unsigned>(count(p.cols, 128)), tiles, static_cast<unsigned>(p.splits)), 256, 0, s>>>(p);
+    p.column_blocks = static_cast<int32_t>(count(p.cols, p.k <= 16 ? 512 : 128));
+    p.row_blocks = static_cast<int32_t>(count(count(p.rows, 16), p.row_tiles));
+    p.blocks = static_cast<int64_t>(p.column_blocks) * p.row_blocks * p.splits;
+}
+
+template <typename T, typename OUT> hipError_t launch_products(const Thin& dx, const Thin& dw, hipStream_t s)
+{
+    const unsigned n = static_cast<unsigned>(dx.blocks), m = static_cast<unsigned>(dw.blocks);
+    if (n && m && dx.k > 16 && dw.k > 16) {
+        long_products<T, OUT><<<n + m, 256, 0, s>>>(dx, dw);
+        return hipGetLastError();
     }
+    if (n && dx.k <= 16) short_product<T, T><<<n, 256, 0, s>>>(dx);
+    else if (n) long_product<T, T, false><<<n, 256, 0, s>>>(dx);
+    VOCAB_TRY(hipGetLastError());
+    if (m && dw.k <= 16) short_product<T, OUT><<<m, 256, 0, s>>>(dw);
+    else if (m) long_product<T, OUT, true><<<m, 256, 0, s>>>(dw);
+    return hipGetLastError();
 }
 
 template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, uint8_t* base, hipStream_t s)
 {
     const int32_t* used = reinterpret_cast<int32_t*>(base + l.used);
+    Thin dx = {}, dw = {};
     if (a.dx) {
-        Thin p = {};
-        p.a = reinterpret_cast<float*>(base + l.dzt);
-        p.lda = l.padded;
-        p.b = a.w;
-        p.ldb = a.ldw;
-        p.rows = a.rows;
-        p.cols = a.cols;
-        p.k = a.vocab;
-        p.k_each = l.k_each;
-        p.splits = l.splits;
-        p.row_tiles = 1;
-        p.by = a.scale;
-        p.c = l.splits > 1 ? base + l.sums : static_cast<uint8_t*>(a.dx);
-        p.ldc = l.splits > 1 ? l.cols_padded : a.lddx;
-        p.used_r = used;
-        launch_thin<T, T>(p, s);
-        VOCAB_TRY(hipGetLastError());
-        if (l.splits > 1) {
-            const dim3 grid(static_cast<unsigned>(count(a.cols, 1024)), static_cast<unsigned>(a.rows));
-            join<T><<<grid, 256, 0, s>>>(p, static_cast<T*>(a.dx), a.lddx, used);
-            VOCAB_TRY(hipGetLastError());
-        }
+        dx.a = reinterpret_cast<float*>(base + l.dzt);
+        dx.lda = l.padded;
+        dx.b = a.w;
+        dx.ldb = a.ldw;
+        dx.rows = a.rows;
+        dx.cols = a.cols;
+        dx.k = a.vocab;
+        dx.k_each = l.k_each;
+        dx.splits = l.splits;
+        dx.row_tiles = 1;
+        dx.by = a.scale;
+        dx.c = l.splits > 1 ? base + l.sums : static_cast<uint8_t*>(a.dx);
+        dx.ldc = l.splits > 1 ? l.cols_padded : a.lddx;
+        dx.used_r = used;
+        set_blocks(dx);
     }
     if (a.dw) {
-        Thin p = {};
-        p.a = reinterpret_cast<float*>(base + l.dz);
-        p.lda = a.vocab;
-        p.b = a.x;
-        p.ldb = a.ldx;
-        p.rows = a.vocab;
-        p.cols = a.cols;
-        p.k = a.rows;
-        p.k_each = l.padded;
-        p.splits = 1;
-        p.used_k = used;
-        p.by = a.scale;
-        p.add = a.accumulate;
-        p.c = a.dw;
-        p.ldc = a.lddw;
+        dw.a = reinterpret_cast<float*>(base + l.dz);
+        dw.lda = a.vocab;
+        dw.b = a.x;
+        dw.ldb = a.ldx;
+        dw.rows = a.vocab;
+        dw.cols = a.cols;
+        dw.k = a.rows;
+        dw.k_each = l.padded;
+        dw.splits = 1;
+        dw.used_k = used;
+        dw.by = a.scale;
+        dw.add = a.accumulate;
+        dw.c = a.dw;
+        dw.ldc = a.lddw;
         // k of at most 16: so many row tiles a wave that about 8,192 waves are left
-        const int64_t tiles = count(a.vocab, 16), waves = tiles * count(a.cols, 128);
-        const int64_t each = a.rows <= 16 ? waves / 8192 : 1, least = count(tiles, 32768);     // blocks along y
-        p.row_tiles = static_cast<int32_t>(each < least ? least : each);
-        if (a.dw_dtype == DTYPE_F32) launch_thin<T, float>(p, s);
-        else launch_thin<T, T>(p, s);
+        const int64_t waves = count(a.vocab, 16) * count(a.cols, 128);
+        const int64_t each = a.rows <= 16 ? waves / 8192 : 1;
+        dw.row_tiles = static_cast<int32_t>(each < 1 ? 1 : each);
+        set_blocks(dw);
+    }
+    if (a.dw_dtype == DTYPE_F32) VOCAB_TRY((launch_products<T, float>(dx, dw, s)));
+    else VOCAB_TRY((launch_products<T, T>(dx, dw, s)));
+    if (a.dx && l.splits > 1) {
+        const dim3 grid(static_cast<unsigned>(count(a.cols, 1024)), static_cast<unsigned>(a.rows));
+        join<T><<<grid, 256, 0, s>>>(dx, static_cast<T*>(a.dx), a.lddx, used);
         VOCAB_TRY(hipGetLastError());
     }
     return hipSuccess;
