@@ -61,6 +61,19 @@ template <int MFMA, int READS, int LOADS, int VALU, int I = 0> __device__ __forc
     if constexpr (I + 1 < MFMA) interleave<MFMA, READS, LOADS, VALU, I + 1>();
 }
 
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+
+// 32 x 32 sums of 16 products of bf16's or fp16's; a lane holds 8 of its row l % 32.
+template <typename T> __device__ __forceinline__ v16f mfma(const v4i& a, const v4i& b, const v16f& c);
+template <> __device__ __forceinline__ v16f mfma<bf16>(const v4i& a, const v4i& b, const v16f& c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ v16f mfma<f16>(const v4i& a, const v4i& b, const v16f& c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+
 // A tile in vector registers.  Accumulators stay in the accumulation
 // registers until here: without this the compiler wants all of them where
 // the conversions after it can read them, and has no room.

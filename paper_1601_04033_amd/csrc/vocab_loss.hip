@@ -12,12 +12,18 @@
 // largest of dz, with p - q cancelling.  They are computed here from the
 // picked logits, put into dz^T in place of what the tile wrote, and left out
 // of dz: dx takes them in fp32, times the rows of W, at the end.
+#include "tiles.hpp"
 #include "vocab_rows.hpp"
 
 namespace fasgd {
 namespace {
 
+
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Pairs of three terms each, those above 2^-24, the smallest first.
+constexpr uint32_t kPairsA = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
+constexpr uint32_t kPairsB = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 
 // ---- rows that take part
 
@@ -143,30 +149,78 @@ template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_o
 
 // ---- forward
 
-// The logits at the entries: a wave for each.
-template <typename T> __global__ __launch_bounds__(kBlock) void pick(VocabArgs a, const int32_t* list, const int32_t* active)
+// The type of a matrix's terms.
+template <typename T> struct Term {
+    using type = T;
+};
+template <> struct Term<float> {
+    using type = bf16;
+};
+
+// The logits at the entries, 32 a wave: the diagonal of the product of their
+// classes' rows and their rows of x, by the instruction and in the order of
+// the tiles, so that they are bit for bit what the tiles put into the sums of
+// powers.  (A row's largest logit is often its target: an error that the sum
+// has and p's numerator has not, or another, is p (1 - p) of itself in dz, not p.
+// 8,192 x 4,096 x 131,072 bf16, dW off by 3.9e-6 with a sum in another order.)
+template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, const int32_t* list, const int32_t* active,
+                                                                const uint16_t* x, int64_t ld_x, int64_t cols_padded)
 {
-    const int64_t all = static_cast<int64_t>(*active) * a.entries;
-    const int lane = threadIdx.x & 63;
-    for (int64_t w = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6); w < all;
-         w += static_cast<int64_t>(gridDim.x) * kWaves) {
-        const int64_t r = list[w / a.entries], at = r * a.entries + w % a.entries;
-        float sum = 0.0f;
-        if (counts(a, at)) {
-            const T* x = static_cast<const T*>(a.x) + r * a.ldx;
-            const T* c = static_cast<const T*>(a.w) + a.index[at] * a.ldw;
-            int64_t k = lane * 8;
-            for (; k + 8 <= a.cols; k += 512) {
-                const Pack<T, 8> p = load_pack<T, 8>(x + k), q = load_pack<T, 8>(c + k);
-                for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(to_float(p.v[e]), to_float(q.v[e]), sum);
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr bool kTerms = sizeof(T) == 4;
+    constexpr int kFlight = kTerms ? 8 : 16;    // steps of 16 on their way
+    const int lane = threadIdx.x, half = lane >> 5;
+    const int64_t all = static_cast<int64_t>(*active) * a.entries, blocks = (all + 31) / 32;
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const int64_t pair = block * 32 + (lane & 31);
+        const int64_t at = pair < all ? pair / a.entries : 0;
+        const int64_t r = list[at], here = r * a.entries + (pair < all ? pair % a.entries : 0);
+        const bool in = pair < all && counts(a, here);
+        const T* w = static_cast<const T*>(a.w) + (in ? a.index[here] : 0) * a.ldw;
+        const uint16_t* row = x + at * ld_x;
+        v16f acc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+        for (int p = 0; p < (kTerms ? 6 : 1); ++p) {
+            const int ta = kTerms ? kPairsA >> (2 * p) & 3u : 0, tb = kTerms ? kPairsB >> (2 * p) & 3u : 0;
+            const uint16_t* b = row + tb * cols_padded;
+            for (int64_t k0 = 8 * half; k0 - 8 * half < a.cols; k0 += 16 * kFlight) {
+                v4i fa[kFlight], fb[kFlight];
+#pragma unroll
+                for (int s = 0; s < kFlight; ++s) {
+                    const int64_t k = k0 + 16 * s;
+                    Pack<T, 8> v;
+                    if (k + 8 <= a.cols) {
+                        v = load_pack<T, 8>(w + k);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v.v[e] = k + e < a.cols ? w[k + e] : from_float<T>(0.0f);
+                    }
+                    if constexpr (kTerms) {
+                        Pack<uint16_t, 8> t;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            uint16_t term[3];
+                            terms_of(v.v[e], term);
+                            t.v[e] = ta == 0 ? term[0] : (ta == 1 ? term[1] : term[2]);
+                        }
+                        fa[s] = __builtin_bit_cast(v4i, t);
+                    } else {
+                        fa[s] = __builtin_bit_cast(v4i, v);
+                    }
+                    fb[s] = k < cols_padded ? *reinterpret_cast<const v4i*>(b + k) : v4i{0, 0, 0, 0};
+                }
+#pragma unroll
+                for (int s = 0; s < kFlight; ++s) acc = mfma<typename Term<T>::type>(fa[s], fb[s], acc);
             }
-            for (; k < a.cols; ++k) {       // the lane whose 8 the row's end cuts
-                sum = __builtin_fmaf(to_float(x[k]), to_float(c[k]), sum);
-            }
-            sum = wave_sum(sum) * a.scale;
         }
-        if (lane == 0) a.picked[at] = sum;
+        // lane l: column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z = 8 * (i >> 2) + 4 * half + (i & 3) == (lane & 31) ? acc[i] : z;
+        if ((lane >> 2 & 1) == half && pair < all) a.picked[here] = in ? z * a.scale : 0.0f;
     }
+#endif
 }
 
 // ---- backward
@@ -422,10 +476,6 @@ hipError_t begin(const VocabArgs& a, bool backward, Plan& p, hipStream_t s)
     return launch_lay_out(x, a.dtype, a.rows, a.cols, s);
 }
 
-// Pairs of three terms each, those above 2^-24, the smallest first.
-constexpr uint32_t kPairsA = 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10;
-constexpr uint32_t kPairsB = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
-
 // The logits of classes first .. first + n - 1: W as an operand where it cannot
 // be read in place (and transposed, for dx), and the product's two sides.
 hipError_t piece_of(const VocabArgs& a, const Plan& p, int64_t first, int64_t n, bool transposed, VocabProduct& q, hipStream_t s)
@@ -491,11 +541,12 @@ hipError_t launch_vocab_forward(const VocabArgs& a, hipStream_t s)
         q.partial_sum = a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr;
         VOCAB_TRY(launch_vocab_product(VOCAB_STATISTICS, q, n, a.rows, s));
     }
-    const int64_t waves = a.rows * a.entries, blocks = (waves + kWaves - 1) / kWaves;
+    const int64_t blocks = (a.rows * a.entries + 31) / 32;
     const unsigned picks = static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20);
-    if (a.dtype == DTYPE_F32) pick<float><<<picks, kBlock, 0, s>>>(a, p.list, p.active);
-    else if (a.dtype == DTYPE_BF16) pick<bf16><<<picks, kBlock, 0, s>>>(a, p.list, p.active);
-    else pick<f16><<<picks, kBlock, 0, s>>>(a, p.list, p.active);
+    const uint16_t* x = p.at<uint16_t>(l.x);
+    if (a.dtype == DTYPE_F32) pick<float><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
+    else if (a.dtype == DTYPE_BF16) pick<bf16><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
+    else pick<f16><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
     VOCAB_TRY(hipGetLastError());
     finish<<<static_cast<unsigned>((a.rows + 7) / 8), kBlock, 0, s>>>(a, p.list, p.active, p.at<float2>(l.partial),
                                                                       a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr,

@@ -20,19 +20,7 @@
 namespace fasgd {
 namespace {
 
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-
 #if defined(__HIP_DEVICE_COMPILE__)
-
-template <typename T> __device__ __forceinline__ v16f mfma(const v4i& a, const v4i& b, const v16f& c);
-template <> __device__ __forceinline__ v16f mfma<bf16>(const v4i& a, const v4i& b, const v16f& c)
-{
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
-}
-template <> __device__ __forceinline__ v16f mfma<f16>(const v4i& a, const v4i& b, const v16f& c)
-{
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
-}
 
 __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
