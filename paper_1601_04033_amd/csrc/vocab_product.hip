@@ -88,14 +88,29 @@ __device__ __forceinline__ void statistics(const v16f (&acc)[N][N], const VocabP
     }
 }
 
-template <typename T> __device__ __forceinline__ uint16_t term(float x)
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
+// Two terms in a word, and the values they stand for.
+template <typename T> __device__ __forceinline__ uint32_t two_terms(float x, float y);
+template <> __device__ __forceinline__ uint32_t two_terms<bf16>(float x, float y)
 {
-    return __builtin_bit_cast(uint16_t, from_float<T>(x));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{x, y}), v2bf));
 }
-template <typename T> __device__ __forceinline__ float term_value(uint16_t x) { return to_float(__builtin_bit_cast(T, x)); }
+template <> __device__ __forceinline__ uint32_t two_terms<f16>(float x, float y)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f{x, y}), v2h));
+}
+template <typename T> __device__ __forceinline__ float low_term(uint32_t u);
+template <> __device__ __forceinline__ float low_term<bf16>(uint32_t u) { return __uint_as_float(u << 16); }
+template <> __device__ __forceinline__ float low_term<f16>(uint32_t u) { return static_cast<float>(__builtin_bit_cast(v2h, u)[0]); }
+template <typename T> __device__ __forceinline__ float high_term(uint32_t u);
+template <> __device__ __forceinline__ float high_term<bf16>(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+template <> __device__ __forceinline__ float high_term<f16>(uint32_t u) { return static_cast<float>(__builtin_bit_cast(v2h, u)[1]); }
 
 // The gradient of a wave's logits, in both layouts.  A lane holds N rows and,
-// at a time, 4 N neighbouring classes.
+// at a time, 4 N neighbouring classes: words of two rows go to dz^T as they are,
+// words of two classes are put together from them.
 template <typename T, int W, int N>
 __device__ __forceinline__ void gradient(const v16f (&acc)[N][N], const VocabProduct& p, int64_t m, int64_t n, int left,
                                          int lane)
@@ -111,11 +126,10 @@ __device__ __forceinline__ void gradient(const v16f (&acc)[N][N], const VocabPro
         b[j] = row.b * up;
     }
     const int terms = p.dz_terms > p.dzt_terms ? p.dz_terms : p.dzt_terms;
-    uint16_t* dz = p.dz + (n + N * (lane & 31)) * p.ld_dz + m;
-    uint16_t* dzt = p.dzt + m * p.ld_dzt + n + N * (lane & 31);
+    uint16_t* dz = p.dz + (n + N * (lane & 31)) * p.ld_dz + m + 4 * N * (lane >> 5);
+    uint16_t* dzt = p.dzt + (m + 4 * N * (lane >> 5)) * p.ld_dzt + n + N * (lane & 31);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const int first = 4 * N * (2 * q + (lane >> 5));    // of the 4 N classes
         float v[4 * N][N];
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -125,38 +139,60 @@ __device__ __forceinline__ void gradient(const v16f (&acc)[N][N], const VocabPro
                 for (int r = 0; r < 4; ++r) {
                     float z = acc[i][j][4 * q + r];
                     asm volatile("" : "+v"(z));     // read out of the accumulation registers here
-                    const float x = __builtin_fmaf(f[j], power(__builtin_fmaf(z, c, -l[j])), -b[j]);
-                    v[r * N + i][j] = first + r * N + i < left ? x : 0.0f;
+                    v[r * N + i][j] = __builtin_fmaf(f[j], power(__builtin_fmaf(z, c, -l[j])), -b[j]);
                 }
-        for (int t = 0; t < terms; ++t) {
-            uint16_t w[4 * N][N];
+        if (left < W) {     // nothing of classes past the last
 #pragma unroll
             for (int k = 0; k < 4 * N; ++k)
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    w[k][j] = term<T>(v[k][j]);
-                    v[k][j] -= term_value<T>(w[k][j]);
+                for (int j = 0; j < N; ++j) v[k][j] = 4 * N * (2 * q + (lane >> 5)) + k < left ? v[k][j] : 0.0f;
+        }
+        for (int t = 0; t < terms; ++t) {
+            uint32_t w[4 * N][N / 2];
+#pragma unroll
+            for (int k = 0; k < 4 * N; ++k)
+#pragma unroll
+                for (int j = 0; j < N; j += 2) {
+                    const uint32_t u = two_terms<T>(v[k][j], v[k][j + 1]);
+                    w[k][j / 2] = u;
+                    v[k][j] -= low_term<T>(u);
+                    v[k][j + 1] -= high_term<T>(u);
                 }
             if (t < p.dzt_terms) {
+                uint16_t* out = dzt + t * p.padded;
 #pragma unroll
                 for (int k = 0; k < 4 * N; ++k) {
-                    Pack<uint16_t, N> x;
+                    Pack<uint32_t, N / 2> x;
 #pragma unroll
-                    for (int j = 0; j < N; ++j) x.v[j] = w[k][j];
-                    store_pack(dzt + (first + k) * p.ld_dzt + t * p.padded, x);
+                    for (int j = 0; j < N / 2; ++j) x.v[j] = w[k][j];
+                    store_pack(reinterpret_cast<uint32_t*>(out + (8 * N * q + k) * p.ld_dzt), x);
                 }
             }
             if (t < p.dz_terms) {
+                uint16_t* out = dz + t * p.classes + 8 * N * q;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    Pack<uint16_t, 4 * N> x;
+                    Pack<uint32_t, 2 * N> x;
 #pragma unroll
-                    for (int k = 0; k < 4 * N; ++k) x.v[k] = w[k][j];
-                    store_pack(dz + j * p.ld_dz + t * p.classes + first, x);
+                    for (int k = 0; k < 4 * N; k += 2)
+                        x.v[k / 2] = __builtin_amdgcn_perm(w[k + 1][j / 2], w[k][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+                    store_pack(reinterpret_cast<uint32_t*>(out + j * p.ld_dz), x);
                 }
             }
         }
     }
+}
+
+// A buffer that is the same in all lanes, said so: where the compiler does not
+// see it, it loops over the lanes' values at each load of a stage (the gradient's
+// product at 8,192 x 16,384 x 4,096 1,130 against @GB@ us).
+__device__ __forceinline__ auto same_buffer(const uint8_t* p, int64_t bytes)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    const uint32_t low = __builtin_amdgcn_readfirstlane(static_cast<int>(at)), high = __builtin_amdgcn_readfirstlane(static_cast<int>(at >> 32));
+    const int64_t most = bytes < 0xffffffffll ? bytes : 0xffffffffll;
+    const uint32_t n = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(most)));
+    return buffer(reinterpret_cast<const uint8_t*>(static_cast<uint64_t>(high) << 32 | low), n);
 }
 
 // Order of a sub-step's instructions for the compiler's scheduler: between
@@ -186,7 +222,7 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     using G = Geometry<W, WM>;
     constexpr int N = G::kTiles;
     __shared__ __attribute__((aligned(16))) uint8_t a0[G::kStageA], b0[G::kStageB], a1[G::kStageA], b1[G::kStageB];
-    const int active = *p.active;
+    const int active = __builtin_amdgcn_readfirstlane(*p.active);
     const int tiles = tiles_m * tiles_n;
     const int id = tile_of(blockIdx.x % tiles, tiles_m, tiles_n);
     const int split = blockIdx.x / tiles;
@@ -218,10 +254,10 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     for (int q = 0; q < G::kLoadsA; ++q) off_a[q] = offset(q, last_a, p.a.ld);
 #pragma unroll
     for (int q = 0; q < G::kLoadsB; ++q) off_b[q] = offset(q, last_b, p.b.ld);
-    const auto ga = buffer(p.a.data + m0 * p.a.ld + static_cast<int64_t>(kb0) * kBytes,
-                           (rows_a - m0) * p.a.ld - static_cast<int64_t>(kb0) * kBytes);
-    const auto gb = buffer(p.b.data + n0 * p.b.ld + static_cast<int64_t>(kb0) * kBytes,
-                           (pad_b - n0) * p.b.ld - static_cast<int64_t>(kb0) * kBytes);
+    const auto ga = same_buffer(p.a.data + m0 * p.a.ld + static_cast<int64_t>(kb0) * kBytes,
+                                (rows_a - m0) * p.a.ld - static_cast<int64_t>(kb0) * kBytes);
+    const auto gb = same_buffer(p.b.data + n0 * p.b.ld + static_cast<int64_t>(kb0) * kBytes,
+                                (pad_b - n0) * p.b.ld - static_cast<int64_t>(kb0) * kBytes);
 
     const int place_a = (wave_m * W + (lane & 31)) * kBytes, place_b = (wave_n * W + (lane & 31)) * kBytes;
     int chunk[4];
@@ -245,13 +281,17 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     int at = 0, pair = 0;
     constexpr int kLoads = G::kLoadsA + G::kLoadsB;
     constexpr int kFirst = kLoads / 2;
+    // (as same_buffer)
+    const int terms = __builtin_amdgcn_readfirstlane(p.terms), along = __builtin_amdgcn_readfirstlane(own_blocks * kBytes);
+    const uint32_t terms_a = __builtin_amdgcn_readfirstlane(p.terms_a), terms_b = __builtin_amdgcn_readfirstlane(p.terms_b);
+    const int plane_a = __builtin_amdgcn_readfirstlane(p.a.plane), plane_b = __builtin_amdgcn_readfirstlane(p.b.plane);
     int at_a, at_b;
     auto next = [&]() {
-        at_a = at + static_cast<int>(p.terms_a >> (2 * pair) & 3u) * p.a.plane;
-        at_b = at + static_cast<int>(p.terms_b >> (2 * pair) & 3u) * p.b.plane;
-        if (at + kBytes < own_blocks * kBytes) {
+        at_a = at + static_cast<int>(terms_a >> (2 * pair) & 3u) * plane_a;
+        at_b = at + static_cast<int>(terms_b >> (2 * pair) & 3u) * plane_b;
+        if (at + kBytes < along) {
             at += kBytes;
-        } else if (pair + 1 < p.terms) {
+        } else if (pair + 1 < terms) {
             ++pair;
             at = 0;
         }
