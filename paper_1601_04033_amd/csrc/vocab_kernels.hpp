@@ -68,6 +68,7 @@ struct VocabRow {
 enum : int { VOCAB_STATISTICS, VOCAB_GRADIENT, VOCAB_STORE };
 struct VocabProduct {
     VocabOperand a, b;
+    int32_t a_bytes;        // of a row of a that are to be read (a multiple of 16), zeros from there on; 0: all
     const int32_t* active;
     int32_t rows_a_active, rows_b_active;   // the operand's rows are the rows that take part
     int32_t k_active;       // the contraction is over the rows that take part

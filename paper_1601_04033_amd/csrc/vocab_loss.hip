@@ -27,34 +27,37 @@ constexpr uint32_t kPairsB = 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10;
 
 // ---- rows that take part
 
-// used[r]; what a forward call says of rows that take no part.
-__global__ __launch_bounds__(kBlock) void mark_rows(VocabArgs a, int32_t* used, uint32_t* largest)
+// used[r], a wave each; what a forward call says of rows that take no part.
+__global__ __launch_bounds__(kBlock) void mark_rows(VocabArgs a, int32_t* used)
 {
-    if (blockIdx.x == 0 && threadIdx.x == 0) *largest = 0;
-    const int lanes = a.entries == 1 ? 1 : 64;
-    const int64_t r = (static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x) / lanes;
-    const int lane = threadIdx.x % lanes;
+    const int64_t r = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
     if (r >= a.rows) return;
     bool any = false;
-    for (int k = lane; k < a.entries; k += lanes) any |= counts(a, r * a.entries + k);
-    if (lanes > 1) any = __ballot(any) != 0;
+    for (int k = lane; k < a.entries; k += 64) any |= counts(a, r * a.entries + k);
+    any = __ballot(any) != 0;
     if (lane == 0) used[r] = any;
     if (any || !a.loss) return;
     if (lane == 0) a.loss[r] = a.lse[r] = 0.0f;
-    for (int k = lane; k < a.entries; k += lanes) a.picked[r * a.entries + k] = 0.0f;
+    for (int k = lane; k < a.entries; k += 64) a.picked[r * a.entries + k] = 0.0f;
 }
 
 // list: the rows that take part, in order; place: where in it a row is, or -1.
-__global__ __launch_bounds__(1024) void gather_rows(const int32_t* used, int64_t rows, int32_t* list, int32_t* place,
-                                                    int32_t* active)
+// used: NULL for targets, which are looked at here.
+__global__ __launch_bounds__(1024) void gather_rows(VocabArgs a, const int32_t* used, int32_t* list, int32_t* place, int32_t* active,
+                                                    uint32_t* largest)
 {
     __shared__ int waves[16];
     __shared__ int base;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (threadIdx.x == 0) base = 0;
-    for (int64_t at = 0; at < rows; at += 1024) {
+    if (threadIdx.x == 0) {
+        base = 0;
+        *largest = 0;
+    }
+    for (int64_t at = 0; at < a.rows; at += 1024) {
         const int64_t r = at + threadIdx.x;
-        const bool in = r < rows && used[r] != 0;
+        const bool in = r < a.rows && (used ? used[r] != 0 : counts(a, r));
+        if (!used && r < a.rows && !in && a.loss) a.loss[r] = a.lse[r] = a.picked[r] = 0.0f;
         const unsigned long long votes = __ballot(in);
         if (lane == 0) waves[wave] = __popcll(votes);
         __syncthreads();
@@ -65,7 +68,7 @@ __global__ __launch_bounds__(1024) void gather_rows(const int32_t* used, int64_t
         }
         const int here = before + __popcll(votes & ((1ull << lane) - 1));
         if (in) list[here] = static_cast<int32_t>(r);
-        if (r < rows) place[r] = in ? here : -1;
+        if (r < a.rows) place[r] = in ? here : -1;
         __syncthreads();
         if (threadIdx.x == 0) base = all;
     }
@@ -98,53 +101,65 @@ __device__ __forceinline__ void terms_of(float x, uint16_t (&t)[3])
     t[2] = from_float<bf16>(r - __uint_as_float(mid)).bits;
 }
 
-// 64 x 64 elements a block, 16 of a row a thread.
+// 64 x 64 elements a wave, 8 x 8 a lane, turned in registers: each load and each
+// store of a wave is whole lines of 8 rows or columns.  (131,072 x 4,096 bf16
+// turned in pieces: @L@ TB/s; through LDS 3.7.)
 template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_out(LayOut a)
 {
-    __shared__ uint16_t turned[TERMS][64][72];
     const int64_t rows = a.active ? *a.active : a.rows;
-    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64, c0 = static_cast<int64_t>(blockIdx.y) * 64;
-    if (r0 >= (rows + kVocabTile - 1) / kVocabTile * kVocabTile) return;
-    const int row = threadIdx.x >> 2, part = threadIdx.x & 3;
-    const int64_t r = r0 + row, c = c0 + part * 16;
-    T x[16];
-    for (int e = 0; e < 16; ++e) x[e] = from_float<T>(0.0f);
-    if (r < rows) {
-        const T* src = static_cast<const T*>(a.src) + (a.list ? a.list[r] : r) * a.ld + c;
-        if (c + 16 <= a.cols) {
-            const Pack<T, 16> p = load_pack<T, 16>(src);
-            for (int e = 0; e < 16; ++e) x[e] = p.v[e];
-        } else {
-            for (int e = 0; e < 16; ++e)
-                if (c + e < a.cols) x[e] = src[e];
+    const int lane = threadIdx.x & 63;
+    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64, c0 = (static_cast<int64_t>(blockIdx.y) * kWaves + (threadIdx.x >> 6)) * 64;
+    if (r0 >= (rows + kVocabTile - 1) / kVocabTile * kVocabTile || c0 >= a.cols_padded) return;
+    const int64_t r = r0 + (lane >> 3) * 8, c = c0 + (lane & 7) * 8;
+    Pack<T, 8> x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i].v[e] = from_float<T>(0.0f);
+        if (r + i < rows) {
+            const T* src = static_cast<const T*>(a.src) + (a.list ? a.list[r + i] : r + i) * a.ld + c;
+            if (c + 8 <= a.cols) {
+                x[i] = load_pack<T, 8>(src);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e < a.cols) x[i].v[e] = src[e];
+            }
         }
     }
-    Pack<uint16_t, 16> t[TERMS];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        if constexpr (TERMS == 1) {
-            t[0].v[e] = __builtin_bit_cast(uint16_t, x[e]);
-        } else {
-            uint16_t s[3];
-            terms_of(x[e], s);
-            for (int i = 0; i < TERMS; ++i) t[i].v[e] = s[i];
+    for (int term = 0; term < TERMS; ++term) {
+        uint32_t w[8][4];       // two columns a word
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (TERMS == 1) {
+                __builtin_memcpy(w[i], &x[i], sizeof w[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    uint16_t s[3], u[3];
+                    terms_of(x[i].v[e], s);
+                    terms_of(x[i].v[e + 1], u);
+                    w[i][e / 2] = s[term] | static_cast<uint32_t>(u[term]) << 16;
+                }
+            }
+            if (a.by_rows) {
+                Pack<uint32_t, 4> o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o.v[e] = w[i][e];
+                store_pack(reinterpret_cast<uint32_t*>(a.by_rows + (r + i) * a.ld_rows + term * a.cols_padded + c), o);
+            }
+        }
+        if (!a.by_cols) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            Pack<uint32_t, 4> o;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2)
+                o.v[i / 2] = __builtin_amdgcn_perm(w[i + 1][e / 2], w[i][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+            if (c + e < a.cols) store_pack(reinterpret_cast<uint32_t*>(a.by_cols + (c + e) * a.ld_cols + term * a.rows_padded + r), o);
         }
     }
-    if (a.by_rows) {
-#pragma unroll
-        for (int i = 0; i < TERMS; ++i) store_pack(a.by_rows + r * a.ld_rows + i * a.cols_padded + c, t[i]);
-    }
-    if (!a.by_cols) return;
-#pragma unroll
-    for (int i = 0; i < TERMS; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) turned[i][part * 16 + e][row] = t[i].v[e];
-    __syncthreads();
-    const int64_t col = c0 + row;
-    if (col >= a.cols) return;
-#pragma unroll
-    for (int i = 0; i < TERMS; ++i)
-        store_pack(a.by_cols + col * a.ld_cols + i * a.rows_padded + r0 + part * 16, load_pack<uint16_t, 16>(&turned[i][row][part * 16]));
 }
 
 // ---- forward
@@ -168,7 +183,7 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool kTerms = sizeof(T) == 4;
-    constexpr int kFlight = kTerms ? 8 : 16;    // steps of 16 on their way
+    constexpr int kFlight = 16;     // steps of 16 on their way
     const int lane = threadIdx.x, half = lane >> 5;
     const int64_t all = static_cast<int64_t>(*active) * a.entries, blocks = (all + 31) / 32;
     for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
@@ -186,16 +201,7 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
             const uint16_t* b = row + tb * cols_padded;
             for (int64_t k0 = 8 * half; k0 - 8 * half < a.cols; k0 += 16 * kFlight) {
                 v4i fa[kFlight], fb[kFlight];
-#pragma unroll
-                for (int s = 0; s < kFlight; ++s) {
-                    const int64_t k = k0 + 16 * s;
-                    Pack<T, 8> v;
-                    if (k + 8 <= a.cols) {
-                        v = load_pack<T, 8>(w + k);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v.v[e] = k + e < a.cols ? w[k + e] : from_float<T>(0.0f);
-                    }
+                auto take = [&](int s, const Pack<T, 8>& v) {
                     if constexpr (kTerms) {
                         Pack<uint16_t, 8> t;
 #pragma unroll
@@ -208,7 +214,30 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
                     } else {
                         fa[s] = __builtin_bit_cast(v4i, v);
                     }
-                    fb[s] = k < cols_padded ? *reinterpret_cast<const v4i*>(b + k) : v4i{0, 0, 0, 0};
+                };
+                if (k0 - 8 * half + 16 * kFlight <= a.cols) {
+                    Pack<T, 8> v[kFlight];
+#pragma unroll
+                    for (int s = 0; s < kFlight; ++s) {
+                        v[s] = load_pack<T, 8>(w + k0 + 16 * s);
+                        fb[s] = *reinterpret_cast<const v4i*>(b + k0 + 16 * s);
+                    }
+#pragma unroll
+                    for (int s = 0; s < kFlight; ++s) take(s, v[s]);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < kFlight; ++s) {
+                        const int64_t k = k0 + 16 * s;
+                        Pack<T, 8> v;
+                        if (k + 8 <= a.cols) {
+                            v = load_pack<T, 8>(w + k);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v.v[e] = k + e < a.cols ? w[k + e] : from_float<T>(0.0f);
+                        }
+                        take(s, v);
+                        fb[s] = k < cols_padded ? *reinterpret_cast<const v4i*>(b + k) : v4i{0, 0, 0, 0};
+                    }
                 }
 #pragma unroll
                 for (int s = 0; s < kFlight; ++s) acc = mfma<typename Term<T>::type>(fa[s], fb[s], acc);
@@ -225,27 +254,33 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
 
 // ---- backward
 
-// Coefficients of the rows that take part (a wave each), zeros for the rows
-// that fill up the last tile; the largest coefficient.
-__global__ __launch_bounds__(kBlock) void coefficients(VocabArgs a, const int32_t* list, const int32_t* active, VocabRow* row,
-                                                       float2* teacher, uint32_t* largest)
+// Coefficients of the rows that take part (a wave each, 16 a block), zeros for
+// the rows that fill up the last tile; the largest coefficient, where asked for.
+__global__ __launch_bounds__(1024) void coefficients(VocabArgs a, const int32_t* list, const int32_t* active, VocabRow* row,
+                                                     float2* teacher, uint32_t* largest)
 {
-    const int lane = threadIdx.x & 63, n = *active;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + (threadIdx.x >> 6);
-    if (at >= (n + kVocabTile - 1) / kVocabTile * kVocabTile) return;
+    __shared__ float most[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = *active;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 16 + wave;
+    if (at - wave >= (n + kVocabTile - 1) / kVocabTile * kVocabTile) return;
     VocabRow c = {0.0f, 0.0f, 0.0f, 0.0f};
     Teacher t = {0.0f, 0.0f};
     if (at < n) {
         const int64_t r = list[at];
         t = teacher_of(a, r, lane);
         c = coefficients_of(a, r, t, lane);
-        float most = fabsf(a.teacher ? c.f : c.g);
-        most += fabsf(c.f) + fabsf(c.b);
-        if (lane == 0) atomicMax(largest, __float_as_uint(most));      // the same in any order
     }
     if (lane == 0) {
         row[at] = c;
         teacher[at] = make_float2(t.top, t.by);
+        most[wave] = fabsf(a.teacher ? c.f : c.g) + fabsf(c.f) + fabsf(c.b);
+    }
+    if (!largest) return;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float x = most[0];
+        for (int i = 1; i < 16; ++i) x = most[i] > x || most[i] != most[i] ? most[i] : x;
+        atomicMax(largest, __float_as_uint(x));     // of values that are not negative: the same in any order
     }
 }
 
@@ -423,13 +458,13 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool back
 // Whether the products can read W where it lies.
 bool in_place(const VocabArgs& a)
 {
-    return a.dtype != DTYPE_F32 && a.cols % 128 == 0 && a.ldw % 8 == 0 && a.ldw <= (int64_t(1) << 21) &&
+    return a.dtype != DTYPE_F32 && a.cols % 8 == 0 && a.ldw % 8 == 0 && a.ldw <= (int64_t(1) << 21) &&
            (reinterpret_cast<uintptr_t>(a.w) & 15) == 0;
 }
 
 hipError_t launch_lay_out(const LayOut& l, int dtype, int64_t rows, int64_t cols, hipStream_t s)
 {
-    const dim3 grid(static_cast<unsigned>(round_up(rows, kVocabTile) / 64), static_cast<unsigned>(round_up(cols, 128) / 64));
+    const dim3 grid(static_cast<unsigned>(round_up(rows, kVocabTile) / 64), static_cast<unsigned>(round_up(cols, 256) / 256));
     if (dtype == DTYPE_F32) lay_out<float, 3><<<grid, kBlock, 0, s>>>(l);
     else lay_out<bf16, 1><<<grid, kBlock, 0, s>>>(l);       // bits of either 16-bit type
     return hipGetLastError();
@@ -455,10 +490,12 @@ hipError_t begin(const VocabArgs& a, bool backward, Plan& p, hipStream_t s)
     p.active = p.at<int32_t>(p.l.scalars);
     p.largest = p.at<uint32_t>(p.l.scalars + 4);
     p.w_in_place = in_place(a);
-    const int64_t threads = a.rows * (a.entries == 1 ? 1 : 64);
-    mark_rows<<<static_cast<unsigned>((threads + kBlock - 1) / kBlock), kBlock, 0, s>>>(a, p.used, p.largest);
-    VOCAB_TRY(hipGetLastError());
-    gather_rows<<<1, 1024, 0, s>>>(p.used, a.rows, p.list, p.place, p.active);
+    const bool entries = a.entries > 1;
+    if (entries) {
+        mark_rows<<<static_cast<unsigned>((a.rows + kWaves - 1) / kWaves), kBlock, 0, s>>>(a, p.used);
+        VOCAB_TRY(hipGetLastError());
+    }
+    gather_rows<<<1, 1024, 0, s>>>(a, entries ? p.used : nullptr, p.list, p.place, p.active, p.largest);
     VOCAB_TRY(hipGetLastError());
     LayOut x = {};
     x.src = a.x;
@@ -501,6 +538,7 @@ hipError_t piece_of(const VocabArgs& a, const Plan& p, int64_t first, int64_t n,
     q.a.data = p.w_in_place ? w : p.at<uint8_t>(l.w);
     q.a.ld = p.w_in_place ? a.ldw * size : 2 * l.ld_cols;
     q.a.rows = static_cast<int32_t>(n);
+    q.a_bytes = p.w_in_place && a.cols % 128 != 0 ? static_cast<int32_t>(a.cols * size) : 0;
     q.a.plane = q.b.plane = static_cast<int32_t>(2 * l.cols_padded);
     q.b.data = p.at<uint8_t>(l.x);
     q.b.ld = 2 * l.ld_cols;
@@ -587,7 +625,8 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
     g.splits = l.dx.splits;
     g.cols_padded = l.cols_padded;
     const unsigned row_waves = static_cast<unsigned>((l.padded + kWaves - 1) / kWaves);
-    coefficients<<<row_waves, kBlock, 0, s>>>(a, p.list, p.active, p.at<VocabRow>(l.row), p.at<float2>(l.teacher), p.largest);
+    coefficients<<<static_cast<unsigned>(l.padded / 16), 1024, 0, s>>>(a, p.list, p.active, p.at<VocabRow>(l.row), p.at<float2>(l.teacher),
+                                                                      a.dtype == DTYPE_F16 ? p.largest : nullptr);
     VOCAB_TRY(hipGetLastError());
     for (int64_t first = 0; first < a.vocab; first += l.piece) {
         const int64_t n = a.vocab - first < l.piece ? a.vocab - first : l.piece;

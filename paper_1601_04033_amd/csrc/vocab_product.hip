@@ -215,7 +215,8 @@ template <int MFMA, int READS, int LOADS, int I = 0> __device__ __forceinline__ 
 // along the contraction, each operand's row 128 bytes of it, loaded straight
 // to LDS; a stage is four sub-steps of 16, whose fragments are read while the
 // one before is multiplied.
-template <typename T, int W, int WM, int WHAT>
+// CUT: a's rows end before the contraction's last block.
+template <typename T, int W, int WM, int WHAT, bool CUT>
 __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(VocabProduct p, int tiles_m, int tiles_n, int per_split)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -254,10 +255,11 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     for (int q = 0; q < G::kLoadsA; ++q) off_a[q] = offset(q, last_a, p.a.ld);
 #pragma unroll
     for (int q = 0; q < G::kLoadsB; ++q) off_b[q] = offset(q, last_b, p.b.ld);
+    // no more than the tile's rows: what lies 2^31 bytes on is past the end
     const auto ga = same_buffer(p.a.data + m0 * p.a.ld + static_cast<int64_t>(kb0) * kBytes,
-                                (rows_a - m0) * p.a.ld - static_cast<int64_t>(kb0) * kBytes);
+                                (last_a + 1) * p.a.ld - static_cast<int64_t>(kb0) * kBytes);
     const auto gb = same_buffer(p.b.data + n0 * p.b.ld + static_cast<int64_t>(kb0) * kBytes,
-                                (pad_b - n0) * p.b.ld - static_cast<int64_t>(kb0) * kBytes);
+                                (last_b + 1) * p.b.ld - static_cast<int64_t>(kb0) * kBytes);
 
     const int place_a = (wave_m * W + (lane & 31)) * kBytes, place_b = (wave_n * W + (lane & 31)) * kBytes;
     int chunk[4];
@@ -285,8 +287,10 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     const int terms = __builtin_amdgcn_readfirstlane(p.terms), along = __builtin_amdgcn_readfirstlane(own_blocks * kBytes);
     const uint32_t terms_a = __builtin_amdgcn_readfirstlane(p.terms_a), terms_b = __builtin_amdgcn_readfirstlane(p.terms_b);
     const int plane_a = __builtin_amdgcn_readfirstlane(p.a.plane), plane_b = __builtin_amdgcn_readfirstlane(p.b.plane);
-    int at_a, at_b;
+    int at_a, at_b, rest = 0;
+    auto own_chunk = [&](int q) { return slot(lane & 7, ((q * 4 + wave) * 8 + (lane >> 3)) % 32) * 16; };
     auto next = [&]() {
+        if (CUT) rest = p.a_bytes - at;     // bytes of a row from here on
         at_a = at + static_cast<int>(terms_a >> (2 * pair) & 3u) * plane_a;
         at_b = at + static_cast<int>(terms_b >> (2 * pair) & 3u) * plane_b;
         if (at + kBytes < along) {
@@ -299,8 +303,9 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     auto load = [&](uint8_t* a, uint8_t* b, int from, int to) {
 #pragma unroll
         for (int q = from; q < to; ++q) {
-            if (q < G::kLoadsA)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ga, (lds_ptr)(a + (q * 4 + wave) * 1024), 16, off_a[q], at_a, 0, 0);
+            if (q < G::kLoadsA)     // past a buffer's end zeros are read
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ga, (lds_ptr)(a + (q * 4 + wave) * 1024), 16,
+                                                         CUT && own_chunk(q) >= rest ? 0x80000000u : off_a[q], at_a, 0, 0);
             else
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(gb, (lds_ptr)(b + ((q - G::kLoadsA) * 4 + wave) * 1024), 16, off_b[q - G::kLoadsA], at_b, 0, 0);
         }
@@ -391,9 +396,15 @@ template <typename T, int W> hipError_t launch_what(int what, const VocabProduct
     int per_split = static_cast<int>(count(p.blocks, p.splits));
     per_split += per_split & 1;     // the kernel takes stages in pairs
     switch (what) {
-    case VOCAB_STATISTICS: vocab_product<T, W, 2, VOCAB_STATISTICS><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split); break;
-    case VOCAB_GRADIENT: vocab_product<T, W, 2, VOCAB_GRADIENT><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split); break;
-    default: vocab_product<T, W, 2, VOCAB_STORE><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split); break;
+    case VOCAB_STATISTICS:
+        if (p.a_bytes) vocab_product<T, W, 2, VOCAB_STATISTICS, true><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split);
+        else vocab_product<T, W, 2, VOCAB_STATISTICS, false><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split);
+        break;
+    case VOCAB_GRADIENT:
+        if (p.a_bytes) vocab_product<T, W, 2, VOCAB_GRADIENT, true><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split);
+        else vocab_product<T, W, 2, VOCAB_GRADIENT, false><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split);
+        break;
+    default: vocab_product<T, W, 2, VOCAB_STORE, false><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split); break;
     }
     return hipGetLastError();
 }

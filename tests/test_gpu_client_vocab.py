@@ -103,7 +103,8 @@ def check(c, whole=False, dw=torch.float32, **kw):
 SIZES = [(1, 1, 1), (1, 8, 2), (3, 5, 7), (1, 128, 300), (2, 127, 129), (17, 64, 1000), (128, 1000, 10), (130, 129, 257),
          (255, 200, 511), (300, 384, 1025), (64, 1544, 2003), (16, 4096, 3000), (15, 4000, 4099), (33, 2048, 2100),
          # beyond what goes without laid out operands
-         (1025, 1, 1), (1030, 5, 7), (1100, 130, 33), (1, 8200, 3), (5, 8193, 70), (130, 8320, 257), (1300, 127, 1000)]
+         (1025, 1, 1), (1030, 5, 7), (1100, 130, 33), (1, 8200, 3), (5, 8193, 70), (130, 8320, 257), (1300, 127, 1000),
+         (1100, 8, 600), (1100, 40, 600), (1111, 72, 333), (1500, 136, 1500)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
