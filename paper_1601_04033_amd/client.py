@@ -472,6 +472,10 @@ def client_vocab_loss_forward(x, w, targets, loss, lse, picked, *, smoothing: fl
     """Softmax cross entropy of the logits logit_scale x w^T for x [rows, cols] and class weights w [vocab, cols]:
     loss, lse and picked (the targets' logits), float32 [rows].  targets: int64 [rows]; one outside [0, vocab) leaves
     its row out.  workspace: uint8, client_vocab_workspace_bytes(rows, cols, vocab, dtype, backward=False) bytes."""
+    rc = (_calls or _native()).client_vocab_loss_forward(
+        x, w, targets, loss, lse, picked, smoothing, z_loss, logit_scale, workspace, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     op = _head(x, w, logit_scale)
     n = op.rows
     pw, nw = _workspace(workspace)
@@ -487,6 +491,11 @@ def client_vocab_loss_backward(x, w, targets, lse, picked, dx, dw, *, dloss=None
     client_vocab_loss_forward (same keyword arguments, its lse and picked): dx like x or None, dw [vocab, cols] float32
     or of w's dtype (accumulate: added to) or None.  workspace: client_vocab_workspace_bytes(rows, cols, vocab, dtype)
     bytes."""
+    rc = (_calls or _native()).client_vocab_loss_backward(
+        x, w, targets, lse, picked, dx, dw, dloss, grad_scale, accumulate, smoothing, z_loss, logit_scale, workspace,
+        stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     op = _head(x, w, logit_scale)
     n = op.rows
     pw, nw = _workspace(workspace)
@@ -502,6 +511,10 @@ def client_vocab_distill_forward(x, w, index, teacher, loss, lse, picked, *, tea
     the softmax of logit_scale x w^T: loss and lse float32 [rows], picked float32 [rows, entries] (the logits at the
     entries).  An entry outside [0, vocab) is left out.  teacher_lse: float32 [rows], the teacher's log-sum-exp over
     its whole vocabulary; None takes the softmax of the row's entries.  workspace as client_vocab_loss_forward."""
+    rc = (_calls or _native()).client_vocab_distill_forward(
+        x, w, index, teacher, loss, lse, picked, teacher_scale, teacher_lse, logit_scale, workspace, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     op = _head(x, w, logit_scale)
     n = op.rows
     pi, pt, k, pl = _teacher(x, index, teacher, teacher_lse)
@@ -516,6 +529,11 @@ def client_vocab_distill_backward(x, w, index, teacher, lse, picked, dx, dw, *, 
                                   logit_scale: float = 1.0, workspace=None, stream=None) -> None:
     """The gradients of client_vocab_distill_forward (same keyword arguments, its lse and picked), as
     client_vocab_loss_backward gives them."""
+    rc = (_calls or _native()).client_vocab_distill_backward(
+        x, w, index, teacher, lse, picked, dx, dw, dloss, grad_scale, accumulate, teacher_scale, teacher_lse, logit_scale,
+        workspace, stream)
+    if rc is not None:
+        return _check(rc) if rc else None
     op = _head(x, w, logit_scale)
     n = op.rows
     pi, pt, k, pl = _teacher(x, index, teacher, teacher_lse)

@@ -45,7 +45,9 @@ static_assert(sizeof(Entry) == kCount * sizeof(void*), "one pointer per name");
 // and the client's, by the order of kClientNames
 constexpr const char* kClientNames[] = {"client_dropout", "client_residual_norm_forward",
                                         "client_residual_norm_backward", "client_fp8_quantize", "client_fp8_matmul",
-                                        "client_fp8_linear"};
+                                        "client_fp8_linear", "client_vocab_loss_forward",
+                                        "client_vocab_loss_backward", "client_vocab_distill_forward",
+                                        "client_vocab_distill_backward"};
 constexpr int kClientCount = sizeof kClientNames / sizeof kClientNames[0];
 struct ClientEntry {
     decltype(&::client_dropout) client_dropout;
@@ -54,6 +56,10 @@ struct ClientEntry {
     decltype(&::client_fp8_quantize) client_fp8_quantize;
     decltype(&::client_fp8_matmul) client_fp8_matmul;
     decltype(&::client_fp8_linear) client_fp8_linear;
+    decltype(&::client_vocab_loss_forward) client_vocab_loss_forward;
+    decltype(&::client_vocab_loss_backward) client_vocab_loss_backward;
+    decltype(&::client_vocab_distill_forward) client_vocab_distill_forward;
+    decltype(&::client_vocab_distill_backward) client_vocab_distill_backward;
 };
 static_assert(sizeof(ClientEntry) == kClientCount * sizeof(void*), "one pointer per name");
 ClientEntry g_client;                 // set by bind_client()
@@ -692,6 +698,76 @@ struct ClientArgs : Args {
         *n = 0;
         return plain && v[i] != Py_None ? tensor(i, c10::ScalarType::Byte, -1, 0, n) : nullptr;
     }
+    // a contiguous int64 tensor [rows] (columns NULL) or [rows][*columns]
+    const int64_t* indices(int i, int64_t rows, int64_t* columns)
+    {
+        if (!plain) return nullptr;
+        try {
+            if (THPVariable_CheckExact(v[i])) {
+                const at::Tensor& t = THPVariable_Unpack(v[i]);
+                if (t.dim() == (columns ? 2 : 1) && t.size(0) == rows) {
+                    if (columns) *columns = t.size(1);
+                    return static_cast<const int64_t*>(tensor(i, c10::ScalarType::Long, -1));
+                }
+            }
+        } catch (...) {
+        }
+        refuse();
+        return nullptr;
+    }
+    // x, w and the scale of their logits
+    client_vocab_head head(int x, int w, int scale)
+    {
+        client_vocab_head op;
+        memset(&op, 0, sizeof op);
+        const Matrix a = matrix(x), b = matrix(w);
+        if (plain && (a.dim != 2 || b.dim != 2 || a.dtype != b.dtype || a.cols != b.cols)) refuse();
+        op.rows = a.rows;
+        op.cols = a.cols;
+        op.vocab = b.rows;
+        op.dtype = a.dtype;
+        op.logit_scale = real(scale);
+        op.x = a.p;
+        op.ld_x = a.ld;
+        op.w = b.p;
+        op.ld_w = b.ld;
+        return op;
+    }
+    // a teacher's logits, contiguous and of x's type, at `columns` classes a row
+    const void* teacher(int i, const client_vocab_head& op, int64_t columns)
+    {
+        const Matrix m = matrix(i);
+        if (plain && (m.dim != 2 || m.dtype != op.dtype || m.rows != op.rows || m.cols != columns || columns > INT32_MAX ||
+                      (m.rows > 1 && m.ld != m.cols)))
+            refuse();
+        return m.p;
+    }
+    // dx, dw, dloss, grad_scale, accumulate
+    struct Gradients {
+        Matrix dx, dw;
+        const float* dloss;
+        float scale;
+        bool add;
+    };
+    Gradients gradients_of(int at, const client_vocab_head& op)
+    {
+        Gradients g;
+        if (plain && v[at] != Py_None) {
+            g.dx = matrix(at);
+            if (plain && (g.dx.dim != 2 || g.dx.dtype != op.dtype || g.dx.rows != op.rows || g.dx.cols != op.cols)) refuse();
+        }
+        g.dw.dtype = CLIENT_F32;
+        if (plain && v[at + 1] != Py_None) {
+            g.dw = matrix(at + 1);
+            if (plain && (g.dw.dim != 2 || (g.dw.dtype != CLIENT_F32 && g.dw.dtype != op.dtype) || g.dw.rows != op.vocab ||
+                          g.dw.cols != op.cols))
+                refuse();
+        }
+        g.dloss = parameters(at + 2, op.rows);
+        g.scale = real(at + 3);
+        g.add = truth(at + 4);
+        return g;
+    }
     // a truth value
     bool truth(int i)
     {
@@ -871,6 +947,89 @@ PyObject* linear_call(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
+// (x, w, targets, loss, lse, picked, smoothing, z_loss, logit_scale, workspace, stream)
+PyObject* vocab_loss_forward_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 11)) return nullptr;
+    ClientArgs a(args);
+    const client_vocab_head op = a.head(0, 1, 8);
+    const int64_t* targets = a.indices(2, op.rows, nullptr);
+    float *loss = a.floats(3, op.rows), *lse = a.floats(4, op.rows), *picked = a.floats(5, op.rows);
+    const float smoothing = a.real(6), z_loss = a.real(7);
+    int64_t ws = 0;
+    void* w = a.workspace(9, &ws);
+    hipStream_t s = a.stream(10);
+    return finish(a, [&] {
+        return g_client.client_vocab_loss_forward(&op, targets, smoothing, z_loss, loss, lse, picked, w,
+                                                  static_cast<size_t>(ws), s);
+    });
+}
+
+// (x, w, targets, lse, picked, dx, dw, dloss, grad_scale, accumulate, smoothing, z_loss, logit_scale, workspace, stream)
+PyObject* vocab_loss_backward_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 15)) return nullptr;
+    ClientArgs a(args);
+    const client_vocab_head op = a.head(0, 1, 12);
+    const int64_t* targets = a.indices(2, op.rows, nullptr);
+    const float *lse = a.floats(3, op.rows), *picked = a.floats(4, op.rows);
+    const ClientArgs::Gradients g = a.gradients_of(5, op);
+    const float smoothing = a.real(10), z_loss = a.real(11);
+    int64_t ws = 0;
+    void* w = a.workspace(13, &ws);
+    hipStream_t s = a.stream(14);
+    return finish(a, [&] {
+        return g_client.client_vocab_loss_backward(&op, targets, smoothing, z_loss, lse, picked, g.dloss, g.scale, g.dx.p,
+                                                   g.dx.ld, g.dw.p, g.dw.ld, g.dw.dtype, g.add, w,
+                                                   static_cast<size_t>(ws), s);
+    });
+}
+
+// (x, w, index, teacher, loss, lse, picked, teacher_scale, teacher_lse, logit_scale, workspace, stream)
+PyObject* vocab_distill_forward_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 12)) return nullptr;
+    ClientArgs a(args);
+    const client_vocab_head op = a.head(0, 1, 9);
+    int64_t k = 0;
+    const int64_t* index = a.indices(2, op.rows, &k);
+    const void* teacher = a.teacher(3, op, k);
+    float *loss = a.floats(4, op.rows), *lse = a.floats(5, op.rows), *picked = a.floats(6, op.rows * k);
+    const float scale = a.real(7);
+    const float* teacher_lse = a.parameters(8, op.rows);
+    int64_t ws = 0;
+    void* w = a.workspace(10, &ws);
+    hipStream_t s = a.stream(11);
+    return finish(a, [&] {
+        return g_client.client_vocab_distill_forward(&op, index, teacher, static_cast<int32_t>(k), scale, teacher_lse, loss,
+                                                     lse, picked, w, static_cast<size_t>(ws), s);
+    });
+}
+
+// (x, w, index, teacher, lse, picked, dx, dw, dloss, grad_scale, accumulate, teacher_scale, teacher_lse, logit_scale,
+// workspace, stream)
+PyObject* vocab_distill_backward_call(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    if (!arity(n, 16)) return nullptr;
+    ClientArgs a(args);
+    const client_vocab_head op = a.head(0, 1, 13);
+    int64_t k = 0;
+    const int64_t* index = a.indices(2, op.rows, &k);
+    const void* teacher = a.teacher(3, op, k);
+    const float *lse = a.floats(4, op.rows), *picked = a.floats(5, op.rows * k);
+    const ClientArgs::Gradients g = a.gradients_of(6, op);
+    const float scale = a.real(11);
+    const float* teacher_lse = a.parameters(12, op.rows);
+    int64_t ws = 0;
+    void* w = a.workspace(14, &ws);
+    hipStream_t s = a.stream(15);
+    return finish(a, [&] {
+        return g_client.client_vocab_distill_backward(&op, index, teacher, static_cast<int32_t>(k), scale, teacher_lse, lse,
+                                                      picked, g.dloss, g.scale, g.dx.p, g.dx.ld, g.dw.p, g.dw.ld,
+                                                      g.dw.dtype, g.add, w, static_cast<size_t>(ws), s);
+    });
+}
+
 // bind_client(addresses of the entry points in kClientNames' order), after bind()
 PyObject* bind_client(PyObject*, PyObject* list)
 {
@@ -938,6 +1097,10 @@ PyMethodDef kMethods[] = {{"bind", bind, METH_VARARGS, nullptr},
                           {kClientNames[3], fast(quantize_call), METH_FASTCALL, nullptr},
                           {kClientNames[4], fast(matmul_call), METH_FASTCALL, nullptr},
                           {kClientNames[5], fast(linear_call), METH_FASTCALL, nullptr},
+                          {kClientNames[6], fast(vocab_loss_forward_call), METH_FASTCALL, nullptr},
+                          {kClientNames[7], fast(vocab_loss_backward_call), METH_FASTCALL, nullptr},
+                          {kClientNames[8], fast(vocab_distill_forward_call), METH_FASTCALL, nullptr},
+                          {kClientNames[9], fast(vocab_distill_backward_call), METH_FASTCALL, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

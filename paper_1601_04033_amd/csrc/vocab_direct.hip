@@ -287,9 +287,16 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
             s += stat[i][threadIdx.x].y * power(stat[i][threadIdx.x].x - m);
             t += stat_sum[i][threadIdx.x];
         }
-        d.partial[blockIdx.x * d.padded + r0 + threadIdx.x] = make_float2(m, s);
-        if (d.partial_sum) d.partial_sum[blockIdx.x * d.padded + r0 + threadIdx.x] = t;
+        if (gridDim.x == 1) {   // all classes were here
+            stat[0][threadIdx.x] = make_float2(__builtin_fmaf(m, kLn2, logf(s)), t * a.scale / static_cast<float>(a.vocab));
+        } else {
+            d.partial[blockIdx.x * d.padded + r0 + threadIdx.x] = make_float2(m, s);
+            if (d.partial_sum) d.partial_sum[blockIdx.x * d.padded + r0 + threadIdx.x] = t;
+        }
     }
+    if (gridDim.x > 1) return;
+    __syncthreads();
+    for (int i = wave; i < rows; i += kLogitWaves) finish_row(a, r0 + i, stat[0][i].x, stat[0][i].y, false, lane);
 #endif
 }
 
@@ -308,6 +315,7 @@ struct Thin {
     float by;
     int32_t add, splits, row_tiles;     // row_tiles: that a wave goes through (k of at most 16)
     int32_t column_blocks, row_blocks;
+    int32_t brief;          // k of at most 16, by short_product
     int64_t blocks;         // in all; 0: not wanted
 };
 
@@ -642,9 +650,10 @@ template <bool GRADIENT> hipError_t launch_logits_of(const VocabArgs& a, const D
     return launch_logits<f16, GRADIENT>(a, d, blocks, s);
 }
 
-void set_blocks(Thin& p)
+void set_blocks(Thin& p, bool brief)
 {
-    p.column_blocks = static_cast<int32_t>(count(p.cols, p.k <= 16 ? 512 : 128));
+    p.brief = brief;
+    p.column_blocks = static_cast<int32_t>(count(p.cols, brief ? 512 : 128));
     p.row_blocks = static_cast<int32_t>(count(count(p.rows, 16), p.row_tiles));
     p.blocks = static_cast<int64_t>(p.column_blocks) * p.row_blocks * p.splits;
 }
@@ -652,14 +661,14 @@ void set_blocks(Thin& p)
 template <typename T, typename OUT> hipError_t launch_products(const Thin& dx, const Thin& dw, hipStream_t s)
 {
     const unsigned n = static_cast<unsigned>(dx.blocks), m = static_cast<unsigned>(dw.blocks);
-    if (n && m && dx.k > 16 && dw.k > 16) {
+    if (n && m && !dx.brief && !dw.brief) {
         long_products<T, OUT><<<n + m, 256, 0, s>>>(dx, dw);
         return hipGetLastError();
     }
-    if (n && dx.k <= 16) short_product<T, T><<<n, 256, 0, s>>>(dx);
+    if (n && dx.brief) short_product<T, T><<<n, 256, 0, s>>>(dx);
     else if (n) long_product<T, T, false><<<n, 256, 0, s>>>(dx);
     VOCAB_TRY(hipGetLastError());
-    if (m && dw.k <= 16) short_product<T, OUT><<<m, 256, 0, s>>>(dw);
+    if (m && dw.brief) short_product<T, OUT><<<m, 256, 0, s>>>(dw);
     else if (m) long_product<T, OUT, true><<<m, 256, 0, s>>>(dw);
     return hipGetLastError();
 }
@@ -683,7 +692,7 @@ template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, u
         dx.c = l.splits > 1 ? base + l.sums : static_cast<uint8_t*>(a.dx);
         dx.ldc = l.splits > 1 ? l.cols_padded : a.lddx;
         dx.used_r = used;
-        set_blocks(dx);
+        set_blocks(dx, a.vocab <= 16 && !(a.dw && a.rows > 16));     // with dW in one launch where that is long
     }
     if (a.dw) {
         dw.a = reinterpret_cast<float*>(base + l.dz);
@@ -704,7 +713,7 @@ template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, u
         const int64_t waves = count(a.vocab, 16) * count(a.cols, 128);
         const int64_t each = a.rows <= 16 ? waves / 8192 : 1;
         dw.row_tiles = static_cast<int32_t>(each < 1 ? 1 : each);
-        set_blocks(dw);
+        set_blocks(dw, a.rows <= 16);
     }
     if (a.dw_dtype == DTYPE_F32) VOCAB_TRY((launch_products<T, float>(dx, dw, s)));
     else VOCAB_TRY((launch_products<T, T>(dx, dw, s)));
@@ -740,7 +749,7 @@ hipError_t launch_vocab_direct_forward(const VocabArgs& a, hipStream_t s)
     d.partial = reinterpret_cast<float2*>(base + l.partial);
     d.partial_sum = a.smoothing != 0.0f ? reinterpret_cast<float*>(base + l.partial_sum) : nullptr;
     VOCAB_TRY(launch_logits_of<false>(a, d, l.blocks, s));
-    finish<<<static_cast<unsigned>(count(a.rows, 8)), kBlock, 0, s>>>(a, nullptr, nullptr, d.partial, d.partial_sum, l.blocks, l.padded);
+    if (l.blocks > 1) finish<<<static_cast<unsigned>(count(a.rows, 8)), kBlock, 0, s>>>(a, nullptr, nullptr, d.partial, d.partial_sum, l.blocks, l.padded);
     return hipGetLastError();
 }
 

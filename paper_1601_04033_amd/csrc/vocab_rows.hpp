@@ -127,6 +127,42 @@ __device__ __forceinline__ VocabRow coefficients_of(const VocabArgs& a, int64_t 
     return c;
 }
 
+// The outputs of row r from its log-sum-exp and the mean of its logits.  taken:
+// known to take part; else that is found here, and what takes no part gets zeros.
+// A whole wave's work.
+__device__ __forceinline__ void finish_row(const VocabArgs& a, int64_t r, float lse, float mean, bool taken, int lane)
+{
+    if (!taken) {
+        bool any = false;
+        for (int k = lane; k < a.entries; k += 64) {
+            const bool in = counts(a, r * a.entries + k);
+            if (!in) a.picked[r * a.entries + k] = 0.0f;
+            any |= in;
+        }
+        if (__ballot(any) == 0) {
+            if (lane == 0) a.loss[r] = a.lse[r] = 0.0f;
+            return;
+        }
+    }
+    float loss = 0.0f;
+    if (!a.teacher) {
+        if (lane == 0) loss = lse - (1.0f - a.smoothing) * a.picked[r] - a.smoothing * mean + a.z_loss * lse * lse;
+    } else {
+        const Teacher t = teacher_of(a, r, lane);
+        const float log_by = logf(t.by);
+        for (int k = lane; k < a.entries; k += 64)
+            if (counts(a, r * a.entries + k)) {
+                const float lw = log_weight(a, t, r * a.entries + k), q = power(lw * kLog2e) * t.by;
+                loss += q == 0.0f ? 0.0f : q * (lw + log_by - (a.picked[r * a.entries + k] - lse));
+            }
+        loss = wave_sum(loss);
+    }
+    if (lane == 0) {
+        a.loss[r] = loss;
+        a.lse[r] = lse;
+    }
+}
+
 // Rows' losses from the statistics of their logits: 8 rows a block, the slots
 // in 32 parts, joined in order.  list: the rows that take part (NULL: all are
 // here, and those that take none are told apart).
@@ -163,41 +199,8 @@ static __global__ __launch_bounds__(kBlock) void finish(VocabArgs a, const int32
         mean_of[at] = all * a.scale / static_cast<float>(a.vocab);
     }
     __syncthreads();
-    const int lane = threadIdx.x & 63;
-    for (int i = threadIdx.x >> 6; i < 8 && first + i < n; i += kWaves) {
-        const int64_t r = list ? list[first + i] : first + i;
-        if (!list) {
-            bool any = false;
-            for (int k = lane; k < a.entries; k += 64) {
-                const bool in = counts(a, r * a.entries + k);
-                if (!in) a.picked[r * a.entries + k] = 0.0f;
-                any |= in;
-            }
-            if (__ballot(any) == 0) {
-                if (lane == 0) a.loss[r] = a.lse[r] = 0.0f;
-                continue;
-            }
-        }
-        const float lse = lse_of[i];
-        float loss = 0.0f;
-        if (!a.teacher) {
-            if (lane == 0)
-                loss = lse - (1.0f - a.smoothing) * a.picked[r] - a.smoothing * mean_of[i] + a.z_loss * lse * lse;
-        } else {
-            const Teacher t = teacher_of(a, r, lane);
-            const float log_by = logf(t.by);
-            for (int k = lane; k < a.entries; k += 64)
-                if (counts(a, r * a.entries + k)) {
-                    const float lw = log_weight(a, t, r * a.entries + k), q = power(lw * kLog2e) * t.by;
-                    loss += q == 0.0f ? 0.0f : q * (lw + log_by - (a.picked[r * a.entries + k] - lse));
-                }
-            loss = wave_sum(loss);
-        }
-        if (lane == 0) {
-            a.loss[r] = loss;
-            a.lse[r] = lse;
-        }
-    }
+    for (int i = threadIdx.x >> 6; i < 8 && first + i < n; i += kWaves)
+        finish_row(a, list ? list[first + i] : first + i, lse_of[i], mean_of[i], list != nullptr, threadIdx.x & 63);
 }
 
 }  // namespace
