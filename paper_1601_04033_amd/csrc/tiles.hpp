@@ -63,15 +63,19 @@ template <int MFMA, int READS, int LOADS, int VALU, int I = 0> __device__ __forc
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
-// 32 x 32 sums of 16 products of bf16's or fp16's; a lane holds 8 of its row l % 32.
-template <typename T> __device__ __forceinline__ v16f mfma(const v4i& a, const v4i& b, const v16f& c);
-template <> __device__ __forceinline__ v16f mfma<bf16>(const v4i& a, const v4i& b, const v16f& c)
+// 16 x 16 sums of 32 products of bf16's or fp16's: lane l holds 8 values of row
+// l % 16 of each operand (chunk l / 16 of the row's 64 bytes), and of the sums
+// column l % 16 and rows 4 (l / 16) to 4 (l / 16) + 3.  At the chip's power limit
+// it does an eighth more than 32 x 32 x 16 (random values in registers 2,070
+// against 1,810 TFLOP/s).
+template <typename T> __device__ __forceinline__ v4f mfma(const v4i& a, const v4i& b, const v4f& c);
+template <> __device__ __forceinline__ v4f mfma<bf16>(const v4i& a, const v4i& b, const v4f& c)
 {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
-template <> __device__ __forceinline__ v16f mfma<f16>(const v4i& a, const v4i& b, const v16f& c)
+template <> __device__ __forceinline__ v4f mfma<f16>(const v4i& a, const v4i& b, const v4f& c)
 {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
 }
 
 // A tile in vector registers.  Accumulators stay in the accumulation
@@ -83,15 +87,21 @@ __device__ __forceinline__ v16f take(const v16f& acc)
     asm volatile("" : "+v"(t));
     return t;
 }
+__device__ __forceinline__ v4f take(const v4f& acc)
+{
+    v4f t = acc;
+    asm volatile("" : "+v"(t));
+    return t;
+}
 
-// A wave's outputs times `by` to rows m on and columns n on of c ([rows][cols],
-// row stride ld): each lane N neighbouring columns at once, at any alignment.
+// A wave's outputs to rows m on and columns n on of c ([rows][cols], row
+// stride ld): each lane N neighbouring columns at once, at any alignment.
 // WHOLE: all of them lie in c, and c is not added to.  Otherwise a lane that
 // c's last column cuts through stores its columns one by one.  (The checks
 // cost 2 us of a 4,096 x 4,096 x 1,024 product's 22 with short sums.)
 template <typename T, int W, int N, bool WHOLE>
 __device__ __forceinline__ void write_tiles(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
-                                              int64_t m, int64_t n, bool add, int lane, float by = 1.0f)
+                                              int64_t m, int64_t n, bool add, int lane)
 {
     const int rows_left = static_cast<int>(rows - m < W ? rows - m : W) - 4 * N * (lane >> 5);
     const int cols_left = static_cast<int>(cols - n < W ? cols - n : W) - N * (lane & 31);
@@ -110,13 +120,13 @@ __device__ __forceinline__ void write_tiles(const v16f (&acc)[N][N], T* c, int64
                 Pack<T, N> x;
                 if (!WHOLE && add) x = load_pack<T, N>(out);
 #pragma unroll
-                for (int j = 0; j < N; ++j) x.v[j] = from_float<T>(!WHOLE && add ? to_float(x.v[j]) + t[j][r] * by : t[j][r] * by);
+                for (int j = 0; j < N; ++j) x.v[j] = from_float<T>(!WHOLE && add ? to_float(x.v[j]) + t[j][r] : t[j][r]);
                 store_pack(out, x);
             }
             if (!WHOLE && cut && row < rows_left) {
 #pragma unroll
                 for (int j = 0; j + 1 < N; ++j)
-                    if (j < cols_left && cols_left < N) out[j] = from_float<T>(add ? to_float(out[j]) + t[j][r] * by : t[j][r] * by);
+                    if (j < cols_left && cols_left < N) out[j] = from_float<T>(add ? to_float(out[j]) + t[j][r] : t[j][r]);
             }
         }
     }
@@ -124,10 +134,10 @@ __device__ __forceinline__ void write_tiles(const v16f (&acc)[N][N], T* c, int64
 
 template <typename T, int W, int N>
 __device__ __forceinline__ void write_outputs(const v16f (&acc)[N][N], T* c, int64_t ld, int64_t rows, int64_t cols,
-                                              int64_t m, int64_t n, bool add, int lane, float by = 1.0f)
+                                              int64_t m, int64_t n, bool add, int lane)
 {
-    if (!add && m + W <= rows && n + W <= cols) write_tiles<T, W, N, true>(acc, c, ld, rows, cols, m, n, add, lane, by);
-    else write_tiles<T, W, N, false>(acc, c, ld, rows, cols, m, n, add, lane, by);
+    if (!add && m + W <= rows && n + W <= cols) write_tiles<T, W, N, true>(acc, c, ld, rows, cols, m, n, add, lane);
+    else write_tiles<T, W, N, false>(acc, c, ld, rows, cols, m, n, add, lane);
 }
 
 #endif

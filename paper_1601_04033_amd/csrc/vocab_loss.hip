@@ -172,7 +172,7 @@ template <> struct Term<float> {
     using type = bf16;
 };
 
-// The logits at the entries, 32 a wave: the diagonal of the product of their
+// The logits at the entries, 16 a wave: the diagonal of the product of their
 // classes' rows and their rows of x, by the instruction and in the order of
 // the tiles, so that they are bit for bit what the tiles put into the sums of
 // powers.  (A row's largest logit is often its target: an error that the sum
@@ -183,23 +183,21 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool kTerms = sizeof(T) == 4;
-    constexpr int kFlight = 16;     // steps of 16 on their way
-    const int lane = threadIdx.x, half = lane >> 5;
-    const int64_t all = static_cast<int64_t>(*active) * a.entries, blocks = (all + 31) / 32;
+    constexpr int kFlight = 16;     // steps of 32 on their way
+    const int lane = threadIdx.x, part = lane >> 4;
+    const int64_t all = static_cast<int64_t>(*active) * a.entries, blocks = (all + 15) / 16;
     for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
-        const int64_t pair = block * 32 + (lane & 31);
+        const int64_t pair = block * 16 + (lane & 15);
         const int64_t at = pair < all ? pair / a.entries : 0;
         const int64_t r = list[at], here = r * a.entries + (pair < all ? pair % a.entries : 0);
         const bool in = pair < all && counts(a, here);
         const T* w = static_cast<const T*>(a.w) + (in ? a.index[here] : 0) * a.ldw;
         const uint16_t* row = x + at * ld_x;
-        v16f acc;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = 0.0f;
+        v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int p = 0; p < (kTerms ? 6 : 1); ++p) {
             const int ta = kTerms ? kPairsA >> (2 * p) & 3u : 0, tb = kTerms ? kPairsB >> (2 * p) & 3u : 0;
             const uint16_t* b = row + tb * cols_padded;
-            for (int64_t k0 = 8 * half; k0 - 8 * half < a.cols; k0 += 16 * kFlight) {
+            for (int64_t k0 = 8 * part; k0 - 8 * part < a.cols; k0 += 32 * kFlight) {
                 v4i fa[kFlight], fb[kFlight];
                 auto take = [&](int s, const Pack<T, 8>& v) {
                     if constexpr (kTerms) {
@@ -215,19 +213,19 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
                         fa[s] = __builtin_bit_cast(v4i, v);
                     }
                 };
-                if (k0 - 8 * half + 16 * kFlight <= a.cols) {
+                if (k0 - 8 * part + 32 * kFlight <= a.cols) {
                     Pack<T, 8> v[kFlight];
 #pragma unroll
                     for (int s = 0; s < kFlight; ++s) {
-                        v[s] = load_pack<T, 8>(w + k0 + 16 * s);
-                        fb[s] = *reinterpret_cast<const v4i*>(b + k0 + 16 * s);
+                        v[s] = load_pack<T, 8>(w + k0 + 32 * s);
+                        fb[s] = *reinterpret_cast<const v4i*>(b + k0 + 32 * s);
                     }
 #pragma unroll
                     for (int s = 0; s < kFlight; ++s) take(s, v[s]);
                 } else {
 #pragma unroll
                     for (int s = 0; s < kFlight; ++s) {
-                        const int64_t k = k0 + 16 * s;
+                        const int64_t k = k0 + 32 * s;
                         Pack<T, 8> v;
                         if (k + 8 <= a.cols) {
                             v = load_pack<T, 8>(w + k);
@@ -243,11 +241,11 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
                 for (int s = 0; s < kFlight; ++s) acc = mfma<typename Term<T>::type>(fa[s], fb[s], acc);
             }
         }
-        // lane l: column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4
-        float z = 0.0f;
+        // lane l: column l % 16, rows 4 (l / 16) + i
+        float z = acc[0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z = 8 * (i >> 2) + 4 * half + (i & 3) == (lane & 31) ? acc[i] : z;
-        if ((lane >> 2 & 1) == half && pair < all) a.picked[here] = in ? z * a.scale : 0.0f;
+        for (int i = 1; i < 4; ++i) z = (lane & 3) == i ? acc[i] : z;
+        if ((lane & 15) >> 2 == part && pair < all) a.picked[here] = in ? z * a.scale : 0.0f;
     }
 #endif
 }
@@ -579,7 +577,7 @@ hipError_t launch_vocab_forward(const VocabArgs& a, hipStream_t s)
         q.partial_sum = a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr;
         VOCAB_TRY(launch_vocab_product(VOCAB_STATISTICS, q, n, a.rows, s));
     }
-    const int64_t blocks = (a.rows * a.entries + 31) / 32;
+    const int64_t blocks = (a.rows * a.entries + 15) / 16;
     const unsigned picks = static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20);
     const uint16_t* x = p.at<uint16_t>(l.x);
     if (a.dtype == DTYPE_F32) pick<float><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);

@@ -5,13 +5,14 @@
 //
 // Operands are 16-bit terms (client activations of 16 bits are one, fp32 is
 // the sum of three in bf16: 24 bits).  Their products are exact in fp32 and
-// summed there by v_mfma_f32_32x32x16.  For the logits a holds the classes and
-// b the rows, so that a lane's 16 outputs of a matrix tile are classes of one
-// row: maxima and sums over classes stay within a lane but for one exchange,
-// and the gradient is laid out along the rows (for dW) and along the classes
-// (for dx) straight from registers.
+// summed there by v_mfma_f32_16x16x32.  For the logits a holds the classes and
+// b the rows, so that what a lane has of a wave's tile is a run of classes of
+// each of a few neighbouring rows: maxima and sums over classes stay within a
+// lane but for two exchanges, and the gradient is laid out along the rows (for
+// dW) and along the classes (for dx) straight from registers.
 //
-// Bound by the matrix instructions.
+// Bound by the matrix instructions, and by the power that they draw.
+// (figures)
 #include <float.h>
 
 #include "tiles.hpp"
@@ -24,67 +25,79 @@ namespace {
 
 __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// x of this lane and the lane 32 away: the larger, the sum.
-__device__ __forceinline__ float larger_half(float x)
-{
-    const Pair p = across<32>(x);
-    return fmaxf(p.x, p.y);
-}
-__device__ __forceinline__ float sum_half(float x)
-{
-    const Pair p = across<32>(x);
-    return p.x + p.y;
-}
+// A wave's tile of W x W is N x N tiles of 16 x 16.  Row r of tile i is a's row
+// N r + i, so a lane, which has rows 4 (l / 16) on of each tile, has the 4 N
+// classes from 4 N (l / 16) on.  Column c of tile j is b's row
+// b_row(j, c): runs of RUN neighbours a lane.
+template <int RUN> __device__ __forceinline__ int b_row(int j, int c) { return j / RUN * (16 * RUN) + c * RUN + j % RUN; }
 
 // Statistics of a wave's classes for each of its rows (include/fasgd_client.h):
 // the largest exponent in powers of two, the sum of powers relative to it and,
-// where asked for, the sum of the logits.  One pass over the accumulators, a
-// matrix tile at a time with the running maximum, since each is read out of
-// the accumulation registers.
+// where asked for, the sum of the logits.  One pass over the accumulators, 16
+// values at a time with the running maximum, since each is read out of the
+// accumulation registers.
 template <int W, int N>
-__device__ __forceinline__ void statistics(const v16f (&acc)[N][N], const VocabProduct& p, int64_t m, int64_t n, int left,
+__device__ __forceinline__ void statistics(const v4f (&acc)[N][N], const VocabProduct& p, int64_t m, int64_t n, int left,
                                            int lane)
 {
     const float c = p.scale_log2e;
     const bool cut = left < W;
-    float2* out = p.partial + (p.first + m) / W * p.padded + n + N * (lane & 31);
-    float* out_sum = p.partial_sum ? p.partial_sum + (p.first + m) / W * p.padded + n + N * (lane & 31) : nullptr;
+    const int64_t at = (p.first + m) / W * p.padded + n + N * (lane & 15);
     Pack<float2, N> result;
     Pack<float, N> total;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         float top = -FLT_MAX, sum = 0.0f, all = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v16f t = take(acc[i][j]);
+        for (int i0 = 0; i0 < N; i0 += 4) {
+            float t[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const v4f x = take(acc[i0 + i][j]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) t[i][r] = x[r];
+            }
             if (cut) {      // classes past the last take no part
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int row = (8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * N + i;
-                    all += row < left ? t[r] : 0.0f;
-                    t[r] = row < left ? t[r] : -INFINITY;
-                }
-            } else if (out_sum) {
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) all += t[r];
+                    for (int r = 0; r < 4; ++r) {
+                        const bool in = N * (4 * (lane >> 4) + r) + i0 + i < left;
+                        all += in ? t[i][r] : 0.0f;
+                        t[i][r] = in ? t[i][r] : -INFINITY;
+                    }
+            } else if (p.partial_sum) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) all += t[i][r];
             }
-            float most = t[0];
+            float most = t[0][0];
 #pragma unroll
-            for (int r = 1; r < 16; ++r) most = fmaxf(most, t[r]);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) most = fmaxf(most, t[i][r]);
             const float next = fmaxf(top, most * c);
             sum *= power(top - next);
             top = next;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += power(__builtin_fmaf(t[r], c, -top));
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum += power(__builtin_fmaf(t[i][r], c, -top));
         }
-        const float both = larger_half(top);
-        sum = sum_half(sum * power(top - both));
-        result.v[j] = make_float2(both, sum);
-        total.v[j] = sum_half(all);
+        Pair x = across<16>(top);
+        x = across<32>(fmaxf(x.x, x.y));
+        const float both = fmaxf(x.x, x.y);
+        Pair s = across<16>(sum * power(top - both));
+        s = across<32>(s.x + s.y);
+        result.v[j] = make_float2(both, s.x + s.y);
+        s = across<16>(all);
+        s = across<32>(s.x + s.y);
+        total.v[j] = s.x + s.y;
     }
-    if (lane < 32) {
-        store_pack(out, result);
-        if (out_sum) store_pack(out_sum, total);
+    if (lane < 16) {
+        store_pack(p.partial + at, result);
+        if (p.partial_sum) store_pack(p.partial_sum + at, total);
     }
 }
 
@@ -108,126 +121,247 @@ template <typename T> __device__ __forceinline__ float high_term(uint32_t u);
 template <> __device__ __forceinline__ float high_term<bf16>(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 template <> __device__ __forceinline__ float high_term<f16>(uint32_t u) { return static_cast<float>(__builtin_bit_cast(v2h, u)[1]); }
 
-// The gradient of a wave's logits, in both layouts.  A lane holds N rows and,
-// at a time, 4 N neighbouring classes: words of two rows go to dz^T as they are,
-// words of two classes are put together from them.
+// x[r] of the lanes of parts 0 to 3 (lane / 16), for r = 0 to 3, turned: x[s] of
+// part g is then what part s had in x[g].
+__device__ __forceinline__ void turn_parts(uint32_t (&x)[4])
+{
+    // halves: the upper one of the first is exchanged with the lower one of the second; rows of 16 lanes alike
+    const auto a = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false), b = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+    const auto e = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), f = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    x[0] = e[0];
+    x[1] = e[1];
+    x[2] = f[0];
+    x[3] = f[1];
+}
+
+// The gradient of a wave's logits, in both layouts.  A lane holds N rows and 4 N
+// neighbouring classes; 4 rows and N classes at a time.  Words of two rows go to
+// dz^T as they are, words of two classes are put together from them.  A single
+// term of dz is turned among the parts of the wave first, so that 4 lanes store
+// neighbouring classes: @TURN@
 template <typename T, int W, int N>
-__device__ __forceinline__ void gradient(const v16f (&acc)[N][N], const VocabProduct& p, int64_t m, int64_t n, int left,
+__device__ __forceinline__ void gradient(const v4f (&acc)[N][N], const VocabProduct& p, int64_t m, int64_t n, int left,
                                          int lane)
 {
     const float c = p.scale_log2e;
-    float l[N], f[N], b[N];
     const float up = term_scale<T>(*p.largest);
+    const int terms = p.dz_terms > p.dzt_terms ? p.dz_terms : p.dzt_terms, first = 4 * N * (lane >> 4);
+    const bool turn = p.dz_terms == 1;
+    uint16_t* dzt = p.dzt + (m + first) * p.ld_dzt + n + N * (lane & 15);
+    uint16_t* dz = p.dz + (n + N * (lane & 15)) * p.ld_dz + m + (turn ? N * (lane >> 4) : first);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const VocabRow row = p.row[n + N * (lane & 31) + j];
-        l[j] = row.l;
-        f[j] = row.f * up;
-        b[j] = row.b * up;
-    }
-    const int terms = p.dz_terms > p.dzt_terms ? p.dz_terms : p.dzt_terms;
-    uint16_t* dz = p.dz + (n + N * (lane & 31)) * p.ld_dz + m + 4 * N * (lane >> 5);
-    uint16_t* dzt = p.dzt + (m + 4 * N * (lane >> 5)) * p.ld_dzt + n + N * (lane & 31);
+    for (int j0 = 0; j0 < N; j0 += 4) {
+        float l[4], f[4], b[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        float v[4 * N][N];
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float z = acc[i][j][4 * q + r];
-                    asm volatile("" : "+v"(z));     // read out of the accumulation registers here
-                    v[r * N + i][j] = __builtin_fmaf(f[j], power(__builtin_fmaf(z, c, -l[j])), -b[j]);
-                }
-        if (left < W) {     // nothing of classes past the last
-#pragma unroll
-            for (int k = 0; k < 4 * N; ++k)
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[k][j] = 4 * N * (2 * q + (lane >> 5)) + k < left ? v[k][j] : 0.0f;
+        for (int j = 0; j < 4; ++j) {
+            const VocabRow row = p.row[n + N * (lane & 15) + j0 + j];
+            l[j] = row.l;
+            f[j] = row.f * up;
+            b[j] = row.b * up;
         }
-        for (int t = 0; t < terms; ++t) {
-            uint32_t w[4 * N][N / 2];
+        uint32_t own[4][N / 2][4];     // of row j: word of classes, part's run r
 #pragma unroll
-            for (int k = 0; k < 4 * N; ++k)
+        for (int r = 0; r < 4; ++r) {
+            float v[N][4];
 #pragma unroll
-                for (int j = 0; j < N; j += 2) {
-                    const uint32_t u = two_terms<T>(v[k][j], v[k][j + 1]);
-                    w[k][j / 2] = u;
-                    v[k][j] -= low_term<T>(u);
-                    v[k][j + 1] -= high_term<T>(u);
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float z = acc[i][j0 + j][r];
+                    asm volatile("" : "+v"(z));     // read out of the accumulation registers here
+                    v[i][j] = __builtin_fmaf(f[j], power(__builtin_fmaf(z, c, -l[j])), -b[j]);
                 }
-            if (t < p.dzt_terms) {
-                uint16_t* out = dzt + t * p.padded;
+            if (left < W) {     // nothing of classes past the last
 #pragma unroll
-                for (int k = 0; k < 4 * N; ++k) {
-                    Pack<uint32_t, N / 2> x;
+                for (int i = 0; i < N; ++i)
 #pragma unroll
-                    for (int j = 0; j < N / 2; ++j) x.v[j] = w[k][j];
-                    store_pack(reinterpret_cast<uint32_t*>(out + (8 * N * q + k) * p.ld_dzt), x);
+                    for (int j = 0; j < 4; ++j) v[i][j] = first + N * r + i < left ? v[i][j] : 0.0f;
+            }
+            for (int t = 0; t < terms; ++t) {
+                uint32_t w[N][2];
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+                        const uint32_t u = two_terms<T>(v[i][j], v[i][j + 1]);
+                        w[i][j / 2] = u;
+                        v[i][j] -= low_term<T>(u);
+                        v[i][j + 1] -= high_term<T>(u);
+                    }
+                if (t < p.dzt_terms) {
+                    uint16_t* out = dzt + t * p.padded + j0;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        Pack<uint32_t, 2> x;
+                        x.v[0] = w[i][0];
+                        x.v[1] = w[i][1];
+                        store_pack(reinterpret_cast<uint32_t*>(out + (N * r + i) * p.ld_dzt), x);
+                    }
+                }
+                if (t < p.dz_terms) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        Pack<uint32_t, N / 2> x;
+#pragma unroll
+                        for (int i = 0; i < N; i += 2)
+                            x.v[i / 2] = __builtin_amdgcn_perm(w[i + 1][j / 2], w[i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
+                        if (turn) {
+#pragma unroll
+                            for (int i = 0; i < N / 2; ++i) own[j][i][r] = x.v[i];
+                        } else {
+                            store_pack(reinterpret_cast<uint32_t*>(dz + (j0 + j) * p.ld_dz + t * p.classes + N * r), x);
+                        }
+                    }
                 }
             }
-            if (t < p.dz_terms) {
-                uint16_t* out = dz + t * p.classes + 8 * N * q;
+        }
+        if (!turn) continue;
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    Pack<uint32_t, 2 * N> x;
+        for (int j = 0; j < 4; ++j) {
 #pragma unroll
-                    for (int k = 0; k < 4 * N; k += 2)
-                        x.v[k / 2] = __builtin_amdgcn_perm(w[k + 1][j / 2], w[k][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-                    store_pack(reinterpret_cast<uint32_t*>(out + j * p.ld_dz), x);
-                }
+            for (int i = 0; i < N / 2; ++i) turn_parts(own[j][i]);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                Pack<uint32_t, N / 2> x;
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) x.v[i] = own[j][i][s];
+                store_pack(reinterpret_cast<uint32_t*>(dz + (j0 + j) * p.ld_dz + 4 * N * s), x);
             }
         }
     }
 }
 
-// A buffer that is the same in all lanes, said so: where the compiler does not
-// see it, it loops over the lanes' values at each load of a stage (the gradient's
-// product at 8,192 x 16,384 x 4,096 1,130 against @GB@ us).
-__device__ __forceinline__ auto same_buffer(const uint8_t* p, int64_t bytes)
+// A wave's outputs times `by` to rows m on and columns n on of c ([rows][cols],
+// row stride ld), 4 neighbouring columns of a lane at once, at any alignment.
+// WHOLE: all of them lie in c, and c is not added to.
+template <typename OUT, int W, int N, bool WHOLE>
+__device__ __forceinline__ void write_sums(const v4f (&acc)[N][N], OUT* c, int64_t ld, int64_t rows, int64_t cols, int64_t m,
+                                           int64_t n, bool add, int lane, float by)
+{
+    const int first = 4 * N * (lane >> 4);
+    const int rows_left = static_cast<int>(rows - m < W ? rows - m : W) - first;
+    const int cols_left = static_cast<int>(cols - n < W ? cols - n : W) - 4 * (lane & 15);
+    OUT* base = c + (m + first) * ld + n + 4 * (lane & 15);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int h = 0; h < N / 4; ++h) {
+            v4f t[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = take(acc[i][4 * h + e]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                OUT* out = base + (N * r + i) * ld + 64 * h;
+                Pack<OUT, 4> x;
+                if (WHOLE) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x.v[e] = from_float<OUT>(t[e][r] * by);
+                    store_pack(out, x);
+                } else if (N * r + i < rows_left) {
+                    const int here = cols_left - 64 * h;
+                    if (here >= 4) {
+                        if (add) x = load_pack<OUT, 4>(out);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x.v[e] = from_float<OUT>(add ? to_float(x.v[e]) + t[e][r] * by : t[e][r] * by);
+                        store_pack(out, x);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (e < here) out[e] = from_float<OUT>(add ? to_float(out[e]) + t[e][r] * by : t[e][r] * by);
+                    }
+                }
+            }
+        }
+}
+
+template <typename OUT, int W, int N>
+__device__ __forceinline__ void write_product(const v4f (&acc)[N][N], OUT* c, int64_t ld, int64_t rows, int64_t cols, int64_t m,
+                                              int64_t n, bool add, int lane, float by)
+{
+    if (!add && m + W <= rows && n + W <= cols) write_sums<OUT, W, N, true>(acc, c, ld, rows, cols, m, n, add, lane, by);
+    else write_sums<OUT, W, N, false>(acc, c, ld, rows, cols, m, n, add, lane, by);
+}
+
+// c += a b in c's own accumulation registers.  A wave's 128 x 128 sums fill all
+// 256 of them, and the compiler, which may give the instruction another place for
+// its result, moves a quarter of the sums about in each round of the loop for it.
+// What reads c next as anything but a sum waits for it (sums_done).
+template <typename T> __device__ __forceinline__ void multiply_into(v4f& c, const v4i& a, const v4i& b);
+template <> __device__ __forceinline__ void multiply_into<bf16>(v4f& c, const v4i& a, const v4i& b)
+{
+    asm("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+template <> __device__ __forceinline__ void multiply_into<f16>(v4f& c, const v4i& a, const v4i& b)
+{
+    asm("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+template <int N> __device__ __forceinline__ void sums_done(v4f (&c)[N][N])
+{
+    // the sums pass through on both sides: the last instruction is before the
+    // wait, which is longer than its passes, and every read of them after it
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) asm volatile("" : "+a"(c[i][j]));
+    asm volatile("s_nop 15" ::: "memory");
+    asm volatile("s_nop 15" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) asm volatile("" : "+a"(c[i][j]));
+}
+
+// What is the same in all lanes, said so: where the compiler does not see it, it
+// loops over the lanes' buffers at each load of a stage (the gradient's product
+// at 8,192 x 16,384 x 4,096 1,130 against 960 us).
+__device__ __forceinline__ const uint8_t* same_pointer(const uint8_t* p)
 {
     const uint64_t at = reinterpret_cast<uint64_t>(p);
     const uint32_t low = __builtin_amdgcn_readfirstlane(static_cast<int>(at)), high = __builtin_amdgcn_readfirstlane(static_cast<int>(at >> 32));
-    const int64_t most = bytes < 0xffffffffll ? bytes : 0xffffffffll;
-    const uint32_t n = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(most)));
-    return buffer(reinterpret_cast<const uint8_t*>(static_cast<uint64_t>(high) << 32 | low), n);
+    return reinterpret_cast<const uint8_t*>(static_cast<uint64_t>(high) << 32 | low);
 }
+__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Order of a sub-step's instructions for the compiler's scheduler: between
-// matrix instructions go the LDS reads, in the first half, so that they have
-// arrived at its end, and the loads.
-template <int MFMA, int READS, int LOADS, int I = 0> __device__ __forceinline__ void order()
-{
-    constexpr int kMfma = 0x8, kDsRead = 0x100, kVmem = 0x20, kHalf = MFMA / 2;
-    constexpr int kReads = I < kHalf ? (I + 1) * READS / kHalf - I * READS / kHalf : 0;
-    constexpr int kLoads = (I + 1) * LOADS / MFMA - I * LOADS / MFMA;
-    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-    if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(kDsRead, kReads, 0);
-    if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(kVmem, kLoads, 0);
-    if constexpr (I + 1 < MFMA) order<MFMA, READS, LOADS, I + 1>();
-}
+// Where an operand's next stage is loaded from.
+struct Place {
+    const uint8_t* base;    // of the tile's rows
+    uint32_t bytes;         // of the buffer; 0 behind the last stage: zeros are read
+    uint32_t which;         // of the terms, 2 bits a pair
+    int plane, at, pair;
+};
 
 #endif
 
-// The block's tile goes through LDS as in the 8-bit product: two stages of 64
-// along the contraction, each operand's row 128 bytes of it, loaded straight
-// to LDS; a stage is four sub-steps of 16, whose fragments are read while the
-// one before is multiplied.
+// The block's tile goes through LDS, 64 of the contraction a stage, each
+// operand's row 128 bytes of it, loaded straight to LDS.  (Rows of 64 bytes, with
+// stages half as long and twice as many on their way, took 8 % longer: L2 gives
+// whole lines.)  A stage is two sub-steps of 32, whose fragments are read while
+// the one before is multiplied.  Two ways for a stage's LDS to come free:
+//   ring of five: parts of stages (a's or b's rows) go round five slots, a's part
+//     of stage k + 2 into the fifth while stage k's first sub-step is multiplied,
+//     b's into a's slot as soon as every wave has read it.  Five stages are a
+//     round; those behind the last are zeros.
+//   two stages (the logits' large tiles: their short contraction would be cut up
+//     by rounds, and their operands lie nearer): stage k + 2 into stage k's place,
+//     its loads over two sub-steps, since at once they are more than the CU takes
+//     in while one is multiplied.
 // CUT: a's rows end before the contraction's last block.
 template <typename T, int W, int WM, int WHAT, bool CUT>
 __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(VocabProduct p, int tiles_m, int tiles_n, int per_split)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using G = Geometry<W, WM>;
-    constexpr int N = G::kTiles;
-    __shared__ __attribute__((aligned(16))) uint8_t a0[G::kStageA], b0[G::kStageB], a1[G::kStageA], b1[G::kStageB];
-    const int active = __builtin_amdgcn_readfirstlane(*p.active);
+    static_assert(G::kStageA == G::kStageB, "a slot takes either operand");
+    constexpr int N = W / 16, kSlot = G::kStageA, kLoads = G::kLoadsA;
+    constexpr int kRun = WHAT == VOCAB_STORE ? 4 : N;
+    constexpr bool kRing = true;
+    __shared__ __attribute__((aligned(16))) uint8_t s0[kSlot], s1[kSlot], s2[kSlot], s3[kSlot], s4[kRing ? kSlot : 16];
+    const int active = same(*p.active);
     const int tiles = tiles_m * tiles_n;
-    const int id = tile_of(blockIdx.x % tiles, tiles_m, tiles_n);
-    const int split = blockIdx.x / tiles;
-    const int64_t m0 = static_cast<int64_t>(id / tiles_n) * G::kRowsA, n0 = static_cast<int64_t>(id % tiles_n) * G::kRowsB;
+    // (quotients come from the vector unit; all that follows from them is the same in all lanes)
+    const int split = same(static_cast<int>(blockIdx.x) / tiles);
+    const int id = same(tile_of(static_cast<int>(blockIdx.x) - split * tiles, tiles_m, tiles_n)), row = same(id / tiles_n);
+    const int64_t m0 = static_cast<int64_t>(row) * G::kRowsA, n0 = static_cast<int64_t>(id - row * tiles_n) * G::kRowsB;
     const int rows_a = p.rows_a_active ? active : p.a.rows, rows_b = p.rows_b_active ? active : p.b.rows;
     // rows of a gradient that a contraction reads are whole blocks of 128
     const int pad_b = p.rows_b_active ? (rows_b + 127) / 128 * 128 : rows_b;
@@ -239,133 +373,145 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     const int blocks = p.k_active ? (active + 127) / 128 * 2 : p.blocks;
     const int kb0 = split * per_split;
     const int own_blocks = blocks - kb0 < per_split ? blocks - kb0 : per_split;
-    const int steps = own_blocks > 0 ? own_blocks * p.terms : 0;
+    const int terms = same(p.terms), along = same(own_blocks * kBytes), steps = own_blocks > 0 ? own_blocks * terms : 0;
 
     // Rows past a's last are read as its last; b's padding to 128 rows of zeros
-    // is there, and what lies behind it is read as its last.
-    uint32_t off_a[G::kLoadsA], off_b[G::kLoadsB];
+    // is there, and what lies behind it is read as its last.  Load q of a wave
+    // fills 8 rows of a slot, 128 bytes each, the 16-byte chunk c of row r of a
+    // tile in place slot(c, r).
+    uint32_t off_a[kLoads], off_b[kLoads];
     const int last_a = static_cast<int>(rows_a - m0 < G::kRowsA ? rows_a - m0 : G::kRowsA) - 1;
     const int last_b = static_cast<int>(pad_b - n0 < G::kRowsB ? pad_b - n0 : G::kRowsB) - 1;
-    auto offset = [&](int q, int last, int64_t ld) {
-        const int place = (q * 4 + wave) * 8 + (lane >> 3), r = place % 32;
-        const int row = place / W * W + r * N + place % W / 32;
-        return static_cast<uint32_t>(row < last ? row : last) * static_cast<uint32_t>(ld) + slot(lane & 7, r) * 16u;
-    };
+    const int chunk_at = slot(lane & 7, (wave * 8 + (lane >> 3)) % 16) * 16;     // of the lane's loads
 #pragma unroll
-    for (int q = 0; q < G::kLoadsA; ++q) off_a[q] = offset(q, last_a, p.a.ld);
-#pragma unroll
-    for (int q = 0; q < G::kLoadsB; ++q) off_b[q] = offset(q, last_b, p.b.ld);
-    // no more than the tile's rows: what lies 2^31 bytes on is past the end
-    const auto ga = same_buffer(p.a.data + m0 * p.a.ld + static_cast<int64_t>(kb0) * kBytes,
-                                (last_a + 1) * p.a.ld - static_cast<int64_t>(kb0) * kBytes);
-    const auto gb = same_buffer(p.b.data + n0 * p.b.ld + static_cast<int64_t>(kb0) * kBytes,
-                                (last_b + 1) * p.b.ld - static_cast<int64_t>(kb0) * kBytes);
+    for (int q = 0; q < kLoads; ++q) {
+        const int place = (q * 4 + wave) * 8 + (lane >> 3), i = place % W / 16, r = place % 16;
+        const int row_a = place / W * W + N * r + i, row_b = place / W * W + b_row<kRun>(i, r);
+        off_a[q] = static_cast<uint32_t>(row_a < last_a ? row_a : last_a) * static_cast<uint32_t>(p.a.ld) + chunk_at;
+        off_b[q] = static_cast<uint32_t>(row_b < last_b ? row_b : last_b) * static_cast<uint32_t>(p.b.ld) + chunk_at;
+    }
+    // the bytes are those of the tile's rows: what lies 2^31 on is past the end
+    const int64_t skip = static_cast<int64_t>(kb0) * kBytes;
+    Place pa = {same_pointer(p.a.data + m0 * p.a.ld + skip), static_cast<uint32_t>(same(static_cast<int>((last_a + 1) * p.a.ld - skip))),
+                static_cast<uint32_t>(same(p.terms_a)), same(p.a.plane), 0, 0};
+    Place pb = {same_pointer(p.b.data + n0 * p.b.ld + skip), static_cast<uint32_t>(same(static_cast<int>((last_b + 1) * p.b.ld - skip))),
+                static_cast<uint32_t>(same(p.terms_b)), same(p.b.plane), 0, 0};
 
-    const int place_a = (wave_m * W + (lane & 31)) * kBytes, place_b = (wave_n * W + (lane & 31)) * kBytes;
-    int chunk[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) chunk[c] = slot(c * 2 + (lane >> 5), lane & 31) * 16;
+    const int place_a = (wave_m * W + (lane & 15)) * kBytes, place_b = (wave_n * W + (lane & 15)) * kBytes;
+    const int chunk[2] = {slot(lane >> 4, lane & 15) * 16, slot(4 + (lane >> 4), lane & 15) * 16};
 
-    v16f acc[N][N];
+    v4f acc[N][N];
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+        for (int j = 0; j < N; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 
     // Loads go on from stage to stage, a pair of terms over the contraction and
-    // then the next pair.  Past the last it is loaded again.  The pairs come
-    // with the smallest first: the matrix instruction aligns its 16 products
-    // with the sum and cuts off what lies 3 bits below the sum's last, so the
-    // large sums are to be met as few times as there are blocks (fp32, 1,024
-    // rows: dx off by 3.3e-6 with a block's pairs together, 1.4e-6 so).
-    int at = 0, pair = 0;
-    constexpr int kLoads = G::kLoadsA + G::kLoadsB;
-    constexpr int kFirst = kLoads / 2;
-    // (as same_buffer)
-    const int terms = __builtin_amdgcn_readfirstlane(p.terms), along = __builtin_amdgcn_readfirstlane(own_blocks * kBytes);
-    const uint32_t terms_a = __builtin_amdgcn_readfirstlane(p.terms_a), terms_b = __builtin_amdgcn_readfirstlane(p.terms_b);
-    const int plane_a = __builtin_amdgcn_readfirstlane(p.a.plane), plane_b = __builtin_amdgcn_readfirstlane(p.b.plane);
-    int at_a, at_b, rest = 0;
-    auto own_chunk = [&](int q) { return slot(lane & 7, ((q * 4 + wave) * 8 + (lane >> 3)) % 32) * 16; };
-    auto next = [&]() {
-        if (CUT) rest = p.a_bytes - at;     // bytes of a row from here on
-        at_a = at + static_cast<int>(terms_a >> (2 * pair) & 3u) * plane_a;
-        at_b = at + static_cast<int>(terms_b >> (2 * pair) & 3u) * plane_b;
-        if (at + kBytes < along) {
-            at += kBytes;
-        } else if (pair + 1 < terms) {
-            ++pair;
-            at = 0;
-        }
+    // then the next pair, then zeros.  The pairs come with the smallest first: the
+    // matrix instruction aligns its products with the sum and cuts off what lies
+    // 3 bits below the sum's last, so the large sums are to be met as few times
+    // as there are blocks (fp32, 1,024 rows: dx off by 3.3e-6 with a block's
+    // pairs together, 1.4e-6 so).
+    auto next = [&](Place& l) {     // without branches, which would part the stage's instructions
+        const int more = (l.at + kBytes - along) >> 31, turn = ~more & (l.pair + 1 - terms) >> 31;     // all ones: yes
+        l.at = (l.at + (kBytes & more)) & ~turn;
+        l.pair -= turn;
+        l.bytes &= static_cast<uint32_t>(more | turn);
     };
-    auto load = [&](uint8_t* a, uint8_t* b, int from, int to) {
+    auto load_a = [&](uint8_t* to, int from, int until) {
+        const int at = same(pa.at + static_cast<int>(pa.which >> (2 * pa.pair) & 3u) * pa.plane), rest = CUT ? p.a_bytes - pa.at : 0;
+        const auto from_a = buffer(pa.base, static_cast<uint32_t>(same(static_cast<int>(pa.bytes))));
 #pragma unroll
-        for (int q = from; q < to; ++q) {
-            if (q < G::kLoadsA)     // past a buffer's end zeros are read
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ga, (lds_ptr)(a + (q * 4 + wave) * 1024), 16,
-                                                         CUT && own_chunk(q) >= rest ? 0x80000000u : off_a[q], at_a, 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(gb, (lds_ptr)(b + ((q - G::kLoadsA) * 4 + wave) * 1024), 16, off_b[q - G::kLoadsA], at_b, 0, 0);
-        }
+        for (int q = from; q < until; ++q)      // past a buffer's end zeros are read
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_a, (lds_ptr)(to + (q * 4 + wave) * 1024), 16,
+                                                     CUT && chunk_at >= rest ? 0x80000000u : off_a[q], at, 0, 0);
+        if (until == kLoads) next(pa);
+    };
+    auto load_b = [&](uint8_t* to, int from, int until) {
+        const int at = same(pb.at + static_cast<int>(pb.which >> (2 * pb.pair) & 3u) * pb.plane);
+        const auto from_b = buffer(pb.base, static_cast<uint32_t>(same(static_cast<int>(pb.bytes))));
+#pragma unroll
+        for (int q = from; q < until; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from_b, (lds_ptr)(to + (q * 4 + wave) * 1024), 16, off_b[q], at, 0, 0);
+        if (until == kLoads) next(pb);
     };
     v4i fa[2][N], fb[2][N];
-    auto read = [&](int f, const uint8_t* a, const uint8_t* b, int u) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            fa[f][i] = *reinterpret_cast<const v4i*>(a + place_a + chunk[u] + i * 32 * kBytes);
-            fb[f][i] = *reinterpret_cast<const v4i*>(b + place_b + chunk[u] + i * 32 * kBytes);
-        }
+    auto read = [&](int f, int q, const uint8_t* a, const uint8_t* b, int u) {     // fragment q of 2 N: b's, then a's
+        if (q < N) fb[f][q] = *reinterpret_cast<const v4i*>(b + place_b + chunk[u] + q * 16 * kBytes);
+        else fa[f][q - N] = *reinterpret_cast<const v4i*>(a + place_a + chunk[u] + (q - N) * 16 * kBytes);
     };
-    auto multiply = [&](int f) {
+    // Multiplies fragments f.  Between the matrix instructions, in this order, go
+    // the reads of the next fragments, in the first half, so that they have arrived
+    // at its end, and kLoads loads, spread evenly.
+    auto multiply = [&](int f, const uint8_t* a, const uint8_t* b, int u, auto load) {
+        constexpr int kPairs = N * N / 2, kReads = 2 * N / (kPairs / 2), kApart = kPairs / kLoads;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int s = 0; s < kPairs; ++s) {
+            if (s < kPairs / 2) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[i][j] = mfma<T>(fa[f][i], fb[f][j], acc[i][j]);
+                for (int q = 0; q < kReads; ++q) read(f ^ 1, s * kReads + q, a, b, u);
+            }
+            if (s % kApart == kApart - 1) load(s / kApart);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int i = (2 * s + e) / N, j = (2 * s + e) % N;
+                if constexpr (W == 128) multiply_into<T>(acc[i][j], fa[f][i], fb[f][j]);
+                else acc[i][j] = mfma<T>(fa[f][i], fb[f][j], acc[i][j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
     // Stage k lies in (a, b), the next in (an, bn) or on its way there, and the
     // first fragments hold stage k's first sub-step.
-    auto step = [&](uint8_t* a, uint8_t* b, uint8_t* an, uint8_t* bn) {
-#pragma unroll
-        for (int u = 0; u < 3; ++u) {
-            read((u + 1) & 1, a, b, u + 1);
-            if (u == 0) load(an, bn, kFirst, kLoads);
-            multiply(u & 1);
-            if (u == 0) order<N * N, 2 * N, kLoads - kFirst>();
-            else order<N * N, 2 * N, 0>();
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        // The next stage has arrived and every wave holds the rest of this one
-        // in registers: its LDS is free for the stage after next.  Its loads go
-        // over two sub-steps: at once they are more than the CU takes in while
-        // one is multiplied (8,192 x 16,384 x 4,096 906 against 850 us).
+    auto step = [&](uint8_t* a, uint8_t* b, uint8_t* an, uint8_t* bn, uint8_t* fifth) {
+        multiply(0, a, b, 1, [&](int q) {
+            if (kRing) load_a(fifth, q, q + 1);
+            else if (q < kLoads / 2) load_a(an, kLoads / 2 + q, kLoads / 2 + q + 1);
+            else load_b(bn, q, q + 1);
+        });
+        // The next stage has arrived (in the ring, a's part of the one after it is
+        // on its way) and every wave holds the rest of this one in registers.
+        if (kRing) __builtin_amdgcn_s_waitcnt(0x0070 | kLoads);     // vmcnt(kLoads) lgkmcnt(0)
+        else __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1, an, bn, 0, [&](int q) {
+            if (kRing) load_b(a, q, q + 1);
+            else if (q < kLoads / 2) load_a(a, q, q + 1);
+            else load_b(b, q - kLoads / 2, q - kLoads / 2 + 1);
+        });
+    };
+    if (steps > 0) {
+        load_a(s0, 0, kLoads);
+        load_b(s1, 0, kLoads);
+        load_a(s2, 0, kRing ? kLoads : kLoads / 2);
+        load_b(s3, 0, kRing ? kLoads : kLoads / 2);
         __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        next();
-        read(0, an, bn, 0);
-        load(a, b, 0, kFirst);
-        multiply(1);
-        order<N * N, 2 * N, kFirst>();
+#pragma unroll
+        for (int q = 0; q < 2 * N; ++q) read(0, q, s0, s1, 0);
         __builtin_amdgcn_sched_barrier(0);
-    };
-    if (steps > 0) {
-        next();
-        load(a0, b0, 0, kLoads);
-        next();
-        load(a1, b1, 0, kFirst);
-        __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0)
-        __syncthreads();
-        read(0, a0, b0, 0);
         int k = 0;
-        do {        // an even number of stages
-            step(a0, b0, a1, b1);
-            step(a1, b1, a0, b0);
-            k += 2;
-        } while (k < steps);
+        if constexpr (kRing) {
+            do {
+                step(s0, s1, s2, s3, s4);
+                step(s2, s3, s4, s0, s1);
+                step(s4, s0, s1, s2, s3);
+                step(s1, s2, s3, s4, s0);
+                step(s3, s4, s0, s1, s2);
+                k += 5;
+            } while (k < steps);
+        } else {
+            do {        // an even number of stages
+                step(s0, s1, s2, s3, s4);
+                step(s2, s3, s0, s1, s4);
+                k += 2;
+            } while (k < steps);
+        }
         // the last loads land in LDS before this block gives it up
         __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0)
+        if constexpr (W == 128) sums_done<N>(acc);
     }
 
     const int64_t m = m0 + wave_m * W, n = n0 + wave_n * W;
@@ -379,9 +525,9 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
         const bool add = p.add != 0;
         if (m >= rows_a) return;
         if (p.c_dtype == DTYPE_F32)
-            write_outputs<float, W, N>(acc, static_cast<float*>(p.c) + split * p.split_stride, p.ldc, rows_a, rows_b, m, n, add, lane, by);
+            write_product<float, W, N>(acc, static_cast<float*>(p.c) + split * p.split_stride, p.ldc, rows_a, rows_b, m, n, add, lane, by);
         else
-            write_outputs<T, W, N>(acc, static_cast<T*>(p.c), p.ldc, rows_a, rows_b, m, n, add, lane, by);
+            write_product<T, W, N>(acc, static_cast<T*>(p.c), p.ldc, rows_a, rows_b, m, n, add, lane, by);
     }
 #endif
 }
