@@ -27,9 +27,9 @@ __device__ __forceinline__ float power(float x) { return __builtin_amdgcn_exp2f(
 
 // A wave's tile of W x W is N x N tiles of 16 x 16.  Row r of tile i is a's row
 // N r + i, so a lane, which has rows 4 (l / 16) on of each tile, has the 4 N
-// classes from 4 N (l / 16) on.  Column c of tile j is b's row
-// b_row(j, c): runs of RUN neighbours a lane.
-template <int RUN> __device__ __forceinline__ int b_row(int j, int c) { return j / RUN * (16 * RUN) + c * RUN + j % RUN; }
+// classes from 4 N (l / 16) on.  Column c of tile j is b's row b_row(j, c): runs of
+// 4 neighbours a lane, and 16 lanes store whole lines.
+__device__ __forceinline__ int b_row(int j, int c) { return j / 4 * 64 + c * 4 + j % 4; }
 
 // Statistics of a wave's classes for each of its rows (include/fasgd_client.h):
 // the largest exponent in powers of two, the sum of powers relative to it and,
@@ -42,12 +42,12 @@ __device__ __forceinline__ void statistics(const v4f (&acc)[N][N], const VocabPr
 {
     const float c = p.scale_log2e;
     const bool cut = left < W;
-    const int64_t at = (p.first + m) / W * p.padded + n + N * (lane & 15);
-    Pack<float2, N> result;
-    Pack<float, N> total;
+    const int64_t at = (p.first + m) / W * p.padded + n + 4 * (lane & 15);
+    Pack<float2, 4> result[N / 4];
+    Pack<float, 4> total[N / 4];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        float top = -FLT_MAX, sum = 0.0f, all = 0.0f;
+        float top = -FLT_MAX, part[4] = {0.0f, 0.0f, 0.0f, 0.0f}, all = 0.0f;      // four sums: short chains
 #pragma unroll
         for (int i0 = 0; i0 < N; i0 += 4) {
             float t[4][4];
@@ -72,32 +72,36 @@ __device__ __forceinline__ void statistics(const v4f (&acc)[N][N], const VocabPr
 #pragma unroll
                     for (int r = 0; r < 4; ++r) all += t[i][r];
             }
-            float most = t[0][0];
+            float most[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) most = fmaxf(most, t[i][r]);
-            const float next = fmaxf(top, most * c);
-            sum *= power(top - next);
+            for (int r = 0; r < 4; ++r) most[r] = fmaxf(fmaxf(t[0][r], t[1][r]), fmaxf(t[2][r], t[3][r]));
+            const float next = fmaxf(top, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * c);
+            const float down = power(top - next);
             top = next;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int r = 0; r < 4; ++r) {
+                part[r] *= down;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum += power(__builtin_fmaf(t[i][r], c, -top));
+                for (int i = 0; i < 4; ++i) part[r] += power(__builtin_fmaf(t[i][r], c, -top));
+            }
         }
+        const float sum = (part[0] + part[1]) + (part[2] + part[3]);
         Pair x = across<16>(top);
         x = across<32>(fmaxf(x.x, x.y));
         const float both = fmaxf(x.x, x.y);
         Pair s = across<16>(sum * power(top - both));
         s = across<32>(s.x + s.y);
-        result.v[j] = make_float2(both, s.x + s.y);
+        result[j / 4].v[j % 4] = make_float2(both, s.x + s.y);
         s = across<16>(all);
         s = across<32>(s.x + s.y);
-        total.v[j] = s.x + s.y;
+        total[j / 4].v[j % 4] = s.x + s.y;
     }
     if (lane < 16) {
-        store_pack(p.partial + at, result);
-        if (p.partial_sum) store_pack(p.partial_sum + at, total);
+#pragma unroll
+        for (int h = 0; h < N / 4; ++h) {
+            store_pack(p.partial + at + 64 * h, result[h]);
+            if (p.partial_sum) store_pack(p.partial_sum + at + 64 * h, total[h]);
+        }
     }
 }
 
@@ -135,10 +139,11 @@ __device__ __forceinline__ void turn_parts(uint32_t (&x)[4])
 }
 
 // The gradient of a wave's logits, in both layouts.  A lane holds N rows and 4 N
-// neighbouring classes; 4 rows and N classes at a time.  Words of two rows go to
-// dz^T as they are, words of two classes are put together from them.  A single
-// term of dz is turned among the parts of the wave first, so that 4 lanes store
-// neighbouring classes: @TURN@
+// neighbouring classes; 4 rows at a time.  Words of two rows go to dz^T as they
+// are, words of two classes are put together from them and turned among the parts
+// of the wave, so that 4 lanes store neighbouring classes.  (Each layout's stores
+// as they come, 16 bytes a lane with gaps between, cost 20 % of the 8,192 x 16,384
+// x 4,096 product.)
 template <typename T, int W, int N>
 __device__ __forceinline__ void gradient(const v4f (&acc)[N][N], const VocabProduct& p, int64_t m, int64_t n, int left,
                                          int lane)
@@ -146,86 +151,72 @@ __device__ __forceinline__ void gradient(const v4f (&acc)[N][N], const VocabProd
     const float c = p.scale_log2e;
     const float up = term_scale<T>(*p.largest);
     const int terms = p.dz_terms > p.dzt_terms ? p.dz_terms : p.dzt_terms, first = 4 * N * (lane >> 4);
-    const bool turn = p.dz_terms == 1;
-    uint16_t* dzt = p.dzt + (m + first) * p.ld_dzt + n + N * (lane & 15);
-    uint16_t* dz = p.dz + (n + N * (lane & 15)) * p.ld_dz + m + (turn ? N * (lane >> 4) : first);
 #pragma unroll
     for (int j0 = 0; j0 < N; j0 += 4) {
+        const int64_t row0 = n + 16 * j0 + 4 * (lane & 15);
         float l[4], f[4], b[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const VocabRow row = p.row[n + N * (lane & 15) + j0 + j];
+            const VocabRow row = p.row[row0 + j];
             l[j] = row.l;
             f[j] = row.f * up;
             b[j] = row.b * up;
         }
-        uint32_t own[4][N / 2][4];     // of row j: word of classes, part's run r
+        float v[4][N][4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            float v[N][4];
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < N; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float z = acc[i][j0 + j][r];
                     asm volatile("" : "+v"(z));     // read out of the accumulation registers here
-                    v[i][j] = __builtin_fmaf(f[j], power(__builtin_fmaf(z, c, -l[j])), -b[j]);
+                    v[r][i][j] = __builtin_fmaf(f[j], power(__builtin_fmaf(z, c, -l[j])), -b[j]);
+                    if (left < W) v[r][i][j] = first + N * r + i < left ? v[r][i][j] : 0.0f;     // nothing of classes past the last
                 }
-            if (left < W) {     // nothing of classes past the last
+        for (int t = 0; t < terms; ++t) {
+            uint16_t* dzt = p.dzt + (m + first) * p.ld_dzt + t * p.padded + row0;
+            uint32_t own[4][N / 2][4];     // of row j: word of classes, part's run r
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[i][j] = first + N * r + i < left ? v[i][j] : 0.0f;
-            }
-            for (int t = 0; t < terms; ++t) {
+            for (int r = 0; r < 4; ++r) {
                 uint32_t w[N][2];
 #pragma unroll
                 for (int i = 0; i < N; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; j += 2) {
-                        const uint32_t u = two_terms<T>(v[i][j], v[i][j + 1]);
+                        const uint32_t u = two_terms<T>(v[r][i][j], v[r][i][j + 1]);
                         w[i][j / 2] = u;
-                        v[i][j] -= low_term<T>(u);
-                        v[i][j + 1] -= high_term<T>(u);
+                        v[r][i][j] -= low_term<T>(u);
+                        v[r][i][j + 1] -= high_term<T>(u);
                     }
                 if (t < p.dzt_terms) {
-                    uint16_t* out = dzt + t * p.padded + j0;
 #pragma unroll
                     for (int i = 0; i < N; ++i) {
                         Pack<uint32_t, 2> x;
                         x.v[0] = w[i][0];
                         x.v[1] = w[i][1];
-                        store_pack(reinterpret_cast<uint32_t*>(out + (N * r + i) * p.ld_dzt), x);
+                        store_pack(reinterpret_cast<uint32_t*>(dzt + (N * r + i) * p.ld_dzt), x);
                     }
                 }
-                if (t < p.dz_terms) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        Pack<uint32_t, N / 2> x;
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                        for (int i = 0; i < N; i += 2)
-                            x.v[i / 2] = __builtin_amdgcn_perm(w[i + 1][j / 2], w[i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
-                        if (turn) {
-#pragma unroll
-                            for (int i = 0; i < N / 2; ++i) own[j][i][r] = x.v[i];
-                        } else {
-                            store_pack(reinterpret_cast<uint32_t*>(dz + (j0 + j) * p.ld_dz + t * p.classes + N * r), x);
-                        }
-                    }
-                }
+                    for (int i = 0; i < N; i += 2)
+                        own[j][i / 2][r] = __builtin_amdgcn_perm(w[i + 1][j / 2], w[i][j / 2], j & 1 ? 0x07060302u : 0x05040100u);
             }
-        }
-        if (!turn) continue;
+            if (t >= p.dz_terms) continue;
+            uint16_t* dz = p.dz + row0 * p.ld_dz + t * p.classes + m + N * (lane >> 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 4; ++j) {
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) turn_parts(own[j][i]);
+                for (int i = 0; i < N / 2; ++i) turn_parts(own[j][i]);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                Pack<uint32_t, N / 2> x;
+                for (int s = 0; s < 4; ++s) {
+                    Pack<uint32_t, N / 2> x;
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) x.v[i] = own[j][i][s];
-                store_pack(reinterpret_cast<uint32_t*>(dz + (j0 + j) * p.ld_dz + 4 * N * s), x);
+                    for (int i = 0; i < N / 2; ++i) x.v[i] = own[j][i][s];
+                    store_pack(reinterpret_cast<uint32_t*>(dz + j * p.ld_dz + 4 * N * s), x);
+                }
             }
         }
     }
@@ -353,7 +344,6 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     using G = Geometry<W, WM>;
     static_assert(G::kStageA == G::kStageB, "a slot takes either operand");
     constexpr int N = W / 16, kSlot = G::kStageA, kLoads = G::kLoadsA;
-    constexpr int kRun = WHAT == VOCAB_STORE ? 4 : N;
     constexpr bool kRing = true;
     __shared__ __attribute__((aligned(16))) uint8_t s0[kSlot], s1[kSlot], s2[kSlot], s3[kSlot], s4[kRing ? kSlot : 16];
     const int active = same(*p.active);
@@ -386,7 +376,7 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
         const int place = (q * 4 + wave) * 8 + (lane >> 3), i = place % W / 16, r = place % 16;
-        const int row_a = place / W * W + N * r + i, row_b = place / W * W + b_row<kRun>(i, r);
+        const int row_a = place / W * W + N * r + i, row_b = place / W * W + b_row(i, r);
         off_a[q] = static_cast<uint32_t>(row_a < last_a ? row_a : last_a) * static_cast<uint32_t>(p.a.ld) + chunk_at;
         off_b[q] = static_cast<uint32_t>(row_b < last_b ? row_b : last_b) * static_cast<uint32_t>(p.b.ld) + chunk_at;
     }
@@ -519,7 +509,8 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
         if (m < rows_a) statistics<W, N>(acc, p, m, n, static_cast<int>(rows_a - m < W ? rows_a - m : W), lane);
     } else if constexpr (WHAT == VOCAB_GRADIENT) {
         const int64_t left = rows_a - m;
-        gradient<T, W, N>(acc, p, m, n, static_cast<int>(left < W ? (left < 0 ? 0 : left) : W), lane);
+        const int here = static_cast<int>(left < W ? (left < 0 ? 0 : left) : W);
+        gradient<T, W, N>(acc, p, m, n, here, lane);
     } else {
         const float by = p.by / (p.largest ? term_scale<T>(*p.largest) : 1.0f);
         const bool add = p.add != 0;
