@@ -270,6 +270,9 @@ fasgd_status vocab_gradients(fasgd::VocabArgs& a, const float* dloss, float grad
         return fail(FASGD_ERR_ARG, "dw_dtype = %d is neither CLIENT_F32 nor dtype = %d", dw_dtype, a.dtype);
     if (dw) FASGD_TRY(check_matrix("dw", dw, ld_dw, a.vocab, a.cols, dw_dtype));
     if (dx && a.rows > 0) FASGD_TRY(check_matrix("dx", dx, ld_dx, a.rows, a.cols, a.dtype));
+    // both are read after parts of the gradients are written
+    if (dx && dx == a.x) return fail(FASGD_ERR_ARG, "dx may not be x");
+    if (dw && dw == a.w) return fail(FASGD_ERR_ARG, "dw may not be w");
     FASGD_TRY(check_vector("dloss", dloss, false));
     a.dloss = dloss;
     a.grad_scale = grad_scale;
