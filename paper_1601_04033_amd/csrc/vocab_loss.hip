@@ -403,13 +403,29 @@ constexpr int64_t kPieceBytes = int64_t(1) << 30;
 // 16,384: rows 32 KB apart 855 us, 512 bytes more 822, 256 more 957).
 int64_t apart(int64_t n) { return ((n + 255) / 256 | 1) * 256; }
 
+// Terms of dz that dW is summed from: one for a dw of 16 bits.  For an fp32 one
+// two of fp16 (22 bits), or two of bf16 (16 bits), whose rounding leaves dW off by
+// 2.6e-6 (relative, root mean square), or three (24 bits).  Sums over m rows in
+// fp32, of the values themselves, are off by 0.6 to 0.9e-6 at 1,100 rows, 1.2 to
+// 1.7e-6 at 4,096 and 1.6 to 2.1e-6 at 8,192, so up to there the third term is
+// worth its time: 3 terms leave 0.4 to 0.9e-6, and a training step of 1,100 x 512 x
+// 32,000 takes 407 instead of 361 us, of 2,048 x 2,048 x 8,192 455 instead of 399, of
+// 8,192 x 2,048 x 8,192 1,483 instead of 1,279.
+constexpr int64_t kThreeTerms = 4096;       // for fewer rows
+int terms_for_dw(int64_t rows, int dtype, int dw_dtype)
+{
+    if (dtype == DTYPE_F32) return 3;
+    if (dw_dtype != DTYPE_F32) return 1;
+    return dtype == DTYPE_BF16 && rows < kThreeTerms ? 3 : 2;
+}
+
 Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool backward)
 {
     Layout l = {};
     l.terms = vocab_terms(dtype);
     l.padded = round_up(rows, kVocabTile);
     l.cols_padded = round_up(cols, 128);
-    const int dzt_terms = l.terms == 1 ? 2 : 3;
+    const int dzt_terms = terms_for_dw(rows, dtype, DTYPE_F32);
     const int64_t each = 2 * (l.padded * (l.terms + dzt_terms) + 2 * l.cols_padded * l.terms);
     int64_t most = kPieceBytes / each / kVocabTile * kVocabTile;
     if (most < 2048) most = 2048;
@@ -420,7 +436,7 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool back
     const int64_t pairs = l.terms == 3 ? 6 : 1;
     l.logits = vocab_plan(l.piece, rows, l.cols_padded / 64 * pairs, 1);
     l.dx = vocab_plan(rows, cols, l.piece / 64 * pairs, kVocabSplits);
-    l.dw = vocab_plan(l.piece, cols, l.padded / 64 * (l.terms == 3 ? 6 : 2), 1);
+    l.dw = vocab_plan(l.piece, cols, l.padded / 64 * (l.terms == 3 ? 6 : dzt_terms), 1);
     l.slots = (vocab + l.logits.wave - 1) / l.logits.wave;
     l.ld_cols = apart(l.terms * l.cols_padded);
     l.ld_rows = apart(l.terms * l.padded);
@@ -612,9 +628,8 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
     g.largest = p.largest;
     g.dz = p.at<uint16_t>(l.dz);
     g.dzt = p.at<uint16_t>(l.dzt);
-    // an fp32 dw takes two terms of a 16-bit type's dz (22 or 16 bits), a 16-bit one takes one
     g.dz_terms = a.dx ? l.terms : 0;
-    g.dzt_terms = !a.dw ? 0 : (l.terms == 3 ? 3 : (a.dw_dtype == DTYPE_F32 ? 2 : 1));
+    g.dzt_terms = a.dw ? terms_for_dw(a.rows, a.dtype, a.dw_dtype) : 0;
     g.classes = l.piece;
     g.padded = l.padded;
     g.ld_dz = l.ld_piece;
@@ -676,7 +691,7 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
             c.k_active = 1;
             c.blocks = static_cast<int32_t>(l.padded / 64);
             c.terms = l.terms == 3 ? 6 : g.dzt_terms;
-            c.terms_a = l.terms == 3 ? kPairsA : (g.dzt_terms == 2 ? 1 : 0);    // the second term of dz, then the first
+            c.terms_a = l.terms == 3 ? kPairsA : (g.dzt_terms == 3 ? 6 : g.dzt_terms - 1);     // dz's smallest term first
             c.terms_b = l.terms == 3 ? kPairsB : 0;
             c.wave = l.dw.wave;
             c.splits = 1;
