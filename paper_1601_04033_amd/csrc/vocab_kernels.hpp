@@ -80,10 +80,14 @@ struct VocabProduct {
     int32_t wave;           // side of a wave's tile, 128 or 64
     float scale_log2e;
     // VOCAB_STATISTICS, a: the vocabulary from class `first` on, b: rows.  For the classes of each
-    // wave's tile (a slot): largest exponent and sum of powers; sum of logits.
+    // wave's tile (a slot): largest exponent and sum of powers; sum of logits; `by` times the logits
+    // at the rows' targets (of row list[i] for b's row i).
     float2* partial;        // [slots][padded]
     float* partial_sum;     // [slots][padded], or NULL
     int64_t first, padded;
+    const int32_t* list;
+    const int64_t* target;  // NULL: not wanted
+    float* picked;
     // VOCAB_GRADIENT, same operands
     const VocabRow* row;    // [padded]
     const uint32_t* largest;        // of the rows' coefficients, as bits (fp16 terms are scaled by it)

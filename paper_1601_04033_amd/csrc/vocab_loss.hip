@@ -172,7 +172,7 @@ template <> struct Term<float> {
     using type = bf16;
 };
 
-// The logits at the entries, 16 a wave: the diagonal of the product of their
+// The logits at a teacher's entries, 16 a wave: the diagonal of the product of their
 // classes' rows and their rows of x, by the instruction and in the order of
 // the tiles, so that they are bit for bit what the tiles put into the sums of
 // powers.  (A row's largest logit is often its target: an error that the sum
@@ -591,15 +591,23 @@ hipError_t launch_vocab_forward(const VocabArgs& a, hipStream_t s)
         q.wave = l.logits.wave;
         q.partial = p.at<float2>(l.partial);
         q.partial_sum = a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr;
+        if (!a.teacher) {
+            q.list = p.list;
+            q.target = a.index;
+            q.picked = a.picked;
+            q.by = a.scale;
+        }
         VOCAB_TRY(launch_vocab_product(VOCAB_STATISTICS, q, n, a.rows, s));
     }
-    const int64_t blocks = (a.rows * a.entries + 15) / 16;
-    const unsigned picks = static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20);
-    const uint16_t* x = p.at<uint16_t>(l.x);
-    if (a.dtype == DTYPE_F32) pick<float><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
-    else if (a.dtype == DTYPE_BF16) pick<bf16><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
-    else pick<f16><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
-    VOCAB_TRY(hipGetLastError());
+    if (a.teacher) {
+        const int64_t blocks = (a.rows * a.entries + 15) / 16;
+        const unsigned picks = static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20);
+        const uint16_t* x = p.at<uint16_t>(l.x);
+        if (a.dtype == DTYPE_F32) pick<float><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
+        else if (a.dtype == DTYPE_BF16) pick<bf16><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
+        else pick<f16><<<picks, 64, 0, s>>>(a, p.list, p.active, x, l.ld_cols, l.cols_padded);
+        VOCAB_TRY(hipGetLastError());
+    }
     finish<<<static_cast<unsigned>((a.rows + 7) / 8), kBlock, 0, s>>>(a, p.list, p.active, p.at<float2>(l.partial),
                                                                       a.smoothing != 0.0f ? p.at<float>(l.partial_sum) : nullptr,
                                                                       l.slots, l.padded);

@@ -109,6 +109,31 @@ __device__ __forceinline__ void statistics(const v4f (&acc)[N][N], const VocabPr
     }
 }
 
+// The logits at the targets that lie among a wave's classes.  Each row's lies in
+// one tile of all, so most of a wave's runs of rows have none.
+template <int W, int N>
+__device__ __forceinline__ void pick_targets(const v4f (&acc)[N][N], const VocabProduct& p, int64_t m, int64_t n, int left,
+                                             int active, int lane)
+{
+    const int first = 4 * N * (lane >> 4);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int64_t at = n + b_row(j, lane & 15);
+        const int row = at < active ? p.list[at] : -1;
+        const int64_t off = row < 0 ? -1 : p.target[row] - (p.first + m);
+        const bool here = off >= first && off < first + 4 * N && off < left;
+        if (__builtin_amdgcn_ballot_w64(here) == 0) continue;
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const v4f x = take(acc[i][j]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z = off == first + N * r + i ? x[r] : z;
+        }
+        if (here) p.picked[row] = z * p.by;
+    }
+}
+
 typedef float v2f __attribute__((ext_vector_type(2)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
@@ -490,7 +515,9 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
 
     const int64_t m = m0 + wave_m * W, n = n0 + wave_n * W;
     if constexpr (WHAT == VOCAB_STATISTICS) {
-        if (m < rows_a) statistics<W, N>(acc, p, m, n, static_cast<int>(rows_a - m < W ? rows_a - m : W), lane);
+        const int here = static_cast<int>(rows_a - m < W ? rows_a - m : W);
+        if (m < rows_a) statistics<W, N>(acc, p, m, n, here, lane);
+        if (m < rows_a && p.target) pick_targets<W, N>(acc, p, m, n, here, active, lane);
     } else if constexpr (WHAT == VOCAB_GRADIENT) {
         const int64_t left = rows_a - m;
         const int here = static_cast<int>(left < W ? (left < 0 ? 0 : left) : W);
