@@ -72,14 +72,17 @@ template <typename T> __device__ __forceinline__ v4i load_chunk(const T* row, in
 
 #endif
 
-// NK: steps of a wave at most.  GRADIENT: dz of the rows, else their statistics
+// NK: steps of a wave at most; 0: any number, with x read beside W, from L2, since
+// the registers do not hold it.  GRADIENT: dz of the rows, else their statistics
 // and the picked logits.
 template <typename T, int NK, bool GRADIENT>
 __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int kBatch = 8;       // groups between two meetings of the waves
-    constexpr int kLoads = NK < 8 ? NK : 8, kParts = NK / kLoads;       // of a group: loads in flight, times
+    constexpr bool kWide = NK == 0;
+    constexpr int kHold = kWide ? 1 : NK;
+    constexpr int kLoads = kWide || NK > 8 ? 8 : NK, kParts = kHold / kLoads;       // of a group: loads in flight, times
     constexpr int kSequence = kParts == 1 ? 2 : kParts;                 // loads with a buffer each of two
     __shared__ v4f part[kLogitWaves][kBatch][64];
     __shared__ float table[16][kBatch * 16 + 4];
@@ -103,10 +106,10 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
     // the steps whose 64 bytes all lie within the rows
     const int whole = cols / Chunk<T>::kStep - first;
 
-    v4i x[NK];
-    {
-        const int i = lane & 15;
-        const T* row = static_cast<const T*>(a.x) + (r0 + (i < rows ? i : 0)) * a.ldx;
+    v4i x[kHold];
+    const T* x_row = static_cast<const T*>(a.x) + (r0 + ((lane & 15) < rows ? lane & 15 : 0)) * a.ldx;
+    if constexpr (!kWide) {
+        const T* row = x_row;
 #pragma unroll
         for (int s = 0; s < NK; ++s) {
             if (s < whole && s < own) x[s] = __builtin_bit_cast(v4i, load_pack<T, Chunk<T>::kValues>(row + k0 + s * Chunk<T>::kStep));
@@ -147,7 +150,8 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
         }
     }
     __syncthreads();
-    if (used[lane & 15] == 0) {     // what a row that is left out holds reaches nothing
+    const bool live = used[lane & 15] != 0;
+    if (!kWide && !live) {      // what a row that is left out holds reaches nothing
 #pragma unroll
         for (int s = 0; s < NK; ++s) x[s] = v4i{0, 0, 0, 0};
     }
@@ -173,7 +177,17 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
     const int64_t groups = (a.vocab + 15) / 16, g0 = static_cast<int64_t>(blockIdx.x) * d.groups_each;
     const int64_t g1 = g0 + d.groups_each < groups ? g0 + d.groups_each : groups;
 
-    v4i w[2][kLoads];
+    v4i w[2][kLoads], beside[2][kWide ? kLoads : 1];
+    auto load_x = [&](int buffer, int at) {
+#pragma unroll
+        for (int s = 0; s < kLoads; ++s) {
+            const int step = at * kLoads + s;
+            v4i v = {0, 0, 0, 0};
+            if (step < whole && step < own) v = __builtin_bit_cast(v4i, load_pack<T, Chunk<T>::kValues>(x_row + k0 + step * Chunk<T>::kStep));
+            else if (step < own) v = load_chunk<T>(x_row, k0 + step * Chunk<T>::kStep, cols);
+            beside[buffer][s] = live ? v : v4i{0, 0, 0, 0};
+        }
+    };
     auto load = [&](int buffer, int64_t group, int at) {
         const int64_t c = group * 16 + (lane & 15);
         const T* row = static_cast<const T*>(a.w) + (c < a.vocab ? c : a.vocab - 1) * a.ldw;
@@ -188,10 +202,35 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
     const float c = a.scale * kLog2e;
     float top = -FLT_MAX, sum = 0.0f, all = 0.0f;      // of this lane's row and the classes it sees
     v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (g0 < g1) load(0, g0, 0);
+    if (!kWide && g0 < g1) load(0, g0, 0);
     for (int64_t b0 = g0; b0 < g1; b0 += kBatch) {
         const int batch = static_cast<int>(g1 - b0 < kBatch ? g1 - b0 : kBatch);
-        for (int g = 0; g < batch; g += kParts == 1 ? 2 : 1) {
+        if constexpr (kWide) {
+            const int parts = (each + kLoads - 1) / kLoads, times = batch * parts;
+            load(0, b0, 0);
+            load_x(0, 0);
+            int here = 0, at = 0;
+            for (int q = 0; q < times; q += 2) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (q + s >= times) break;
+                    const bool last = at + 1 == parts;
+                    if (q + s + 1 < times) {
+                        load(s ^ 1, b0 + here + (last ? 1 : 0), last ? 0 : at + 1);
+                        load_x(s ^ 1, last ? 0 : at + 1);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i) acc = tile(static_cast<const T*>(nullptr), w[s][i], beside[s][i], acc);
+                    if (last) {
+                        part[wave][here][lane] = acc;
+                        acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                    }
+                    here += last;
+                    at = last ? 0 : at + 1;
+                }
+            }
+        }
+        for (int g = 0; !kWide && g < batch; g += kParts == 1 ? 2 : 1) {
 #pragma unroll
             for (int s = 0; s < kSequence; ++s) {
                 const int here = kParts == 1 ? g + s : g, at = kParts == 1 ? 0 : s;
@@ -201,7 +240,7 @@ __global__ __launch_bounds__(kLogitThreads) void logits(VocabArgs a, Direct d)
                 if (next < g1) load((s + 1) & 1, next, last ? 0 : s + 1);
                 if (here < batch) {
 #pragma unroll
-                    for (int i = 0; i < kLoads; ++i) acc = tile(static_cast<const T*>(nullptr), w[s & 1][i], x[at * kLoads + i], acc);
+                    for (int i = 0; i < kLoads; ++i) acc = tile(static_cast<const T*>(nullptr), w[s & 1][i], x[kWide ? 0 : at * kLoads + i], acc);
                     if (last) {
                         part[wave][here][lane] = acc;
                         acc = v4f{0.0f, 0.0f, 0.0f, 0.0f};
@@ -313,9 +352,9 @@ struct Thin {
     int64_t ldc;
     const int32_t* used_r;  // rows of c that take part, zeros for the others (NULL: all)
     float by;
-    int32_t add, splits, row_tiles;     // row_tiles: that a wave goes through (k of at most 16)
+    int32_t add, splits, row_tiles;     // row_tiles: that a wave goes through (short_product)
     int32_t column_blocks, row_blocks;
-    int32_t brief;          // k of at most 16, by short_product
+    int32_t brief;          // k of at most 16 times this, by short_product; 0: by long_product
     int64_t blocks;         // in all; 0: not wanted
 };
 
@@ -358,17 +397,18 @@ template <typename OUT, int N> __device__ __forceinline__ void store_values(cons
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
-// k of at most 16: b's values stay in registers, the row tiles go by.  Bound by
+// k of at most 16 KB: b's values stay in registers, the row tiles go by.  Bound by
 // the stores of c, so a lane's columns are 4 neighbours in each half of the
 // wave's 128: 16 lanes store 256 bytes.
-template <typename T, typename OUT> __device__ __forceinline__ void thin_short(const Thin& p, int column_block, int64_t row_block)
+template <typename T, typename OUT, int KB> __device__ __forceinline__ void thin_short(const Thin& p, int column_block, int64_t row_block)
 {
     const int lane = threadIdx.x & 63;
     const int64_t n0 = (static_cast<int64_t>(column_block) * 4 + (threadIdx.x >> 6)) * 128, n = n0 + 4 * (lane & 15);
     if (n0 >= p.cols) return;
-    float held[4][8];
+    constexpr int kSteps = 4 * KB;
+    float held[kSteps][8];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < kSteps; ++s) {
         const int64_t k = 4 * s + (lane >> 4);
         const bool in = k < p.k && (!p.used_k || p.used_k[k]);
         Pack<T, 4> v[2];
@@ -381,25 +421,25 @@ template <typename T, typename OUT> __device__ __forceinline__ void thin_short(c
     }
     const int64_t t0 = row_block * p.row_tiles;
     const float* at = p.a + (lane >> 4) * p.lda + (lane & 15);
-    auto take_a = [&](int64_t r0, float (&x)[4]) {
+    auto take_a = [&](int64_t r0, float (&x)[kSteps]) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int s = 0; s < kSteps; ++s)
             x[s] = 4 * s + (lane >> 4) < p.k && r0 + (lane & 15) < p.rows ? at[4 * s * p.lda + r0] : 0.0f;
     };
-    float x[4];
+    float x[kSteps];
     take_a(t0 * 16, x);
     const bool plain = n0 + 128 <= p.cols && !p.used_r && !p.add;     // nothing to look at per store
     OUT* out = static_cast<OUT*>(p.c) + (t0 * 16 + 4 * (lane >> 4)) * p.ldc + n;
     for (int t = 0; t < p.row_tiles; ++t, out += 16 * p.ldc) {
         const int64_t r0 = (t0 + t) * 16;
         if (r0 >= p.rows) return;
-        float next[4];
+        float next[kSteps];
         take_a(r0 + 16, next);
         v4f acc[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int s = 0; s < kSteps; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[s], held[s][e], acc[e], 0, 0, 0);
         if (plain && r0 + 16 <= p.rows) {
@@ -425,7 +465,7 @@ template <typename T, typename OUT> __device__ __forceinline__ void thin_short(c
                 }
         }
 #pragma unroll
-        for (int s = 0; s < 4; ++s) x[s] = next[s];
+        for (int s = 0; s < kSteps; ++s) x[s] = next[s];
     }
 }
 
@@ -490,15 +530,18 @@ __device__ __forceinline__ void thin_long(const Thin& p, v4f (&part)[4][8][64], 
         }
     }
     for (; kb < k1; kb += 4 * kStep) {      // what is cut by the end of k or of the columns
+        Loads l;
+#pragma unroll
         for (int s = 0; s < kFlight; ++s) {
             const int64_t k = kb + 4 * s + (lane >> 4);
-            const bool in = k < k1 && (!MASK || p.used_k[k]);
-            const float x = in ? a[k * p.lda] : 0.0f;
-            Pack<T, 8> v;
-            if (in) v = load_values<T, 8>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, in ? to_float(v.v[e]) : 0.0f, acc[e], 0, 0, 0);
+            l.in[s] = k < k1 && (!MASK || p.used_k[k]);
+            l.x[s] = 0.0f;
+            if (l.in[s]) {
+                l.x[s] = a[k * p.lda];
+                l.v[s] = load_values<T, 8>(static_cast<const T*>(p.b) + k * p.ldb, n, p.cols);
+            }
         }
+        multiply(l);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) part[wave][e][lane] = acc[e];
@@ -539,11 +582,11 @@ __device__ __forceinline__ int64_t in_runs(int64_t all)
 #endif
 
 // dW of a few rows; dx of a few classes.
-template <typename T, typename OUT> __global__ __launch_bounds__(256, 3) void short_product(Thin p)
+template <typename T, typename OUT, int KB> __global__ __launch_bounds__(256, KB < 4 ? 3 : 2) void short_product(Thin p)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     const int64_t id = in_runs(p.blocks);
-    thin_short<T, OUT>(p, static_cast<int>(id % p.column_blocks), id / p.column_blocks);
+    thin_short<T, OUT, KB>(p, static_cast<int>(id % p.column_blocks), id / p.column_blocks);
 #endif
 }
 
@@ -566,8 +609,9 @@ template <typename T, typename OUT> __global__ __launch_bounds__(256, 2) void lo
 #endif
 }
 
-// dx from the splits' parts, in order: 4 columns a thread.
-template <typename T> __global__ __launch_bounds__(256) void join(Thin p, T* out, int64_t ld, const int32_t* used)
+// An output from the splits' parts, in order: 4 columns a thread.  used: rows
+// that take part (NULL: all).
+template <typename T> __global__ __launch_bounds__(256) void join(Thin p, T* out, int64_t ld, const int32_t* used, int add)
 {
     const int64_t r = blockIdx.y, n = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
     if (n >= p.cols) return;
@@ -580,10 +624,11 @@ template <typename T> __global__ __launch_bounds__(256) void join(Thin p, T* out
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[e] += x.v[e];
     }
-    const bool in = used[r] != 0;
+    const bool in = !used || used[r] != 0;
+    out += r * ld + n;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (n + e < p.cols) out[r * ld + n + e] = from_float<T>(in ? s[e] * p.by : 0.0f);
+        if (n + e < p.cols) out[e] = from_float<T>((in ? s[e] * p.by : 0.0f) + (add ? to_float(out[e]) : 0.0f));
 }
 
 int64_t count(int64_t x, int64_t side) { return (x + side - 1) / side; }
@@ -592,9 +637,9 @@ int64_t count(int64_t x, int64_t side) { return (x + side - 1) / side; }
 
 struct Layout {
     int64_t padded, cols_padded, groups_each, blocks;
-    int splits;
-    int64_t k_each;
-    int64_t used, dz, dzt, sums, partial, partial_sum, bytes;
+    int splits, dw_splits;
+    int64_t k_each, dw_each;
+    int64_t used, dz, dzt, sums, dw_sums, partial, partial_sum, bytes;
 };
 
 Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, bool backward)
@@ -604,7 +649,7 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, bool backward)
     l.cols_padded = count(cols, 128) * 128;
     // a block a CU
     const int64_t groups = count(vocab, 16), row_tiles = l.padded / 16;
-    l.groups_each = count(groups * row_tiles, 256);
+    l.groups_each = count(groups, row_tiles < 256 ? 256 / row_tiles : 1);
     l.blocks = count(groups, l.groups_each);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -624,6 +669,13 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, bool backward)
         l.dz = take(4 * rows * vocab);
         l.dzt = take(4 * l.padded * vocab);
         l.sums = take(l.splits > 1 ? 4 * l.splits * l.padded * l.cols_padded : 0);
+        // dW alike, of few classes: the rows split (6,575 x 350 x 25 fp32: 460 us in one part, 78 so, with the forward pass)
+        s = 512 / (groups * l.cols_padded / 128);
+        if (s > count(rows, 256)) s = count(rows, 256);
+        if (s < 1) s = 1;
+        l.dw_each = count(count(rows, s), 4) * 4;
+        l.dw_splits = static_cast<int>(count(rows, l.dw_each));
+        l.dw_sums = take(l.dw_splits > 1 ? 4 * l.dw_splits * groups * 16 * l.cols_padded : 0);
     } else {
         l.partial = take(8 * l.blocks * l.padded);
         l.partial_sum = take(4 * l.blocks * l.padded);
@@ -639,7 +691,8 @@ template <typename T, bool GRADIENT> hipError_t launch_logits(const VocabArgs& a
     if (each <= 2) logits<T, 2, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
     else if (each <= 8) logits<T, 8, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
     else if (each <= 16) logits<T, 16, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
-    else logits<T, 32, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
+    else if (each <= 32) logits<T, 32, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
+    else logits<T, 0, GRADIENT><<<grid, kLogitThreads, 0, s>>>(a, d);
     return hipGetLastError();
 }
 
@@ -652,7 +705,7 @@ template <bool GRADIENT> hipError_t launch_logits_of(const VocabArgs& a, const D
 
 void set_blocks(Thin& p, bool brief)
 {
-    p.brief = brief;
+    p.brief = !brief ? 0 : (p.k <= 16 ? 1 : (p.k <= 32 ? 2 : 4));
     p.column_blocks = static_cast<int32_t>(count(p.cols, brief ? 512 : 128));
     p.row_blocks = static_cast<int32_t>(count(count(p.rows, 16), p.row_tiles));
     p.blocks = static_cast<int64_t>(p.column_blocks) * p.row_blocks * p.splits;
@@ -665,10 +718,12 @@ template <typename T, typename OUT> hipError_t launch_products(const Thin& dx, c
         long_products<T, OUT><<<n + m, 256, 0, s>>>(dx, dw);
         return hipGetLastError();
     }
-    if (n && dx.brief) short_product<T, T><<<n, 256, 0, s>>>(dx);
+    if (n && dx.brief) short_product<T, T, 1><<<n, 256, 0, s>>>(dx);
     else if (n) long_product<T, T, false><<<n, 256, 0, s>>>(dx);
     VOCAB_TRY(hipGetLastError());
-    if (m && dw.brief) short_product<T, OUT><<<m, 256, 0, s>>>(dw);
+    if (m && dw.brief == 1) short_product<T, OUT, 1><<<m, 256, 0, s>>>(dw);
+    else if (m && dw.brief == 2) short_product<T, OUT, 2><<<m, 256, 0, s>>>(dw);
+    else if (m && dw.brief) short_product<T, OUT, 4><<<m, 256, 0, s>>>(dw);
     else if (m) long_product<T, OUT, true><<<m, 256, 0, s>>>(dw);
     return hipGetLastError();
 }
@@ -702,24 +757,31 @@ template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, u
         dw.rows = a.vocab;
         dw.cols = a.cols;
         dw.k = a.rows;
-        dw.k_each = l.padded;
-        dw.splits = 1;
+        dw.k_each = l.dw_each;
+        dw.splits = l.dw_splits;
         dw.used_k = used;
         dw.by = a.scale;
-        dw.add = a.accumulate;
-        dw.c = a.dw;
-        dw.ldc = a.lddw;
-        // k of at most 16: so many row tiles a wave that about 8,192 waves are left
+        dw.add = l.dw_splits > 1 ? 0 : a.accumulate;
+        dw.c = l.dw_splits > 1 ? base + l.dw_sums : static_cast<uint8_t*>(a.dw);
+        dw.ldc = l.dw_splits > 1 ? l.cols_padded : a.lddw;
+        // by short_product: so many row tiles a wave that about 8,192 waves are left
         const int64_t waves = count(a.vocab, 16) * count(a.cols, 128);
-        const int64_t each = a.rows <= 16 ? waves / 8192 : 1;
+        const bool brief = a.rows <= 16 || (a.rows <= 64 && waves >= 2048);
+        const int64_t each = brief ? waves / 8192 : 1;
         dw.row_tiles = static_cast<int32_t>(each < 1 ? 1 : each);
-        set_blocks(dw, a.rows <= 16);
+        set_blocks(dw, brief);
     }
     if (a.dw_dtype == DTYPE_F32) VOCAB_TRY((launch_products<T, float>(dx, dw, s)));
     else VOCAB_TRY((launch_products<T, T>(dx, dw, s)));
     if (a.dx && l.splits > 1) {
         const dim3 grid(static_cast<unsigned>(count(a.cols, 1024)), static_cast<unsigned>(a.rows));
-        join<T><<<grid, 256, 0, s>>>(dx, static_cast<T*>(a.dx), a.lddx, used);
+        join<T><<<grid, 256, 0, s>>>(dx, static_cast<T*>(a.dx), a.lddx, used, 0);
+        VOCAB_TRY(hipGetLastError());
+    }
+    if (a.dw && l.dw_splits > 1) {
+        const dim3 grid(static_cast<unsigned>(count(a.cols, 1024)), static_cast<unsigned>(a.vocab));
+        if (a.dw_dtype == DTYPE_F32) join<float><<<grid, 256, 0, s>>>(dw, static_cast<float*>(a.dw), a.lddw, nullptr, a.accumulate);
+        else join<T><<<grid, 256, 0, s>>>(dw, static_cast<T*>(a.dw), a.lddw, nullptr, a.accumulate);
         VOCAB_TRY(hipGetLastError());
     }
     return hipSuccess;
@@ -727,11 +789,23 @@ template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, u
 
 }  // namespace
 
-// 16 rows, or small sums, with a row of W in the registers of 8 waves.
+// A few rows, or less time by what this way and the other took of m x d x V,
+// forward and backward (the other lays operands out, which costs the weights
+// several times over, and goes through six products of fp32, in long sums where
+// there are few tiles).  This way and the other, us, bf16: 17 x 4,096 x 32,768 389 and
+// 655; 32 x 8,192 x 65,536 1,458 and 2,436; 40 x 2,000 x 30,000 403 and 326; 64 x 4,096 x
+// 4,096 146 and 168; 1,024 x 1,024 x 1,024 103 and 107; 128 x 8,192 x 4,096 369 and 279;
+// 512 x 1,024 x 4,096 183 and 108; 3,063 x 3,371 x 139 348 and 242.  fp32: 17 x 4,096 x
+// 32,768 627 and 2,603; 64 x 512 x 65,536 361 and 694; 128 x 8,192 x 4,096 714 and 1,331;
+// 1,024 x 1,024 x 1,024 146 and 233; 1,024 x 2,048 x 2,048 505 and 364.
 bool vocab_direct(int64_t rows, int64_t cols, int64_t vocab, int dtype)
 {
-    if (cols * static_cast<int64_t>(dtype_size(dtype)) > 16384) return false;
-    return (rows <= 16 && rows * vocab <= (int64_t(1) << 26)) || (rows <= 1024 && rows * vocab <= (int64_t(1) << 24) && rows * vocab * cols <= (int64_t(1) << 28));
+    const bool single = dtype == DTYPE_F32;
+    if (rows <= (single ? 64 : 32) && rows * vocab <= (int64_t(1) << 26)) return true;
+    if (rows > (1 << 19) || rows * vocab > (int64_t(1) << (single ? 24 : 21))) return false;
+    const double w = static_cast<double>(vocab) * static_cast<double>(cols), all = w * static_cast<double>(count(rows, 16) * 16);
+    return single ? 100e-9 * all <= 100.0 + 0.12 * static_cast<double>(cols) + 6.5e-6 * w
+                  : 75e-9 * all <= 60.0 + 0.02 * static_cast<double>(cols);
 }
 
 size_t vocab_direct_bytes(int64_t rows, int64_t cols, int64_t vocab, bool backward)

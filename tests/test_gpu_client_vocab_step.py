@@ -163,6 +163,30 @@ def test_many_entries(dtype, m, d, V, K):
     check(Case(dtype, m, d, V, K=K, seed=1), whole=True)
 
 
+# rows too wide for a block's registers; a few rows more than 16 against many classes; many rows of few classes
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, d, V", [(17, 5000, 300), (5, 8232, 70), (20, 16500, 33), (1, 20011, 5), (20, 1000, 5000),
+                                     (40, 1001, 5003), (64, 960, 6007), (6575, 35, 25), (3001, 130, 40), (70001, 24, 9)])
+def test_shapes(dtype, m, d, V):
+    check(Case(dtype, m, d, V, out=0.2 if m > 5 else 0.0, gaps=d % 2))
+    check(Case(dtype, m, d, V, K=3, out=0.2 if m > 5 else 0.0), dw=DTYPES[dtype])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, d, V", [(3001, 130, 40), (40, 1001, 5003)])
+def test_accumulation(dtype, m, d, V):
+    """dw is added to what is there: a sum and its rounding to fp32 apart from the gradient alone."""
+    c = Case(dtype, m, d, V)
+    _, lse, picked = forward(c)
+    _, alone = backward(c, lse, picked)
+    dw = torch.randn(V, d, device="cuda")
+    before = dw.clone()
+    ws = torch.empty(fa.client_vocab_workspace_bytes(m, d, V, c.dt), device="cuda", dtype=torch.uint8)
+    fa.client_vocab_loss_backward(c.x, c.w, c.index, lse, picked, None, dw, dloss=c.dloss, accumulate=True, workspace=ws)
+    # a multiplication added in one rounding, or rounded first
+    assert ((dw.double() - (before.double() + alone.double())).abs() <= U * (dw.double().abs() + 2 * alone.double().abs())).all()
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("m", [3, 1100])
 @pytest.mark.parametrize("K", [0, 5])
