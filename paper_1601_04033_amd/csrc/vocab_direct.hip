@@ -7,6 +7,11 @@
 // takes operands from global memory straight into registers (16 x 16 tiles:
 // 16-bit types as they are, fp32 by the fp32 instruction), and the gradient of
 // the logits is held in fp32.
+//
+// Measured (bf16, 4,096 columns, 131,072 classes): logits of 1 row 190 us, 5.6 TB/s
+// of W; of 16 rows 223 to 238, 4.6; dx of 16 rows 236, 4.5; dW 399, 5.4 TB/s of
+// stores.  More rows than 16 read W again for each 16, from L2 or the last-level
+// cache: 1,024 x 1,024 x 1,024 fp32 45 us forward, 48 TFLOP/s.
 #include <float.h>
 
 #include "fp8_math.hpp"

@@ -18,7 +18,6 @@
 namespace fasgd {
 namespace {
 
-
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 // Pairs of three terms each, those above 2^-24, the smallest first.
@@ -178,6 +177,8 @@ template <> struct Term<float> {
 // powers.  (A row's largest logit is often its target: an error that the sum
 // has and p's numerator has not, or another, is p (1 - p) of itself in dz, not p.
 // 8,192 x 4,096 x 131,072 bf16, dW off by 3.9e-6 with a sum in another order.)
+// Bound by W's rows and the chain of loads, 16 steps on their way (4,096 rows of 64
+// entries, 4,096 columns bf16: 365 us, 5.9 TB/s; 1,531 rows of 50: 45 us).
 template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, const int32_t* list, const int32_t* active,
                                                                 const uint16_t* x, int64_t ld_x, int64_t cols_padded)
 {
@@ -296,7 +297,8 @@ struct Gradient {
     int64_t cols_padded;
 };
 
-// The entries of a piece's classes: into dz^T, and out of dz.  A wave a row.
+// The entries of a piece's classes: into dz^T, and out of dz.  A wave a row.  Bound
+// by stores of 2 bytes, a line each (4,096 rows of 64 entries: 43 us a piece).
 template <typename T> __global__ __launch_bounds__(kBlock) void place_entries(VocabArgs a, Gradient g)
 {
     const int lane = threadIdx.x & 63;
@@ -320,7 +322,9 @@ template <typename T> __global__ __launch_bounds__(kBlock) void place_entries(Vo
     }
 }
 
-// dx of a row: the products' sums and the entries', times the logits' scale.
+// dx of a row: the products' sums and the entries', times the logits' scale.  A
+// block a row; bound by the entries' rows of W (4,096 rows of 64, 4,096 columns
+// bf16: 2.1 GB in 430 us, 5 TB/s; 8,192 rows of one target 60 us).
 template <typename T, typename TERM> __global__ __launch_bounds__(kBlock) void finish_dx(VocabArgs a, Gradient g)
 {
     __shared__ float value[kMostEntries];
