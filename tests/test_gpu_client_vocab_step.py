@@ -240,3 +240,8 @@ def test_offsets_beyond_32_bits(m):
         # dz in two bf16 terms, off by 2^-12 of itself for its logit
         assert ((dw[at:at + step] - dz.t() @ X).abs() <= 2.0 ** -10 * (dz.abs().t() @ X.abs()) + 1e-30).all(), at
     assert ((dx - total).abs() <= 2.0 ** -7.5 * total.abs() + 2.0 ** -8 * most).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_as_many_rows_as_there_may_be(dtype):
+    check(Case(dtype, 2 ** 20, 8, 4, out=0.1))
