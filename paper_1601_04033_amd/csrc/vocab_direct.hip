@@ -3,7 +3,8 @@
 //
 // A few rows against a large vocabulary are bound by reading W (twice forward
 // and backward, and once more for dx) and writing dW; a small problem by its
-// chain of launches.  So there are two a pass or three, the matrix instruction
+// chain of launches.  So there are one or two forward and two to five backward,
+// the matrix instruction
 // takes operands from global memory straight into registers (16 x 16 tiles:
 // 16-bit types as they are, fp32 by the fp32 instruction), and the gradient of
 // the logits is held in fp32.
