@@ -146,7 +146,8 @@ __device__ __forceinline__ void finish_row(const VocabArgs& a, int64_t r, float 
     }
     float loss = 0.0f;
     if (!a.teacher) {
-        if (lane == 0) loss = lse - (1.0f - a.smoothing) * a.picked[r] - a.smoothing * mean + a.z_loss * lse * lse;
+        // without smoothing the mean plays no part: that of logits beside masked classes is -infinity, and 0 times it NaN
+        if (lane == 0) loss = lse - (1.0f - a.smoothing) * a.picked[r] - (a.smoothing != 0.0f ? a.smoothing * mean : 0.0f) + a.z_loss * lse * lse;
     } else {
         const Teacher t = teacher_of(a, r, lane);
         const float log_by = logf(t.by);

@@ -1,0 +1,53 @@
+"""The losses over a vocabulary where some logits are not finite: classes
+masked by the lowest value of a type or by -infinity (through a column of W that
+a constant activation meets)."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_client_vocab import DTYPES, Case, forward
+from vocab_reference import Reference
+from vocab_ways import way
+
+pytestmark = pytest.mark.gpu
+
+# one block sees all classes (few of them; many rows); many blocks; tiles, whose last rows fill none
+FORMS = [(5, 24, 12, "direct"), (3001, 130, 40, "direct"), (17, 64, 1000, "direct"), (2100, 72, 8200, "tiles")]
+CASES = [(*form, dtype, value) for form in FORMS for dtype in DTYPES for value in ("lowest", "-inf")
+         if not (form[3] == "tiles" and dtype == "fp32" and value == "-inf")]
+
+
+class Masked:
+    """A case over the classes that are not masked, and the same among masked ones.  The masked ones weigh nothing, so
+    every result is the first one's; dw of the masked classes is 0."""
+
+    def __init__(self, dtype, m, d, V, K, value, seed=5):
+        g = torch.Generator().manual_seed(seed)
+        left = torch.zeros(V, dtype=torch.bool)
+        left[torch.randperm(V, generator=g)[: V - max(2, V // 3)]] = True
+        self.left = left.cuda()
+        at = self.left.nonzero()[:, 0]
+        self.small = Case(dtype, m, d, len(at), K, seed=seed)
+        dt = self.small.dt
+        self.small.x[:, -1], self.small.w[:, -1] = 1.0, 0.0
+        self.full = Case(dtype, m, d, len(at), K, seed=seed)
+        self.full.x = self.small.x
+        self.full.w = torch.randn(V, d, generator=g).to(dt).cuda() * d ** -0.5
+        self.full.w[at] = self.small.w
+        self.full.w[~self.left, -1] = torch.finfo(dt).min if value == "lowest" else -math.inf
+        self.full.index = at[self.small.index]
+
+    def reference(self, **kw):
+        c = self.small
+        return Reference(c.x, c.w, c.index, teacher=c.teacher, dloss=c.dloss, **kw)
+
+
+@pytest.mark.parametrize("K", [0, 3])
+@pytest.mark.parametrize("m, d, V, form, dtype, value", CASES)
+def test_losses_beside_masked_classes(m, d, V, form, dtype, K, value):
+    assert way(m, d, V, DTYPES[dtype]) == form
+    c = Masked(dtype, m, d, V, K, value)
+    ref = c.reference()
+    for name, got in zip(("loss", "lse", "picked"), forward(c.full)):
+        ref.check(name, got)
