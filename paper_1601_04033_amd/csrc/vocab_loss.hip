@@ -79,7 +79,10 @@ __global__ __launch_bounds__(1024) void gather_rows(VocabArgs a, const int32_t* 
 
 // A matrix as the products read it: by_rows, rows of [terms][cols_padded], and /
 // or by_cols, columns of [terms][rows_padded], zeros in the padding.  list: its
-// rows are these of src (as many as `active` says).
+// rows are these of src (as many as `active` says), and what fills up the last
+// tile are copies of the last of them.  With coefficients of 0 those weigh nothing
+// in dW, and their logits are NaN only where that row's are; an infinite weight
+// makes a row of zeros NaN, and with it dW of the class that it masks.
 struct LayOut {
     const void* src;
     int64_t ld, rows, cols;
@@ -115,8 +118,8 @@ template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_o
     for (int i = 0; i < 8; ++i) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[i].v[e] = from_float<T>(0.0f);
-        if (r + i < rows) {
-            const T* src = static_cast<const T*>(a.src) + (a.list ? a.list[r + i] : r + i) * a.ld + c;
+        if (rows > 0 && (a.list || r + i < rows)) {
+            const T* src = static_cast<const T*>(a.src) + (a.list ? a.list[r + i < rows ? r + i : rows - 1] : r + i) * a.ld + c;
             if (c + 8 <= a.cols) {
                 x[i] = load_pack<T, 8>(src);
             } else {
@@ -253,8 +256,9 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
 
 // ---- backward
 
-// Coefficients of the rows that take part (a wave each, 16 a block), zeros for
-// the rows that fill up the last tile; the largest coefficient, where asked for.
+// Coefficients of the rows that take part (a wave each, 16 a block), zeros beside
+// the last one's log-sum-exp for the rows that fill up the last tile (copies of
+// it); the largest coefficient, where asked for.
 __global__ __launch_bounds__(1024) void coefficients(VocabArgs a, const int32_t* list, const int32_t* active, VocabRow* row,
                                                      float2* teacher, uint32_t* largest)
 {
@@ -268,6 +272,8 @@ __global__ __launch_bounds__(1024) void coefficients(VocabArgs a, const int32_t*
         const int64_t r = list[at];
         t = teacher_of(a, r, lane);
         c = coefficients_of(a, r, t, lane);
+    } else {
+        c.l = a.lse[list[n - 1]] * kLog2e;
     }
     if (lane == 0) {
         row[at] = c;

@@ -391,8 +391,8 @@ __global__ __launch_bounds__(kThreads, W >= 96 ? 1 : 2) void vocab_product(Vocab
     const int own_blocks = blocks - kb0 < per_split ? blocks - kb0 : per_split;
     const int terms = same(p.terms), along = same(own_blocks * kBytes), steps = own_blocks > 0 ? own_blocks * terms : 0;
 
-    // Rows past a's last are read as its last; b's padding to 128 rows of zeros
-    // is there, and what lies behind it is read as its last.  Load q of a wave
+    // Rows past a's last are read as its last; b's are padded to 128,
+    // and what lies behind that is read as the last of it.  Load q of a wave
     // fills 8 rows of a slot, 128 bytes each, the 16-byte chunk c of row r of a
     // tile in place slot(c, r).
     uint32_t off_a[kLoads], off_b[kLoads];

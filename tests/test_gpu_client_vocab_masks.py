@@ -6,7 +6,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_client_vocab import DTYPES, Case, forward
+from test_gpu_client_vocab import DTYPES, Case, backward, forward
 from vocab_reference import Reference
 from vocab_ways import way
 
@@ -51,3 +51,18 @@ def test_losses_beside_masked_classes(m, d, V, form, dtype, K, value):
     ref = c.reference()
     for name, got in zip(("loss", "lse", "picked"), forward(c.full)):
         ref.check(name, got)
+
+
+@pytest.mark.parametrize("K", [0, 3])
+@pytest.mark.parametrize("m, d, V, form, dtype, value", CASES)
+def test_gradients_beside_masked_classes(m, d, V, form, dtype, K, value):
+    assert way(m, d, V, DTYPES[dtype]) == form
+    c = Masked(dtype, m, d, V, K, value)
+    ref = c.reference()
+    _, lse, picked = forward(c.full)
+    dx, dw = backward(c.full, lse, picked)
+    if value == "-inf":     # 0 times -infinity in the column of the masks
+        dx, ref.dx, ref.tol_dx = dx[:, :-1], ref.dx[:, :-1], ref.tol_dx[:, :-1]
+    ref.check("dx", dx)
+    ref.check("dw", dw[c.left])
+    assert (dw[~c.left] == 0).all()
