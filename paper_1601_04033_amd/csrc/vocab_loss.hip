@@ -92,15 +92,22 @@ struct LayOut {
 };
 
 // fp32 in three bf16 terms: the first two cut off, so that none exceeds the
-// value, the last rounded.
+// value, the last rounded.  An infinite value is its first term alone.  That is
+// multiplied by all terms of the other value, of which none may be 0 then: those
+// that are become 2^-126 with the value's sign, which adds less than 2^-26 of a
+// finite product, as values below 2^-100 are left as they are.
 __device__ __forceinline__ void terms_of(float x, uint16_t (&t)[3])
 {
-    const uint32_t hi = __float_as_uint(x) & 0xffff0000u;
-    const float r = x - __uint_as_float(hi);
+    constexpr uint32_t kInfinity = 0x7f800000u, kSmall = 0x0d800000u;      // 2^-100
+    const uint32_t bits = __float_as_uint(x), size = bits & 0x7fffffffu;
+    const uint32_t hi = size > kInfinity ? bits | 0x00400000u : bits & 0xffff0000u;    // NaN stays NaN
+    const float r = size < kInfinity ? x - __uint_as_float(hi) : 0.0f;
     const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
+    const uint32_t least = size < kSmall ? 0u : (bits >> 16 & 0x8000u) | 0x0080u;
+    const uint16_t last = from_float<bf16>(r - __uint_as_float(mid)).bits;
     t[0] = static_cast<uint16_t>(hi >> 16);
-    t[1] = static_cast<uint16_t>(mid >> 16);
-    t[2] = from_float<bf16>(r - __uint_as_float(mid)).bits;
+    t[1] = static_cast<uint16_t>(mid << 1 == 0 ? least : mid >> 16);
+    t[2] = static_cast<uint16_t>((last & 0x7fffu) == 0 ? least : last);
 }
 
 // 64 x 64 elements a wave, 8 x 8 a lane, turned in registers: each load and each

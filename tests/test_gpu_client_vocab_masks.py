@@ -14,8 +14,7 @@ pytestmark = pytest.mark.gpu
 
 # one block sees all classes (few of them; many rows); many blocks; tiles, whose last rows fill none
 FORMS = [(5, 24, 12, "direct"), (3001, 130, 40, "direct"), (17, 64, 1000, "direct"), (2100, 72, 8200, "tiles")]
-CASES = [(*form, dtype, value) for form in FORMS for dtype in DTYPES for value in ("lowest", "-inf")
-         if not (form[3] == "tiles" and dtype == "fp32" and value == "-inf")]
+CASES = [(*form, dtype, value) for form in FORMS for dtype in DTYPES for value in ("lowest", "-inf")]
 
 
 class Masked:
@@ -66,3 +65,23 @@ def test_gradients_beside_masked_classes(m, d, V, form, dtype, K, value):
     ref.check("dx", dx)
     ref.check("dw", dw[c.left])
     assert (dw[~c.left] == 0).all()
+
+
+@pytest.mark.parametrize("m, d, V, form", FORMS)
+def test_infinite_weights_beside_any_activation(m, d, V, form):
+    """fp32: an infinite weight and an activation of few or many bits, of either sign, have an infinite product.  A class
+    of logits of infinity makes its row's log-sum-exp no number or infinity, one of -infinity is as if it were not there."""
+    c = Masked("fp32", m, d, V, 0, "-inf")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = c.full.x[:, -1]
+    x.copy_(torch.rand(m, device="cuda", generator=g) + 0.5)
+    x[::3] = 2.0 ** -40
+    x[1::3] *= -1.0
+    ref = c.reference()     # w is 0 there for the classes that are not masked
+    loss, lse, picked = forward(c.full)
+    for name, got in (("loss", loss), ("lse", lse), ("picked", picked)):
+        got = got.clone()
+        if name != "picked":
+            assert not torch.isfinite(got[1::3]).any()
+            got[1::3] = getattr(ref, name)[1::3].float()
+        ref.check(name, got)
