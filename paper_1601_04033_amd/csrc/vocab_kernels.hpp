@@ -113,13 +113,14 @@ VocabPlan vocab_plan(int64_t m, int64_t n, int64_t stages, int most_splits);
 hipError_t launch_vocab_product(int what, const VocabProduct& p, int64_t m, int64_t n, hipStream_t s);
 
 // What a gradient's terms are multiplied by: 1 in bf16; in fp16, whose range
-// is short, the power of two that takes the largest coefficient to 2^14.
+// is short, the power of two that takes the largest coefficient to 2^14 (infinity
+// is a sum beyond fp32's range, below 2^130).
 template <typename T> __device__ __forceinline__ float term_scale(uint32_t largest);
 template <> __device__ __forceinline__ float term_scale<bf16>(uint32_t) { return 1.0f; }
 template <> __device__ __forceinline__ float term_scale<f16>(uint32_t largest)
 {
     const int e = static_cast<int>(largest >> 23);
-    if (e == 0 || e == 255) return 1.0f;
+    if (e == 0) return 1.0f;
     const int up = 127 + 14 - (e - 127);
     return __uint_as_float(static_cast<uint32_t>(up < 1 ? 1 : (up > 254 ? 254 : up)) << 23);
 }

@@ -285,13 +285,16 @@ __global__ __launch_bounds__(1024) void coefficients(VocabArgs a, const int32_t*
     if (lane == 0) {
         row[at] = c;
         teacher[at] = make_float2(t.top, t.by);
-        most[wave] = fabsf(a.teacher ? c.f : c.g) + fabsf(c.f) + fabsf(c.b);
+        // A row that is not finite has no say in the others' scale.  (A sum of finite
+        // parts may be infinity: term_scale takes it for a value below 2^130.)
+        const float entry = fabsf(a.teacher ? c.f : c.g), f = fabsf(c.f), b = fabsf(c.b);
+        most[wave] = entry <= FLT_MAX && f <= FLT_MAX && b <= FLT_MAX ? entry + f + b : 0.0f;
     }
     if (!largest) return;
     __syncthreads();
     if (threadIdx.x == 0) {
         float x = most[0];
-        for (int i = 1; i < 16; ++i) x = most[i] > x || most[i] != most[i] ? most[i] : x;
+        for (int i = 1; i < 16; ++i) x = fmaxf(x, most[i]);
         atomicMax(largest, __float_as_uint(x));     // of values that are not negative: the same in any order
     }
 }

@@ -1,6 +1,6 @@
-"""The losses over a vocabulary where some logits are not finite: classes
+"""The losses over a vocabulary where some logits or rows are not finite: classes
 masked by the lowest value of a type or by -infinity (through a column of W that
-a constant activation meets)."""
+a constant activation meets), and a row that has gone astray among others."""
 import math
 
 import pytest
@@ -85,3 +85,44 @@ def test_infinite_weights_beside_any_activation(m, d, V, form):
             assert not torch.isfinite(got[1::3]).any()
             got[1::3] = getattr(ref, name)[1::3].float()
         ref.check(name, got)
+
+
+@pytest.mark.parametrize("K", [0, 5])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bad", ["x is NaN", "x is infinite", "dloss is NaN", "dloss is -NaN", "dloss is infinite"])
+@pytest.mark.parametrize("m, d, V, form", [(200, 72, 333, "direct"), (2100, 72, 8200, "tiles")])
+def test_a_row_that_is_not_finite_is_its_own_affair(m, d, V, form, bad, dtype, K):
+    """The other rows' results are as if it had been left out; dw takes every row."""
+    assert way(m, d, V, DTYPES[dtype]) == form
+    c = Case(dtype, m, d, V, K)
+    at = 77
+    without = c.index.clone()
+    without[at] = -100
+    ref = Reference(c.x, c.w, without, teacher=c.teacher, dloss=c.dloss)
+    if bad.startswith("x"):
+        c.x[at, 3] = math.nan if bad.endswith("NaN") else math.inf
+    elif bad.endswith("-NaN"):
+        c.dloss.view(torch.int32)[at] = -1
+    else:
+        c.dloss[at] = math.nan if bad.endswith("NaN") else math.inf
+    loss, lse, picked = forward(c)
+    dx, dw = backward(c, lse, picked)
+    assert not torch.isfinite(dx[at]).all()
+    for name, got in (("loss", loss), ("lse", lse), ("picked", picked), ("dx", dx)):
+        got = got.clone()
+        got[at] = 0.0
+        ref.check(name, got)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_coefficients_whose_sum_is_beyond_fp32(dtype):
+    """One row's coefficients are finite, their sum is not: dw is right."""
+    m, d, V = 2100, 72, 8200
+    assert way(m, d, V, DTYPES[dtype]) == "tiles"
+    c = Case(dtype, m, d, V)
+    c.x *= 2.0 ** -6
+    c.dloss[77] = 3e38
+    _, lse, picked = forward(c)
+    _, dw = backward(c, lse, picked)
+    ref = Reference(c.x, c.w, c.index, dloss=c.dloss)
+    ref.check("dw", dw)
