@@ -90,7 +90,7 @@ struct VocabProduct {
     float* picked;
     // VOCAB_GRADIENT, same operands
     const VocabRow* row;    // [padded]
-    const uint32_t* largest;        // of the rows' coefficients, as bits (fp16 terms are scaled by it)
+    const uint32_t* largest;        // of the rows' coefficients, as bits (fp16 terms of dz^T are scaled by it)
     uint16_t *dz, *dzt;     // rows of [dz_terms][classes] and of [dzt_terms][padded], ld_dz and ld_dzt values apart
     int64_t ld_dz, ld_dzt;
     int32_t dz_terms, dzt_terms;    // 0: not wanted
@@ -114,7 +114,8 @@ hipError_t launch_vocab_product(int what, const VocabProduct& p, int64_t m, int6
 
 // What a gradient's terms are multiplied by: 1 in bf16; in fp16, whose range
 // is short, the power of two that takes the largest coefficient to 2^14 (infinity
-// is a sum beyond fp32's range, below 2^130).
+// is a sum beyond fp32's range, below 2^130).  dW sums over the rows, so the
+// largest is that of all rows; a row of dx is its own affair.
 template <typename T> __device__ __forceinline__ float term_scale(uint32_t largest);
 template <> __device__ __forceinline__ float term_scale<bf16>(uint32_t) { return 1.0f; }
 template <> __device__ __forceinline__ float term_scale<f16>(uint32_t largest)
@@ -123,6 +124,11 @@ template <> __device__ __forceinline__ float term_scale<f16>(uint32_t largest)
     if (e == 0) return 1.0f;
     const int up = 127 + 14 - (e - 127);
     return __uint_as_float(static_cast<uint32_t>(up < 1 ? 1 : (up > 254 ? 254 : up)) << 23);
+}
+
+template <typename T> __device__ __forceinline__ float row_scale(const VocabRow& row)
+{
+    return term_scale<T>(__float_as_uint(fabsf(row.f) + fabsf(row.b)));     // of dz but for its entries
 }
 
 }  // namespace fasgd

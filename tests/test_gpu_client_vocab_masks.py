@@ -126,3 +126,23 @@ def test_coefficients_whose_sum_is_beyond_fp32(dtype):
     _, dw = backward(c, lse, picked)
     ref = Reference(c.x, c.w, c.index, dloss=c.dloss)
     ref.check("dw", dw)
+
+
+@pytest.mark.parametrize("K", [0, 5])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, d, V, form", [(200, 72, 333, "direct"), (2100, 72, 8200, "tiles")])
+def test_rows_that_weigh_little_beside_others(m, d, V, form, dtype, K):
+    """dx of a row is as good with a small dloss as with a large one: it is in proportion, and so is how far it may be
+    off, but for the smallest numbers of its type."""
+    assert way(m, d, V, DTYPES[dtype]) == form
+    c = Case(dtype, m, d, V, K)
+    c.w += 0.25         # so that the softmax's part of dx is not small beside the targets'
+    g = torch.Generator().manual_seed(9)
+    c.dloss = (10.0 ** (-7.0 * torch.rand(m, generator=g))).cuda()
+    ref = Reference(c.x, c.w, c.index, teacher=c.teacher)
+    _, lse, picked = forward(c)
+    dx, _ = backward(c, lse, picked, grad_scale=2.0 ** 14)
+    least = 2.0 ** -25 if dtype == "fp16" else 0.0
+    by = (c.dloss.double() * 2.0 ** 14)[:, None]
+    ref.dx, ref.tol_dx = ref.dx * by, (ref.tol_dx - least) * by + least
+    ref.check("dx", dx)
