@@ -279,9 +279,10 @@ fasgd_status client_vocab_loss_forward(const client_vocab_head* op, const int64_
  *   dx = logit_scale dz w (dtype),  dw = logit_scale dz^T x (dw_dtype:
  *   CLIENT_F32 or dtype; accumulate != 0: added to what dw holds).
  * Either may be NULL.  dx may not be x, nor dw be w.  In the products dz has
- * 24 bits for an fp32 dw (fp16 22; bf16 with 4,096 rows or more 16), and the
- * type's own precision for a dx or dw of 16 bits, but for its entries at the
- * targets, which dx takes in fp32.  Sums are taken in a fixed order.
+ * 24 bits for an fp32 dw (fp16 22), and the type's own precision for a dx or
+ * dw of 16 bits, but for its entries at the targets, which dx takes in fp32.
+ * fp16 holds no part of dz below 2^-39 of its row's largest coefficient for dx,
+ * of the largest of all rows for dw.  Sums are taken in a fixed order.
  */
 fasgd_status client_vocab_loss_backward(const client_vocab_head* op, const int64_t* targets, float smoothing, float z_loss,
                                         const float* lse, const float* picked, const float* dloss, float grad_scale,

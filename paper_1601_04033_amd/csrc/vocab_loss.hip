@@ -423,20 +423,20 @@ constexpr int64_t kPieceBytes = int64_t(1) << 30;
 // 16,384: rows 32 KB apart 855 us, 512 bytes more 822, 256 more 957).
 int64_t apart(int64_t n) { return ((n + 255) / 256 | 1) * 256; }
 
-// Terms of dz that dW is summed from: one for a dw of 16 bits.  For an fp32 one
-// two of fp16 (22 bits), or two of bf16 (16 bits), whose rounding leaves dW off by
-// 2.6e-6 (relative, root mean square), or three (24 bits).  Sums over m rows in
-// fp32, of the values themselves, are off by 0.6 to 0.9e-6 at 1,100 rows, 1.2 to
-// 1.7e-6 at 4,096 and 1.6 to 2.1e-6 at 8,192, so up to there the third term is
-// worth its time: 3 terms leave 0.4 to 0.9e-6, and a training step of 1,100 x 512 x
-// 32,000 takes 407 instead of 361 us, of 2,048 x 2,048 x 8,192 455 instead of 399, of
-// 8,192 x 2,048 x 8,192 1,483 instead of 1,279.
-constexpr int64_t kThreeTerms = 4096;       // for fewer rows
-int terms_for_dw(int64_t rows, int dtype, int dw_dtype)
+// Terms of dz that dW is summed from.  For an fp32 one two of fp16 (22 bits) or
+// three of bf16 (24): with two, 16 bits, dW is off by 1.7 to 2.7e-6 (relative, root
+// mean square) where fp32 sums of 4,096 to 8,192 rows, of the values themselves, are
+// off by 1.0 to 2.5e-6; with three by 0.5 to 1.2e-6.  (A training step of 8,192 x 4,096
+// x 131,072 takes 38.9 ms with three and 33.0 with two, of 8,192 x 1,024 x 32,000 3.3 and
+// 2.9, of 4,096 x 2,048 x 16,384 1.58 and 1.36.)  For a dw of 16 bits one: its rounding
+// comes on top of dW's own, which is of the same size (fp16, 1,777 x 1,544 x 32,003:
+// 3.2e-4 off, with two terms 2.5e-4, all of it dW's; bf16 2.3e-3 and 1.7e-3), and the
+// training step takes 803 instead of 937 us.
+int terms_for_dw(int dtype, int dw_dtype)
 {
     if (dtype == DTYPE_F32) return 3;
     if (dw_dtype != DTYPE_F32) return 1;
-    return dtype == DTYPE_BF16 && rows < kThreeTerms ? 3 : 2;
+    return dtype == DTYPE_BF16 ? 3 : 2;
 }
 
 Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool backward)
@@ -445,8 +445,9 @@ Layout layout_of(int64_t rows, int64_t cols, int64_t vocab, int dtype, bool back
     l.terms = vocab_terms(dtype);
     l.padded = round_up(rows, kVocabTile);
     l.cols_padded = round_up(cols, 128);
-    const int dzt_terms = terms_for_dw(rows, dtype, DTYPE_F32);
-    const int64_t each = 2 * (l.padded * (l.terms + dzt_terms) + 2 * l.cols_padded * l.terms);
+    const int dzt_terms = terms_for_dw(dtype, DTYPE_F32);
+    // (bf16's third term comes on top: shorter pieces would leave more of the chip idle)
+    const int64_t each = 2 * (l.padded * (l.terms == 3 ? 6 : 3) + 2 * l.cols_padded * l.terms);
     int64_t most = kPieceBytes / each / kVocabTile * kVocabTile;
     if (most < 2048) most = 2048;
     if (most > int64_t(1) << 20) most = int64_t(1) << 20;
@@ -657,7 +658,7 @@ hipError_t launch_vocab_backward(const VocabArgs& a, hipStream_t s)
     g.dz = p.at<uint16_t>(l.dz);
     g.dzt = p.at<uint16_t>(l.dzt);
     g.dz_terms = a.dx ? l.terms : 0;
-    g.dzt_terms = a.dw ? terms_for_dw(a.rows, a.dtype, a.dw_dtype) : 0;
+    g.dzt_terms = a.dw ? terms_for_dw(a.dtype, a.dw_dtype) : 0;
     g.classes = l.piece;
     g.padded = l.padded;
     g.ld_dz = l.ld_piece;

@@ -217,3 +217,19 @@ def test_bits_of_a_weight_gradient(dtype, m):
     else:                                       # two terms, each rounding off half a step of what was left
         half = torch.finfo(dt).eps / 2
         assert ((dw[:-1] - want).abs() <= half * half * want).all()
+
+
+@pytest.mark.parametrize("m", [4096, 8200])
+def test_all_bits_of_a_weight_gradient_of_many_rows(m):
+    """bf16: as above, dz has its 24 bits in dw however many rows there are."""
+    d, V, part = m, 1030, 64
+    assert way(m, d, V, torch.bfloat16) == "tiles"
+    x, w = torch.eye(m, device="cuda", dtype=torch.bfloat16), torch.zeros(V, d, device="cuda", dtype=torch.bfloat16)
+    dloss = (0.5 + torch.rand(m, generator=torch.Generator().manual_seed(m))).cuda()
+    zero, dw = torch.zeros(m, device="cuda"), torch.full((V, d), math.nan, device="cuda")
+    ws = torch.empty(fa.client_vocab_workspace_bytes(m, d, V, w.dtype), device="cuda", dtype=torch.uint8)
+    target = torch.arange(m, device="cuda") % part
+    fa.client_vocab_loss_backward(x, w, target, zero, zero, None, dw, dloss=dloss, workspace=ws)
+    want = dloss.repeat(V, 1)
+    want[target, torch.arange(m, device="cuda")] = 0.0      # p - 1
+    assert torch.equal(dw, want)
