@@ -183,6 +183,9 @@ size_t linear_operand_bytes(int64_t m, int64_t k)
     return static_cast<size_t>(round_up(m * round_up(k, 128) + round_up(k, 128) / 128 * round_up(m, 4), 256));
 }
 
+// A matrix's row stride, where it is used: a buffer is as long as its rows are apart.
+int64_t stride_of(int64_t ld, int64_t rows, int64_t cols) { return rows > 1 ? ld : cols; }
+
 // What the losses over a vocabulary share.
 fasgd_status vocab_setup(const client_vocab_head* op, fasgd::VocabArgs& a)
 {
@@ -205,8 +208,8 @@ fasgd_status vocab_setup(const client_vocab_head* op, fasgd::VocabArgs& a)
     a.scale = op->logit_scale;
     a.x = op->x;
     a.w = op->w;
-    a.ldx = op->ld_x;
-    a.ldw = op->ld_w;
+    a.ldx = stride_of(op->ld_x, a.rows, a.cols);
+    a.ldw = stride_of(op->ld_w, a.vocab, a.cols);
     return FASGD_OK;
 }
 
@@ -278,8 +281,8 @@ fasgd_status vocab_gradients(fasgd::VocabArgs& a, const float* dloss, float grad
     a.grad_scale = grad_scale;
     a.dx = dx;
     a.dw = dw;
-    a.lddx = ld_dx;
-    a.lddw = ld_dw;
+    a.lddx = stride_of(ld_dx, a.rows, a.cols);
+    a.lddw = stride_of(ld_dw, a.vocab, a.cols);
     a.dw_dtype = dw_dtype;
     a.accumulate = accumulate != 0;
     return FASGD_OK;
