@@ -753,7 +753,9 @@ template <typename T> hipError_t backward(const VocabArgs& a, const Layout& l, u
         dx.c = l.splits > 1 ? base + l.sums : static_cast<uint8_t*>(a.dx);
         dx.ldc = l.splits > 1 ? l.cols_padded : a.lddx;
         dx.used_r = used;
-        set_blocks(dx, a.vocab <= 16 && !(a.dw && a.rows > 16));     // with dW in one launch where that is long
+        // with dW in one launch where that is long, as long as a launch stays well below 2^32 threads
+        const bool together = a.dw && a.rows > 16 && count(a.rows, 16) * count(a.cols, 128) <= (int64_t(1) << 23);
+        set_blocks(dx, a.vocab <= 16 && !together);
     }
     if (a.dw) {
         dw.a = reinterpret_cast<float*>(base + l.dz);
