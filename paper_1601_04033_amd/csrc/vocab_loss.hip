@@ -92,28 +92,34 @@ struct LayOut {
 };
 
 // fp32 in three bf16 terms: the first two cut off, so that none exceeds the
-// value, the last rounded.  An infinite value is its first term alone.  That is
-// multiplied by all terms of the other value, of which none may be 0 then: those
-// that are become 2^-126 with the value's sign, which adds less than 2^-26 of a
-// finite product, as values below 2^-100 are left as they are.
-__device__ __forceinline__ void terms_of(float x, uint16_t (&t)[3])
+// value, the last rounded.  An infinite value is an infinite first term and finite
+// ones of its sign.  A weight's meets all terms of an activation, of which none
+// may be 0 then (`FILL`): a term has at least 2^-26 of 2^-100, or of the value
+// where that is less, which adds no more than 2^-26 of a finite product.
+template <int TERM, bool FILL> __device__ __forceinline__ uint16_t term_of(float x)
 {
-    constexpr uint32_t kInfinity = 0x7f800000u, kSmall = 0x0d800000u;      // 2^-100
-    const uint32_t bits = __float_as_uint(x), size = bits & 0x7fffffffu;
-    const uint32_t hi = size > kInfinity ? bits | 0x00400000u : bits & 0xffff0000u;    // NaN stays NaN
-    const float r = size < kInfinity ? x - __uint_as_float(hi) : 0.0f;
-    const uint32_t mid = __float_as_uint(r) & 0xffff0000u;
-    const uint32_t least = size < kSmall ? 0u : (bits >> 16 & 0x8000u) | 0x0080u;
-    const uint16_t last = from_float<bf16>(r - __uint_as_float(mid)).bits;
-    t[0] = static_cast<uint16_t>(hi >> 16);
-    t[1] = static_cast<uint16_t>(mid << 1 == 0 ? least : mid >> 16);
-    t[2] = static_cast<uint16_t>((last & 0x7fffu) == 0 ? least : last);
+    if constexpr (TERM == 0) return static_cast<uint16_t>(__float_as_uint(__builtin_canonicalizef(x)) >> 16);   // NaN without its lower bits
+    constexpr uint32_t kUpper = 0xffff0000u;
+    const float finite = __builtin_amdgcn_fmed3f(x, -FLT_MAX, FLT_MAX);
+    const float rest = finite - __uint_as_float(__float_as_uint(finite) & kUpper);
+    const float second = __uint_as_float(__float_as_uint(rest) & kUpper);
+    uint32_t term = TERM == 1 ? __float_as_uint(second) >> 16 : from_float<bf16>(rest - second).bits;
+    if constexpr (FILL) {
+        const float least = fminf(fabsf(x), 0x1p-100f) * 0x1p-26f, size = __uint_as_float((term & 0x7fffu) << 16);
+        term = __float_as_uint(fmaxf(size, least)) >> 16 | (__float_as_uint(x) >> 16 & 0x8000u);
+    }
+    return static_cast<uint16_t>(term);
+}
+
+template <bool FILL> __device__ __forceinline__ uint16_t term_at(float x, int term)
+{
+    return term == 0 ? term_of<0, FILL>(x) : (term == 1 ? term_of<1, FILL>(x) : term_of<2, FILL>(x));
 }
 
 // 64 x 64 elements a wave, 8 x 8 a lane, turned in registers: each load and each
 // store of a wave is whole lines of 8 rows or columns.  (131,072 x 4,096 bf16
 // turned in pieces: 4.2 TB/s; through LDS 3.7.)
-template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_out(LayOut a)
+template <typename T, int TERMS, bool FILL> __global__ __launch_bounds__(kBlock, 2) void lay_out(LayOut a)
 {
     const int64_t rows = a.active ? *a.active : a.rows;
     const int lane = threadIdx.x & 63;
@@ -146,10 +152,7 @@ template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_o
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    uint16_t s[3], u[3];
-                    terms_of(x[i].v[e], s);
-                    terms_of(x[i].v[e + 1], u);
-                    w[i][e / 2] = s[term] | static_cast<uint32_t>(u[term]) << 16;
+                    w[i][e / 2] = term_at<FILL>(x[i].v[e], term) | static_cast<uint32_t>(term_at<FILL>(x[i].v[e + 1], term)) << 16;
                 }
             }
             if (a.by_rows) {
@@ -173,13 +176,18 @@ template <typename T, int TERMS> __global__ __launch_bounds__(kBlock) void lay_o
 
 // ---- forward
 
-// The type of a matrix's terms.
-template <typename T> struct Term {
-    using type = T;
-};
-template <> struct Term<float> {
-    using type = bf16;
-};
+#if defined(__HIP_DEVICE_COMPILE__)
+template <int TERM, int N> __device__ __forceinline__ void multiply_terms(const Pack<float, 8> (&v)[N], const v4i (&b)[N], v4f& acc)
+{
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+        Pack<uint16_t, 8> t;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t.v[e] = term_of<TERM, false>(v[s].v[e]);
+        acc = mfma<bf16>(__builtin_bit_cast(v4i, t), b[s], acc);
+    }
+}
+#endif
 
 // The logits at a teacher's entries, 16 a wave: the diagonal of the product of their
 // classes' rows and their rows of x, by the instruction and in the order of
@@ -189,12 +197,12 @@ template <> struct Term<float> {
 // 8,192 x 4,096 x 131,072 bf16, dW off by 3.9e-6 with a sum in another order.)
 // Bound by W's rows and the chain of loads, 16 steps on their way (4,096 rows of 64
 // entries, 4,096 columns bf16: 365 us, 5.9 TB/s; 1,531 rows of 50: 45 us).
-template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, const int32_t* list, const int32_t* active,
+template <typename T> __global__ __launch_bounds__(64, 2) void pick(VocabArgs a, const int32_t* list, const int32_t* active,
                                                                 const uint16_t* x, int64_t ld_x, int64_t cols_padded)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool kTerms = sizeof(T) == 4;
-    constexpr int kFlight = 16;     // steps of 32 on their way
+    constexpr int kFlight = kTerms ? 8 : 16;        // steps of 32 on their way
     const int lane = threadIdx.x, part = lane >> 4;
     const int64_t all = static_cast<int64_t>(*active) * a.entries, blocks = (all + 15) / 16;
     for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
@@ -209,47 +217,37 @@ template <typename T> __global__ __launch_bounds__(64) void pick(VocabArgs a, co
             const int ta = kTerms ? kPairsA >> (2 * p) & 3u : 0, tb = kTerms ? kPairsB >> (2 * p) & 3u : 0;
             const uint16_t* b = row + tb * cols_padded;
             for (int64_t k0 = 8 * part; k0 - 8 * part < a.cols; k0 += 32 * kFlight) {
-                v4i fa[kFlight], fb[kFlight];
-                auto take = [&](int s, const Pack<T, 8>& v) {
-                    if constexpr (kTerms) {
-                        Pack<uint16_t, 8> t;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            uint16_t term[3];
-                            terms_of(v.v[e], term);
-                            t.v[e] = ta == 0 ? term[0] : (ta == 1 ? term[1] : term[2]);
-                        }
-                        fa[s] = __builtin_bit_cast(v4i, t);
-                    } else {
-                        fa[s] = __builtin_bit_cast(v4i, v);
-                    }
-                };
+                v4i fb[kFlight];
+                Pack<T, 8> v[kFlight];
                 if (k0 - 8 * part + 32 * kFlight <= a.cols) {
-                    Pack<T, 8> v[kFlight];
 #pragma unroll
                     for (int s = 0; s < kFlight; ++s) {
                         v[s] = load_pack<T, 8>(w + k0 + 32 * s);
                         fb[s] = *reinterpret_cast<const v4i*>(b + k0 + 32 * s);
                     }
-#pragma unroll
-                    for (int s = 0; s < kFlight; ++s) take(s, v[s]);
                 } else {
 #pragma unroll
                     for (int s = 0; s < kFlight; ++s) {
                         const int64_t k = k0 + 32 * s;
-                        Pack<T, 8> v;
                         if (k + 8 <= a.cols) {
-                            v = load_pack<T, 8>(w + k);
+                            v[s] = load_pack<T, 8>(w + k);
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v.v[e] = k + e < a.cols ? w[k + e] : from_float<T>(0.0f);
+                            for (int e = 0; e < 8; ++e) v[s].v[e] = k + e < a.cols ? w[k + e] : from_float<T>(0.0f);
                         }
-                        take(s, v);
                         fb[s] = k < cols_padded ? *reinterpret_cast<const v4i*>(b + k) : v4i{0, 0, 0, 0};
                     }
                 }
+                if constexpr (!kTerms) {
 #pragma unroll
-                for (int s = 0; s < kFlight; ++s) acc = mfma<typename Term<T>::type>(fa[s], fb[s], acc);
+                    for (int s = 0; s < kFlight; ++s) acc = mfma<T>(__builtin_bit_cast(v4i, v[s]), fb[s], acc);
+                } else if (ta == 0) {       // the same in all lanes
+                    multiply_terms<0>(v, fb, acc);
+                } else if (ta == 1) {
+                    multiply_terms<1>(v, fb, acc);
+                } else {
+                    multiply_terms<2>(v, fb, acc);
+                }
             }
         }
         // lane l: column l % 16, rows 4 (l / 16) + i
@@ -500,8 +498,9 @@ bool in_place(const VocabArgs& a)
 hipError_t launch_lay_out(const LayOut& l, int dtype, int64_t rows, int64_t cols, hipStream_t s)
 {
     const dim3 grid(static_cast<unsigned>(round_up(rows, kVocabTile) / 64), static_cast<unsigned>(round_up(cols, 256) / 256));
-    if (dtype == DTYPE_F32) lay_out<float, 3><<<grid, kBlock, 0, s>>>(l);
-    else lay_out<bf16, 1><<<grid, kBlock, 0, s>>>(l);       // bits of either 16-bit type
+    if (dtype == DTYPE_F32 && l.list) lay_out<float, 3, true><<<grid, kBlock, 0, s>>>(l);
+    else if (dtype == DTYPE_F32) lay_out<float, 3, false><<<grid, kBlock, 0, s>>>(l);
+    else lay_out<bf16, 1, false><<<grid, kBlock, 0, s>>>(l);       // bits of either 16-bit type
     return hipGetLastError();
 }
 
