@@ -281,8 +281,8 @@ fasgd_status client_vocab_loss_forward(const client_vocab_head* op, const int64_
  * Either may be NULL.  dx may not be x, nor dw be w.  In the products dz has
  * 24 bits for an fp32 dw (fp16 22), and the type's own precision for a dx or
  * dw of 16 bits, but for its entries at the targets, which dx takes in fp32.
- * fp16 holds no part of dz below 2^-39 of its row's largest coefficient for dx,
- * of the largest of all rows for dw.  Sums are taken in a fixed order.
+ * fp16 holds no part of dz below 2^-36 of its row's largest coefficient for dx,
+ * 2^-39 of the largest of all rows for dw.  Sums are taken in a fixed order.
  */
 fasgd_status client_vocab_loss_backward(const client_vocab_head* op, const int64_t* targets, float smoothing, float z_loss,
                                         const float* lse, const float* picked, const float* dloss, float grad_scale,

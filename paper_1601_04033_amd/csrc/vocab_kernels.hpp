@@ -2,6 +2,8 @@
 // called by the C ABI after it has validated every argument.
 #pragma once
 
+#include <float.h>
+
 #include "client_kernels.hpp"
 
 namespace fasgd {
@@ -114,8 +116,8 @@ hipError_t launch_vocab_product(int what, const VocabProduct& p, int64_t m, int6
 
 // What a gradient's terms are multiplied by: 1 in bf16; in fp16, whose range
 // is short, the power of two that takes the largest coefficient to 2^14 (infinity
-// is a sum beyond fp32's range, below 2^130).  dW sums over the rows, so the
-// largest is that of all rows; a row of dx is its own affair.
+// is a sum beyond fp32's range, below 2^130).  dW sums over the rows, so that
+// is the largest of all rows.
 template <typename T> __device__ __forceinline__ float term_scale(uint32_t largest);
 template <> __device__ __forceinline__ float term_scale<bf16>(uint32_t) { return 1.0f; }
 template <> __device__ __forceinline__ float term_scale<f16>(uint32_t largest)
@@ -126,9 +128,14 @@ template <> __device__ __forceinline__ float term_scale<f16>(uint32_t largest)
     return __uint_as_float(static_cast<uint32_t>(up < 1 ? 1 : (up > 254 ? 254 : up)) << 23);
 }
 
-template <typename T> __device__ __forceinline__ float row_scale(const VocabRow& row)
+// A row of dx is its own affair: where its coefficients are far below the largest,
+// they are taken to 2^14 by themselves.  Rows of much the same size share `up`, the
+// scale of all, and their terms with dz^T.
+template <typename T> __device__ __forceinline__ float row_scale(const VocabRow& row, float up)
 {
-    return term_scale<T>(__float_as_uint(fabsf(row.f) + fabsf(row.b)));     // of dz but for its entries
+    const float own = term_scale<T>(__float_as_uint(fabsf(row.f) + fabsf(row.b)));
+    return own <= 8.0f * up || fabsf(row.f) + fabsf(row.b) < FLT_MIN ? up : own;
 }
+template <> __device__ __forceinline__ float row_scale<bf16>(const VocabRow&, float) { return 1.0f; }
 
 }  // namespace fasgd

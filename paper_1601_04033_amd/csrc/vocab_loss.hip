@@ -372,7 +372,7 @@ template <typename T, typename TERM> __global__ __launch_bounds__(kBlock) void f
     }
     __syncthreads();
     const int n = entries;
-    const float by = a.scale / row_scale<TERM>(g.row[at]);
+    const float by = a.scale / row_scale<TERM>(g.row[at], term_scale<TERM>(*g.largest));
     const T* w = static_cast<const T*>(a.w);
     for (int64_t c = threadIdx.x * 4; c < a.cols; c += kBlock * 4) {
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f}, own[4] = {0.0f, 0.0f, 0.0f, 0.0f};
