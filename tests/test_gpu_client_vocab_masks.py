@@ -141,7 +141,10 @@ def test_rows_that_weigh_little_beside_others(m, d, V, form, dtype, K):
     c.dloss = (10.0 ** (-7.0 * torch.rand(m, generator=g))).cuda()
     ref = Reference(c.x, c.w, c.index, teacher=c.teacher)
     _, lse, picked = forward(c)
-    dx, _ = backward(c, lse, picked, grad_scale=2.0 ** 14)
+    dx, dw = backward(c, lse, picked, grad_scale=2.0 ** 14)
+    Reference(c.x, c.w, c.index, teacher=c.teacher, dloss=c.dloss, grad_scale=2.0 ** 14).check("dw", dw)
+    assert torch.equal(backward(c, lse, picked, dx=False, grad_scale=2.0 ** 14)[1], dw)
+    assert torch.equal(backward(c, lse, picked, dw=None, grad_scale=2.0 ** 14)[0], dx)
     least = 2.0 ** -25 if dtype == "fp16" else 0.0
     by = (c.dloss.double() * 2.0 ** 14)[:, None]
     ref.dx, ref.tol_dx = ref.dx * by, (ref.tol_dx - least) * by + least
