@@ -18,6 +18,7 @@ namespace {
 constexpr int kBlock = 256;
 constexpr int kWaves = kBlock / 64;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2eRest = 1.92596303e-8f;    // what fp32 leaves of log2(e)
 
 __device__ __forceinline__ float wave_sum(float x)
 {
@@ -124,6 +125,10 @@ __device__ __forceinline__ VocabRow coefficients_of(const VocabArgs& a, int64_t 
         c.f = c.g * wave_sum(q);
         c.b = 0.0f;
     }
+    // What rounding took from l, the same in all of the row's probabilities: into
+    // their factor.  (A log-sum-exp of 12 or more: up to 6.6e-7 of each.)
+    const float rest = __builtin_fmaf(lse, kLog2eRest, __builtin_fmaf(lse, kLog2e, -c.l));
+    if (fabsf(rest) < 1.0f) c.f = __builtin_fmaf(c.f, -rest * kLn2, c.f);
     return c;
 }
 

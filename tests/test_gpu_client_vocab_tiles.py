@@ -233,3 +233,27 @@ def test_all_bits_of_a_weight_gradient_of_many_rows(m):
     want = dloss.repeat(V, 1)
     want[target, torch.arange(m, device="cuda")] = 0.0      # p - 1
     assert torch.equal(dw, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [0, 1])
+@pytest.mark.parametrize("m, V, form", [(48, 100, "direct"), (1100, 4099, "tiles")])
+def test_probabilities_of_a_given_log_sum_exp(dtype, K, m, V, form):
+    """With w of zeros p is exp(-lse), whose exponent in powers of two is not a number of 24 bits.  The power is off by a
+    step, 2 u, its factor and their product by u each and what the factor takes up by as much (u = 2^-24); fp16 holds
+    dz in 22 bits."""
+    d, dt, u = m, DTYPES[dtype], 2.0 ** -24
+    assert way(m, d, V, dt) == form
+    lse = (11.2 + 10.0 * torch.rand(m, generator=torch.Generator().manual_seed(2))).cuda()
+    x, w = torch.eye(m, device="cuda", dtype=dt), torch.zeros(V, d, device="cuda", dtype=dt)
+    target, zero = torch.full((m,), V - 1, device="cuda"), torch.zeros(m, device="cuda")
+    dw = torch.full((V, d), math.nan, device="cuda")
+    kw = dict(grad_scale=2.0 ** 10, workspace=torch.empty(fa.client_vocab_workspace_bytes(m, d, V, dt), device="cuda", dtype=torch.uint8))
+    if K:
+        fa.client_vocab_distill_backward(x, w, target[:, None], torch.zeros(m, 1, device="cuda", dtype=dt), lse, zero[:, None],
+                                         None, dw, **kw)
+    else:
+        fa.client_vocab_loss_backward(x, w, target, lse, zero, None, dw, **kw)
+    want = 2.0 ** 10 * torch.exp(-lse.double())
+    held = (2.0 ** -22 if form == "tiles" else 0.0) * want + 2.0 ** -28 if dtype == "fp16" else u * want
+    assert ((dw[:-1] - want).abs() <= 5 * u * want + held).all()
