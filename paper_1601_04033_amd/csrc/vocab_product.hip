@@ -14,9 +14,10 @@
 // Bound by the matrix instructions, and by the power that they draw: without
 // loads, 16 x 16 x 32 instructions alone reach 2,070 TFLOP/s on random operands
 // (2,450 on zeros), 32 x 32 x 16 ones 1,810.  Measured, bf16, 8,192 rows, pieces of
-// 16,384 classes, 4,096 columns: statistics 855 us (1,285 TFLOP/s), gradient with
-// both layouts 860 (1,280), dx 770 (1,425), dW from two terms 1,550 (1,420); the
-// vendor's library 690 to 800 for one such product with nothing before or after.
+// 16,384 classes, 4,096 columns: statistics 850 us (1,295 TFLOP/s), gradient with
+// one term along the rows and three along the classes 980 (1,120; with two 920), dx
+// 770 (1,425), dW from three terms 2,330 (1,415; from two 1,550); the vendor's
+// library 690 to 800 for one such product with nothing before or after.
 #include <float.h>
 #include <type_traits>
 
